@@ -282,6 +282,112 @@ gf_status gformer_attn_bwd(const void* q, const void* k, const void* v, const vo
                            const gformer_params* p, void* workspace, size_t workspace_bytes,
                            void* hip_stream);
 
+/* ---- Packed sequences and the paged cache ---------------------------------------------------
+ * Causal softmax attention over all keys (section II-A, Eq. 1 with the whole prefix for a window) in the forms
+ * that training on packed documents and a serving engine use: sequences of different lengths one behind
+ * another with no padding between them, query heads that share key heads, and keys and values of many
+ * sequences in pages of one cache.  All of them: d in {64, 128}, element types GF_F32 and GF_BF16, H a
+ * multiple of Hkv, query head h reads key head h / (H / Hkv); fp32 arithmetic and statistics, with bf16 only the
+ * operands of the matrix products are rounded (weights, and in the backward pass the gradients of the
+ * scores).  Conventions (alignment, asynchrony, errors, the device of the stream) as at the top of this file;
+ * strides are multiples of 8 elements, all-zero strides mean dense, a row (token) stride may not exceed 2^20.
+ * Integer arrays are DEVICE pointers to int32, 4-byte aligned, and are read on the device alone: offsets,
+ * lengths and page numbers out of range never make a call read or write outside the tensors it was
+ * given, but what it then computes is not defined beyond what is said below.
+ *
+ * Sequence s has queries cu_q[s] .. cu_q[s+1]-1 and keys cu_k[s] .. cu_k[s+1]-1 (cu_k == NULL: the same),
+ * offsets ascending from 0; a sequence may be empty.  Query i of nq sees keys j <= i + nk - nq: with nk > nq
+ * the prompt goes on behind keys that are already there, with nk < nq the first nq - nk queries see
+ * nothing (output 0, lse -infinity).  Keys that a query does not see have no part in its result, also where they
+ * hold infinities or NaN. */
+typedef struct gformer_packed_params {
+  uint32_t struct_size;   /* = sizeof(gformer_packed_params)                                 */
+  int32_t dtype;          /* gf_dtype of all tensors but lse                                 */
+  int32_t zero_tail;      /* 0: rows behind the last sequence (of out; dq; dk, dv) are left  */
+                          /* as they were.  1: they are set to zero (lse never is)           */
+  float softmax_scale;    /* multiplies q.k; any finite value                                */
+  int64_t q_stride[2], k_stride[2], v_stride[2], o_stride[2]; /* (row, head) element strides  */
+  int64_t do_stride[2], dq_stride[2], dk_stride[2], dv_stride[2]; /* gformer_packed_attn_bwd */
+} gformer_packed_params;
+
+/* struct_size set, dtype = GF_BF16, softmax_scale = 1, the rest zero */
+void gformer_packed_params_init(gformer_packed_params* p);
+
+/*   q   : device [total_q, H, d], k, v : device [total_k, Hkv, d], read
+ *   out : device [total_q, H, d], written; may not alias an input
+ *   lse : device fp32 [H, total_q] dense, written with the natural logarithm of every query's sum of
+ *         exponentials (what the backward pass needs), or NULL
+ * total_q or total_k of 0, or n_seqs == 0, are fine. */
+gf_status gformer_packed_attn_fwd(const void* q, const void* k, const void* v, void* out, float* lse,
+                                  const int32_t* cu_q, const int32_t* cu_k, int n_seqs, int total_q,
+                                  int total_k, int H, int Hkv, int d,
+                                  const gformer_packed_params* p, void* hip_stream);
+
+/* Gradients of the above.
+ *   out, lse   : what the forward pass wrote, read
+ *   dout       : gradient with respect to out, read
+ *   dq, dk, dv : written; may not alias an input or overlap each other
+ *   workspace  : device, gformer_packed_attn_bwd_workspace_bytes bytes, 256-byte aligned
+ * dk and dv sum over the query heads that share a key head, in one fixed order: equal calls give equal bits. */
+size_t gformer_packed_attn_bwd_workspace_bytes(int total_q, int total_k, int n_seqs, int H, int Hkv, int d,
+                                               const gformer_packed_params* p);
+gf_status gformer_packed_attn_bwd(const void* q, const void* k, const void* v, const void* out,
+                                  const float* lse, const void* dout, void* dq, void* dk, void* dv,
+                                  const int32_t* cu_q, const int32_t* cu_k, int n_seqs, int total_q,
+                                  int total_k, int H, int Hkv, int d, const gformer_packed_params* p,
+                                  void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* The paged cache: kpages and vpages are [n_pages, Hkv, page_size, d] through (page, head, token) strides;
+ * token t of sequence s lies in page table[s][t / page_size], slot t % page_size, table being int32
+ * [sequences, table_width] dense.  A page number outside [0, n_pages) is no page: its tokens are not seen and
+ * not written.  Pages may be shared between sequences as long as nobody writes into them.
+ * page_size: a power of two from 8 to 65536; table_width * page_size at most 2^30. */
+typedef struct gformer_paged_params {
+  uint32_t struct_size;   /* = sizeof(gformer_paged_params)                                  */
+  int32_t dtype;          /* gf_dtype of all tensors                                         */
+  int32_t page_size;      /* tokens per page                                                 */
+  float softmax_scale;    /* gformer_paged_decode: multiplies q.k; any finite value          */
+  int64_t q_stride[2], o_stride[2]; /* (sequence, head); gformer_paged_decode                */
+  int64_t k_stride[2], v_stride[2]; /* (sequence, head) or, in gformer_paged_fill, (row, head) */
+  int64_t kpage_stride[3], vpage_stride[3]; /* (page, head, token)                           */
+} gformer_paged_params;
+
+/* struct_size set, dtype = GF_BF16, page_size = 64, softmax_scale = 1, dense strides */
+void gformer_paged_params_init(gformer_paged_params* p);
+
+/* One new token of B sequences: its key and value go to their slot, and its queries see the lens[b] cached
+ * tokens and the new one.
+ *   q, out : device [B, H, d], read / written; out may not alias an input
+ *   k, v   : device [B, Hkv, d], read; both NULL: nothing is written and the queries see the lens[b] cached
+ *            tokens alone (none: output 0)
+ *   lens   : device int32 [B], tokens of every sequence in the cache before the call.  A row whose length is
+ *            negative, or leaves no room, is idle: output 0, nothing written
+ *   max_len : at least the longest sequence's tokens, the new one included, or 0 for what the table can hold:
+ *            sizes the launch and the workspace.  A longer sequence counts as having no room.
+ * No two sequences of one call may write into the same slot. */
+size_t gformer_paged_decode_workspace_bytes(int B, int H, int Hkv, int d, int table_width, int max_len,
+                                            const gformer_paged_params* p);
+gf_status gformer_paged_decode(const void* q, const void* k, const void* v, void* out, void* kpages,
+                               void* vpages, const int32_t* table, const int32_t* lens, int B, int H,
+                               int Hkv, int d, int n_pages, int table_width, int max_len,
+                               const gformer_paged_params* p, void* workspace, size_t workspace_bytes,
+                               void* hip_stream);
+
+/* Packed rows (a prompt's keys and values, [total, Hkv, d]) into the cache: row i of sequence s becomes its
+ * token start[s] + i.  Rows behind the last sequence, and tokens in front of 0, behind the table's end or of no
+ * page are left out. */
+gf_status gformer_paged_fill(const void* k, const void* v, void* kpages, void* vpages,
+                             const int32_t* table, const int32_t* start, const int32_t* cu, int n_seqs,
+                             int total, int Hkv, int d, int n_pages, int table_width,
+                             const gformer_paged_params* p, void* hip_stream);
+
+/* Pages src[i] -> dst[i], whole, keys and values (what forking a sequence and compacting the cache need).  A
+ * pair with a number outside [0, n_pages) is left out.  Destinations differ from each other and from every
+ * source but their own.  [n_pages, Hkv, page_size, d] may stand for more than one layer's heads. */
+gf_status gformer_pages_copy(void* kpages, void* vpages, const int32_t* src, const int32_t* dst,
+                             int n_copies, int Hkv, int d, int n_pages, const gformer_paged_params* p,
+                             void* hip_stream);
+
 /* Positive random features as a pre-map of Q or K for the linear heads.  Section III-A names
  * "positive orthogonal random features" for the linear part and Algorithm 1 "random feature
  * maps"; neither prints them, so the formula is the construction of the work they cite:

@@ -29,6 +29,9 @@ EXPORTS = ("gformer_params_init", "gformer_attn_workspace_bytes", "gformer_attn_
            "gformer_attn_bwd_workspace_bytes", "gformer_attn_bwd",
            "gformer_feature_params_init",
            "gformer_random_features",
+           "gformer_packed_params_init", "gformer_packed_attn_fwd", "gformer_packed_attn_bwd_workspace_bytes",
+           "gformer_packed_attn_bwd", "gformer_paged_params_init", "gformer_paged_decode_workspace_bytes",
+           "gformer_paged_decode", "gformer_paged_fill", "gformer_pages_copy",
            "gformer_partition_balance", "gformer_partition_heads",
            "gformer_status_string", "gformer_version")
 
@@ -63,6 +66,19 @@ class GformerFeatureParams(ctypes.Structure):
                 ("x_stride", ctypes.c_int64 * 3), ("o_stride", ctypes.c_int64 * 3)]
 
 
+class GformerPackedParams(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("dtype", ctypes.c_int32), ("zero_tail", ctypes.c_int32),
+                ("softmax_scale", ctypes.c_float),
+                *((f"{x}_stride", ctypes.c_int64 * 2) for x in ("q", "k", "v", "o", "do", "dq", "dk", "dv"))]
+
+
+class GformerPagedParams(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("dtype", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("softmax_scale", ctypes.c_float),
+                *((f"{x}_stride", ctypes.c_int64 * 2) for x in ("q", "o", "k", "v")),
+                *((f"{x}_stride", ctypes.c_int64 * 3) for x in ("kpage", "vpage"))]
+
+
 class GformerPartitionInputs(ctypes.Structure):
     _fields_ = [("struct_size", ctypes.c_uint32), ("reserved0", ctypes.c_int32),
                 ("p", ctypes.c_double), ("size", ctypes.c_double),
@@ -76,6 +92,7 @@ class GformerError(RuntimeError):
         self.status = status
 
 
+_Int64x2 = ctypes.c_int64 * 2
 _Int64x3 = ctypes.c_int64 * 3
 _lib = None
 
@@ -119,6 +136,26 @@ def lib():
         L.gformer_random_features.restype = ctypes.c_int
         L.gformer_random_features.argtypes = [ctypes.c_void_p] * 3 + [ctypes.c_int] * 5 + \
             [FP, ctypes.c_void_p]
+        PP, GP = ctypes.POINTER(GformerPackedParams), ctypes.POINTER(GformerPagedParams)
+        for name, init in (("packed", PP), ("paged", GP)):
+            getattr(L, f"gformer_{name}_params_init").restype = None
+            getattr(L, f"gformer_{name}_params_init").argtypes = [init]
+        L.gformer_packed_attn_fwd.restype = ctypes.c_int
+        L.gformer_packed_attn_fwd.argtypes = [ctypes.c_void_p] * 7 + [ctypes.c_int] * 6 + [PP, ctypes.c_void_p]
+        L.gformer_packed_attn_bwd_workspace_bytes.restype = ctypes.c_size_t
+        L.gformer_packed_attn_bwd_workspace_bytes.argtypes = [ctypes.c_int] * 6 + [PP]
+        L.gformer_packed_attn_bwd.restype = ctypes.c_int
+        L.gformer_packed_attn_bwd.argtypes = [ctypes.c_void_p] * 11 + [ctypes.c_int] * 6 + \
+            [PP, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]
+        L.gformer_paged_decode_workspace_bytes.restype = ctypes.c_size_t
+        L.gformer_paged_decode_workspace_bytes.argtypes = [ctypes.c_int] * 6 + [GP]
+        L.gformer_paged_decode.restype = ctypes.c_int
+        L.gformer_paged_decode.argtypes = [ctypes.c_void_p] * 8 + [ctypes.c_int] * 7 + \
+            [GP, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]
+        L.gformer_paged_fill.restype = ctypes.c_int
+        L.gformer_paged_fill.argtypes = [ctypes.c_void_p] * 7 + [ctypes.c_int] * 6 + [GP, ctypes.c_void_p]
+        L.gformer_pages_copy.restype = ctypes.c_int
+        L.gformer_pages_copy.argtypes = [ctypes.c_void_p] * 4 + [ctypes.c_int] * 4 + [GP, ctypes.c_void_p]
         L.gformer_partition_balance.restype = ctypes.c_int
         L.gformer_partition_balance.argtypes = [ctypes.POINTER(GformerPartitionInputs),
                                                 ctypes.POINTER(ctypes.c_double),
@@ -482,6 +519,231 @@ def gformer_attn_bwd(q, k, v, dout, dq, dk, dv, window: int, n_sparse_heads: int
     if st != GF_OK:
         raise GformerError(st, gformer_status_string(st))
     return dq, dk, dv
+
+
+# ---- packed sequences and the paged cache ------------------------------------------------------
+
+def _row_strides(name, t):
+    """Strides of a [rows, heads, d] or [pages, heads, tokens, d] tensor without the last; those of single
+    rows, which say nothing, as if it were dense."""
+    shape, s = t.shape, t.stride()
+    if s[-1] != 1 and shape[-1] > 1:
+        raise ValueError(f"{name}: the last dimension must be contiguous")
+    out, dense = [], shape[-1]
+    for n, x in zip(reversed(shape[:-1]), reversed(s[:-1])):
+        if n > 1 and x == 0:
+            raise ValueError(f"{name}: broadcast dimensions (stride 0) are not supported")
+        out.append(x if n > 1 else dense)
+        dense *= max(n, 1)
+    return out[::-1]
+
+
+def _tensors(like, n_dims, **tensors):
+    """Device tensors of one type, one device and `n_dims` dimensions."""
+    import torch
+
+    if like.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError(f"unsupported dtype {like.dtype}")
+    for name, t in tensors.items():
+        if not t.is_cuda:
+            raise ValueError(f"{name} must be a device tensor: there is no CPU path")
+        if t.dtype != like.dtype or t.device != like.device:
+            raise ValueError(f"{name} must have the type and device of the others")
+        if t.dim() != n_dims:
+            raise ValueError(f"{name} must have {n_dims} dimensions")
+    return GF_BF16 if like.dtype == torch.bfloat16 else GF_F32
+
+
+def _numbers(like, shape, **tensors):
+    """Dense int32 tensors on the device of `like`; a None in `shape` fits any size."""
+    import torch
+
+    for name, t in tensors.items():
+        if not t.is_cuda or t.device != like.device or t.dtype != torch.int32 or not t.is_contiguous():
+            raise ValueError(f"{name} must be a dense int32 tensor on the device of the others")
+        if t.dim() != len(shape) or any(n is not None and n != x for n, x in zip(shape, t.shape)):
+            raise ValueError(f"{name} must be of shape {list(shape)}")
+
+
+def _packed_shapes(q, k, v, cu_q, cu_k, **like_q):
+    for name, t in like_q.items():
+        if t.shape != q.shape:
+            raise ValueError(f"{name} must be of q's shape")
+    if k.shape != v.shape or k.shape[2] != q.shape[2]:
+        raise ValueError("q must be [total_q, H, d], k and v [total_k, Hkv, d]")
+    if cu_q.numel() < 1:
+        raise ValueError("cu_q must hold n_seqs + 1 offsets")
+    _numbers(q, (None,), cu_q=cu_q)
+    if cu_k is not None:
+        _numbers(q, cu_q.shape, cu_k=cu_k)
+    elif k.shape[0] != q.shape[0]:
+        raise ValueError("cu_k may be left out only where q and k have the same rows")
+
+
+def _call(entry, like, stream, *args):
+    """entry(*args, stream) with the tensors' device current."""
+    import torch
+
+    if stream is None:
+        stream = _current_stream(like)
+    if torch.cuda.current_device() == like.get_device():
+        st = entry(*args, stream)
+    else:
+        with torch.cuda.device(like.device):
+            st = entry(*args, stream)
+    if st != GF_OK:
+        raise GformerError(st, gformer_status_string(st))
+
+
+def _scratch(need, workspace, like, stream):
+    """(address, bytes) of the caller's workspace, or of one for this call."""
+    import torch
+
+    if workspace is None:
+        if need == 0:
+            return None, 0, 0
+        workspace = torch.empty(need, dtype=torch.uint8, device=like.device) if stream is None else _workspace(need, like, stream)
+    elif not workspace.is_cuda or workspace.device != like.device or not workspace.is_contiguous():
+        raise ValueError("workspace must be a dense tensor on the device of the others")
+    return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def make_packed_params(dtype=GF_BF16, softmax_scale=1.0, zero_tail=0, **strides) -> GformerPackedParams:
+    """strides: q_stride=, k_stride=, ... as (row, head)."""
+    p = GformerPackedParams(ctypes.sizeof(GformerPackedParams), int(dtype), int(zero_tail), float(softmax_scale))
+    for name, val in strides.items():
+        setattr(p, name, _Int64x2(*val))
+    return p
+
+
+def make_paged_params(dtype=GF_BF16, page_size=64, softmax_scale=1.0, **strides) -> GformerPagedParams:
+    """strides: q_stride=, ... as (sequence or row, head), kpage_stride=, vpage_stride= as (page, head, token)."""
+    p = GformerPagedParams(ctypes.sizeof(GformerPagedParams), int(dtype), int(page_size), float(softmax_scale))
+    for name, val in strides.items():
+        setattr(p, name, (_Int64x2 if len(val) == 2 else _Int64x3)(*val))
+    return p
+
+
+def gformer_packed_attn_fwd(q, k, v, out, cu_q, cu_k=None, *, lse=None, softmax_scale=1.0, zero_tail=0,
+                            stream: Optional[int] = None):
+    """Causal attention over packed sequences on device tensors: q, out [total_q, H, d], k, v [total_k, Hkv, d]
+    (any strides with a contiguous last dimension); cu_q, cu_k int32 [n_seqs + 1] offsets (cu_k=None: the same
+    sequences); lse, optional: dense fp32 [H, total_q], written."""
+    import torch
+
+    dtype = _tensors(q, 3, q=q, k=k, v=v, out=out)
+    _packed_shapes(q, k, v, cu_q, cu_k, out=out)
+    T, H, d = q.shape
+    if lse is not None and (lse.device != q.device or lse.dtype != torch.float32 or lse.shape != (H, T) or not lse.is_contiguous()):
+        raise ValueError("lse must be dense fp32 [H, total_q]")
+    p = make_packed_params(dtype, softmax_scale, zero_tail, q_stride=_row_strides("q", q), k_stride=_row_strides("k", k),
+                           v_stride=_row_strides("v", v), o_stride=_row_strides("out", out))
+    _call(lib().gformer_packed_attn_fwd, q, stream, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
+          None if lse is None else lse.data_ptr(), cu_q.data_ptr(), None if cu_k is None else cu_k.data_ptr(),
+          cu_q.numel() - 1, T, k.shape[0], H, k.shape[1], d, ctypes.byref(p))
+    return out
+
+
+def gformer_packed_attn_bwd_workspace_bytes(total_q, total_k, n_seqs, H, Hkv, d, params=None) -> int:
+    return int(lib().gformer_packed_attn_bwd_workspace_bytes(total_q, total_k, n_seqs, H, Hkv, d,
+                                                             ctypes.byref(params or make_packed_params())))
+
+
+def gformer_packed_attn_bwd(q, k, v, out, lse, dout, dq, dk, dv, cu_q, cu_k=None, *, softmax_scale=1.0, zero_tail=0,
+                            workspace=None, stream: Optional[int] = None):
+    """Gradients of gformer_packed_attn_fwd from what it wrote (out, lse) and the gradient dout of out."""
+    import torch
+
+    dtype = _tensors(q, 3, q=q, k=k, v=v, out=out, dout=dout, dq=dq, dk=dk, dv=dv)
+    _packed_shapes(q, k, v, cu_q, cu_k, out=out, dout=dout, dq=dq)
+    if dk.shape != k.shape or dv.shape != v.shape:
+        raise ValueError("dk and dv must be of k's shape")
+    T, H, d = q.shape
+    if lse.device != q.device or lse.dtype != torch.float32 or lse.shape != (H, T) or not lse.is_contiguous():
+        raise ValueError("lse must be dense fp32 [H, total_q]")
+    p = make_packed_params(dtype, softmax_scale, zero_tail, q_stride=_row_strides("q", q), k_stride=_row_strides("k", k),
+                           v_stride=_row_strides("v", v), o_stride=_row_strides("out", out), do_stride=_row_strides("dout", dout),
+                           dq_stride=_row_strides("dq", dq), dk_stride=_row_strides("dk", dk), dv_stride=_row_strides("dv", dv))
+    sizes = (cu_q.numel() - 1, T, k.shape[0], H, k.shape[1], d)
+    need = gformer_packed_attn_bwd_workspace_bytes(T, k.shape[0], *sizes[:1], *sizes[3:], p)
+    workspace, at, held = _scratch(need, workspace, q, stream)
+    _call(lib().gformer_packed_attn_bwd, q, stream, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(),
+          dout.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), cu_q.data_ptr(),
+          None if cu_k is None else cu_k.data_ptr(), *sizes, ctypes.byref(p), at, held)
+    return dq, dk, dv
+
+
+def gformer_paged_decode_workspace_bytes(B, H, Hkv, d, max_len, params=None, table_width=None) -> int:
+    """For sequences of up to max_len tokens, the new one included (0: what a table of table_width pages holds)."""
+    p = params or make_paged_params()
+    if table_width is None:
+        table_width = -(-max_len // p.page_size)
+    return int(lib().gformer_paged_decode_workspace_bytes(B, H, Hkv, d, table_width, max_len, ctypes.byref(p)))
+
+
+def _paged(like, kpages, vpages, Hkv, d):
+    _tensors(like, 4, kpages=kpages, vpages=vpages)
+    if kpages.shape != vpages.shape or kpages.shape[1] != Hkv or kpages.shape[3] != d:
+        raise ValueError("kpages and vpages must be [n_pages, Hkv, page_size, d]")
+    return {"page_size": kpages.shape[2], "kpage_stride": _row_strides("kpages", kpages),
+            "vpage_stride": _row_strides("vpages", vpages)}
+
+
+def gformer_paged_decode(q, k, v, out, kpages, vpages, table, lens, *, max_len=0, softmax_scale=1.0, workspace=None,
+                         stream: Optional[int] = None):
+    """One new token of every sequence over a paged cache, on device tensors: q, out [B, H, d]; k, v [B, Hkv, d], the new
+    keys and values, which go to their slots (both None: they are there already); kpages, vpages
+    [n_pages, Hkv, page_size, d] (any strides with a contiguous last dimension); table int32 [B, table_width]; lens int32
+    [B], the tokens in the cache before the call (negative: an idle row).  max_len bounds the longest
+    sequence's tokens, the new one included (0: what the table holds)."""
+    if (k is None) != (v is None):
+        raise ValueError("k and v come together, or neither")
+    new = {} if k is None else {"k": k, "v": v}
+    dtype = _tensors(q, 3, q=q, out=out, **new)
+    B, H, d = q.shape
+    Hkv = kpages.shape[1] if kpages.dim() == 4 else 0
+    if out.shape != q.shape or any(x.shape != (B, Hkv, d) for x in new.values()):
+        raise ValueError("q and out must be [B, H, d], k and v [B, Hkv, d]")
+    _numbers(q, (B, None), table=table)
+    _numbers(q, (B,), lens=lens)
+    strides = {f"{n}_stride": _row_strides(n, t) for n, t in {"q": q, **new}.items()}
+    p = make_paged_params(dtype, softmax_scale=softmax_scale, o_stride=_row_strides("out", out), **strides,
+                          **_paged(q, kpages, vpages, Hkv, d))
+    width = table.shape[1]
+    need = gformer_paged_decode_workspace_bytes(B, H, Hkv, d, max_len, p, width)
+    workspace, at, held = _scratch(need, workspace, q, stream)
+    _call(lib().gformer_paged_decode, q, stream, q.data_ptr(), None if k is None else k.data_ptr(),
+          None if v is None else v.data_ptr(), out.data_ptr(), kpages.data_ptr(), vpages.data_ptr(), table.data_ptr(),
+          lens.data_ptr(), B, H, Hkv, d, kpages.shape[0], width, int(max_len), ctypes.byref(p), at, held)
+    return out
+
+
+def gformer_paged_fill(k, v, kpages, vpages, table, start, cu, *, stream: Optional[int] = None):
+    """Packed keys and values [total, Hkv, d] into a paged cache: row i of sequence s becomes its token start[s] + i.
+    table int32 [n_seqs, table_width], start int32 [n_seqs], cu int32 [n_seqs + 1]."""
+    dtype = _tensors(k, 3, k=k, v=v)
+    if k.shape != v.shape or cu.numel() < 1:
+        raise ValueError("k and v must be [total, Hkv, d], cu [n_seqs + 1]")
+    T, Hkv, d = k.shape
+    n = cu.numel() - 1
+    _numbers(k, (n + 1,), cu=cu)
+    _numbers(k, (n, None), table=table)
+    _numbers(k, (n,), start=start)
+    p = make_paged_params(dtype, k_stride=_row_strides("k", k), v_stride=_row_strides("v", v), **_paged(k, kpages, vpages, Hkv, d))
+    _call(lib().gformer_paged_fill, k, stream, k.data_ptr(), v.data_ptr(), kpages.data_ptr(), vpages.data_ptr(), table.data_ptr(),
+          start.data_ptr(), cu.data_ptr(), n, T, Hkv, d, kpages.shape[0], table.shape[1], ctypes.byref(p))
+
+
+def gformer_pages_copy(kpages, vpages, src, dst, *, stream: Optional[int] = None):
+    """Pages src[i] -> dst[i] of a paged cache (int32 device tensors), whole, keys and values; no destination may be another
+    one or another's source."""
+    dtype = _tensors(kpages, 4, kpages=kpages, vpages=vpages)
+    P, Hkv, _, d = kpages.shape
+    _numbers(kpages, (None,), src=src)
+    _numbers(kpages, (src.numel(),), dst=dst)
+    p = make_paged_params(dtype, **_paged(kpages, kpages, vpages, Hkv, d))
+    _call(lib().gformer_pages_copy, kpages, stream, kpages.data_ptr(), vpages.data_ptr(), src.data_ptr(), dst.data_ptr(),
+          src.numel(), Hkv, d, P, ctypes.byref(p))
 
 
 def gformer_partition_balance(p, size, flops_per0, flops_per1, perf0, perf1):

@@ -65,6 +65,8 @@ struct SideStream {
 SideStream g_side[kMaxDevices];
 std::mutex g_enqueue_mutex;
 
+}  // namespace
+
 // The device a call works on: the current one, which must also be the device of the caller's
 // stream when that is not the null stream (kernels launched on a stream run on the stream's
 // device, while per-device state below is looked up by the current one).
@@ -83,6 +85,8 @@ hipError_t call_device(hipStream_t s, int* dev) {
   if (*dev < 0 || *dev >= kMaxDevices) return hipErrorInvalidDevice;
   return hipSuccess;
 }
+
+namespace {
 
 hipError_t side_stream_for_current_device(hipStream_t caller, SideStream** out) {
   int dev = 0;

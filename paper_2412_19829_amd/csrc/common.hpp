@@ -229,5 +229,7 @@ constexpr int kMfmaWindowRows = 128;    // query rows per workgroup, MFMA window
 constexpr int kMfmaWindowThreads = 256;
 int mfma_linear_threads(int d, int query_halves);   // of a read-out's workgroup
 int device_compute_units();   // of the current device; 256 (MI355X) in a process without one
+// The device a call works on; an error where the stream is another one's.
+hipError_t call_device(hipStream_t s, int* dev);
 
 }  // namespace gformer

@@ -1,0 +1,154 @@
+"""A paged key-value cache: which sequence holds which pages (host), and the tensors that the library's
+entry points take (device).
+
+A sequence's row of `table` lists its pages, `lens` its tokens.  Pages are counted by the sequences that hold them: a
+fork shares the full ones, which nobody writes again, and takes a copy of the last one if that is partly filled.
+Every change of the bookkeeping is checked before it is made, so a refused call leaves the cache as it was.
+The copies run on torch's current stream; `table` and `lens` are uploaded in order with it.
+"""
+from __future__ import annotations
+
+import torch
+
+from . import binding as gb
+
+
+class PagedCache:
+    """Room for `n_pages` pages of `page_size` tokens, for up to `max_seqs` sequences of up to `max_pages` pages, `n_heads` key
+    heads of size `d` in each of `layers` layers."""
+
+    def __init__(self, n_pages: int, page_size: int, n_heads: int, d: int, max_seqs: int, max_pages: int, *, layers: int = 1,
+                 dtype=torch.bfloat16, device="cuda"):
+        if min(n_pages, page_size, n_heads, d, max_seqs, max_pages, layers) < 1:
+            raise ValueError("sizes must be positive")
+        self.page_size, self.n_heads, self.max_pages = page_size, n_heads, max_pages
+        self.kpages = torch.zeros(n_pages, layers * n_heads, page_size, d, dtype=dtype, device=device)
+        self.vpages = torch.zeros_like(self.kpages)
+        self.table = torch.full((max_seqs, max_pages), -1, dtype=torch.int32, device=device)
+        self.lens = torch.full((max_seqs,), -1, dtype=torch.int32, device=device)   # -1: an idle row
+        self._held = [0] * n_pages                         # sequences that hold the page
+        self._free = list(range(n_pages - 1, -1, -1))      # the lowest last: taken first
+        self._pages = [None] * max_seqs                    # per sequence; None: no such sequence
+        self._len = [-1] * max_seqs
+
+    def layer(self, i: int):
+        """(kpages, vpages) of one layer, as views."""
+        heads = slice(i * self.n_heads, (i + 1) * self.n_heads)
+        return self.kpages[:, heads], self.vpages[:, heads]
+
+    @property
+    def free_pages(self) -> int:
+        return len(self._free)
+
+    def length(self, seq: int) -> int:
+        self._check(seq)
+        return self._len[seq]
+
+    def pages(self, seq: int) -> list:
+        self._check(seq)
+        return list(self._pages[seq])
+
+    def _check(self, seq):
+        if not 0 <= seq < len(self._pages) or self._pages[seq] is None:
+            raise ValueError(f"no sequence {seq}")
+
+    def _slot(self):
+        for s, p in enumerate(self._pages):
+            if p is None:
+                return s
+        raise RuntimeError("the cache holds as many sequences as it can")
+
+    def _take(self, n):
+        if n > len(self._free):
+            raise RuntimeError(f"the cache is full: {n} pages wanted, {len(self._free)} free")
+        taken = [self._free.pop() for _ in range(n)]
+        for p in taken:
+            self._held[p] = 1
+        return taken
+
+    def _upload(self):
+        rows = [(p or []) + [-1] * (self.max_pages - len(p or [])) for p in self._pages]
+        self.table.copy_(torch.tensor(rows, dtype=torch.int32))
+        self.lens.copy_(torch.tensor(self._len, dtype=torch.int32))
+
+    def _copy(self, pairs):
+        if pairs:
+            src, dst = torch.tensor(pairs, dtype=torch.int32).t().contiguous().to(self.table.device)
+            gb.gformer_pages_copy(self.kpages, self.vpages, src, dst)
+
+    def open(self, tokens: int = 0) -> int:
+        """A new sequence of `tokens` tokens, whose keys and values the caller writes (gformer_paged_fill)."""
+        n = -(-tokens // self.page_size)
+        if tokens < 0 or n > self.max_pages:
+            raise ValueError(f"a sequence has 0 to {self.max_pages * self.page_size} tokens")
+        seq = self._slot()
+        self._pages[seq], self._len[seq] = self._take(n), tokens
+        self._upload()
+        return seq
+
+    def fork(self, seq: int) -> int:
+        """A sequence that goes on from the same tokens."""
+        self._check(seq)
+        new, mine = self._slot(), self._pages[seq]
+        partly = self._len[seq] % self.page_size != 0
+        full = len(mine)
+        if partly or full * self.page_size > self._len[seq]:
+            full = self._len[seq] // self.page_size
+        own = self._take(1 if partly else 0)
+        if partly:
+            self._copy([(mine[full], own[0])])
+        for p in mine[:full]:
+            self._held[p] += 1
+        self._pages[new], self._len[new] = mine[:full] + own, self._len[seq]
+        self._upload()
+        return new
+
+    def free(self, seq: int) -> None:
+        """Gives a sequence's pages back, as far as no other holds them."""
+        self._check(seq)
+        for p in self._pages[seq]:
+            self._held[p] -= 1
+            if self._held[p] == 0:
+                self._free.append(p)
+        self._free.sort(reverse=True)
+        self._pages[seq], self._len[seq] = None, -1
+        self._upload()
+
+    def reserve(self, seqs) -> None:
+        """A slot for the next token of each of `seqs`: what a step needs before it writes."""
+        seqs = list(dict.fromkeys(seqs))
+        for s in seqs:
+            self._check(s)
+            if self._len[s] >= self.max_pages * self.page_size:
+                raise ValueError(f"sequence {s} is as long as it can be")
+        short = [s for s in seqs if len(self._pages[s]) * self.page_size == self._len[s]]
+        if short:
+            for s, p in zip(short, self._take(len(short))):
+                self._pages[s].append(p)
+            self._upload()
+
+    def advance(self, seqs) -> None:
+        """After a step that wrote one token of each of `seqs` in every layer."""
+        seqs = list(dict.fromkeys(seqs))
+        for s in seqs:
+            self._check(s)
+            if len(self._pages[s]) * self.page_size <= self._len[s]:
+                raise ValueError(f"sequence {s} has no slot for the token: reserve() comes first")
+        for s in seqs:
+            self._len[s] += 1
+        self._upload()
+
+    def compact(self) -> int:
+        """Moves the pages in use to the cache's front; returns how many were moved."""
+        used = sorted(p for p, n in enumerate(self._held) if n)
+        holes = [p for p in range(len(used)) if not self._held[p]]
+        moved = dict(zip(used[len(used) - len(holes):], holes))
+        self._copy(list(moved.items()))
+        for old, new in moved.items():
+            self._held[new], self._held[old] = self._held[old], 0
+        for pages in self._pages:
+            if pages:
+                pages[:] = [moved.get(p, p) for p in pages]
+        self._free = [p for p in range(len(self._held) - 1, -1, -1) if not self._held[p]]
+        self._upload()
+        return len(moved)

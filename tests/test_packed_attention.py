@@ -1,0 +1,288 @@
+"""Attention over packed sequences against the formulas in 64 bits, with bounds that count its roundings."""
+from __future__ import annotations
+
+import ctypes
+
+import pytest
+import torch
+
+from paper_2412_19829_amd import binding as gb
+from tests import packed_reference as ref
+
+gpu = pytest.mark.gpu
+NAN, INF = float("nan"), float("inf")
+
+
+# ---- the reference itself, and refusals (CPU) ------------------------------------------------------
+
+def test_reference_gradients_against_differences():
+    gen = torch.Generator().manual_seed(3)
+    q, k, v, g = (torch.randn(n, 8, dtype=torch.float64, generator=gen) for n in (5, 7, 7, 5))
+    got = ref.sequence(q, k, v, g, 0.7, "f32")
+    for name, x in (("dq", q), ("dk", k), ("dv", v)):
+        for at in [(0, 0), (2, 5), (4, 7)]:
+            step, loss = 1e-6, []
+            for sign in (1, -1):
+                y = x.clone()
+                y[at] += sign * step
+                args = {"dq": (y, k, v), "dk": (q, y, v), "dv": (q, k, y)}[name]
+                loss.append((ref.sequence(*args, None, 0.7, "f32")["out"][0] * g).sum())
+            assert abs((loss[0] - loss[1]) / (2 * step) - got[name][0][at]) < 1e-7
+
+
+A = 1 << 20   # an aligned address that nothing reads: every call below is refused on the host
+
+
+def fwd(p=None, q=A, k=2 * A, v=3 * A, out=4 * A, lse=5 * A, cu_q=6 * A, cu_k=0, n=2, tq=8, tk=8, H=4, Hkv=2, d=64):
+    p = p or gb.make_packed_params()
+    return gb.lib().gformer_packed_attn_fwd(q, k, v, out, lse, cu_q, cu_k, n, tq, tk, H, Hkv, d, ctypes.byref(p), None)
+
+
+def bwd(p=None, ws=7 * A, ws_bytes=1 << 20, dq=8 * A, dk=9 * A, dv=10 * A, lse=5 * A, cu_k=0, tq=8, tk=8, dout=11 * A):
+    p = p or gb.make_packed_params()
+    return gb.lib().gformer_packed_attn_bwd(A, 2 * A, 3 * A, 4 * A, lse, dout, dq, dk, dv, 6 * A, cu_k, 2, tq, tk, 4, 2, 64,
+                                            ctypes.byref(p), ws, ws_bytes, None)
+
+
+def wrong(**kw):
+    p = gb.make_packed_params()
+    for name, val in kw.items():
+        setattr(p, name, val if not isinstance(val, tuple) else (ctypes.c_int64 * 2)(*val))
+    return p
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(q=0), 1), (dict(out=0), 1), (dict(cu_q=0), 1), (dict(k=0), 1), (dict(q=A + 8), 1), (dict(cu_q=A + 2), 1), (dict(out=A), 1),
+    (dict(n=-1), 1), (dict(tq=-1), 1), (dict(H=3), 1), (dict(Hkv=0), 1), (dict(H=0), 1), (dict(d=96), 2), (dict(tk=9), 1),
+    (dict(p=wrong(struct_size=8)), 1), (dict(p=wrong(dtype=2)), 1), (dict(p=wrong(zero_tail=2)), 1), (dict(p=wrong(softmax_scale=NAN)), 1),
+    (dict(p=wrong(softmax_scale=INF)), 1), (dict(p=wrong(q_stride=(60, 64))), 1), (dict(p=wrong(q_stride=(256, -64))), 1),
+    (dict(p=wrong(k_stride=(32, 64))), 1), (dict(p=wrong(v_stride=((1 << 20) + 8, 64))), 2), (dict(tq=2 ** 31 - 1, tk=2 ** 31 - 1, H=256), 2),
+])
+def test_forward_refusals(kw, status):
+    assert fwd(**kw) == status
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(ws=0), 3), (dict(ws_bytes=127), 3), (dict(ws=A + 16), 1), (dict(dq=0), 1), (dict(lse=0), 1), (dict(dout=0), 1), (dict(dq=A), 1),
+    (dict(dk=9 * A, dv=9 * A), 1), (dict(dv=5 * A), 1), (dict(dk=A + 8), 1), (dict(tk=7), 1), (dict(p=wrong(dk_stride=(8, 64))), 1),
+])
+def test_backward_refusals(kw, status):
+    assert bwd(**kw) == status
+
+
+def test_empty_calls():
+    assert fwd(tq=0, tk=0, q=0, k=0, v=0, out=0, cu_q=0) == gb.GF_OK
+    assert bwd(tq=0, tk=0) == gb.GF_OK
+    assert gb.gformer_packed_attn_bwd_workspace_bytes(10, 10, 1, 4, 2, 64) == 256
+    assert gb.gformer_packed_attn_bwd_workspace_bytes(10, 10, 1, 4, 3, 64) == 0
+
+
+def test_binding_refuses_what_it_would_misread():
+    t = torch.zeros(4, 2, 64)
+    with pytest.raises(ValueError, match="device tensor"):
+        gb.gformer_packed_attn_fwd(t, t, t, t, torch.zeros(2, dtype=torch.int32))
+    with pytest.raises(ValueError, match="broadcast"):
+        gb._row_strides("q", t[:, :1].expand(4, 3, 64))
+    assert gb._row_strides("q", t[:1].as_strided((1, 2, 64), (0, 64, 1))) == [128, 64]
+
+
+# ---- GPU -------------------------------------------------------------------------------------------
+
+SHAPES = [
+    # lens_q, lens_k (None: the same)
+    ([1], None),
+    ([3, 1, 2], None),
+    ([0, 5, 0], None),
+    ([128], None),
+    ([127, 129, 64], None),
+    ([33, 300, 65], None),
+    ([1, 40, 0, 130], [77, 40, 9, 257]),       # queries behind keys that are there already
+    ([20, 140, 3], [5, 0, 2]),                 # queries that see nothing
+]
+
+
+def tensors(lens_q, lens_k, H, Hkv, d, dtype, seed, tail=0, layout="dense"):
+    gen = torch.Generator().manual_seed(seed)
+    make = lambda n, h: torch.randn(n, h, d, generator=gen).to(ref.TYPES[dtype]).cuda()
+    tq, tk = sum(lens_q) + tail, sum(lens_k) + tail
+    if layout == "fused" and tq == tk:         # one projection's output
+        x = make(tq, H + 2 * Hkv)
+        q, k, v = x[:, :H], x[:, H:H + Hkv], x[:, H + Hkv:]
+    else:
+        q, k, v = make(tq, H), make(tk, Hkv), make(tk, Hkv)
+        if layout == "heads":                  # [heads, rows, d] in memory
+            q, k, v = (x.transpose(0, 1).contiguous().transpose(0, 1) for x in (q, k, v))
+    return q, k, v, make(tq, H)
+
+
+def cu(lens):
+    return torch.tensor(ref.offsets(lens), dtype=torch.int32).cuda()
+
+
+def run(q, k, v, g, lens_q, lens_k, scale, zero_tail=0, fill=7.0, same=False):
+    out, dq, dk, dv = (torch.full(x.shape, fill, dtype=q.dtype, device="cuda") for x in (q, q, k, k))
+    lse = torch.full((q.shape[1], q.shape[0]), fill, device="cuda")
+    cq, ck = cu(lens_q), None if same else cu(lens_k)
+    gb.gformer_packed_attn_fwd(q, k, v, out, cq, ck, lse=lse, softmax_scale=scale, zero_tail=zero_tail)
+    gb.gformer_packed_attn_bwd(q, k, v, out, lse, g, dq, dk, dv, cq, ck, softmax_scale=scale, zero_tail=zero_tail)
+    torch.cuda.synchronize()
+    return {"out": out, "lse": lse, "dq": dq, "dk": dk, "dv": dv}
+
+
+def compare(got, want, lens_q, lens_k):
+    nq, nk = sum(lens_q), sum(lens_k)
+    for name, (x, bound) in want.items():
+        n = nk if name in ("dk", "dv") else nq
+        if name == "lse":
+            ref.check(got[name][:, :n], x[:, :n], bound[:, :n], name)
+        else:
+            ref.check(got[name][:n], x[:n], bound[:n], name)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("H,Hkv", [(2, 2), (6, 2), (4, 1)])
+@pytest.mark.parametrize("shape", range(len(SHAPES)))
+def test_values_and_gradients(dtype, d, H, Hkv, shape):
+    lens_q, lens_k = SHAPES[shape]
+    same = lens_k is None
+    lens_k = lens_q if same else lens_k
+    q, k, v, g = tensors(lens_q, lens_k, H, Hkv, d, dtype, 10 * shape + H, layout="fused" if same else "heads")
+    got = run(q, k, v, g, lens_q, lens_k, d ** -0.5, same=same)
+    compare(got, ref.packed(q, k, v, g, lens_q, lens_k, d ** -0.5, dtype), lens_q, lens_k)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("scale", [-0.2, 0.0, 1.5])
+def test_scales(dtype, scale):
+    lens = [70, 200]
+    q, k, v, g = tensors(lens, lens, 2, 1, 64, dtype, 5)
+    compare(run(q, k, v, g, lens, lens, scale), ref.packed(q, k, v, g, lens, lens, scale, dtype), lens, lens)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_many_short_sequences(dtype):
+    lens = [(7 * i) % 5 for i in range(300)]   # the search for a tile's sequence takes more than one step
+    q, k, v, g = tensors(lens, lens, 2, 2, 64, dtype, 6)
+    compare(run(q, k, v, g, lens, lens, 0.125), ref.packed(q, k, v, g, lens, lens, 0.125, dtype), lens, lens)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("zero", [0, 1])
+def test_rows_behind_the_last_sequence(dtype, zero):
+    lens, tail = [5, 130], 300
+    q, k, v, g = tensors(lens, lens, 2, 2, 64, dtype, 7, tail=tail)
+    for x in (q, k, v, g):
+        x[sum(lens):] = NAN
+    got = run(q, k, v, g, lens, lens, 0.125, zero_tail=zero)
+    compare(got, ref.packed(q[:135], k[:135], v[:135], g[:135], lens, lens, 0.125, dtype), lens, lens)
+    for name in ("out", "dq", "dk", "dv"):
+        assert (got[name][sum(lens):] == (0.0 if zero else 7.0)).all(), name
+    assert (got["lse"][:, sum(lens):] == 7.0).all()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("bad", [NAN, INF, -INF])
+def test_what_a_row_does_not_see_has_no_part_in_it(dtype, d, bad):
+    # sequence 0: a key and a value that only its later queries see, and a query and a gradient that are no part of what
+    # later keys get; sequence 1 sees nothing of either
+    lens, at = [150, 90], 70
+    q, k, v, g = tensors(lens, lens, 2, 1, d, dtype, 8)
+    clean = ref.packed(q, k, v, g, lens, lens, 0.1, dtype)
+    for name, x in (("k", k), ("v", v)):
+        kept = x[at].clone()
+        x[at] = bad
+        got = run(q, k, v, g, lens, lens, 0.1)
+        for rows in (slice(0, at), slice(150, 240)):
+            for n in ("out", "dq"):
+                ref.check(got[n][rows], clean[n][0][rows], clean[n][1][rows], f"{n} with {name} of a later key {bad}")
+            ref.check(got["lse"][:, rows], clean["lse"][0][:, rows], clean["lse"][1][:, rows], "lse")
+        x[at] = kept
+    for name, x in (("q", q), ("g", g)):
+        kept = x[at].clone()
+        x[at] = bad
+        got = run(q, k, v, g, lens, lens, 0.1)
+        for rows in (slice(at + 1, 150), slice(150, 240)):
+            for n in ("dk", "dv"):
+                ref.check(got[n][rows], clean[n][0][rows], clean[n][1][rows], f"{n} with {name} of an earlier query {bad}")
+        x[at] = kept
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_row_that_sees_no_number_is_none(dtype):
+    lens = [100]
+    q, k, v, g = tensors(lens, lens, 1, 1, 64, dtype, 9)
+    v[10] = NAN
+    out = run(q, k, v, g, lens, lens, 0.1)["out"]
+    assert torch.isnan(out[10:]).all() and not torch.isnan(out[:10]).any()
+
+
+@gpu
+def test_large_scores_and_offsets_out_of_range():
+    lens = [64, 200]
+    q, k, v, g = tensors(lens, lens, 2, 2, 64, "bf16", 11)
+    compare(run(q * 16, k * 16, v, g, lens, lens, 1.0), ref.packed(q * 16, k * 16, v, g, lens, lens, 1.0, "bf16"), lens, lens)
+    # offsets past the tensors, or descending: computed on what there is, nothing outside is touched
+    out = torch.zeros(264 + 64, 2, 64, dtype=q.dtype, device="cuda")
+    for bad in ([0, 64, 5000], [0, 300, 100], [-7, 64, 264]):
+        gb.gformer_packed_attn_fwd(q, k, v, out[:264], torch.tensor(bad, dtype=torch.int32).cuda())
+    torch.cuda.synchronize()
+    assert (out[264:] == 0).all()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_wrapper(dtype):
+    from paper_2412_19829_amd.autograd import gformer_packed_attention
+    lens, tail = [90, 1, 140], 20
+    q, k, v, g = tensors(lens, lens, 4, 2, 64, dtype, 12, tail=tail)
+    want = ref.packed(q, k, v, g, lens, lens, 0.125, dtype)
+    leaves = [x.clone().requires_grad_(True) for x in (q, k, v)]
+    out = gformer_packed_attention(*leaves, cu(lens), softmax_scale=0.125)
+    out.backward(g.transpose(0, 1).contiguous().transpose(0, 1))
+    for name, x in zip(("out", "dq", "dk", "dv"), (out, *(t.grad for t in leaves))):
+        ref.check(x, *want[name], name)
+    # a gradient that is one number broadcast, and views of one fused tensor as leaves
+    x = torch.cat([q, k, v], 1).requires_grad_(True)
+    gformer_packed_attention(x[:, :4], x[:, 4:6], x[:, 6:], cu(lens), softmax_scale=0.125).float().sum().backward()
+    want = ref.packed(q, k, v, torch.ones_like(q) * (torch.arange(251) < 231)[:, None, None].cuda(), lens, lens, 0.125, dtype)
+    for name, at in (("dq", slice(0, 4)), ("dk", slice(4, 6)), ("dv", slice(6, 8))):
+        ref.check(x.grad[:, at], *want[name], name)
+
+
+@gpu
+def test_captured_and_on_another_stream():
+    lens = [300, 41]
+    q, k, v, g = tensors(lens, lens, 4, 2, 128, "bf16", 13)
+    want = run(q, k, v, g, lens, lens, 0.1)
+    out, dq, dk, dv = (torch.empty_like(x) for x in (q, q, k, k))
+    lse = torch.empty(4, q.shape[0], device="cuda")
+    ws = torch.empty(gb.gformer_packed_attn_bwd_workspace_bytes(341, 341, 2, 4, 2, 128), dtype=torch.uint8, device="cuda")
+    offs = cu(lens)
+
+    def step():
+        gb.gformer_packed_attn_fwd(q, k, v, out, offs, lse=lse, softmax_scale=0.1)
+        gb.gformer_packed_attn_bwd(q, k, v, out, lse, g, dq, dk, dv, offs, softmax_scale=0.1, workspace=ws)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(3):
+        for x in (out, dq, dk, dv, lse):
+            x.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        for name, x in zip(("out", "dq", "dk", "dv", "lse"), (out, dq, dk, dv, lse)):
+            assert torch.equal(x, want[name]), name     # no atomics: equal calls give equal bits
+        run(q, k, v, g, lens, lens, 0.1)

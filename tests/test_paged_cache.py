@@ -1,0 +1,421 @@
+"""The paged cache: one new token over it, what fills and moves its pages, and its bookkeeping."""
+from __future__ import annotations
+
+import ctypes
+import math
+import random
+
+import pytest
+import torch
+
+from paper_2412_19829_amd import binding as gb
+from paper_2412_19829_amd.paged import PagedCache
+from tests import packed_reference as ref
+
+gpu = pytest.mark.gpu
+NAN = float("nan")
+A = 1 << 20
+
+
+# ---- refusals and bookkeeping (CPU) ----------------------------------------------------------------
+
+def wrong(**kw):
+    p = gb.make_paged_params()
+    for name, val in kw.items():
+        setattr(p, name, val if not isinstance(val, tuple) else (ctypes.c_int64 * len(val))(*val))
+    return p
+
+
+def decode(p=None, q=A, k=2 * A, v=3 * A, out=4 * A, kp=5 * A, vp=6 * A, table=7 * A, lens=8 * A, B=2, H=4, Hkv=2, d=64, pages=9,
+           width=4, max_len=0, ws=9 * A, ws_bytes=1 << 30):
+    p = p or gb.make_paged_params()
+    return gb.lib().gformer_paged_decode(q, k, v, out, kp, vp, table, lens, B, H, Hkv, d, pages, width, max_len, ctypes.byref(p), ws,
+                                         ws_bytes, None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(q=0), 1), (dict(k=0), 1), (dict(v=0), 1), (dict(lens=0), 1), (dict(table=0), 1), (dict(kp=0), 1), (dict(out=A), 1),
+    (dict(out=5 * A), 1), (dict(vp=5 * A), 1), (dict(q=A + 8), 1), (dict(lens=A + 1), 1), (dict(B=-1), 1), (dict(H=5), 1), (dict(Hkv=0), 1),
+    (dict(d=32), 2), (dict(pages=0), 1), (dict(pages=-1), 1), (dict(width=-1), 1), (dict(max_len=-1), 1), (dict(width=1 << 25), 2),
+    (dict(p=wrong(page_size=4)), 2), (dict(p=wrong(page_size=0)), 1), (dict(p=wrong(page_size=48)), 2), (dict(p=wrong(page_size=1 << 17)), 2),
+    (dict(p=wrong(struct_size=4)), 1), (dict(p=wrong(dtype=7)), 1), (dict(p=wrong(softmax_scale=NAN)), 1), (dict(p=wrong(q_stride=(60, 64))), 1),
+    (dict(p=wrong(kpage_stride=(8192, 4096, 32))), 1), (dict(p=wrong(vpage_stride=(8192, -64, 64))), 1),
+    (dict(width=64, ws=0), 3), (dict(width=64, ws_bytes=255), 3), (dict(width=64, ws=A + 16), 1), (dict(B=1 << 30, H=4), 2),
+])
+def test_decode_refusals(kw, status):
+    assert decode(**kw) == status
+
+
+def test_fill_and_copy_refusals():
+    p = gb.make_paged_params()
+    fill = lambda *a, p=p: gb.lib().gformer_paged_fill(*a, ctypes.byref(p), None)
+    ptrs = [i * A for i in range(1, 8)]
+    assert fill(*ptrs, 2, 0, 2, 64, 9, 4) == gb.GF_OK and fill(*ptrs, 0, 5, 2, 64, 9, 4) == gb.GF_OK
+    for i in range(7):
+        assert fill(*(0 if i == j else x for j, x in enumerate(ptrs)), 2, 5, 2, 64, 9, 4) == gb.GF_ERR_INVALID_ARG
+    assert fill(*ptrs, -1, 5, 2, 64, 9, 4) == fill(*ptrs, 2, -5, 2, 64, 9, 4) == gb.GF_ERR_INVALID_ARG
+    assert fill(*ptrs, 2, 5, 2, 64, 9, 4, p=wrong(page_size=12)) == gb.GF_ERR_UNSUPPORTED
+    copy = lambda *a, p=p: gb.lib().gformer_pages_copy(*a, ctypes.byref(p), None)
+    assert copy(A, 2 * A, 3 * A, 4 * A, 0, 2, 64, 9) == gb.GF_OK
+    assert copy(0, 2 * A, 3 * A, 4 * A, 1, 2, 64, 9) == copy(A, A, 3 * A, 4 * A, 1, 2, 64, 9) == gb.GF_ERR_INVALID_ARG
+    assert copy(A, 2 * A, 3 * A, 4 * A, -1, 2, 64, 9) == copy(A, 2 * A, 3 * A, 0, 1, 2, 64, 9) == gb.GF_ERR_INVALID_ARG
+    assert copy(A, 2 * A, 3 * A, 4 * A, 1, 2, 80, 9) == copy(A, 2 * A, 3 * A, 4 * A, 1 << 30, 2, 64, 9) == gb.GF_ERR_UNSUPPORTED
+
+
+def test_workspace_is_what_the_chunks_take():
+    b = gb.gformer_paged_decode_workspace_bytes
+    assert b(1, 4, 2, 64, 100) == 0                     # one chunk: nothing to join
+    assert b(1, 4, 3, 64, 1 << 15) == 0                 # refused
+    need = b(1, 32, 8, 128, 1 << 15)
+    assert need % 256 == 0 and need >= 2 * 32 * 130 * 4
+    assert b(1, 32, 8, 128, 0, table_width=1 << 9) == need
+
+
+class Copies:
+    """What the cache would have copied."""
+    def __init__(self, monkeypatch):
+        self.pairs = []
+        monkeypatch.setattr(gb, "gformer_pages_copy", lambda k, v, src, dst: self.pairs.append((src.tolist(), dst.tolist())))
+
+
+def cache(**kw):
+    return PagedCache(**{**dict(n_pages=12, page_size=8, n_heads=2, d=64, max_seqs=4, max_pages=5, device="cpu"), **kw})
+
+
+def test_bookkeeping(monkeypatch):
+    done, c = Copies(monkeypatch), cache()
+    a = c.open(20)
+    assert c.pages(a) == [0, 1, 2] and c.length(a) == 20 and c.lens.tolist() == [20, -1, -1, -1]
+    b = c.fork(a)                                       # two full pages shared, the third copied
+    assert c.pages(b) == [0, 1, 3] and done.pairs == [([2], [3])] and c.free_pages == 8
+    for _ in range(4):
+        c.reserve([a])
+        c.advance([a])
+    assert c.length(a) == 24 and c.pages(a) == [0, 1, 2]
+    d = c.fork(a)                                       # every page full: nothing copied
+    assert c.pages(d) == [0, 1, 2] and len(done.pairs) == 1
+    c.reserve([a, d, a])
+    assert c.pages(a)[3] == 4 and c.pages(d)[3] == 5
+    e = c.fork(a)                                       # reserved but not written: not part of the fork
+    assert c.pages(e) == [0, 1, 2]
+    with pytest.raises(RuntimeError, match="sequences"):
+        c.open(1)
+    c.free(a)
+    assert c.table[a].tolist() == [-1] * 5 and c.lens[a] == -1 and c.free_pages == 7
+    c.free(b)
+    assert c.free_pages == 8 and sorted(p for p, n in enumerate(c._held) if n) == [0, 1, 2, 5]
+    assert c.compact() == 1 and done.pairs[-1] == ([5], [3]) and c.pages(d) == [0, 1, 2, 3]
+    assert c.compact() == 0 and c.table[d].tolist() == [0, 1, 2, 3, -1]
+    with pytest.raises(ValueError, match="no sequence"):
+        c.free(a)
+    with pytest.raises(ValueError, match="no slot"):
+        c.advance([e])
+
+
+def test_a_refused_call_changes_nothing(monkeypatch):
+    Copies(monkeypatch)
+    c = cache(n_pages=4)
+    a = c.open(30)
+    before = (list(c._held), list(c._free), [list(p or []) for p in c._pages], list(c._len))
+    for call in (lambda: c.open(8), lambda: c.fork(a), lambda: c.open(41), lambda: c.open(-1), lambda: c.reserve([a, 3])):
+        with pytest.raises((RuntimeError, ValueError)):
+            call()
+        assert before == (c._held, c._free, [list(p or []) for p in c._pages], c._len)
+
+
+def test_random_lives(monkeypatch):
+    Copies(monkeypatch)
+    rng, c, live = random.Random(5), cache(n_pages=20, max_seqs=6), []
+    for _ in range(500):
+        try:
+            what = rng.choice(["open", "fork", "free", "step", "step", "step", "compact"])
+            if what == "open":
+                live.append(c.open(rng.randint(0, 40)))
+            elif what == "fork" and live:
+                live.append(c.fork(rng.choice(live)))
+            elif what == "free" and live:
+                c.free(live.pop(rng.randrange(len(live))))
+            elif what == "step" and live:
+                some = rng.sample(live, rng.randint(1, len(live)))
+                c.reserve(some)
+                c.advance(some)
+            elif what == "compact":
+                c.compact()
+                assert sorted(c._free) == list(range(20 - len(c._free), 20))
+        except (RuntimeError, ValueError):
+            pass
+        held = [0] * 20
+        for s in live:
+            for p in c.pages(s):
+                held[p] += 1
+            assert len(c.pages(s)) * 8 >= c.length(s)
+        assert held == c._held and sorted(c._free) == [p for p, n in enumerate(held) if not n]
+        # what a sequence still writes into is its own
+        assert all(held[c.pages(s)[c.length(s) // 8]] == 1 for s in live if c.length(s) // 8 < len(c.pages(s)))
+
+
+# ---- GPU -------------------------------------------------------------------------------------------
+
+def make(lens, H, Hkv, d, page, dtype, seed, new=True, width=None, fill=NAN, layout="heads"):
+    """A cache whose pages lie anywhere, with `fill` in every slot that holds no token, and the new token."""
+    gen = torch.Generator().manual_seed(seed)
+    dt = ref.TYPES[dtype]
+    need = [max(1, -(-(x + 1) // page)) for x in lens]
+    pages, width = sum(need) + 2, width or max(need)
+    order = torch.randperm(pages, generator=gen).tolist()
+    shape = (pages, Hkv, page, d) if layout == "heads" else (pages, page, Hkv, d)
+    kp, vp = (torch.full(shape, fill, dtype=dt) for _ in range(2))
+    if layout != "heads":
+        kp, vp = kp.transpose(1, 2), vp.transpose(1, 2)
+    table = torch.full((len(lens), width), -1, dtype=torch.int32)
+    ks, vs = [], []
+    for b, n in enumerate(lens):
+        own = [order.pop() for _ in range(need[b])]
+        table[b, :len(own)] = torch.tensor(own)
+        k, v = (torch.randn(max(n, 0), Hkv, d, generator=gen).to(dt) for _ in range(2))
+        for t in range(n):
+            kp[own[t // page], :, t % page], vp[own[t // page], :, t % page] = k[t], v[t]
+        ks.append(k)
+        vs.append(v)
+    q = torch.randn(len(lens), H, d, generator=gen).to(dt)
+    k, v = (torch.randn(len(lens), Hkv, d, generator=gen).to(dt) if new else None for _ in range(2))
+    dev = lambda t: None if t is None else t.cuda()
+    return dict(q=dev(q), k=dev(k), v=dev(v), kpages=kp.cuda(), vpages=vp.cuda(), table=table.cuda(),
+                lens=torch.tensor(lens, dtype=torch.int32).cuda()), ks, vs
+
+
+def expect(x, ks, vs, scale, dtype):
+    """out and its bound, from the sequences' rows."""
+    q = x["q"].cpu()
+    out, bound = torch.zeros(q.shape, dtype=torch.float64), torch.zeros(q.shape, dtype=torch.float64)
+    for b in range(q.shape[0]):
+        k, v = ks[b], vs[b]
+        if x["k"] is not None and x["lens"][b] >= 0:
+            k, v = torch.cat([k, x["k"][b:b + 1].cpu()]), torch.cat([v, x["v"][b:b + 1].cpu()])
+        if len(k):
+            # numerator and denominator see the same rounded weights, so the bound has the weight's rounding twice
+            G = q.shape[1] // k.shape[1]
+            for h in range(q.shape[1]):
+                kh, vh = k[:, h // G].double(), v[:, h // G].double()
+                got = ref.sequence(q[b, h:h + 1].double(), kh, vh, None, scale, dtype)
+                p = torch.softmax(scale * (q[b, h].double() @ kh.T), 0)
+                out[b, h] = got["out"][0][0]
+                bound[b, h] = got["out"][1][0] + ref.HALF[dtype] * (p @ vh.abs()) + 64 * ref.U * (p @ vh.abs())
+    return out, bound
+
+
+def step(x, scale, **kw):
+    out = torch.full_like(x["q"], 7.0)
+    gb.gformer_paged_decode(x["q"], x["k"], x["v"], out, x["kpages"], x["vpages"], x["table"], x["lens"], softmax_scale=scale, **kw)
+    torch.cuda.synchronize()
+    return out
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("H,Hkv", [(3, 3), (8, 2), (16, 1), (40, 2)])
+@pytest.mark.parametrize("page", [8, 64])
+@pytest.mark.parametrize("new", [True, False])
+def test_decode(dtype, d, H, Hkv, page, new):
+    lens = [0, 1, 7, 8, 31, 32, 33, 127, 128, 700]
+    x, ks, vs = make(lens, H, Hkv, d, page, dtype, H + page, new, layout="heads" if page == 8 else "tokens")
+    before = (x["kpages"].clone(), x["vpages"].clone())
+    got = step(x, d ** -0.5)
+    ref.check(got, *expect(x, ks, vs, d ** -0.5, dtype), "out")
+    for pages, old, rows in ((x["kpages"], before[0], x["k"]), (x["vpages"], before[1], x["v"])):
+        if new:                                          # the new token's slot, and nothing else
+            for b, t in enumerate(lens):
+                old[x["table"][b, t // page].long(), :, t % page] = rows[b]
+        assert torch.equal(pages.view(torch.int16 if dtype == "bf16" else torch.int32), old.view(torch.int16 if dtype == "bf16" else torch.int32))
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("scale", [-0.3, 0.0, 2.0])
+def test_decode_scales(dtype, scale):
+    x, ks, vs = make([40, 300], 4, 2, 64, 16, dtype, 3)
+    ref.check(step(x, scale), *expect(x, ks, vs, scale, dtype), "out")
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_long_and_short_sequences_in_one_call(dtype):
+    lens = [9000, 3, 2500, 0]
+    x, ks, vs = make(lens, 8, 2, 128, 128, dtype, 4)
+    want = expect(x, ks, vs, 0.09, dtype)
+    ref.check(step(x, 0.09), *want, "bound by the table")
+    ref.check(step(x, 0.09, max_len=9001), *want, "bound by max_len")
+    # a bound that is too small: the sequence is idle, the others are not
+    got = step(x, 0.09, max_len=2501)
+    assert (got[0] == 0).all()
+    ref.check(got[1:], want[0][1:], want[1][1:], "the others")
+
+
+@gpu
+def test_idle_rows_and_pages_that_are_none():
+    lens = [-1, 20, 64, -2147483648, 2147483647, 30]
+    x, ks, vs = make([max(0, min(n, 64)) for n in lens], 4, 2, 64, 16, "f32", 5)
+    x["lens"] = torch.tensor(lens, dtype=torch.int32).cuda()
+    x["table"] = torch.cat([x["table"][:, :4], torch.full((6, 0), -1, dtype=torch.int32).cuda()], 1).contiguous()
+    before = x["kpages"].clone()
+    # sequence 2 is full (four pages of 16): no room for a token
+    x["table"][5, 0] = 1 << 30                           # the first 16 tokens of sequence 5 are not there
+    got = step(x, 0.125)
+    for b in (0, 2, 3, 4):
+        assert (got[b] == 0).all(), b
+    want = expect({**x, "lens": [20, 30], **{n: x[n][[1, 5]] for n in "qkv"}}, [ks[1], ks[5][16:]], [vs[1], vs[5][16:]], 0.125, "f32")
+    ref.check(got[[1, 5]], *want, "out")
+    changed = (torch.nan_to_num(x["kpages"], 9.0) != torch.nan_to_num(before, 9.0)).any(-1).any(1).nonzero().tolist()
+    assert sorted(changed) == sorted([[int(x["table"][1, 1]), 4], [int(x["table"][5, 1]), 14]])
+    # the new token's page is none: it is seen, and not written
+    x["table"][1, 1] = -5
+    before = x["kpages"].clone()
+    got = step(x, 0.125)
+    want = expect({**x, "lens": [16], **{n: x[n][[1]] for n in "qkv"}}, [ks[1][:16]], [vs[1][:16]], 0.125, "f32")
+    ref.check(got[[1]], *want, "out")
+    assert torch.equal(torch.nan_to_num(x["kpages"], 9.0), torch.nan_to_num(before, 9.0))
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_fill(dtype):
+    gen = torch.Generator().manual_seed(1)
+    lens, start, page, Hkv, d = [5, 0, 70, 33, 9], [0, 3, 30, -4, 60], 16, 3, 64
+    k, v = (torch.randn(sum(lens) + 40, 2 * Hkv, d, generator=gen).to(ref.TYPES[dtype]).cuda()[:, i::2] for i in range(2))
+    width, pages = 5, 30
+    table = torch.randperm(pages, generator=gen)[:25].view(5, 5).to(torch.int32)
+    table[2, 3], table[3, 0] = pages, -1
+    kp, vp = (torch.zeros(pages, page, Hkv, d, dtype=k.dtype).cuda().transpose(1, 2) for _ in range(2))
+    want = [kp.clone(), vp.clone()]
+    at = 0
+    for s, n in enumerate(lens):
+        for i in range(n):
+            t = start[s] + i
+            if 0 <= t < width * page and 0 <= table[s, t // page] < pages:
+                for w, x in zip(want, (k, v)):
+                    w[int(table[s, t // page]), :, t % page] = x[at + i]
+        at += n
+    gb.gformer_paged_fill(k, v, kp, vp, table.cuda(), torch.tensor(start, dtype=torch.int32).cuda(),
+                          torch.tensor(ref.offsets(lens), dtype=torch.int32).cuda())
+    torch.cuda.synchronize()
+    assert torch.equal(kp, want[0]) and torch.equal(vp, want[1])
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,page", [(64, 8), (128, 64), (64, 512)])
+def test_copy(dtype, d, page):
+    gen = torch.Generator().manual_seed(2)
+    kp, vp = (torch.randn(9, 3, page, d, generator=gen).to(ref.TYPES[dtype]).cuda() for _ in range(2))
+    vp = vp.transpose(1, 2).contiguous().transpose(1, 2)
+    want = [kp.clone(), vp.clone()]
+    src, dst = [8, 1, 7, 3, -1, 2], [0, 4, 9, 3, 5, 6]     # 9 and -1 are no pages; 3 onto itself
+    for w in want:
+        for s, t in ((8, 0), (1, 4), (2, 6)):
+            w[t] = w[s].clone()
+    gb.gformer_pages_copy(kp, vp, *(torch.tensor(x, dtype=torch.int32).cuda() for x in (src, dst)))
+    torch.cuda.synchronize()
+    assert torch.equal(kp, want[0]) and torch.equal(vp, want[1])
+
+
+@gpu
+def test_pages_past_32_bit_offsets():
+    page, Hkv, d, pages = 64, 8, 128, (1 << 31) // (64 * 8 * 128) + 40
+    kp, vp = (torch.empty(pages, Hkv, page, d, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    gen = torch.Generator().manual_seed(6)
+    k, v = (torch.randn(150, Hkv, d, generator=gen).bfloat16().cuda() for _ in range(2))
+    q = torch.randn(1, 32, d, generator=gen).bfloat16().cuda()
+    table = torch.tensor([[pages - 1, pages - 3, pages - 2]], dtype=torch.int32).cuda()
+    zero = torch.zeros(1, dtype=torch.int32).cuda()
+    gb.gformer_paged_fill(k[:149], v[:149], kp, vp, table, zero, torch.tensor([0, 149], dtype=torch.int32).cuda())
+    out = torch.empty_like(q)
+    gb.gformer_paged_decode(q, k[149:], v[149:], out, kp, vp, table, zero + 149, softmax_scale=0.1)
+    x = dict(q=q, k=k[149:], v=v[149:], lens=[149])
+    want = expect(x, [k[:149].cpu()], [v[:149].cpu()], 0.1, "bf16")
+    ref.check(out, *want, "out")
+    gb.gformer_pages_copy(kp, vp, table[0, :2].contiguous(), torch.tensor([pages - 4, 0], dtype=torch.int32).cuda())
+    moved = torch.tensor([[pages - 4, 0, pages - 2]], dtype=torch.int32).cuda()
+    again = torch.empty_like(q)
+    gb.gformer_paged_decode(q, None, None, again, kp, vp, moved, zero + 150, softmax_scale=0.1)
+    torch.cuda.synchronize()
+    ref.check(again, *want, "out from the copies")
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_prompt_then_tokens_then_a_fork(dtype):
+    """Two layers' worth of a serving run: prompts, tokens, a fork that goes its own way, a sequence freed, compaction, more
+    tokens; every row against the formulas over the sequence's own keys."""
+    H, Hkv, d, layers, scale = 6, 2, 64, 2, 0.125
+    gen = torch.Generator().manual_seed(7)
+    rnd = lambda *s: torch.randn(*s, generator=gen).to(ref.TYPES[dtype]).cuda()
+    c = PagedCache(40, 16, Hkv, d, 4, 8, layers=layers, dtype=ref.TYPES[dtype])
+    for pages in (c.kpages, c.vpages):
+        pages.fill_(NAN)
+    c.free(c.open(33))                                   # pages 0 .. 2 come first again
+    lens = [37, 50, 16]
+    seqs = [c.open(n) for n in lens]
+    cu = torch.tensor(ref.offsets(lens), dtype=torch.int32).cuda()
+    rows = [{} for _ in range(layers)]                   # per layer: sequence -> (keys, values)
+    start = torch.zeros(3, dtype=torch.int32).cuda()
+    for i in range(layers):
+        q, k, v = rnd(103, H, d), rnd(103, Hkv, d), rnd(103, Hkv, d)
+        out = gb.gformer_packed_attn_fwd(q, k, v, torch.empty_like(q), cu, softmax_scale=scale)
+        gb.gformer_paged_fill(k, v, *c.layer(i), c.table[:3], start, cu)
+        ref.check(out, *ref.packed(q, k, v, None, lens, lens, scale, dtype)["out"], "prompt")
+        for s, a, n in zip(seqs, ref.offsets(lens), lens):
+            rows[i][s] = (k[a:a + n].cpu(), v[a:a + n].cpu())
+
+    def tokens(live):
+        c.reserve(live)
+        for i in range(layers):
+            q, k, v = rnd(4, H, d), rnd(4, Hkv, d), rnd(4, Hkv, d)
+            got = gb.gformer_paged_decode(q, k, v, torch.empty_like(q), *c.layer(i), c.table, c.lens, softmax_scale=scale)
+            held = [rows[i].get(s, (torch.zeros(0, Hkv, d), torch.zeros(0, Hkv, d))) for s in range(4)]
+            x = dict(q=q, k=k, v=v, lens=c.lens.cpu())
+            ref.check(got, *expect(x, [h[0] for h in held], [h[1] for h in held], scale, dtype), "token")
+            for s in live:
+                rows[i][s] = tuple(torch.cat([old, new[s:s + 1].cpu()]) for old, new in zip(rows[i][s], (k, v)))
+        c.advance(live)
+
+    for _ in range(3):
+        tokens(seqs)
+    fork = c.fork(seqs[1])
+    for r in rows:
+        r[fork] = r[seqs[1]]
+    for _ in range(12):
+        tokens(seqs + [fork])
+    c.free(seqs[0])
+    for r in rows:
+        del r[seqs[0]]
+    assert c.compact() > 0
+    for _ in range(2):
+        tokens([seqs[1], seqs[2], fork])
+
+
+@gpu
+def test_captured_step():
+    x, ks, vs = make([300, 2000, 5], 8, 2, 128, 64, "bf16", 8)
+    want = expect(x, ks, vs, 0.1, "bf16")
+    out = torch.empty_like(x["q"])
+    need = gb.gformer_paged_decode_workspace_bytes(3, 8, 2, 128, 0, table_width=x["table"].shape[1])
+    spaces = [torch.empty(max(need, 1), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    graphs = []
+    for ws in spaces:
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            gb.gformer_paged_decode(**x, out=out, softmax_scale=0.1, workspace=ws)
+        torch.cuda.synchronize()
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            gb.gformer_paged_decode(**x, out=out, softmax_scale=0.1, workspace=ws)
+    first = None
+    for n in range(4):
+        out.zero_()
+        graphs[n % 2].replay()
+        torch.cuda.synchronize()
+        ref.check(out, *want, "replay")
+        first = out.clone() if first is None else first
+        assert torch.equal(out, first) and torch.equal(step(x, 0.1), first)
