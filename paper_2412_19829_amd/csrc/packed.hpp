@@ -89,16 +89,23 @@ template <typename T> __device__ __forceinline__ uint32_t not_finite(u32x4 x) {
   return r;
 }
 
-// A tile of R streamed rows on its way from memory to LDS, 16 bytes a lane.  Rows past `last` re-read it: in bounds, and
-// masked later.
+// A tile of R streamed rows on its way from memory to LDS, 16 bytes a lane: a uniform base and an offset of the thread's
+// own that never changes, so a load costs no address registers.  Rows past `last` re-read it: in bounds, and masked
+// later.
 template <typename T, int D, int R> struct Stage {
   static constexpr int C = D * (int)sizeof(T) / 16, STEP = kPackedThreads / C, N = R / STEP;
   static_assert(N * STEP == R, "whole rows");
   u32x4 x[N];
+  // rows r0 .. r0 + R - 1; r0 <= last.  A tile's rows lie within 2^28 bytes (the row stride is at most 2^20 elements)
   __device__ __forceinline__ void load(const T* base, int64_t stride, int r0, int last, int tid) {
+    const uint32_t bytes = (uint32_t)stride * sizeof(T), col = 16 * (tid % C), off = tid / C * bytes + col;
+    const char* from = reinterpret_cast<const char*>(base + r0 * stride);
+    const int left = min(last - r0, R - 1);
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-      x[i] = *reinterpret_cast<const u32x4*>(base + (int64_t)min(r0 + tid / C + i * STEP, last) * stride + (16 / (int)sizeof(T)) * (tid % C));
+    for (int i = 0; i < N; ++i) {
+      const int first = min(i * STEP, left);   // uniform
+      x[i] = *reinterpret_cast<const u32x4*>(from + (size_t)first * bytes + (size_t)min(off, (left - first) * bytes + col));
+    }
   }
   template <int ROW> __device__ __forceinline__ void store(T* tile, int tid) const {
 #pragma unroll
@@ -152,6 +159,21 @@ template <int D> struct Products<uint16_t, D> {
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks) s = mfma32(lds_read16(p + 16 * ks), r.x[ks], s);
     return s;
+  }
+  // the same with the resident rows in LDS too, at `own`
+  static __device__ __forceinline__ f32x16 scores_lds(const T* rows, const T* own, int lane) {
+    const int at = (lane & 31) * ROW + 8 * (lane >> 5);
+    f32x16 s;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) s = mfma32(lds_read16(rows + at + 16 * ks), lds_read16(own + at + 16 * ks), s);
+    return s;
+  }
+  static __device__ __forceinline__ void to_lds(const Resident& r, T* own, int lane) {
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks)
+      *reinterpret_cast<u32x4*>(own + (lane & 31) * ROW + 8 * (lane >> 5) + 16 * ks) = as_u32x4(r.x[ks]);
   }
   static __device__ __forceinline__ Weights weights(const float (&p)[16]) {
     Weights w;
@@ -304,11 +326,10 @@ template <typename T, int D> __device__ __forceinline__ void zero_rows(T* to, in
     *reinterpret_cast<u32x4*>(to + r * stride + (16 / (int)sizeof(T)) * (tid % C)) = u32x4{0, 0, 0, 0};
 }
 
-template <typename T, int D> struct PackedTiles {
-  using P = Products<T, D>;
-  T x[2][P::R * P::ROW], y[2][P::R * P::ROW];   // K and V, or Q and dO
-  float lse[2][P::R], delta[2][P::R];           // statistics of the streamed queries (dk and dv)
-  int odd[3];                                   // tile it holds values that are not finite: odd[it % 3]
+template <typename T, int D, int R> struct alignas(16) PackedTiles {
+  T x[2][R * Products<T, D>::ROW], y[2][R * Products<T, D>::ROW];   // K and V, or Q and dO
+  float lse[2][R], delta[2][R];   // statistics of the streamed queries (dk and dv)
+  int odd[3];                     // tile it holds values that are not finite: odd[it % 3]
 };
 
 }  // namespace

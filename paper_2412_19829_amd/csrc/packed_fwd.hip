@@ -12,7 +12,7 @@ template <typename T, int D> __global__ __launch_bounds__(kPackedThreads) void p
   using P = Products<T, D>;
   constexpr int R = P::R, ROW = P::ROW, NS = R / 32, MT = D / 32;
   extern __shared__ __align__(16) unsigned char smem_raw[];
-  auto& sm = *reinterpret_cast<PackedTiles<T, D>*>(smem_raw);
+  auto& sm = *reinterpret_cast<PackedTiles<T, D, Products<T, D>::R>*>(smem_raw);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, ln = lane & 31, lh = lane >> 5;
 
   // Heads fastest, the heads that share keys Hkv apart: workgroups are dealt to the 8 XCDs in turn, so that those of one key
@@ -121,7 +121,7 @@ template <typename T, int D> __global__ __launch_bounds__(kPackedThreads) void p
 }
 
 template <typename T, int D> hipError_t launch(const PackedArgs& a, hipStream_t s) {
-  const size_t smem = sizeof(PackedTiles<T, D>);
+  const size_t smem = sizeof(PackedTiles<T, D, Products<T, D>::R>);
   auto kern = packed_fwd_kernel<T, D>;
   if (hipError_t e = allow_lds(kern, smem); e != hipSuccess) return e;
   const int64_t tiles = packed_tiles(a.total_q, a.n_seqs, kPackedRows);
