@@ -120,13 +120,21 @@ template <typename T, int D, int R> struct Stage {
   }
 };
 
+// The largest of three (v_maximum3_f32), or no number.  Left to the compiler, which knows how long after a matrix
+// instruction its result may be read: an asm statement would hide the reader from it.
+__device__ __forceinline__ float maximum3(float a, float b, float c) {
+  return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c);
+}
+
 // The matrix products of one wave, for 32 resident and 32 streamed rows.
 template <typename T, int D> struct Products;
 
 template <int D> struct Products<uint16_t, D> {
   using T = uint16_t;
   static constexpr int R = 64;                               // streamed rows per tile
-  static constexpr int ROW = D == 128 ? D + 24 : D + 8;      // 12 (36) dwords mod 64: rows and transposes (mfma.hpp)
+  // row strides in LDS of tiles read by rows, transposed, and both ways (mfma.hpp): 4, 16 and 12 dwords mod 64 at d = 128,
+  // 36, 48 and 36 at d = 64
+  static constexpr int BY_ROWS = D + 8, TURNED = D + 32, BOTH = D == 128 ? D + 24 : D + 8;
   struct Resident { bf16x8 x[D / 16]; };
   struct Weights { bf16x8 x[2]; };
   // this lane's resident row: elements 16 ks + 8 lh .. +7; `flip` changes its sign
@@ -151,7 +159,7 @@ template <int D> struct Products<uint16_t, D> {
     return sum_over_halves(s);
   }
   // 32 streamed rows from `rows` against the resident ones
-  static __device__ __forceinline__ f32x16 scores(const T* rows, const Resident& r, int lane) {
+  template <int ROW> static __device__ __forceinline__ f32x16 scores(const T* rows, const Resident& r, int lane) {
     const T* p = rows + (lane & 31) * ROW + 8 * (lane >> 5);
     f32x16 s;
 #pragma unroll
@@ -161,19 +169,19 @@ template <int D> struct Products<uint16_t, D> {
     return s;
   }
   // the same with the resident rows in LDS too, at `own`
-  static __device__ __forceinline__ f32x16 scores_lds(const T* rows, const T* own, int lane) {
-    const int at = (lane & 31) * ROW + 8 * (lane >> 5);
+  template <int ROW> static __device__ __forceinline__ f32x16 scores_lds(const T* rows, const T* own, int lane) {
+    const int at = (lane & 31) * ROW + 8 * (lane >> 5), own_at = (lane & 31) * BY_ROWS + 8 * (lane >> 5);
     f32x16 s;
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[i] = 0.f;
 #pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks) s = mfma32(lds_read16(rows + at + 16 * ks), lds_read16(own + at + 16 * ks), s);
+    for (int ks = 0; ks < D / 16; ++ks) s = mfma32(lds_read16(rows + at + 16 * ks), lds_read16(own + own_at + 16 * ks), s);
     return s;
   }
   static __device__ __forceinline__ void to_lds(const Resident& r, T* own, int lane) {
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks)
-      *reinterpret_cast<u32x4*>(own + (lane & 31) * ROW + 8 * (lane >> 5) + 16 * ks) = as_u32x4(r.x[ks]);
+      *reinterpret_cast<u32x4*>(own + (lane & 31) * BY_ROWS + 8 * (lane >> 5) + 16 * ks) = as_u32x4(r.x[ks]);
   }
   static __device__ __forceinline__ Weights weights(const float (&p)[16]) {
     Weights w;
@@ -187,7 +195,7 @@ template <int D> struct Products<uint16_t, D> {
     return w;
   }
   // acc += rows^T weights
-  static __device__ __forceinline__ void product(f32x16 (&acc)[D / 32], const T* rows, const Weights& w, int lane) {
+  template <int ROW> static __device__ __forceinline__ void product(f32x16 (&acc)[D / 32], const T* rows, const Weights& w, int lane) {
     const T* p = rows + 4 * (lane >> 5) * ROW + lds_operand_tr_lane_offset(ROW, lane);
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb)
@@ -197,8 +205,9 @@ template <int D> struct Products<uint16_t, D> {
   }
   // The same row by row, for tiles that hold values which are not finite: zero times such a value is no number, so a row is
   // left out of a lane's sums, not weighted with zero, where first <= row < end does not hold.
-  static __device__ __forceinline__ void product_by_rows(f32x16 (&acc)[D / 32], const T* rows, const Weights& w, int first,
-                                                                   int end, int lane) {
+  template <int ROW>
+  static __device__ __forceinline__ void product_by_rows(f32x16 (&acc)[D / 32], const T* rows, const Weights& w, int first, int end,
+                                                         int lane) {
     const T* p = rows + 4 * (lane >> 5) * ROW + lds_operand_tr_lane_offset(ROW, lane);
 #pragma unroll
     for (int mt = 0; mt < D / 32; ++mt)                   // one tile of sums at a time: this is rare, and must not cost registers
@@ -231,7 +240,7 @@ template <int D> struct Products<uint16_t, D> {
 template <int D> struct Products<float, D> {
   using T = float;
   static constexpr int R = 32;
-  static constexpr int ROW = D + 4;   // 4 dwords mod 64: 16-byte row reads without conflicts
+  static constexpr int BY_ROWS = D + 4, TURNED = D + 4, BOTH = D + 4;   // 4 dwords mod 64: 16-byte row reads without conflicts
   struct Resident { f32x4_t x[D / 8]; };
   struct Weights { float x[16]; };
   static __device__ __forceinline__ f32x16 mfma(float a, float b, f32x16 c) {
@@ -250,7 +259,7 @@ template <int D> struct Products<float, D> {
       for (int j = 0; j < 4; ++j) s = fmaf(a.x[i][j], b.x[i][j], s);
     return sum_over_halves(s);
   }
-  static __device__ __forceinline__ f32x16 scores(const T* rows, const Resident& r, int lane) {
+  template <int ROW> static __device__ __forceinline__ f32x16 scores(const T* rows, const Resident& r, int lane) {
     const T* p = rows + (lane & 31) * ROW + 4 * (lane >> 5);
     f32x16 s;
 #pragma unroll
@@ -269,15 +278,16 @@ template <int D> struct Products<float, D> {
     for (int i = 0; i < 16; ++i) w.x[i] = p[i];
     return w;
   }
-  static __device__ __forceinline__ void product(f32x16 (&acc)[D / 32], const T* rows, const Weights& w, int lane) {
+  template <int ROW> static __device__ __forceinline__ void product(f32x16 (&acc)[D / 32], const T* rows, const Weights& w, int lane) {
     const T* p = rows + 4 * (lane >> 5) * ROW + (lane & 31);
 #pragma unroll
     for (int r = 0; r < 16; ++r)
 #pragma unroll
       for (int mt = 0; mt < D / 32; ++mt) acc[mt] = mfma(p[(8 * (r / 4) + r % 4) * ROW + 32 * mt], w.x[r], acc[mt]);
   }
-  static __device__ __forceinline__ void product_by_rows(f32x16 (&acc)[D / 32], const T* rows, const Weights& w, int first,
-                                                                   int end, int lane) {
+  template <int ROW>
+  static __device__ __forceinline__ void product_by_rows(f32x16 (&acc)[D / 32], const T* rows, const Weights& w, int first, int end,
+                                                         int lane) {
     const T* p = rows + 4 * (lane >> 5) * ROW + (lane & 31);
 #pragma unroll
     for (int mt = 0; mt < D / 32; ++mt)
@@ -298,11 +308,11 @@ template <int D> struct Products<float, D> {
 };
 
 // A wave's 32 resident rows of sums (lane: one row; register (mt, 4 g + i): column 32 mt + 8 g + 4 lh + i) times `by`,
-// through 32 ROW elements of LDS that are its own, to whole rows in memory.
+// through 32 BY_ROWS elements of LDS that are its own, to whole rows in memory.
 template <typename T, int D>
 __device__ __forceinline__ void put_rows(const f32x16 (&acc)[D / 32], float by, T* own, T* to, int64_t stride, int rows, int lane) {
   using P = Products<T, D>;
-  T* p = own + (lane & 31) * P::ROW + 4 * (lane >> 5);
+  T* p = own + (lane & 31) * P::BY_ROWS + 4 * (lane >> 5);
 #pragma unroll
   for (int mt = 0; mt < D / 32; ++mt)
 #pragma unroll
@@ -314,7 +324,7 @@ __device__ __forceinline__ void put_rows(const f32x16 (&acc)[D / 32], float by, 
   for (int i = 0; i < 32 * C / 64; ++i) {
     const int row = lane / C + i * (64 / C);
     if (row < rows)
-      *reinterpret_cast<u32x4*>(to + row * stride + E * (lane % C)) = *reinterpret_cast<const u32x4*>(own + row * P::ROW + E * (lane % C));
+      *reinterpret_cast<u32x4*>(to + row * stride + E * (lane % C)) = *reinterpret_cast<const u32x4*>(own + row * P::BY_ROWS + E * (lane % C));
   }
   wave_sync();
 }
@@ -326,8 +336,8 @@ template <typename T, int D> __device__ __forceinline__ void zero_rows(T* to, in
     *reinterpret_cast<u32x4*>(to + r * stride + (16 / (int)sizeof(T)) * (tid % C)) = u32x4{0, 0, 0, 0};
 }
 
-template <typename T, int D, int R> struct alignas(16) PackedTiles {
-  T x[2][R * Products<T, D>::ROW], y[2][R * Products<T, D>::ROW];   // K and V, or Q and dO
+template <typename T, int R, int XROW, int YROW> struct alignas(16) PackedTiles {
+  T x[2][R * XROW], y[2][R * YROW];   // K and V, or Q and dO, in rows of XROW and YROW elements
   float lse[2][R], delta[2][R];   // statistics of the streamed queries (dk and dv)
   int odd[3];                     // tile it holds values that are not finite: odd[it % 3]
 };

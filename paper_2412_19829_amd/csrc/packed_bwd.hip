@@ -19,16 +19,17 @@ constexpr int kQueryTile = 32;   // queries per tile of the dk, dv pass
 template <typename T, int D> constexpr int kStreams = kWaves<T, D>;
 // its value rows stay in LDS where their registers are wanted for the sums
 template <typename T, int D> constexpr bool kValuesInLds = sizeof(T) == 2 && D == 128;
+template <typename T, int D> using DqTiles = PackedTiles<T, kKeyTile<T, D>, Products<T, D>::BOTH, Products<T, D>::BY_ROWS>;
 template <typename T, int D> struct KeyTiles {
-  PackedTiles<T, D, kQueryTile> stream[kStreams<T, D>];
-  T v[kValuesInLds<T, D> ? kPackedRows * Products<T, D>::ROW : 1];
+  PackedTiles<T, kQueryTile, Products<T, D>::BOTH, Products<T, D>::BOTH> stream[kStreams<T, D>];
+  T v[kValuesInLds<T, D> ? kPackedRows * Products<T, D>::BY_ROWS : 1];
 };
 
 template <typename T, int D> __global__ __launch_bounds__(kPackedThreads, (kWaves<T, D>)) void packed_dq_kernel(PackedArgs a, int tiles) {
   using P = Products<T, D>;
-  constexpr int R = kKeyTile<T, D>, ROW = P::ROW, NS = R / 32, MT = D / 32;
+  constexpr int R = kKeyTile<T, D>, KROW = P::BOTH, VROW = P::BY_ROWS, NS = R / 32, MT = D / 32;
   extern __shared__ __align__(16) unsigned char smem_raw[];
-  auto& sm = *reinterpret_cast<PackedTiles<T, D, R>*>(smem_raw);
+  auto& sm = *reinterpret_cast<DqTiles<T, D>*>(smem_raw);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, ln = lane & 31, lh = lane >> 5;
 
   const int hh = blockIdx.x % a.H, kvh = hh % a.Hkv, h = kvh * (a.H / a.Hkv) + hh / a.Hkv;
@@ -80,7 +81,7 @@ template <typename T, int D> __global__ __launch_bounds__(kPackedThreads, (kWave
     const T *kt = sm.x[t & 1], *vt = sm.y[t & 1];
 #pragma unroll
     for (int n = 0; n < NS; ++n) {
-      const f32x16 s = P::scores(kt + 32 * n * ROW, q, lane), dp = P::scores(vt + 32 * n * ROW, g, lane);
+      const f32x16 s = P::template scores<KROW>(kt + 32 * n * KROW, q, lane), dp = P::template scores<VROW>(vt + 32 * n * VROW, g, lane);
       float ds[16];
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
@@ -88,14 +89,14 @@ template <typename T, int D> __global__ __launch_bounds__(kPackedThreads, (kWave
         if (MASK && t0 + 32 * n + 8 * (r / 4) + 4 * lh + r % 4 > seen) ds[r] = 0.f;
       }
       const typename P::Weights w = P::weights(ds);
-      if (MASK && sm.odd[t % 3]) P::product_by_rows(dq, kt + 32 * n * ROW, w, 0, seen + 1 - t0 - 32 * n, lane);
-      else P::product(dq, kt + 32 * n * ROW, w, lane);
+      if (MASK && sm.odd[t % 3]) P::template product_by_rows<KROW>(dq, kt + 32 * n * KROW, w, 0, seen + 1 - t0 - 32 * n, lane);
+      else P::template product<KROW>(dq, kt + 32 * n * KROW, w, lane);
     }
   };
   for (int t = 0; t < n_tiles; ++t) {
     const int t0 = t * R;
-    ks.template store<ROW>(sm.x[t & 1], tid);
-    vs.template store<ROW>(sm.y[t & 1], tid);
+    ks.template store<KROW>(sm.x[t & 1], tid);
+    vs.template store<VROW>(sm.y[t & 1], tid);
     if (t0 + R - 1 > i0 + off && ks.odd()) sm.odd[t % 3] = 1;   // some query of the workgroup does not see the whole tile
     if (tid == 0) sm.odd[(t + 1) % 3] = 0;
     lds_barrier();
@@ -109,13 +110,13 @@ template <typename T, int D> __global__ __launch_bounds__(kPackedThreads, (kWave
   }
   lds_barrier();
   if (q0 < nq)
-    put_rows<T, D>(dq, a.scale, reinterpret_cast<T*>(smem_raw) + wave * 32 * ROW, rows_of<T>(a.dq, a.dqs, qbase + q0, h), a.dqs[0],
+    put_rows<T, D>(dq, a.scale, reinterpret_cast<T*>(smem_raw) + wave * 32 * VROW, rows_of<T>(a.dq, a.dqs, qbase + q0, h), a.dqs[0],
                    min(32, nq - q0), lane);
 }
 
 template <typename T, int D> __global__ __launch_bounds__((kPackedThreads * kStreams<T, D>), (kWaves<T, D>)) void packed_dkdv_kernel(PackedArgs a, int tiles) {
   using P = Products<T, D>;
-  constexpr int R = kQueryTile, ROW = P::ROW, NS = R / 32, MT = D / 32;
+  constexpr int R = kQueryTile, ROW = P::BOTH, NS = R / 32, MT = D / 32;
   extern __shared__ __align__(16) unsigned char smem_raw[];
   constexpr int S = kStreams<T, D>;
   auto& all = *reinterpret_cast<KeyTiles<T, D>*>(smem_raw);
@@ -146,7 +147,7 @@ template <typename T, int D> __global__ __launch_bounds__((kPackedThreads * kStr
   typename P::Resident k, v;
   P::load(k, rows_of<T>(a.k, a.ks, kbase + jc, kvh), lane, a.scale < 0.f);
   P::load(v, rows_of<T>(a.v, a.vs, kbase + jc, kvh), lane, false);
-  T* const own_v = all.v + (kValuesInLds<T, D> ? wave * 32 * ROW : 0);
+  T* const own_v = all.v + (kValuesInLds<T, D> ? wave * 32 * P::BY_ROWS : 0);
   if constexpr (kValuesInLds<T, D>)
     if (stream == 0) P::to_lds(v, own_v, lane);   // read behind the first barrier
   const float sc = (a.scale == 0.f ? 1e-30f : fabsf(a.scale)) * kLog2e;
@@ -182,7 +183,7 @@ template <typename T, int D> __global__ __launch_bounds__((kPackedThreads * kStr
       const float* delta = sm.delta[it & 1] + 32 * n + 4 * lh;
       const int lo = from - t0 - 32 * n, hi = nq - t0 - 32 * n;   // rows that see this lane's key
       float p[16], ds[16];
-      const f32x16 s = P::scores(qt + 32 * n * ROW, k, lane);
+      const f32x16 s = P::template scores<ROW>(qt + 32 * n * ROW, k, lane);
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         const f32x4_t l4 = *reinterpret_cast<const f32x4_t*>(lse + 8 * g);
@@ -194,11 +195,11 @@ template <typename T, int D> __global__ __launch_bounds__((kPackedThreads * kStr
         }
       }
       f32x16 dp;
-      if constexpr (kValuesInLds<T, D>) dp = P::scores_lds(gt + 32 * n * ROW, own_v, lane);
-      else dp = P::scores(gt + 32 * n * ROW, v, lane);
+      if constexpr (kValuesInLds<T, D>) dp = P::template scores_lds<ROW>(gt + 32 * n * ROW, own_v, lane);
+      else dp = P::template scores<ROW>(gt + 32 * n * ROW, v, lane);
       const typename P::Weights wp = P::weights(p);
-      if (MASK && sm.odd[it % 3]) P::product_by_rows(dv, gt + 32 * n * ROW, wp, lo, hi, lane);
-      else P::product(dv, gt + 32 * n * ROW, wp, lane);
+      if (MASK && sm.odd[it % 3]) P::template product_by_rows<ROW>(dv, gt + 32 * n * ROW, wp, lo, hi, lane);
+      else P::template product<ROW>(dv, gt + 32 * n * ROW, wp, lane);
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         const f32x4_t d4 = *reinterpret_cast<const f32x4_t*>(delta + 8 * g);
@@ -210,8 +211,8 @@ template <typename T, int D> __global__ __launch_bounds__((kPackedThreads * kStr
         }
       }
       const typename P::Weights wd = P::weights(ds);
-      if (MASK && sm.odd[it % 3]) P::product_by_rows(dk, qt + 32 * n * ROW, wd, lo, hi, lane);
-      else P::product(dk, qt + 32 * n * ROW, wd, lane);
+      if (MASK && sm.odd[it % 3]) P::template product_by_rows<ROW>(dk, qt + 32 * n * ROW, wd, lo, hi, lane);
+      else P::template product<ROW>(dk, qt + 32 * n * ROW, wd, lane);
     }
   };
   for (int it = stream, n = 0; it - stream < total; it += S, ++n) {   // the streams meet at every barrier
@@ -256,14 +257,14 @@ template <typename T, int D> __global__ __launch_bounds__((kPackedThreads * kStr
     if (stream) return;
   }
   if (k0 < nk) {
-    T* own = reinterpret_cast<T*>(smem_raw) + wave * 32 * ROW;
+    T* own = reinterpret_cast<T*>(smem_raw) + wave * 32 * P::BY_ROWS;
     put_rows<T, D>(dk, a.scale, own, rows_of<T>(a.dk, a.dks, kbase + k0, kvh), a.dks[0], min(32, nk - k0), lane);
     put_rows<T, D>(dv, 1.f, own, rows_of<T>(a.dv, a.dvs, kbase + k0, kvh), a.dvs[0], min(32, nk - k0), lane);
   }
 }
 
 template <typename T, int D> hipError_t launch(const PackedArgs& a, hipStream_t s) {
-  const size_t dq_smem = sizeof(PackedTiles<T, D, kKeyTile<T, D>>), dkdv_smem = sizeof(KeyTiles<T, D>);
+  const size_t dq_smem = sizeof(DqTiles<T, D>), dkdv_smem = sizeof(KeyTiles<T, D>);
   auto dq = packed_dq_kernel<T, D>;
   auto dkdv = packed_dkdv_kernel<T, D>;
   if (hipError_t e = allow_lds(dq, dq_smem); e != hipSuccess) return e;

@@ -8,11 +8,13 @@
 namespace gformer {
 namespace {
 
-template <typename T, int D> __global__ __launch_bounds__(kPackedThreads) void packed_fwd_kernel(PackedArgs a, int tiles) {
+template <typename T, int D> using FwdTiles = PackedTiles<T, Products<T, D>::R, Products<T, D>::BY_ROWS, Products<T, D>::TURNED>;
+
+template <typename T, int D> __global__ __launch_bounds__(kPackedThreads, (sizeof(T) == 4 && D == 128 ? 1 : 2)) void packed_fwd_kernel(PackedArgs a, int tiles) {
   using P = Products<T, D>;
-  constexpr int R = P::R, ROW = P::ROW, NS = R / 32, MT = D / 32;
+  constexpr int R = P::R, KROW = P::BY_ROWS, VROW = P::TURNED, NS = R / 32, MT = D / 32;
   extern __shared__ __align__(16) unsigned char smem_raw[];
-  auto& sm = *reinterpret_cast<PackedTiles<T, D, Products<T, D>::R>*>(smem_raw);
+  auto& sm = *reinterpret_cast<FwdTiles<T, D>*>(smem_raw);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, ln = lane & 31, lh = lane >> 5;
 
   // Heads fastest, the heads that share keys Hkv apart: workgroups are dealt to the 8 XCDs in turn, so that those of one key
@@ -56,25 +58,14 @@ template <typename T, int D> __global__ __launch_bounds__(kPackedThreads) void p
   }
   if (tid < 3) sm.odd[tid] = 0;
   lds_barrier();
-  for (int t = 0; t < n_tiles; ++t) {
+  auto attend = [&](int t, auto mask_tag) {
+    constexpr bool MASK = decltype(mask_tag)::value;
     const int t0 = t * R;
-    T *kt = sm.x[t & 1], *vt = sm.y[t & 1];
-    const bool cut = t0 + R - 1 > i0 + off;   // some query of the workgroup does not see the whole tile
-    ks.template store<ROW>(kt, tid);
-    vs.template store<ROW>(vt, tid);
-    if (cut && vs.odd()) sm.odd[t % 3] = 1;
-    if (tid == 0) sm.odd[(t + 1) % 3] = 0;
-    lds_barrier();
-    if (t + 1 < n_tiles) {
-      ks.load(kp, a.ks[0], t0 + R, nk - 1, tid);
-      vs.load(vp, a.vs[0], t0 + R, nk - 1, tid);
-    }
-    if (t0 > min(q0 + 31, nq - 1) + off) continue;   // nothing for this wave
+    const T *kt = sm.x[t & 1], *vt = sm.y[t & 1];
     f32x16 s[NS];
 #pragma unroll
-    for (int n = 0; n < NS; ++n) s[n] = P::scores(kt + 32 * n * ROW, q, lane);
-    const bool mask = t0 + R - 1 > q0 + off;
-    if (mask) {
+    for (int n = 0; n < NS; ++n) s[n] = P::template scores<KROW>(kt + 32 * n * KROW, q, lane);
+    if (MASK) {
 #pragma unroll
       for (int n = 0; n < NS; ++n)
 #pragma unroll
@@ -84,7 +75,7 @@ template <typename T, int D> __global__ __launch_bounds__(kPackedThreads) void p
 #pragma unroll
     for (int n = 0; n < NS; ++n)
 #pragma unroll
-      for (int r = 0; r < 16; r += 2) top = max3(top, s[n][r], s[n][r + 1]);
+      for (int r = 0; r < 16; r += 2) top = maximum3(top, s[n][r], s[n][r + 1]);
     top = max_over_halves(top * sc);
     // The reference follows the maximum lazily: sums are rescaled where it grows by more than 8, so weights stay below 2^8
     if (__builtin_amdgcn_ballot_w64(top > m + 8.f) != 0) {
@@ -97,7 +88,6 @@ template <typename T, int D> __global__ __launch_bounds__(kPackedThreads) void p
         for (int r = 0; r < 16; ++r) o[mt][r] *= by;
     }
     const float ref = m == -INFINITY ? 0.f : m;
-    const bool by_rows = mask && sm.odd[t % 3];
 #pragma unroll
     for (int n = 0; n < NS; ++n) {
       float p[16];
@@ -107,21 +97,36 @@ template <typename T, int D> __global__ __launch_bounds__(kPackedThreads) void p
         l += p[r];   // before it is rounded for the product: the log-sum-exp is kept in 32 bits
       }
       const typename P::Weights w = P::weights(p);
-      if (by_rows) P::product_by_rows(o, vt + 32 * n * ROW, w, 0, seen + 1 - t0 - 32 * n, lane);
-      else P::product(o, vt + 32 * n * ROW, w, lane);
+      if (MASK && sm.odd[t % 3]) P::template product_by_rows<VROW>(o, vt + 32 * n * VROW, w, 0, seen + 1 - t0 - 32 * n, lane);
+      else P::template product<VROW>(o, vt + 32 * n * VROW, w, lane);
     }
+  };
+  for (int t = 0; t < n_tiles; ++t) {
+    const int t0 = t * R;
+    ks.template store<KROW>(sm.x[t & 1], tid);
+    vs.template store<VROW>(sm.y[t & 1], tid);
+    if (t0 + R - 1 > i0 + off && vs.odd()) sm.odd[t % 3] = 1;   // some query of the workgroup does not see the whole tile
+    if (tid == 0) sm.odd[(t + 1) % 3] = 0;
+    lds_barrier();
+    if (t + 1 < n_tiles) {
+      ks.load(kp, a.ks[0], t0 + R, nk - 1, tid);
+      vs.load(vp, a.vs[0], t0 + R, nk - 1, tid);
+    }
+    if (t0 > min(q0 + 31, nq - 1) + off) continue;   // nothing for this wave
+    if (t0 + R - 1 > q0 + off) attend(t, std::true_type{});
+    else attend(t, std::false_type{});
   }
   l = sum_over_halves(l);
   if (a.lse && lh == 0 && i < nq)
     a.lse[(int64_t)h * a.total_q + qbase + i] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
   lds_barrier();   // every wave is done with the tiles
   if (q0 < nq)
-    put_rows<T, D>(o, l == 0.f ? 0.f : 1.f / l, reinterpret_cast<T*>(smem_raw) + wave * 32 * ROW,
+    put_rows<T, D>(o, l == 0.f ? 0.f : 1.f / l, reinterpret_cast<T*>(smem_raw) + wave * 32 * KROW,
                    rows_of<T>(a.out, a.os, qbase + q0, h), a.os[0], min(32, nq - q0), lane);
 }
 
 template <typename T, int D> hipError_t launch(const PackedArgs& a, hipStream_t s) {
-  const size_t smem = sizeof(PackedTiles<T, D, Products<T, D>::R>);
+  const size_t smem = sizeof(FwdTiles<T, D>);
   auto kern = packed_fwd_kernel<T, D>;
   if (hipError_t e = allow_lds(kern, smem); e != hipSuccess) return e;
   const int64_t tiles = packed_tiles(a.total_q, a.n_seqs, kPackedRows);
