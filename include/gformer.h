@@ -315,16 +315,18 @@ void gformer_packed_params_init(gformer_packed_params* p);
 
 /*   q   : device [total_q, H, d], k, v : device [total_k, Hkv, d], read
  *   out : device [total_q, H, d], written; may not alias an input
+ *   out_rest : device, laid out like out, written with what rounding to bf16 took from out, as bf16, or NULL.  Not
+ *         for GF_F32 (NULL there).  A backward pass that has it does not see out's rounding
  *   lse : device fp32 [H, total_q] dense, written with the natural logarithm of every query's sum of
  *         exponentials (what the backward pass needs), or NULL
  * total_q or total_k of 0, or n_seqs == 0, are fine. */
-gf_status gformer_packed_attn_fwd(const void* q, const void* k, const void* v, void* out, float* lse,
-                                  const int32_t* cu_q, const int32_t* cu_k, int n_seqs, int total_q,
-                                  int total_k, int H, int Hkv, int d,
+gf_status gformer_packed_attn_fwd(const void* q, const void* k, const void* v, void* out, void* out_rest,
+                                  float* lse, const int32_t* cu_q, const int32_t* cu_k, int n_seqs,
+                                  int total_q, int total_k, int H, int Hkv, int d,
                                   const gformer_packed_params* p, void* hip_stream);
 
 /* Gradients of the above.
- *   out, lse   : what the forward pass wrote, read
+ *   out, out_rest, lse : what the forward pass wrote, read (out_rest: or NULL)
  *   dout       : gradient with respect to out, read
  *   dq, dk, dv : written; may not alias an input or overlap each other
  *   workspace  : device, gformer_packed_attn_bwd_workspace_bytes bytes, 256-byte aligned
@@ -332,7 +334,7 @@ gf_status gformer_packed_attn_fwd(const void* q, const void* k, const void* v, v
 size_t gformer_packed_attn_bwd_workspace_bytes(int total_q, int total_k, int n_seqs, int H, int Hkv, int d,
                                                const gformer_packed_params* p);
 gf_status gformer_packed_attn_bwd(const void* q, const void* k, const void* v, const void* out,
-                                  const float* lse, const void* dout, void* dq, void* dk, void* dv,
+                                  const void* out_rest, const float* lse, const void* dout, void* dq, void* dk, void* dv,
                                   const int32_t* cu_q, const int32_t* cu_k, int n_seqs, int total_q,
                                   int total_k, int H, int Hkv, int d, const gformer_packed_params* p,
                                   void* workspace, size_t workspace_bytes, void* hip_stream);

@@ -57,22 +57,23 @@ class _GformerPackedAttention(torch.autograd.Function):
     def forward(ctx, q, k, v, cu_q, cu_k, softmax_scale):
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         lse = torch.empty(q.shape[1], q.shape[0], dtype=torch.float32, device=q.device)
-        gb.gformer_packed_attn_fwd(q, k, v, out, cu_q, cu_k, lse=lse, softmax_scale=softmax_scale, zero_tail=1)
-        ctx.save_for_backward(q, k, v, out, lse, cu_q, cu_k)
+        rest = torch.empty_like(out) if q.dtype == torch.bfloat16 and any(ctx.needs_input_grad) else None
+        gb.gformer_packed_attn_fwd(q, k, v, out, cu_q, cu_k, lse=lse, out_rest=rest, softmax_scale=softmax_scale, zero_tail=1)
+        ctx.save_for_backward(q, k, v, out, rest, lse, cu_q, cu_k)
         ctx.softmax_scale = softmax_scale
         return out
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dout):
-        q, k, v, out, lse, cu_q, cu_k = ctx.saved_tensors
+        q, k, v, out, rest, lse, cu_q, cu_k = ctx.saved_tensors
         if not _fits(dout):
             dout = dout.contiguous()
             if not _fits(dout):
                 dout = dout.clone(memory_format=torch.contiguous_format)
         dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
-        gb.gformer_packed_attn_bwd(q, k, v, out, lse, dout, dq, dk, dv, cu_q, cu_k, softmax_scale=ctx.softmax_scale,
-                                   zero_tail=1)
+        gb.gformer_packed_attn_bwd(q, k, v, out, lse, dout, dq, dk, dv, cu_q, cu_k, out_rest=rest,
+                                   softmax_scale=ctx.softmax_scale, zero_tail=1)
         return dq, dk, dv, None, None, None
 
 

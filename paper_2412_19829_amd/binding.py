@@ -141,11 +141,11 @@ def lib():
             getattr(L, f"gformer_{name}_params_init").restype = None
             getattr(L, f"gformer_{name}_params_init").argtypes = [init]
         L.gformer_packed_attn_fwd.restype = ctypes.c_int
-        L.gformer_packed_attn_fwd.argtypes = [ctypes.c_void_p] * 7 + [ctypes.c_int] * 6 + [PP, ctypes.c_void_p]
+        L.gformer_packed_attn_fwd.argtypes = [ctypes.c_void_p] * 8 + [ctypes.c_int] * 6 + [PP, ctypes.c_void_p]
         L.gformer_packed_attn_bwd_workspace_bytes.restype = ctypes.c_size_t
         L.gformer_packed_attn_bwd_workspace_bytes.argtypes = [ctypes.c_int] * 6 + [PP]
         L.gformer_packed_attn_bwd.restype = ctypes.c_int
-        L.gformer_packed_attn_bwd.argtypes = [ctypes.c_void_p] * 11 + [ctypes.c_int] * 6 + \
+        L.gformer_packed_attn_bwd.argtypes = [ctypes.c_void_p] * 12 + [ctypes.c_int] * 6 + \
             [PP, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]
         L.gformer_paged_decode_workspace_bytes.restype = ctypes.c_size_t
         L.gformer_paged_decode_workspace_bytes.argtypes = [ctypes.c_int] * 6 + [GP]
@@ -624,11 +624,21 @@ def make_paged_params(dtype=GF_BF16, page_size=64, softmax_scale=1.0, **strides)
     return p
 
 
-def gformer_packed_attn_fwd(q, k, v, out, cu_q, cu_k=None, *, lse=None, softmax_scale=1.0, zero_tail=0,
+def _rest(out, rest):
+    """Address of the tensor that holds what rounding took from `out`."""
+    if rest is None:
+        return None
+    if rest.dtype != out.dtype or rest.device != out.device or rest.shape != out.shape or rest.stride() != out.stride():
+        raise ValueError("out_rest must be laid out like out")
+    return rest.data_ptr()
+
+
+def gformer_packed_attn_fwd(q, k, v, out, cu_q, cu_k=None, *, lse=None, out_rest=None, softmax_scale=1.0, zero_tail=0,
                             stream: Optional[int] = None):
     """Causal attention over packed sequences on device tensors: q, out [total_q, H, d], k, v [total_k, Hkv, d]
     (any strides with a contiguous last dimension); cu_q, cu_k int32 [n_seqs + 1] offsets (cu_k=None: the same
-    sequences); lse, optional: dense fp32 [H, total_q], written."""
+    sequences).  Optional and written, for the backward pass: lse, dense fp32 [H, total_q], and (bf16 only) out_rest, laid
+    out like out, what rounding took from it."""
     import torch
 
     dtype = _tensors(q, 3, q=q, k=k, v=v, out=out)
@@ -639,7 +649,7 @@ def gformer_packed_attn_fwd(q, k, v, out, cu_q, cu_k=None, *, lse=None, softmax_
     p = make_packed_params(dtype, softmax_scale, zero_tail, q_stride=_row_strides("q", q), k_stride=_row_strides("k", k),
                            v_stride=_row_strides("v", v), o_stride=_row_strides("out", out))
     _call(lib().gformer_packed_attn_fwd, q, stream, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
-          None if lse is None else lse.data_ptr(), cu_q.data_ptr(), None if cu_k is None else cu_k.data_ptr(),
+          _rest(out, out_rest), None if lse is None else lse.data_ptr(), cu_q.data_ptr(), None if cu_k is None else cu_k.data_ptr(),
           cu_q.numel() - 1, T, k.shape[0], H, k.shape[1], d, ctypes.byref(p))
     return out
 
@@ -649,9 +659,10 @@ def gformer_packed_attn_bwd_workspace_bytes(total_q, total_k, n_seqs, H, Hkv, d,
                                                              ctypes.byref(params or make_packed_params())))
 
 
-def gformer_packed_attn_bwd(q, k, v, out, lse, dout, dq, dk, dv, cu_q, cu_k=None, *, softmax_scale=1.0, zero_tail=0,
-                            workspace=None, stream: Optional[int] = None):
-    """Gradients of gformer_packed_attn_fwd from what it wrote (out, lse) and the gradient dout of out."""
+def gformer_packed_attn_bwd(q, k, v, out, lse, dout, dq, dk, dv, cu_q, cu_k=None, *, out_rest=None, softmax_scale=1.0,
+                            zero_tail=0, workspace=None, stream: Optional[int] = None):
+    """Gradients of gformer_packed_attn_fwd from what it wrote (out, lse, out_rest) and the gradient dout of
+    out."""
     import torch
 
     dtype = _tensors(q, 3, q=q, k=k, v=v, out=out, dout=dout, dq=dq, dk=dk, dv=dv)
@@ -667,8 +678,8 @@ def gformer_packed_attn_bwd(q, k, v, out, lse, dout, dq, dk, dv, cu_q, cu_k=None
     sizes = (cu_q.numel() - 1, T, k.shape[0], H, k.shape[1], d)
     need = gformer_packed_attn_bwd_workspace_bytes(T, k.shape[0], *sizes[:1], *sizes[3:], p)
     workspace, at, held = _scratch(need, workspace, q, stream)
-    _call(lib().gformer_packed_attn_bwd, q, stream, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(),
-          dout.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), cu_q.data_ptr(),
+    _call(lib().gformer_packed_attn_bwd, q, stream, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _rest(out, out_rest),
+          lse.data_ptr(), dout.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), cu_q.data_ptr(),
           None if cu_k is None else cu_k.data_ptr(), *sizes, ctypes.byref(p), at, held)
     return dq, dk, dv
 

@@ -8,9 +8,9 @@
 // where dk and dv of a key head sum over the H / Hkv query heads that share it.
 //
 // All three passes keep 32 rows a wave resident (queries, or keys in the pass that gives dk and dv) and stream the
-// others through LDS.  The products are taken with the streamed rows as the A operand's, so a lane holds one
-// resident row and 16 streamed rows of each 32x32 score tile, and the weights feed the next product from their
-// registers (mfma.hpp has the layouts).
+// others through LDS, tile by tile, loaded straight into it some tiles ahead.  The products are taken with the
+// streamed rows as the A operand's, so a lane holds one resident row and 16 streamed rows of each 32x32 score tile, and
+// the weights feed the next product from their registers (mfma.hpp has the layouts).
 #pragma once
 
 #include <type_traits>
@@ -23,6 +23,7 @@ namespace gformer {
 struct PackedArgs {
   const void *q, *k, *v, *dout;   // dout: backward pass only
   void *out, *dq, *dk, *dv;       // out: written by the forward pass, read by the backward pass
+  void* rest;                     // what rounding took from out, in bf16 and laid out like it; may be null
   float* lse;                     // [H, total_q], natural logarithm; may be null in the forward pass
   float* delta;                   // [H, total_q], workspace of the backward pass
   const int32_t *cu_q, *cu_k;     // [n_seqs + 1]
@@ -78,52 +79,106 @@ template <typename T> __device__ __forceinline__ T* rows_of(void* p, const int64
   return reinterpret_cast<T*>(p) + row * st[0] + head * st[1];
 }
 
-// Whether any of 16 bytes' elements is infinite or no number.
-template <typename T> __device__ __forceinline__ uint32_t not_finite(u32x4 x) {
-  uint32_t r = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if constexpr (sizeof(T) == 2) r |= ((x[i] & 0x7fff7fffu) + 0x00800080u) & 0x80008000u;
-    else r |= ((x[i] & 0x7fffffffu) + 0x00800000u) & 0x80000000u;
-  }
-  return r;
-}
-
-// A tile of R streamed rows on its way from memory to LDS, 16 bytes a lane: a uniform base and an offset of the thread's
-// own that never changes, so a load costs no address registers.  Rows past `last` re-read it: in bounds, and masked
-// later.
-template <typename T, int D, int R> struct Stage {
-  static constexpr int C = D * (int)sizeof(T) / 16, STEP = kPackedThreads / C, N = R / STEP;
-  static_assert(N * STEP == R, "whole rows");
-  u32x4 x[N];
-  // rows r0 .. r0 + R - 1; r0 <= last.  A tile's rows lie within 2^28 bytes (the row stride is at most 2^20 elements)
-  __device__ __forceinline__ void load(const T* base, int64_t stride, int r0, int last, int tid) {
-    const uint32_t bytes = (uint32_t)stride * sizeof(T), col = 16 * (tid % C), off = tid / C * bytes + col;
-    const char* from = reinterpret_cast<const char*>(base + r0 * stride);
-    const int left = min(last - r0, R - 1);
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int first = min(i * STEP, left);   // uniform
-      x[i] = *reinterpret_cast<const u32x4*>(from + (size_t)first * bytes + (size_t)min(off, (left - first) * bytes + col));
-    }
-  }
-  template <int ROW> __device__ __forceinline__ void store(T* tile, int tid) const {
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-      *reinterpret_cast<u32x4*>(tile + (tid / C + i * STEP) * ROW + (16 / (int)sizeof(T)) * (tid % C)) = x[i];
-  }
-  __device__ __forceinline__ bool odd() const {
-    uint32_t r = 0;
-#pragma unroll
-    for (int i = 0; i < N; ++i) r |= not_finite<T>(x[i]);
-    return r != 0;
-  }
-};
-
 // The largest of three (v_maximum3_f32), or no number.  Left to the compiler, which knows how long after a matrix
 // instruction its result may be read: an asm statement would hide the reader from it.
 __device__ __forceinline__ float maximum3(float a, float b, float c) {
   return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c);
+}
+
+// A tile of R streamed rows in LDS: rows one behind another with no padding, as a load into LDS writes them (64 lanes, 16
+// bytes each, in lane order), the 16-byte pieces of row r at places that differ by swz(r).  swz moves bits of r about, so
+// swz(a ^ b) = swz(a) ^ swz(b), and makes both ways of reading free of bank conflicts: 16 rows at one column take the 16 pieces
+// of 256 bytes, and so do 4 neighbouring rows (8 with the other half of the wave) at two neighbouring pieces.
+template <typename T, int D, int R> struct Tile {
+  static constexpr int E = 16 / (int)sizeof(T), C = D / E;   // elements a piece, pieces a row
+  static constexpr int RPI = 64 / C;                          // rows an instruction loads
+  static constexpr int SIZE = R * D;
+  __host__ __device__ static constexpr int swz(int r) {
+    return C == 8 ? (((r >> 1) & 3) << 1) | ((r >> 3) & 1) : ((r & 7) << 1) | ((r >> 3) & 1);
+  }
+  static constexpr int loads(int waves) { return R / (RPI * waves); }
+  // Rows r0 .. r0 + R - 1 of [rows, D] at `base`, by W waves; those past `last` are row `last`: in bounds, and masked later.
+  // A uniform base and an offset of the lane's own; a tile's rows lie within 2^28 bytes (a row stride is at most 2^20 elements).
+  template <int W> static __device__ __forceinline__ void load(T* tile, const T* base, int64_t stride, int r0, int last, int wave, int lane) {
+    static_assert(loads(W) * RPI * W == R, "whole rows");
+    const uint32_t bytes = (uint32_t)stride * (int)sizeof(T);
+    const int row = RPI * wave + lane / C, left = min(last - r0, R - 1);
+    const uint32_t piece = (lane % C) ^ swz(row);
+    const char* from = reinterpret_cast<const char*>(base + r0 * stride);
+#pragma unroll
+    for (int j = 0; j < loads(W); ++j) {
+      const int first = min(RPI * W * j, left);   // uniform
+      const uint32_t off = (uint32_t)min(row, left - first) * bytes + 16 * (piece ^ swz(RPI * W * j));
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(from + (size_t)first * bytes + off),
+                                       (__attribute__((address_space(3))) void*)(tile + (wave + W * j) * 64 * E), 16, 0, 0);
+    }
+  }
+  // Whether 32 rows hold a value that is infinite or no number; the answer is the wave's.
+  static __device__ __forceinline__ bool odd(const T* rows, int lane) {
+    uint32_t r = 0;
+#pragma unroll
+    for (int i = 0; i < 32 * C / 64; ++i) {
+      const u32x4 x = *reinterpret_cast<const u32x4*>(rows + (64 * i + lane) * E);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if constexpr (sizeof(T) == 2) r |= ((x[j] & 0x7fff7fffu) + 0x00800080u) & 0x80008000u;
+        else r |= ((x[j] & 0x7fffffffu) + 0x00800000u) & 0x80000000u;
+      }
+    }
+    return __builtin_amdgcn_ballot_w64(r != 0) != 0;
+  }
+};
+
+// Whether any wave of the workgroup says so (all have passed a barrier since `flag`'s place was last in use).
+__device__ __forceinline__ bool any_wave(int* flag, bool x) {
+  if (threadIdx.x == 0) *flag = 0;
+  lds_barrier();
+  if (x) *flag = 1;
+  lds_barrier();
+  x = *flag != 0;
+  lds_barrier();   // the flag's place may be written again
+  return x;
+}
+
+// Every load of this wave has arrived but the latest N (loads return in order).
+template <int N> __device__ __forceinline__ void loads_left() {
+  static_assert(N < 64);
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
+// LDS by its byte addresses.  A tile starts at a multiple of 256 bytes, so the pieces of a row (and of the rows 16 further
+// on) differ from a lane's first one by an exclusive or: one instruction a read, where addresses kept ready would take
+// the registers of the sums.  lds_lane() keeps the compiler from doing that.
+__device__ __forceinline__ uint32_t lds_lane(const void* tile, int bytes) {
+  uint32_t at = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)tile + bytes;
+  asm volatile("" : "+v"(at));
+  return at;
+}
+template <typename V> __device__ __forceinline__ V lds_get(uint32_t at) {
+  return *reinterpret_cast<const __attribute__((address_space(3))) V*>(at);
+}
+// Transposed reads (mfma.hpp) at x and y, the latter OFF bytes further on, 64 bytes apart by exclusive or for the tiles of sums.
+// One statement that also waits for them: the compiler takes the builtin for a read of what the loads into LDS still write,
+// and would wait for those, tiles ahead, each time.
+template <int N, int X, int OFF> __device__ __forceinline__ void lds_get_turned(bf16x8 (&to)[N], uint32_t at, uint32_t other) {
+  u32x2 x[N], y[N];
+  if constexpr (N == 4)
+    asm volatile("ds_read_b64_tr_b16 %0, %8 offset:%16\n\tds_read_b64_tr_b16 %4, %12 offset:%17\n\t"
+                 "ds_read_b64_tr_b16 %1, %9 offset:%16\n\tds_read_b64_tr_b16 %5, %13 offset:%17\n\t"
+                 "ds_read_b64_tr_b16 %2, %10 offset:%16\n\tds_read_b64_tr_b16 %6, %14 offset:%17\n\t"
+                 "ds_read_b64_tr_b16 %3, %11 offset:%16\n\tds_read_b64_tr_b16 %7, %15 offset:%17\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(y[0]), "=&v"(y[1]), "=&v"(y[2]), "=&v"(y[3])
+                 : "v"(at), "v"(at ^ 64), "v"(at ^ 128), "v"(at ^ 192), "v"(other), "v"(other ^ 64), "v"(other ^ 128), "v"(other ^ 192),
+                   "n"(X), "n"(X + OFF)
+                 : "memory");
+  else
+    asm volatile("ds_read_b64_tr_b16 %0, %4 offset:%8\n\tds_read_b64_tr_b16 %2, %6 offset:%9\n\t"
+                 "ds_read_b64_tr_b16 %1, %5 offset:%8\n\tds_read_b64_tr_b16 %3, %7 offset:%9\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(x[0]), "=&v"(x[1]), "=&v"(y[0]), "=&v"(y[1])
+                 : "v"(at), "v"(at ^ 64), "v"(other), "v"(other ^ 64), "n"(X), "n"(X + OFF)
+                 : "memory");
+#pragma unroll
+  for (int i = 0; i < N; ++i) to[i] = as_bf16x8(u32x4{x[i][0], x[i][1], y[i][0], y[i][1]});
 }
 
 // The matrix products of one wave, for 32 resident and 32 streamed rows.
@@ -131,10 +186,7 @@ template <typename T, int D> struct Products;
 
 template <int D> struct Products<uint16_t, D> {
   using T = uint16_t;
-  static constexpr int R = 64;                               // streamed rows per tile
-  // row strides in LDS of tiles read by rows, transposed, and both ways (mfma.hpp): 4, 16 and 12 dwords mod 64 at d = 128,
-  // 36, 48 and 36 at d = 64
-  static constexpr int BY_ROWS = D + 8, TURNED = D + 32, BOTH = D == 128 ? D + 24 : D + 8;
+  using L = Tile<T, D, 32>;
   struct Resident { bf16x8 x[D / 16]; };
   struct Weights { bf16x8 x[2]; };
   // this lane's resident row: elements 16 ks + 8 lh .. +7; `flip` changes its sign
@@ -158,30 +210,41 @@ template <int D> struct Products<uint16_t, D> {
     }
     return sum_over_halves(s);
   }
-  // 32 streamed rows from `rows` against the resident ones
-  template <int ROW> static __device__ __forceinline__ f32x16 scores(const T* rows, const Resident& r, int lane) {
-    const T* p = rows + (lane & 31) * ROW + 8 * (lane >> 5);
+  // where a lane reads, in bytes: row l % 32, piece 2 ks + lh; and of the transposed reads, piece 4 mt + l / 16 % 2 * 2 + l / 2 % 2
+  // of row 4 lh + l / 4 % 4
+  static __device__ __forceinline__ int row_at(int lane) { return 2 * ((lane & 31) * D + 8 * ((lane >> 5) ^ L::swz(lane & 31))); }
+  static __device__ __forceinline__ int turned_at(int lane) {
+    const int row = 4 * (lane >> 5) + ((lane >> 2) & 3), piece = 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
+    return 2 * (row * D + 8 * (piece ^ L::swz(row)) + 4 * (lane & 1));
+  }
+  template <int KB> static __device__ __forceinline__ void turned(bf16x8 (&x)[D / 32], uint32_t at) {
+    lds_get_turned<D / 32, 32 * KB * D, 16 * D>(x, at, at ^ (16 * L::swz(8)));
+  }
+  static __device__ __forceinline__ bf16x8 piece(uint32_t at, int ks) { return as_bf16x8(lds_get<u32x4>(at ^ (32 * ks))); }
+  // 32 streamed rows against the resident ones
+  static __device__ __forceinline__ f32x16 scores(const T* rows, const Resident& r, int lane) {
+    const uint32_t at = lds_lane(rows, row_at(lane));
     f32x16 s;
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[i] = 0.f;
 #pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks) s = mfma32(lds_read16(p + 16 * ks), r.x[ks], s);
+    for (int ks = 0; ks < D / 16; ++ks) s = mfma32(piece(at, ks), r.x[ks], s);
     return s;
   }
-  // the same with the resident rows in LDS too, at `own`
-  template <int ROW> static __device__ __forceinline__ f32x16 scores_lds(const T* rows, const T* own, int lane) {
-    const int at = (lane & 31) * ROW + 8 * (lane >> 5), own_at = (lane & 31) * BY_ROWS + 8 * (lane >> 5);
+  // the same with the resident rows in a tile of LDS too
+  static __device__ __forceinline__ f32x16 scores_lds(const T* rows, const T* own, int lane) {
+    const uint32_t at = lds_lane(rows, row_at(lane)), own_at = lds_lane(own, row_at(lane));
     f32x16 s;
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[i] = 0.f;
 #pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks) s = mfma32(lds_read16(rows + at + 16 * ks), lds_read16(own + own_at + 16 * ks), s);
+    for (int ks = 0; ks < D / 16; ++ks) s = mfma32(piece(at, ks), piece(own_at, ks), s);
     return s;
   }
   static __device__ __forceinline__ void to_lds(const Resident& r, T* own, int lane) {
+    const int at = row_at(lane) / 2;
 #pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks)
-      *reinterpret_cast<u32x4*>(own + (lane & 31) * BY_ROWS + 8 * (lane >> 5) + 16 * ks) = as_u32x4(r.x[ks]);
+    for (int ks = 0; ks < D / 16; ++ks) *reinterpret_cast<u32x4*>(own + (at ^ (16 * ks))) = as_u32x4(r.x[ks]);
   }
   static __device__ __forceinline__ Weights weights(const float (&p)[16]) {
     Weights w;
@@ -195,36 +258,44 @@ template <int D> struct Products<uint16_t, D> {
     return w;
   }
   // acc += rows^T weights
-  template <int ROW> static __device__ __forceinline__ void product(f32x16 (&acc)[D / 32], const T* rows, const Weights& w, int lane) {
-    const T* p = rows + 4 * (lane >> 5) * ROW + lds_operand_tr_lane_offset(ROW, lane);
+  static __device__ __forceinline__ void product(f32x16 (&acc)[D / 32], const T* rows, const Weights& w, int lane) {
+    const uint32_t at = lds_lane(rows, turned_at(lane));
+    bf16x8 x[D / 32];
+    turned<0>(x, at);
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
+    for (int mt = 0; mt < D / 32; ++mt) acc[mt] = mfma32(x[mt], w.x[0], acc[mt]);
+    turned<1>(x, at);
 #pragma unroll
-      for (int mt = 0; mt < D / 32; ++mt)
-        acc[mt] = mfma32(lds_operand_tr_at(p, ROW, 16 * kb, 16 * kb + 8, 32 * mt), w.x[kb], acc[mt]);
+    for (int mt = 0; mt < D / 32; ++mt) acc[mt] = mfma32(x[mt], w.x[1], acc[mt]);
   }
   // The same row by row, for tiles that hold values which are not finite: zero times such a value is no number, so a row is
-  // left out of a lane's sums, not weighted with zero, where first <= row < end does not hold.
-  template <int ROW>
+  // left out of a lane's sums, not weighted with zero, where first <= row < end does not hold.  The kernels look for such
+  // values in the tiles that some of a wave's rows see in part, and where they find one take the whole workgroup's sums again
+  // in a second loop that has this: in the first one it would cost registers.
   static __device__ __forceinline__ void product_by_rows(f32x16 (&acc)[D / 32], const T* rows, const Weights& w, int first, int end,
                                                          int lane) {
-    const T* p = rows + 4 * (lane >> 5) * ROW + lds_operand_tr_lane_offset(ROW, lane);
-#pragma unroll
-    for (int mt = 0; mt < D / 32; ++mt)                   // one tile of sums at a time: this is rare, and must not cost registers
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
+    const uint32_t at = lds_lane(rows, turned_at(lane));
+    auto half = [&](auto kb) {
+      constexpr int KB = decltype(kb)::value;
+      bf16x8 x[D / 32];
+      turned<KB>(x, at);
 #pragma unroll 1
-        for (int e = 0; e < 16; ++e) {                    // row 16 kb + e: half e / 4 % 2, slot 4 (e / 8) + e % 4
-          const int slot = 4 * (e / 8) + e % 4, row = 16 * kb + e;
-          const bool mine = (lane >> 5) == ((e / 4) & 1);
-          u32x4 keep;
+      for (int e = 0; e < 16; ++e) {                      // row 16 KB + e: half e / 4 % 2, slot 4 (e / 8) + e % 4
+        const int slot = 4 * (e / 8) + e % 4, row = 16 * KB + e;
+        const bool mine = (lane >> 5) == ((e / 4) & 1);
+        u32x4 keep;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) keep[i] = mine && slot / 2 == i ? (slot & 1 ? 0xffff0000u : 0x0000ffffu) : 0u;
-          const bf16x8 a = as_bf16x8(as_u32x4(lds_operand_tr_at(p, ROW, 16 * kb, 16 * kb + 8, 32 * mt)) & keep);
-          const f32x16 with = mfma32(a, as_bf16x8(as_u32x4(w.x[kb]) & keep), acc[mt]);
+        for (int i = 0; i < 4; ++i) keep[i] = mine && slot / 2 == i ? (slot & 1 ? 0xffff0000u : 0x0000ffffu) : 0u;
+#pragma unroll
+        for (int mt = 0; mt < D / 32; ++mt) {
+          const f32x16 with = mfma32(as_bf16x8(as_u32x4(x[mt]) & keep), as_bf16x8(as_u32x4(w.x[KB]) & keep), acc[mt]);
 #pragma unroll
           for (int r = 0; r < 16; ++r) acc[mt][r] = row >= first && row < end ? with[r] : acc[mt][r];
         }
+      }
+    };
+    half(std::integral_constant<int, 0>{});
+    half(std::integral_constant<int, 1>{});
   }
   static __device__ __forceinline__ void put4(T* p, float a, float b, float c, float d) {
     u32x2 x;
@@ -232,6 +303,7 @@ template <int D> struct Products<uint16_t, D> {
     x[1] = pack_bf16(c, d);
     *reinterpret_cast<u32x2*>(p) = x;
   }
+  static __device__ __forceinline__ float rest(float x) { return x - bf16_lo(pack_bf16(x, 0.f)); }   // what rounding takes
 };
 
 // Single precision, on v_mfma_f32_32x32x2_f32: a k-step has one slot for each half of the wave.  A contraction along
@@ -239,8 +311,7 @@ template <int D> struct Products<uint16_t, D> {
 // register r of both halves stands for, 8 (r / 4) + 4 lh + r % 4.
 template <int D> struct Products<float, D> {
   using T = float;
-  static constexpr int R = 32;
-  static constexpr int BY_ROWS = D + 4, TURNED = D + 4, BOTH = D + 4;   // 4 dwords mod 64: 16-byte row reads without conflicts
+  using L = Tile<T, D, 32>;
   struct Resident { f32x4_t x[D / 8]; };
   struct Weights { float x[16]; };
   static __device__ __forceinline__ f32x16 mfma(float a, float b, f32x16 c) {
@@ -259,14 +330,14 @@ template <int D> struct Products<float, D> {
       for (int j = 0; j < 4; ++j) s = fmaf(a.x[i][j], b.x[i][j], s);
     return sum_over_halves(s);
   }
-  template <int ROW> static __device__ __forceinline__ f32x16 scores(const T* rows, const Resident& r, int lane) {
-    const T* p = rows + (lane & 31) * ROW + 4 * (lane >> 5);
+  static __device__ __forceinline__ f32x16 scores(const T* rows, const Resident& r, int lane) {
+    const uint32_t at = lds_lane(rows, 4 * ((lane & 31) * D + 4 * ((lane >> 5) ^ L::swz(lane & 31))));
     f32x16 s;
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[i] = 0.f;
 #pragma unroll
     for (int i = 0; i < D / 8; ++i) {
-      const f32x4_t a = *reinterpret_cast<const f32x4_t*>(p + 8 * i);
+      const f32x4_t a = lds_get<f32x4_t>(at ^ (32 * i));
 #pragma unroll
       for (int j = 0; j < 4; ++j) s = mfma(a[j], r.x[i][j], s);
     }
@@ -278,17 +349,24 @@ template <int D> struct Products<float, D> {
     for (int i = 0; i < 16; ++i) w.x[i] = p[i];
     return w;
   }
-  template <int ROW> static __device__ __forceinline__ void product(f32x16 (&acc)[D / 32], const T* rows, const Weights& w, int lane) {
-    const T* p = rows + 4 * (lane >> 5) * ROW + (lane & 31);
+  // column 32 mt + l % 32 of row 8 (r / 4) + 4 lh + r % 4
+  static __device__ __forceinline__ int turned_at(int lane) {
+    return 4 * (4 * (lane >> 5) * D + 4 * (((lane & 31) >> 2) ^ L::swz(4 * (lane >> 5))) + (lane & 3));
+  }
+  static __device__ __forceinline__ float turned(uint32_t at, int r, int mt) {
+    const int row = 8 * (r / 4) + r % 4;
+    return lds_get<float>((at ^ (128 * mt) ^ (16 * L::swz(row))) + 4 * row * D);
+  }
+  static __device__ __forceinline__ void product(f32x16 (&acc)[D / 32], const T* rows, const Weights& w, int lane) {
+    const uint32_t at = lds_lane(rows, turned_at(lane));
 #pragma unroll
     for (int r = 0; r < 16; ++r)
 #pragma unroll
-      for (int mt = 0; mt < D / 32; ++mt) acc[mt] = mfma(p[(8 * (r / 4) + r % 4) * ROW + 32 * mt], w.x[r], acc[mt]);
+      for (int mt = 0; mt < D / 32; ++mt) acc[mt] = mfma(turned(at, r, mt), w.x[r], acc[mt]);
   }
-  template <int ROW>
   static __device__ __forceinline__ void product_by_rows(f32x16 (&acc)[D / 32], const T* rows, const Weights& w, int first, int end,
                                                          int lane) {
-    const T* p = rows + 4 * (lane >> 5) * ROW + (lane & 31);
+    const uint32_t at = lds_lane(rows, turned_at(lane));
 #pragma unroll
     for (int mt = 0; mt < D / 32; ++mt)
 #pragma unroll
@@ -297,7 +375,7 @@ template <int D> struct Products<float, D> {
         for (int half = 0; half < 2; ++half) {
           const int row = 8 * (r / 4) + 4 * half + r % 4;
           const bool mine = (lane >> 5) == half;
-          const f32x16 with = mfma(mine ? p[(8 * (r / 4) + r % 4) * ROW + 32 * mt] : 0.f, mine ? w.x[r] : 0.f, acc[mt]);
+          const f32x16 with = mfma(mine ? turned(at, r, mt) : 0.f, mine ? w.x[r] : 0.f, acc[mt]);
 #pragma unroll
           for (int i = 0; i < 16; ++i) acc[mt][i] = row >= first && row < end ? with[i] : acc[mt][i];
         }
@@ -305,26 +383,28 @@ template <int D> struct Products<float, D> {
   static __device__ __forceinline__ void put4(T* p, float a, float b, float c, float d) {
     *reinterpret_cast<f32x4_t*>(p) = f32x4_t{a, b, c, d};
   }
+  static __device__ __forceinline__ float rest(float) { return 0.f; }
 };
 
 // A wave's 32 resident rows of sums (lane: one row; register (mt, 4 g + i): column 32 mt + 8 g + 4 lh + i) times `by`,
-// through 32 BY_ROWS elements of LDS that are its own, to whole rows in memory.
-template <typename T, int D>
+// through kPutRow 32 elements of LDS that are its own, to whole rows in memory.  REST: what rounding takes from them instead.
+template <typename T, int D> constexpr int kPutRow = D + 16 / (int)sizeof(T);
+template <typename T, int D, bool REST = false>
 __device__ __forceinline__ void put_rows(const f32x16 (&acc)[D / 32], float by, T* own, T* to, int64_t stride, int rows, int lane) {
   using P = Products<T, D>;
-  T* p = own + (lane & 31) * P::BY_ROWS + 4 * (lane >> 5);
+  T* p = own + (lane & 31) * kPutRow<T, D> + 4 * (lane >> 5);
+  auto value = [&](int mt, int r) { return REST ? P::rest(acc[mt][r] * by) : acc[mt][r] * by; };
 #pragma unroll
   for (int mt = 0; mt < D / 32; ++mt)
 #pragma unroll
-    for (int g = 0; g < 4; ++g)
-      P::put4(p + 32 * mt + 8 * g, acc[mt][4 * g] * by, acc[mt][4 * g + 1] * by, acc[mt][4 * g + 2] * by, acc[mt][4 * g + 3] * by);
+    for (int g = 0; g < 4; ++g) P::put4(p + 32 * mt + 8 * g, value(mt, 4 * g), value(mt, 4 * g + 1), value(mt, 4 * g + 2), value(mt, 4 * g + 3));
   wave_sync();
   constexpr int C = D * (int)sizeof(T) / 16, E = 16 / (int)sizeof(T);
 #pragma unroll
   for (int i = 0; i < 32 * C / 64; ++i) {
     const int row = lane / C + i * (64 / C);
     if (row < rows)
-      *reinterpret_cast<u32x4*>(to + row * stride + E * (lane % C)) = *reinterpret_cast<const u32x4*>(own + row * P::BY_ROWS + E * (lane % C));
+      *reinterpret_cast<u32x4*>(to + row * stride + E * (lane % C)) = *reinterpret_cast<const u32x4*>(own + row * kPutRow<T, D> + E * (lane % C));
   }
   wave_sync();
 }
@@ -335,12 +415,6 @@ template <typename T, int D> __device__ __forceinline__ void zero_rows(T* to, in
   for (int r = tid / C; r < rows; r += kPackedThreads / C)
     *reinterpret_cast<u32x4*>(to + r * stride + (16 / (int)sizeof(T)) * (tid % C)) = u32x4{0, 0, 0, 0};
 }
-
-template <typename T, int R, int XROW, int YROW> struct alignas(16) PackedTiles {
-  T x[2][R * XROW], y[2][R * YROW];   // K and V, or Q and dO, in rows of XROW and YROW elements
-  float lse[2][R], delta[2][R];   // statistics of the streamed queries (dk and dv)
-  int odd[3];                     // tile it holds values that are not finite: odd[it % 3]
-};
 
 }  // namespace
 }  // namespace gformer

@@ -136,8 +136,8 @@ void gformer_paged_params_init(gformer_paged_params* p) {
   p->softmax_scale = 1.f;
 }
 
-gf_status gformer_packed_attn_fwd(const void* q, const void* k, const void* v, void* out, float* lse, const int32_t* cu_q,
-                                  const int32_t* cu_k, int n_seqs, int total_q, int total_k, int H, int Hkv, int d,
+gf_status gformer_packed_attn_fwd(const void* q, const void* k, const void* v, void* out, void* out_rest, float* lse,
+                                  const int32_t* cu_q, const int32_t* cu_k, int n_seqs, int total_q, int total_k, int H, int Hkv, int d,
                                   const gformer_packed_params* p, void* hip_stream) {
   PackedArgs a;
   gf_status st = check_packed(n_seqs, total_q, total_k, H, Hkv, d, p, &a);
@@ -145,13 +145,16 @@ gf_status gformer_packed_attn_fwd(const void* q, const void* k, const void* v, v
   if (total_q == 0) return GF_OK;
   if (!q || !out || !cu_q || (total_k > 0 && (!k || !v))) return GF_ERR_INVALID_ARG;
   if (!cu_k && total_q != total_k) return GF_ERR_INVALID_ARG;
-  if (misaligned(bits(q, k, v, out), 16) || misaligned(bits(lse, cu_q, cu_k), 4)) return GF_ERR_INVALID_ARG;
-  if (out == q || out == k || out == v) return GF_ERR_INVALID_ARG;
+  if (misaligned(bits(q, k, v, out, out_rest), 16) || misaligned(bits(lse, cu_q, cu_k), 4)) return GF_ERR_INVALID_ARG;
+  for (const void* x : {q, k, v})
+    if (out == x || (out_rest && out_rest == x)) return GF_ERR_INVALID_ARG;
+  if (out_rest == out || (out_rest && p->dtype == GF_F32)) return GF_ERR_INVALID_ARG;
   if ((st = check_device(hip_stream)) != GF_OK) return st;
   a.q = q;
   a.k = k;
   a.v = v;
   a.out = out;
+  a.rest = out_rest;
   a.lse = lse;
   a.cu_q = cu_q;
   a.cu_k = cu_k ? cu_k : cu_q;
@@ -165,8 +168,8 @@ size_t gformer_packed_attn_bwd_workspace_bytes(int total_q, int total_k, int n_s
   return ((size_t)total_q * H * sizeof(float) + 255) / 256 * 256;
 }
 
-gf_status gformer_packed_attn_bwd(const void* q, const void* k, const void* v, const void* out, const float* lse, const void* dout,
-                                  void* dq, void* dk, void* dv, const int32_t* cu_q, const int32_t* cu_k, int n_seqs, int total_q,
+gf_status gformer_packed_attn_bwd(const void* q, const void* k, const void* v, const void* out, const void* out_rest,
+                                  const float* lse, const void* dout, void* dq, void* dk, void* dv, const int32_t* cu_q, const int32_t* cu_k, int n_seqs, int total_q,
                                   int total_k, int H, int Hkv, int d, const gformer_packed_params* p, void* workspace,
                                   size_t workspace_bytes, void* hip_stream) {
   PackedArgs a;
@@ -175,8 +178,9 @@ gf_status gformer_packed_attn_bwd(const void* q, const void* k, const void* v, c
   if (total_q == 0 && total_k == 0) return GF_OK;
   if (!cu_q || (total_q > 0 && (!q || !out || !lse || !dout || !dq)) || (total_k > 0 && (!k || !v || !dk || !dv))) return GF_ERR_INVALID_ARG;
   if (!cu_k && total_q != total_k) return GF_ERR_INVALID_ARG;
-  if (misaligned(bits(q, k, v, out, dout, dq, dk, dv), 16) || misaligned(bits(lse, cu_q, cu_k), 4)) return GF_ERR_INVALID_ARG;
-  const void* in[] = {q, k, v, out, dout, lse};
+  if (out_rest && p->dtype == GF_F32) return GF_ERR_INVALID_ARG;
+  if (misaligned(bits(q, k, v, out, out_rest, dout, dq, dk, dv), 16) || misaligned(bits(lse, cu_q, cu_k), 4)) return GF_ERR_INVALID_ARG;
+  const void* in[] = {q, k, v, out, out_rest, dout, lse};
   void* grads[] = {dq, dk, dv};
   for (int i = 0; i < 3; ++i) {
     for (const void* x : in)
@@ -191,7 +195,8 @@ gf_status gformer_packed_attn_bwd(const void* q, const void* k, const void* v, c
   a.k = k;
   a.v = v;
   a.dout = dout;
-  a.out = const_cast<void*>(out);   // read by this pass
+  a.out = const_cast<void*>(out);   // read by this pass, and so are the rest of it and lse
+  a.rest = const_cast<void*>(out_rest);
   a.lse = const_cast<float*>(lse);
   a.dq = dq;
   a.dk = dk;

@@ -19,18 +19,28 @@ constexpr int kQueryTile = 32;   // queries per tile of the dk, dv pass
 template <typename T, int D> constexpr int kStreams = kWaves<T, D>;
 // its value rows stay in LDS where their registers are wanted for the sums
 template <typename T, int D> constexpr bool kValuesInLds = sizeof(T) == 2 && D == 128;
-template <typename T, int D> using DqTiles = PackedTiles<T, kKeyTile<T, D>, Products<T, D>::BOTH, Products<T, D>::BY_ROWS>;
-template <typename T, int D> struct KeyTiles {
-  PackedTiles<T, kQueryTile, Products<T, D>::BOTH, Products<T, D>::BOTH> stream[kStreams<T, D>];
-  T v[kValuesInLds<T, D> ? kPackedRows * Products<T, D>::BY_ROWS : 1];
+constexpr int kBuffers = 3;      // tiles in LDS: one in use, two on their way
+template <typename T, int D> struct alignas(256) DqTiles {
+  T k[kBuffers][kKeyTile<T, D> * D], v[kBuffers][kKeyTile<T, D> * D];
+  int flag;
+};
+template <typename T, int D> struct alignas(256) QueryTiles {
+  T q[kBuffers][kQueryTile * D], g[kBuffers][kQueryTile * D];
+  float stats[kBuffers][2 * kQueryTile];   // a tile's lse, then its delta
+};
+template <typename T, int D> struct alignas(256) KeyTiles {
+  QueryTiles<T, D> stream[kStreams<T, D>];
+  T v[kValuesInLds<T, D> ? kPackedRows * D : 8];
+  int flag;
 };
 
 template <typename T, int D> __global__ __launch_bounds__(kPackedThreads, (kWaves<T, D>)) void packed_dq_kernel(PackedArgs a, int tiles) {
   using P = Products<T, D>;
-  constexpr int R = kKeyTile<T, D>, KROW = P::BOTH, VROW = P::BY_ROWS, NS = R / 32, MT = D / 32;
-  extern __shared__ __align__(16) unsigned char smem_raw[];
+  constexpr int R = kKeyTile<T, D>, NS = R / 32, MT = D / 32, W = kPackedThreads / 64;
+  using L = Tile<T, D, R>;
+  extern __shared__ __align__(256) unsigned char smem_raw[];
   auto& sm = *reinterpret_cast<DqTiles<T, D>*>(smem_raw);
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, ln = lane & 31, lh = lane >> 5;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), ln = lane & 31, lh = lane >> 5;
 
   const int hh = blockIdx.x % a.H, kvh = hh % a.Hkv, h = kvh * (a.H / a.Hkv) + hh / a.Hkv;
   const SeqTile at = find_tile<kPackedRows>(a.cu_q, a.n_seqs, a.total_q, tiles - 1 - blockIdx.x / a.H, lane);
@@ -50,7 +60,11 @@ template <typename T, int D> __global__ __launch_bounds__(kPackedThreads, (kWave
   typename P::Resident q, g;
   P::load(g, rows_of<T>((const void*)a.out, a.os, qbase + ic, h), lane, false);
   P::load(q, rows_of<T>(a.dout, a.gs, qbase + ic, h), lane, false);
-  const float delta = P::dot(q, g);
+  float delta = P::dot(q, g);
+  if (sizeof(T) == 2 && a.rest) {   // out's rounding would cost dq and dk half as much again as that of the weights
+    P::load(g, rows_of<T>((const void*)a.rest, a.os, qbase + ic, h), lane, false);
+    delta += P::dot(q, g);
+  }
   g = q;
   P::load(q, rows_of<T>(a.q, a.qs, qbase + ic, h), lane, a.scale < 0.f);
   const int64_t stat = (int64_t)h * a.total_q + qbase + ic;
@@ -59,70 +73,69 @@ template <typename T, int D> __global__ __launch_bounds__(kPackedThreads, (kWave
   const float sc = (a.scale == 0.f ? 1e-30f : fabsf(a.scale)) * kLog2e;
 
   f32x16 dq[MT];
-#pragma unroll
-  for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) dq[mt][r] = 0.f;
 
   const T* kp = rows_of<T>(a.k, a.ks, kbase, kvh);
   const T* vp = rows_of<T>(a.v, a.vs, kbase, kvh);
   const int last_key = min(i0 + kPackedRows, nq) - 1 + off;
   const int n_tiles = last_key < 0 ? 0 : last_key / R + 1;
-  Stage<T, D, R> ks, vs;
-  if (n_tiles) {
-    ks.load(kp, a.ks[0], 0, nk - 1, tid);
-    vs.load(vp, a.vs[0], 0, nk - 1, tid);
-  }
-  if (tid < 3) sm.odd[tid] = 0;
-  lds_barrier();
-  auto sums = [&](int t, auto mask_tag) {
-    constexpr bool MASK = decltype(mask_tag)::value;
+  auto load = [&](int t) {
+    L::template load<W>(sm.k[t % kBuffers], kp, a.ks[0], t * R, nk - 1, wave, lane);
+    L::template load<W>(sm.v[t % kBuffers], vp, a.vs[0], t * R, nk - 1, wave, lane);
+  };
+  bool odd = false;
+  auto sums = [&](int t, auto by_rows) {
     const int t0 = t * R;
-    const T *kt = sm.x[t & 1], *vt = sm.y[t & 1];
+    const bool mask = t0 + R - 1 > q0 + off;   // some query of the wave does not see the whole tile
+    const T *kt = sm.k[t % kBuffers], *vt = sm.v[t % kBuffers];
 #pragma unroll
     for (int n = 0; n < NS; ++n) {
-      const f32x16 s = P::template scores<KROW>(kt + 32 * n * KROW, q, lane), dp = P::template scores<VROW>(vt + 32 * n * VROW, g, lane);
+      const f32x16 s = P::scores(kt + 32 * n * D, q, lane), dp = P::scores(vt + 32 * n * D, g, lane);
       float ds[16];
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        ds[r] = __builtin_amdgcn_exp2f(fmaf(s[r], sc, -lse)) * (dp[r] - delta);
-        if (MASK && t0 + 32 * n + 8 * (r / 4) + 4 * lh + r % 4 > seen) ds[r] = 0.f;
+      for (int r = 0; r < 16; ++r) ds[r] = __builtin_amdgcn_exp2f(fmaf(s[r], sc, -lse)) * (dp[r] - delta);
+      if (mask) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) ds[r] = t0 + 32 * n + 8 * (r / 4) + 4 * lh + r % 4 > seen ? 0.f : ds[r];
       }
       const typename P::Weights w = P::weights(ds);
-      if (MASK && sm.odd[t % 3]) P::template product_by_rows<KROW>(dq, kt + 32 * n * KROW, w, 0, seen + 1 - t0 - 32 * n, lane);
-      else P::template product<KROW>(dq, kt + 32 * n * KROW, w, lane);
+      if (by_rows && mask && L::odd(kt + 32 * n * D, lane)) P::product_by_rows(dq, kt + 32 * n * D, w, 0, seen + 1 - t0 - 32 * n, lane);
+      else P::product(dq, kt + 32 * n * D, w, lane);
+      if (!by_rows && mask) odd = odd || L::odd(kt + 32 * n * D, lane);
     }
   };
-  for (int t = 0; t < n_tiles; ++t) {
-    const int t0 = t * R;
-    ks.template store<KROW>(sm.x[t & 1], tid);
-    vs.template store<VROW>(sm.y[t & 1], tid);
-    if (t0 + R - 1 > i0 + off && ks.odd()) sm.odd[t % 3] = 1;   // some query of the workgroup does not see the whole tile
-    if (tid == 0) sm.odd[(t + 1) % 3] = 0;
-    lds_barrier();
-    if (t + 1 < n_tiles) {
-      ks.load(kp, a.ks[0], t0 + R, nk - 1, tid);
-      vs.load(vp, a.vs[0], t0 + R, nk - 1, tid);
+  auto pass = [&](auto by_rows) {
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) dq[mt][r] = 0.f;
+    for (int t = 0; t < kBuffers - 1; ++t)
+      if (t < n_tiles) load(t);
+    for (int t = 0; t < n_tiles; ++t) {
+      if (t + 1 < n_tiles) loads_left<2 * L::loads(W)>();
+      else loads_left<0>();
+      lds_barrier();   // tile t is there, and nobody reads tile t - 1 any more
+      if (t + kBuffers - 1 < n_tiles) load(t + kBuffers - 1);
+      if (t * R <= min(q0 + 31, nq - 1) + off) sums(t, by_rows);   // else nothing for this wave
     }
-    if (t0 > min(q0 + 31, nq - 1) + off) continue;
-    if (t0 + R - 1 > q0 + off) sums(t, std::true_type{});
-    else sums(t, std::false_type{});
-  }
-  lds_barrier();
+    lds_barrier();   // every wave is done with the tiles
+  };
+  pass(std::false_type{});
+  if (any_wave(&sm.flag, odd)) pass(std::true_type{});
   if (q0 < nq)
-    put_rows<T, D>(dq, a.scale, reinterpret_cast<T*>(smem_raw) + wave * 32 * VROW, rows_of<T>(a.dq, a.dqs, qbase + q0, h), a.dqs[0],
+    put_rows<T, D>(dq, a.scale, reinterpret_cast<T*>(smem_raw) + wave * 32 * kPutRow<T, D>, rows_of<T>(a.dq, a.dqs, qbase + q0, h), a.dqs[0],
                    min(32, nq - q0), lane);
 }
 
 template <typename T, int D> __global__ __launch_bounds__((kPackedThreads * kStreams<T, D>), (kWaves<T, D>)) void packed_dkdv_kernel(PackedArgs a, int tiles) {
   using P = Products<T, D>;
-  constexpr int R = kQueryTile, ROW = P::BOTH, NS = R / 32, MT = D / 32;
-  extern __shared__ __align__(16) unsigned char smem_raw[];
+  constexpr int R = kQueryTile, MT = D / 32, W = kPackedThreads / 64;
+  using L = Tile<T, D, R>;
+  extern __shared__ __align__(256) unsigned char smem_raw[];
   constexpr int S = kStreams<T, D>;
   auto& all = *reinterpret_cast<KeyTiles<T, D>*>(smem_raw);
   const int stream = __builtin_amdgcn_readfirstlane(threadIdx.x / kPackedThreads);
   auto& sm = all.stream[stream];
-  const int tid = threadIdx.x % kPackedThreads, lane = tid & 63, wave = tid >> 6, ln = lane & 31, lh = lane >> 5;
+  const int tid = threadIdx.x % kPackedThreads, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), ln = lane & 31, lh = lane >> 5;
 
   // first tiles first: the most queries see them
   const int kvh = blockIdx.x % a.Hkv;
@@ -147,93 +160,98 @@ template <typename T, int D> __global__ __launch_bounds__((kPackedThreads * kStr
   typename P::Resident k, v;
   P::load(k, rows_of<T>(a.k, a.ks, kbase + jc, kvh), lane, a.scale < 0.f);
   P::load(v, rows_of<T>(a.v, a.vs, kbase + jc, kvh), lane, false);
-  T* const own_v = all.v + (kValuesInLds<T, D> ? wave * 32 * P::BY_ROWS : 0);
+  T* const own_v = all.v + (kValuesInLds<T, D> ? wave * 32 * D : 0);
   if constexpr (kValuesInLds<T, D>)
     if (stream == 0) P::to_lds(v, own_v, lane);   // read behind the first barrier
   const float sc = (a.scale == 0.f ? 1e-30f : fabsf(a.scale)) * kLog2e;
 
   f32x16 dk[MT], dv[MT];
-#pragma unroll
-  for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) dk[mt][r] = dv[mt][r] = 0.f;
 
   // the tiles of queries that see any of the workgroup's keys, for every head of the group in turn
   const int first_tile = max(j0 - off, 0) / R;
   const int per_head = nq == 0 ? 0 : (nq - 1) / R + 1 - first_tile, G = a.H / a.Hkv, total = max(per_head, 0) * G;
-  Stage<T, D, R> qs, gs;
-  float stat = 0.f;   // threads 0 .. R-1: lse of a query, R .. 2R-1: delta
-  auto load = [&](int it) {
-    const int h = kvh * G + it / per_head, t0 = (first_tile + it % per_head) * R;
-    qs.load(rows_of<T>(a.q, a.qs, qbase, h), a.qs[0], t0, nq - 1, tid);
-    gs.load(rows_of<T>(a.dout, a.gs, qbase, h), a.gs[0], t0, nq - 1, tid);
-    const int64_t at_stat = (int64_t)h * a.total_q + qbase;
-    if (tid < R) stat = a.lse[at_stat + min(t0 + tid, nq - 1)] * kLog2e;
-    else if (tid < 2 * R) stat = a.delta[at_stat + min(t0 + tid - R, nq - 1)];
+  // the stream's n-th tile, queries `t` R .. of head `g` of the group; its next one
+  struct Place { int g, t; };
+  auto next = [&](Place& p) {
+    for (p.t += S; p.t - first_tile >= per_head; p.t -= per_head) ++p.g;
   };
-  if (stream < total) load(stream);
-  if (tid < 3) sm.odd[tid] = 0;
-  lds_barrier();
-  auto sums = [&](int it, int t0, auto mask_tag) {   // tile number `it` of the stream
-    constexpr bool MASK = decltype(mask_tag)::value;
-    const T *qt = sm.x[it & 1], *gt = sm.y[it & 1];
-#pragma unroll
-    for (int n = 0; n < NS; ++n) {
-      const float* lse = sm.lse[it & 1] + 32 * n + 4 * lh;
-      const float* delta = sm.delta[it & 1] + 32 * n + 4 * lh;
-      const int lo = from - t0 - 32 * n, hi = nq - t0 - 32 * n;   // rows that see this lane's key
-      float p[16], ds[16];
-      const f32x16 s = P::template scores<ROW>(qt + 32 * n * ROW, k, lane);
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const f32x4_t l4 = *reinterpret_cast<const f32x4_t*>(lse + 8 * g);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int i = 8 * g + 4 * lh + e;
-          p[4 * g + e] = __builtin_amdgcn_exp2f(fmaf(s[4 * g + e], sc, -l4[e]));
-          if (MASK && (i < lo || i >= hi)) p[4 * g + e] = 0.f;
-        }
-      }
-      f32x16 dp;
-      if constexpr (kValuesInLds<T, D>) dp = P::template scores_lds<ROW>(gt + 32 * n * ROW, own_v, lane);
-      else dp = P::template scores<ROW>(gt + 32 * n * ROW, v, lane);
-      const typename P::Weights wp = P::weights(p);
-      if (MASK && sm.odd[it % 3]) P::template product_by_rows<ROW>(dv, gt + 32 * n * ROW, wp, lo, hi, lane);
-      else P::template product<ROW>(dv, gt + 32 * n * ROW, wp, lane);
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const f32x4_t d4 = *reinterpret_cast<const f32x4_t*>(delta + 8 * g);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int i = 8 * g + 4 * lh + e;
-          ds[4 * g + e] = p[4 * g + e] * (dp[4 * g + e] - d4[e]);
-          if (MASK && (i < lo || i >= hi)) ds[4 * g + e] = 0.f;
-        }
-      }
-      const typename P::Weights wd = P::weights(ds);
-      if (MASK && sm.odd[it % 3]) P::template product_by_rows<ROW>(dk, qt + 32 * n * ROW, wd, lo, hi, lane);
-      else P::template product<ROW>(dk, qt + 32 * n * ROW, wd, lane);
-    }
+  auto load = [&](const Place& p, int n) {
+    const int h = kvh * G + p.g, t0 = p.t * R, to = n % kBuffers;
+    L::template load<W>(sm.q[to], rows_of<T>(a.q, a.qs, qbase, h), a.qs[0], t0, nq - 1, wave, lane);
+    L::template load<W>(sm.g[to], rows_of<T>(a.dout, a.gs, qbase, h), a.gs[0], t0, nq - 1, wave, lane);
+    // one word a lane: lse of the tile's queries, then their delta; every wave brings the same
+    const float* stats = lane < R ? a.lse : a.delta;
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(stats + (int64_t)h * a.total_q + qbase + min(t0 + lane % R, nq - 1)),
+                                     (__attribute__((address_space(3))) void*)sm.stats[to], 4, 0, 0);
   };
-  for (int it = stream, n = 0; it - stream < total; it += S, ++n) {   // the streams meet at every barrier
-    const bool on = it < total;
-    const int t0 = on ? (first_tile + it % per_head) * R : 0;
-    const bool end = t0 + R > nq;
-    if (on) {
-      qs.template store<ROW>(sm.x[n & 1], tid);
-      gs.template store<ROW>(sm.y[n & 1], tid);
-      if (tid < R) sm.lse[n & 1][tid] = stat;
-      else if (tid < 2 * R) sm.delta[n & 1][tid - R] = stat;
-      if ((end || t0 < min(j0 + kPackedRows, nk) - 1 - off) && (qs.odd() || gs.odd())) sm.odd[n % 3] = 1;
+  constexpr int LOADS = 2 * L::loads(W) + 1;
+  bool odd = false;
+  auto sums = [&](int n, int t0, auto by_rows) {
+    // some query of the tile does not see all of the wave's keys, or is none
+    const bool mask = t0 + R > nq || t0 < min(k0 + 31, nk - 1) - off;
+    const T *qt = sm.q[n % kBuffers], *gt = sm.g[n % kBuffers];
+    const float* stats = sm.stats[n % kBuffers] + 4 * lh;
+    const int lo = from - t0, hi = nq - t0;   // rows that see this lane's key
+    auto hidden = [&](int r) { return 8 * (r / 4) + 4 * lh + r % 4 < lo || 8 * (r / 4) + 4 * lh + r % 4 >= hi; };
+    float p[16], ds[16];
+    const f32x16 s = P::scores(qt, k, lane);
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const f32x4_t l4 = *reinterpret_cast<const f32x4_t*>(stats + 8 * g);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) p[4 * g + e] = __builtin_amdgcn_exp2f(fmaf(s[4 * g + e], sc, -kLog2e * l4[e]));
     }
-    if (tid == 0) sm.odd[(n + 1) % 3] = 0;
-    lds_barrier();
-    if (it + S < total) load(it + S);
-    if (!on || k0 >= nk || t0 + R - 1 < k0 - off) continue;   // no key here, or none that a query of the tile sees
-    if (end || t0 < min(k0 + 31, nk - 1) - off) sums(n, t0, std::true_type{});
-    else sums(n, t0, std::false_type{});
-  }
-  lds_barrier();
+    if (mask) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) p[r] = hidden(r) ? 0.f : p[r];
+    }
+    const typename P::Weights wp = P::weights(p);
+    if (by_rows && mask && L::odd(gt, lane)) P::product_by_rows(dv, gt, wp, lo, hi, lane);
+    else P::product(dv, gt, wp, lane);
+    f32x16 dp;
+    if constexpr (kValuesInLds<T, D>) dp = P::scores_lds(gt, own_v, lane);
+    else dp = P::scores(gt, v, lane);
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const f32x4_t d4 = *reinterpret_cast<const f32x4_t*>(stats + R + 8 * g);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) ds[4 * g + e] = p[4 * g + e] * (dp[4 * g + e] - d4[e]);
+    }
+    if (mask) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) ds[r] = hidden(r) ? 0.f : ds[r];
+    }
+    const typename P::Weights wd = P::weights(ds);
+    if (by_rows && mask && L::odd(qt, lane)) P::product_by_rows(dk, qt, wd, lo, hi, lane);
+    else P::product(dk, qt, wd, lane);
+    if (!by_rows && mask) odd = odd || L::odd(qt, lane) || L::odd(gt, lane);
+  };
+  auto pass = [&](auto by_rows) {
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) dk[mt][r] = dv[mt][r] = 0.f;
+    if (total == 0) return;
+    Place now{0, first_tile - S + stream}, ahead = now;
+    next(now);
+    for (int n = 0; n < kBuffers - 1; ++n) {
+      next(ahead);
+      if (stream + S * n < total) load(ahead, n);
+    }
+    for (int it = stream, n = 0; it - stream < total; it += S, ++n, next(now)) {   // the streams meet at every barrier
+      if (it + S < total) loads_left<LOADS>();
+      else loads_left<0>();
+      lds_barrier();   // tile n is there, and nobody reads tile n - 1 any more
+      next(ahead);
+      if (it + (kBuffers - 1) * S < total) load(ahead, n + kBuffers - 1);
+      const int t0 = now.t * R;
+      // else no tile, no key, or none that a query of the tile sees
+      if (it < total && k0 < nk && t0 + R - 1 >= k0 - off) sums(n, t0, by_rows);
+    }
+    lds_barrier();   // every wave is done with the tiles
+  };
+  pass(std::false_type{});
+  if (any_wave(&all.flag, odd)) pass(std::true_type{});
   if constexpr (S > 1) {
     // the second stream's sums, a register of 64 lanes at a time
     static_assert(S == 2 && sizeof(KeyTiles<T, D>) >= kPackedRows * D * sizeof(float));
@@ -257,7 +275,7 @@ template <typename T, int D> __global__ __launch_bounds__((kPackedThreads * kStr
     if (stream) return;
   }
   if (k0 < nk) {
-    T* own = reinterpret_cast<T*>(smem_raw) + wave * 32 * P::BY_ROWS;
+    T* own = reinterpret_cast<T*>(smem_raw) + wave * 32 * kPutRow<T, D>;
     put_rows<T, D>(dk, a.scale, own, rows_of<T>(a.dk, a.dks, kbase + k0, kvh), a.dks[0], min(32, nk - k0), lane);
     put_rows<T, D>(dv, 1.f, own, rows_of<T>(a.dv, a.dvs, kbase + k0, kvh), a.dvs[0], min(32, nk - k0), lane);
   }

@@ -1,21 +1,28 @@
 // Forward pass of attention over packed sequences (packed.hpp has the formulas): softmax in one pass over the keys, with a
 // running maximum and sum per query.
 //
-// A workgroup holds 128 queries of one head, 32 a wave, and streams key and value tiles through two LDS buffers:
-// the next tile's rows come into registers while the present one is used.
+// A workgroup holds 128 queries of one head, 32 a wave, and streams key and value tiles through two LDS buffers: the next
+// tile's rows arrive while the present one is used.
 #include "packed.hpp"
+
+#include <algorithm>
 
 namespace gformer {
 namespace {
 
-template <typename T, int D> using FwdTiles = PackedTiles<T, Products<T, D>::R, Products<T, D>::BY_ROWS, Products<T, D>::TURNED>;
+template <typename T> constexpr int kFwdTile = sizeof(T) == 2 ? 64 : 32;   // keys per tile
+template <typename T, int D> struct alignas(256) FwdTiles {
+  T k[2][kFwdTile<T> * D], v[2][kFwdTile<T> * D];
+  int flag;
+};
 
 template <typename T, int D> __global__ __launch_bounds__(kPackedThreads, (sizeof(T) == 4 && D == 128 ? 1 : 2)) void packed_fwd_kernel(PackedArgs a, int tiles) {
   using P = Products<T, D>;
-  constexpr int R = P::R, KROW = P::BY_ROWS, VROW = P::TURNED, NS = R / 32, MT = D / 32;
-  extern __shared__ __align__(16) unsigned char smem_raw[];
+  constexpr int R = kFwdTile<T>, NS = R / 32, MT = D / 32, W = kPackedThreads / 64;
+  using L = Tile<T, D, R>;
+  extern __shared__ __align__(256) unsigned char smem_raw[];
   auto& sm = *reinterpret_cast<FwdTiles<T, D>*>(smem_raw);
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, ln = lane & 31, lh = lane >> 5;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), ln = lane & 31, lh = lane >> 5;
 
   // Heads fastest, the heads that share keys Hkv apart: workgroups are dealt to the 8 XCDs in turn, so that those of one key
   // head meet in few of them.  Last tiles first: they see the most keys.
@@ -41,31 +48,25 @@ template <typename T, int D> __global__ __launch_bounds__(kPackedThreads, (sizeo
   const float sc = (a.scale == 0.f ? 1e-30f : fabsf(a.scale)) * kLog2e;
 
   f32x16 o[MT];
-#pragma unroll
-  for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) o[mt][r] = 0.f;
-  float m = -INFINITY, l = 0.f;   // running maximum (base 2) and this half's share of the sum
+  float m, l;   // running maximum (base 2) and this half's share of the sum
 
   const T* kp = rows_of<T>(a.k, a.ks, kbase, kvh);
   const T* vp = rows_of<T>(a.v, a.vs, kbase, kvh);
   const int last_key = min(i0 + kPackedRows, nq) - 1 + off;   // of the workgroup; < 0: no query sees any
   const int n_tiles = last_key < 0 ? 0 : last_key / R + 1;
-  Stage<T, D, R> ks, vs;
-  if (n_tiles) {
-    ks.load(kp, a.ks[0], 0, nk - 1, tid);
-    vs.load(vp, a.vs[0], 0, nk - 1, tid);
-  }
-  if (tid < 3) sm.odd[tid] = 0;
-  lds_barrier();
-  auto attend = [&](int t, auto mask_tag) {
-    constexpr bool MASK = decltype(mask_tag)::value;
+  auto load = [&](int t) {
+    L::template load<W>(sm.k[t & 1], kp, a.ks[0], t * R, nk - 1, wave, lane);
+    L::template load<W>(sm.v[t & 1], vp, a.vs[0], t * R, nk - 1, wave, lane);
+  };
+  bool odd = false;
+  auto attend = [&](int t, auto by_rows) {
     const int t0 = t * R;
-    const T *kt = sm.x[t & 1], *vt = sm.y[t & 1];
+    const bool mask = t0 + R - 1 > q0 + off;   // some query of the wave does not see the whole tile
+    const T *kt = sm.k[t & 1], *vt = sm.v[t & 1];
     f32x16 s[NS];
 #pragma unroll
-    for (int n = 0; n < NS; ++n) s[n] = P::template scores<KROW>(kt + 32 * n * KROW, q, lane);
-    if (MASK) {
+    for (int n = 0; n < NS; ++n) s[n] = P::scores(kt + 32 * n * D, q, lane);
+    if (mask) {
 #pragma unroll
       for (int n = 0; n < NS; ++n)
 #pragma unroll
@@ -97,36 +98,42 @@ template <typename T, int D> __global__ __launch_bounds__(kPackedThreads, (sizeo
         l += p[r];   // before it is rounded for the product: the log-sum-exp is kept in 32 bits
       }
       const typename P::Weights w = P::weights(p);
-      if (MASK && sm.odd[t % 3]) P::template product_by_rows<VROW>(o, vt + 32 * n * VROW, w, 0, seen + 1 - t0 - 32 * n, lane);
-      else P::template product<VROW>(o, vt + 32 * n * VROW, w, lane);
+      if (by_rows && mask && L::odd(vt + 32 * n * D, lane)) P::product_by_rows(o, vt + 32 * n * D, w, 0, seen + 1 - t0 - 32 * n, lane);
+      else P::product(o, vt + 32 * n * D, w, lane);
+      if (!by_rows && mask) odd = odd || L::odd(vt + 32 * n * D, lane);
     }
   };
-  for (int t = 0; t < n_tiles; ++t) {
-    const int t0 = t * R;
-    ks.template store<KROW>(sm.x[t & 1], tid);
-    vs.template store<VROW>(sm.y[t & 1], tid);
-    if (t0 + R - 1 > i0 + off && vs.odd()) sm.odd[t % 3] = 1;   // some query of the workgroup does not see the whole tile
-    if (tid == 0) sm.odd[(t + 1) % 3] = 0;
-    lds_barrier();
-    if (t + 1 < n_tiles) {
-      ks.load(kp, a.ks[0], t0 + R, nk - 1, tid);
-      vs.load(vp, a.vs[0], t0 + R, nk - 1, tid);
+  auto pass = [&](auto by_rows) {
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[mt][r] = 0.f;
+    m = -INFINITY;
+    l = 0.f;
+    if (n_tiles) load(0);
+    for (int t = 0; t < n_tiles; ++t) {
+      loads_left<0>();
+      lds_barrier();   // tile t is there, and nobody reads tile t - 1 any more
+      if (t + 1 < n_tiles) load(t + 1);
+      if (t * R <= min(q0 + 31, nq - 1) + off) attend(t, by_rows);   // else nothing for this wave
     }
-    if (t0 > min(q0 + 31, nq - 1) + off) continue;   // nothing for this wave
-    if (t0 + R - 1 > q0 + off) attend(t, std::true_type{});
-    else attend(t, std::false_type{});
-  }
+    lds_barrier();   // every wave is done with the tiles
+  };
+  pass(std::false_type{});
+  if (any_wave(&sm.flag, odd)) pass(std::true_type{});
   l = sum_over_halves(l);
   if (a.lse && lh == 0 && i < nq)
     a.lse[(int64_t)h * a.total_q + qbase + i] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
-  lds_barrier();   // every wave is done with the tiles
-  if (q0 < nq)
-    put_rows<T, D>(o, l == 0.f ? 0.f : 1.f / l, reinterpret_cast<T*>(smem_raw) + wave * 32 * KROW,
-                   rows_of<T>(a.out, a.os, qbase + q0, h), a.os[0], min(32, nq - q0), lane);
+  if (q0 < nq) {
+    T* own = reinterpret_cast<T*>(smem_raw) + wave * 32 * kPutRow<T, D>;
+    const float by = l == 0.f ? 0.f : 1.f / l;
+    put_rows<T, D>(o, by, own, rows_of<T>(a.out, a.os, qbase + q0, h), a.os[0], min(32, nq - q0), lane);
+    if (sizeof(T) == 2 && a.rest) put_rows<T, D, true>(o, by, own, rows_of<T>(a.rest, a.os, qbase + q0, h), a.os[0], min(32, nq - q0), lane);
+  }
 }
 
 template <typename T, int D> hipError_t launch(const PackedArgs& a, hipStream_t s) {
-  const size_t smem = sizeof(FwdTiles<T, D>);
+  constexpr size_t smem = std::max(sizeof(FwdTiles<T, D>), kPackedRows * kPutRow<T, D> * sizeof(T));   // the rows leave through it
   auto kern = packed_fwd_kernel<T, D>;
   if (hipError_t e = allow_lds(kern, smem); e != hipSuccess) return e;
   const int64_t tiles = packed_tiles(a.total_q, a.n_seqs, kPackedRows);

@@ -33,14 +33,14 @@ def test_reference_gradients_against_differences():
 A = 1 << 20   # an aligned address that nothing reads: every call below is refused on the host
 
 
-def fwd(p=None, q=A, k=2 * A, v=3 * A, out=4 * A, lse=5 * A, cu_q=6 * A, cu_k=0, n=2, tq=8, tk=8, H=4, Hkv=2, d=64):
+def fwd(p=None, q=A, k=2 * A, v=3 * A, out=4 * A, rest=0, lse=5 * A, cu_q=6 * A, cu_k=0, n=2, tq=8, tk=8, H=4, Hkv=2, d=64):
     p = p or gb.make_packed_params()
-    return gb.lib().gformer_packed_attn_fwd(q, k, v, out, lse, cu_q, cu_k, n, tq, tk, H, Hkv, d, ctypes.byref(p), None)
+    return gb.lib().gformer_packed_attn_fwd(q, k, v, out, rest, lse, cu_q, cu_k, n, tq, tk, H, Hkv, d, ctypes.byref(p), None)
 
 
-def bwd(p=None, ws=7 * A, ws_bytes=1 << 20, dq=8 * A, dk=9 * A, dv=10 * A, lse=5 * A, cu_k=0, tq=8, tk=8, dout=11 * A):
+def bwd(p=None, ws=7 * A, ws_bytes=1 << 20, dq=8 * A, dk=9 * A, dv=10 * A, lse=5 * A, cu_k=0, tq=8, tk=8, dout=11 * A, rest=0):
     p = p or gb.make_packed_params()
-    return gb.lib().gformer_packed_attn_bwd(A, 2 * A, 3 * A, 4 * A, lse, dout, dq, dk, dv, 6 * A, cu_k, 2, tq, tk, 4, 2, 64,
+    return gb.lib().gformer_packed_attn_bwd(A, 2 * A, 3 * A, 4 * A, rest, lse, dout, dq, dk, dv, 6 * A, cu_k, 2, tq, tk, 4, 2, 64,
                                             ctypes.byref(p), ws, ws_bytes, None)
 
 
@@ -65,6 +65,7 @@ def test_forward_refusals(kw, status):
 @pytest.mark.parametrize("kw,status", [
     (dict(ws=0), 3), (dict(ws_bytes=127), 3), (dict(ws=A + 16), 1), (dict(dq=0), 1), (dict(lse=0), 1), (dict(dout=0), 1), (dict(dq=A), 1),
     (dict(dk=9 * A, dv=9 * A), 1), (dict(dv=5 * A), 1), (dict(dk=A + 8), 1), (dict(tk=7), 1), (dict(p=wrong(dk_stride=(8, 64))), 1),
+    (dict(rest=8 * A), 1), (dict(rest=12 * A, p=gb.make_packed_params(gb.GF_F32)), 1),
 ])
 def test_backward_refusals(kw, status):
     assert bwd(**kw) == status
@@ -119,14 +120,15 @@ def cu(lens):
     return torch.tensor(ref.offsets(lens), dtype=torch.int32).cuda()
 
 
-def run(q, k, v, g, lens_q, lens_k, scale, zero_tail=0, fill=7.0, same=False):
+def run(q, k, v, g, lens_q, lens_k, scale, zero_tail=0, fill=7.0, same=False, rest=False):
     out, dq, dk, dv = (torch.full(x.shape, fill, dtype=q.dtype, device="cuda") for x in (q, q, k, k))
     lse = torch.full((q.shape[1], q.shape[0]), fill, device="cuda")
+    rest = torch.full_like(out, fill) if rest and q.dtype == torch.bfloat16 else None
     cq, ck = cu(lens_q), None if same else cu(lens_k)
-    gb.gformer_packed_attn_fwd(q, k, v, out, cq, ck, lse=lse, softmax_scale=scale, zero_tail=zero_tail)
-    gb.gformer_packed_attn_bwd(q, k, v, out, lse, g, dq, dk, dv, cq, ck, softmax_scale=scale, zero_tail=zero_tail)
+    gb.gformer_packed_attn_fwd(q, k, v, out, cq, ck, lse=lse, out_rest=rest, softmax_scale=scale, zero_tail=zero_tail)
+    gb.gformer_packed_attn_bwd(q, k, v, out, lse, g, dq, dk, dv, cq, ck, out_rest=rest, softmax_scale=scale, zero_tail=zero_tail)
     torch.cuda.synchronize()
-    return {"out": out, "lse": lse, "dq": dq, "dk": dk, "dv": dv}
+    return {"out": out, "lse": lse, "dq": dq, "dk": dk, "dv": dv, "rest": rest}
 
 
 def compare(got, want, lens_q, lens_k):
@@ -151,6 +153,24 @@ def test_values_and_gradients(dtype, d, H, Hkv, shape):
     q, k, v, g = tensors(lens_q, lens_k, H, Hkv, d, dtype, 10 * shape + H, layout="fused" if same else "heads")
     got = run(q, k, v, g, lens_q, lens_k, d ** -0.5, same=same)
     compare(got, ref.packed(q, k, v, g, lens_q, lens_k, d ** -0.5, dtype), lens_q, lens_k)
+
+
+@gpu
+@pytest.mark.parametrize("d", [64, 128])
+def test_what_rounding_takes_from_the_output(d):
+    """out + rest is the output before its rounding, up to rest's own; dq and dk then come nearer to the formula's."""
+    lens = [200, 70]
+    q, k, v, g = tensors(lens, lens, 4, 2, d, "bf16", 15)
+    want = ref.packed(q, k, v, g, lens, lens, d ** -0.5, "bf16")
+    plain, got = run(q, k, v, g, lens, lens, d ** -0.5), run(q, k, v, g, lens, lens, d ** -0.5, rest=True)
+    compare(got, want, lens, lens)
+    assert torch.equal(plain["out"], got["out"])
+    both = got["out"].double().cpu() + got["rest"].double().cpu()
+    # what is left: the weights' rounding, and half a step of rest's, which is half a step of out at most
+    ref.check(both, want["out"][0], want["out"][1] - ref.HALF["bf16"] * want["out"][0].abs() * (1 - 2 * ref.HALF["bf16"]), "out + rest")
+    for name in ("dq", "dk"):
+        off = [(x[name].double().cpu() - want[name][0]).norm() for x in (plain, got)]
+        assert off[1] < off[0], name
 
 
 @gpu
