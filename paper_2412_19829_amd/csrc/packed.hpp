@@ -25,7 +25,7 @@ struct PackedArgs {
   void *out, *dq, *dk, *dv;       // out: written by the forward pass, read by the backward pass
   void* rest;                     // what rounding took from out, in bf16 and laid out like it; may be null
   float* lse;                     // [H, total_q], natural logarithm; may be null in the forward pass
-  float* delta;                   // [H, total_q], workspace of the backward pass
+  float* stats;                   // [2, H, total_q], workspace of the backward pass: lse in base 2, and -delta
   const int32_t *cu_q, *cu_k;     // [n_seqs + 1]
   int n_seqs, total_q, total_k, H, Hkv, d;
   int zero_tail;                  // rows behind the last sequence are set to zero
@@ -183,6 +183,7 @@ template <int N, int X, int OFF> __device__ __forceinline__ void lds_get_turned(
 
 // The matrix products of one wave, for 32 resident and 32 streamed rows.
 template <typename T, int D> struct Products;
+constexpr f32x16 kZeroTile = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 
 template <int D> struct Products<uint16_t, D> {
   using T = uint16_t;
@@ -221,24 +222,33 @@ template <int D> struct Products<uint16_t, D> {
     lds_get_turned<D / 32, 32 * KB * D, 16 * D>(x, at, at ^ (16 * L::swz(8)));
   }
   static __device__ __forceinline__ bf16x8 piece(uint32_t at, int ks) { return as_bf16x8(lds_get<u32x4>(at ^ (32 * ks))); }
-  // 32 streamed rows against the resident ones
-  static __device__ __forceinline__ f32x16 scores(const T* rows, const Resident& r, int lane) {
+  // 32 streamed rows against the resident ones, added to s
+  static __device__ __forceinline__ f32x16 scores(const T* rows, const Resident& r, int lane, f32x16 s = kZeroTile) {
     const uint32_t at = lds_lane(rows, row_at(lane));
-    f32x16 s;
+    // all reads first: left alone, the compiler has each product wait for its own
+    bf16x8 x[D / 16];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s[i] = 0.f;
+    for (int ks = 0; ks < D / 16; ++ks) x[ks] = piece(at, ks);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks) s = mfma32(piece(at, ks), r.x[ks], s);
+    for (int ks = 0; ks < D / 16; ++ks) s = mfma32(x[ks], r.x[ks], s);
     return s;
   }
   // the same with the resident rows in a tile of LDS too
-  static __device__ __forceinline__ f32x16 scores_lds(const T* rows, const T* own, int lane) {
+  static __device__ __forceinline__ f32x16 scores_lds(const T* rows, const T* own, int lane, f32x16 s) {
     const uint32_t at = lds_lane(rows, row_at(lane)), own_at = lds_lane(own, row_at(lane));
-    f32x16 s;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s[i] = 0.f;
+    for (int k0 = 0; k0 < D / 16; k0 += 2) {
+      bf16x8 x[2], y[2];
 #pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks) s = mfma32(piece(at, ks), piece(own_at, ks), s);
+      for (int ks = 0; ks < 2; ++ks) {
+        x[ks] = piece(at, k0 + ks);
+        y[ks] = piece(own_at, k0 + ks);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) s = mfma32(x[ks], y[ks], s);
+    }
     return s;
   }
   static __device__ __forceinline__ void to_lds(const Resident& r, T* own, int lane) {
@@ -330,16 +340,18 @@ template <int D> struct Products<float, D> {
       for (int j = 0; j < 4; ++j) s = fmaf(a.x[i][j], b.x[i][j], s);
     return sum_over_halves(s);
   }
-  static __device__ __forceinline__ f32x16 scores(const T* rows, const Resident& r, int lane) {
+  static __device__ __forceinline__ f32x16 scores(const T* rows, const Resident& r, int lane, f32x16 s = kZeroTile) {
     const uint32_t at = lds_lane(rows, 4 * ((lane & 31) * D + 4 * ((lane >> 5) ^ L::swz(lane & 31))));
-    f32x16 s;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s[i] = 0.f;
+    for (int i0 = 0; i0 < D / 8; i0 += 4) {
+      f32x4_t a[4];
 #pragma unroll
-    for (int i = 0; i < D / 8; ++i) {
-      const f32x4_t a = lds_get<f32x4_t>(at ^ (32 * i));
+      for (int i = 0; i < 4; ++i) a[i] = lds_get<f32x4_t>(at ^ (32 * (i0 + i)));
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) s = mfma(a[j], r.x[i][j], s);
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s = mfma(a[i][j], r.x[i0 + i][j], s);
     }
     return s;
   }

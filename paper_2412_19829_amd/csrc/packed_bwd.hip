@@ -1,6 +1,6 @@
 // Backward pass of attention over packed sequences (packed.hpp has the formulas), in two passes that take the
 // weights again from the scores and the forward pass's log-sum-exp:
-//   dq      queries resident, keys and values streamed; also leaves delta for the other pass
+//   dq      queries resident, keys and values streamed; also leaves both statistics of a query for the other pass
 //   dk, dv  keys resident, the queries of every head that shares them streamed, one head after another: their sums
 //           need no atomics, and come out in one order
 #include "packed.hpp"
@@ -12,7 +12,8 @@ namespace {
 template <typename T, int D> constexpr int kWaves = sizeof(T) == 4 && D == 128 ? 1 : 2;
 // keys per tile of the dq pass
 template <typename T, int D> constexpr int kKeyTile = sizeof(T) == 2 && D == 64 ? 64 : 32;
-constexpr int kQueryTile = 32;   // queries per tile of the dk, dv pass
+// queries per tile of the dk, dv pass
+template <typename T, int D> constexpr int kQueryTile = sizeof(T) == 2 && D == 64 ? 64 : 32;
 // That pass's workgroups take the query tiles of their keys in this many streams, four waves each, whose sums are joined at
 // the end.  A causal sequence's first keys are seen by all its queries, its last by few, and there are only as many workgroups as
 // key tiles and key heads: the longest one decides, and with two streams it takes half as long.
@@ -25,8 +26,8 @@ template <typename T, int D> struct alignas(256) DqTiles {
   int flag;
 };
 template <typename T, int D> struct alignas(256) QueryTiles {
-  T q[kBuffers][kQueryTile * D], g[kBuffers][kQueryTile * D];
-  float stats[kBuffers][2 * kQueryTile];   // a tile's lse, then its delta
+  T q[kBuffers][kQueryTile<T, D> * D], g[kBuffers][kQueryTile<T, D> * D];
+  float stats[kBuffers][2 * kQueryTile<T, D>];   // in base 2: lse of the queries, then -delta
 };
 template <typename T, int D> struct alignas(256) KeyTiles {
   QueryTiles<T, D> stream[kStreams<T, D>];
@@ -68,8 +69,8 @@ template <typename T, int D> __global__ __launch_bounds__(kPackedThreads, (kWave
   g = q;
   P::load(q, rows_of<T>(a.q, a.qs, qbase + ic, h), lane, a.scale < 0.f);
   const int64_t stat = (int64_t)h * a.total_q + qbase + ic;
-  if (lh == 0 && i < nq) a.delta[stat] = delta;
   const float lse = a.lse[stat] * kLog2e;
+  if (i < nq) a.stats[stat + (lh ? (int64_t)a.H * a.total_q : 0)] = lh ? -delta : lse;
   const float sc = (a.scale == 0.f ? 1e-30f : fabsf(a.scale)) * kLog2e;
 
   f32x16 dq[MT];
@@ -128,7 +129,7 @@ template <typename T, int D> __global__ __launch_bounds__(kPackedThreads, (kWave
 
 template <typename T, int D> __global__ __launch_bounds__((kPackedThreads * kStreams<T, D>), (kWaves<T, D>)) void packed_dkdv_kernel(PackedArgs a, int tiles) {
   using P = Products<T, D>;
-  constexpr int R = kQueryTile, MT = D / 32, W = kPackedThreads / 64;
+  constexpr int R = kQueryTile<T, D>, MT = D / 32, W = kPackedThreads / 64;
   using L = Tile<T, D, R>;
   extern __shared__ __align__(256) unsigned char smem_raw[];
   constexpr int S = kStreams<T, D>;
@@ -179,18 +180,22 @@ template <typename T, int D> __global__ __launch_bounds__((kPackedThreads * kStr
     const int h = kvh * G + p.g, t0 = p.t * R, to = n % kBuffers;
     L::template load<W>(sm.q[to], rows_of<T>(a.q, a.qs, qbase, h), a.qs[0], t0, nq - 1, wave, lane);
     L::template load<W>(sm.g[to], rows_of<T>(a.dout, a.gs, qbase, h), a.gs[0], t0, nq - 1, wave, lane);
-    // one word a lane: lse of the tile's queries, then their delta; every wave brings the same
-    const float* stats = lane < R ? a.lse : a.delta;
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(stats + (int64_t)h * a.total_q + qbase + min(t0 + lane % R, nq - 1)),
-                                     (__attribute__((address_space(3))) void*)sm.stats[to], 4, 0, 0);
+    // one word a lane: what is left of a wave, or the other statistic; every wave brings the same
+#pragma unroll
+    for (int x = 0; x < R / 32; ++x) {
+      const int64_t at_stat = (int64_t)(R == 64 ? x : lane / 32) * a.H * a.total_q + (int64_t)h * a.total_q + qbase + min(t0 + lane % R, nq - 1);
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(a.stats + at_stat),
+                                       (__attribute__((address_space(3))) void*)(sm.stats[to] + 64 * x), 4, 0, 0);
+    }
   };
-  constexpr int LOADS = 2 * L::loads(W) + 1;
+  constexpr int LOADS = 2 * L::loads(W) + R / 32;
   bool odd = false;
-  auto sums = [&](int n, int t0, auto by_rows) {
-    // some query of the tile does not see all of the wave's keys, or is none
-    const bool mask = t0 + R > nq || t0 < min(k0 + 31, nk - 1) - off;
-    const T *qt = sm.q[n % kBuffers], *gt = sm.g[n % kBuffers];
-    const float* stats = sm.stats[n % kBuffers] + 4 * lh;
+  // 32 of the queries of the stream's n-th tile, from t0 on
+  auto sums = [&](int n, int part, int t0, auto by_rows) {
+    // some query does not see all of the wave's keys, or is none
+    const bool mask = t0 + 32 > nq || t0 < min(k0 + 31, nk - 1) - off;
+    const T *qt = sm.q[n % kBuffers] + 32 * part * D, *gt = sm.g[n % kBuffers] + 32 * part * D;
+    const float* stats = sm.stats[n % kBuffers] + 32 * part + 4 * lh;
     const int lo = from - t0, hi = nq - t0;   // rows that see this lane's key
     auto hidden = [&](int r) { return 8 * (r / 4) + 4 * lh + r % 4 < lo || 8 * (r / 4) + 4 * lh + r % 4 >= hi; };
     float p[16], ds[16];
@@ -199,7 +204,7 @@ template <typename T, int D> __global__ __launch_bounds__((kPackedThreads * kStr
     for (int g = 0; g < 4; ++g) {
       const f32x4_t l4 = *reinterpret_cast<const f32x4_t*>(stats + 8 * g);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) p[4 * g + e] = __builtin_amdgcn_exp2f(fmaf(s[4 * g + e], sc, -kLog2e * l4[e]));
+      for (int e = 0; e < 4; ++e) p[4 * g + e] = __builtin_amdgcn_exp2f(fmaf(s[4 * g + e], sc, -l4[e]));
     }
     if (mask) {
 #pragma unroll
@@ -208,15 +213,17 @@ template <typename T, int D> __global__ __launch_bounds__((kPackedThreads * kStr
     const typename P::Weights wp = P::weights(p);
     if (by_rows && mask && L::odd(gt, lane)) P::product_by_rows(dv, gt, wp, lo, hi, lane);
     else P::product(dv, gt, wp, lane);
-    f32x16 dp;
-    if constexpr (kValuesInLds<T, D>) dp = P::scores_lds(gt, own_v, lane);
-    else dp = P::scores(gt, v, lane);
+    f32x16 dp;   // the sums start from -delta
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
       const f32x4_t d4 = *reinterpret_cast<const f32x4_t*>(stats + R + 8 * g);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) ds[4 * g + e] = p[4 * g + e] * (dp[4 * g + e] - d4[e]);
+      for (int e = 0; e < 4; ++e) dp[4 * g + e] = d4[e];
     }
+    if constexpr (kValuesInLds<T, D>) dp = P::scores_lds(gt, own_v, lane, dp);
+    else dp = P::scores(gt, v, lane, dp);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) ds[r] = p[r] * dp[r];
     if (mask) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) ds[r] = hidden(r) ? 0.f : ds[r];
@@ -246,7 +253,9 @@ template <typename T, int D> __global__ __launch_bounds__((kPackedThreads * kStr
       if (it + (kBuffers - 1) * S < total) load(ahead, n + kBuffers - 1);
       const int t0 = now.t * R;
       // else no tile, no key, or none that a query of the tile sees
-      if (it < total && k0 < nk && t0 + R - 1 >= k0 - off) sums(n, t0, by_rows);
+#pragma unroll
+      for (int x = 0; x < R / 32; ++x)
+        if (it < total && k0 < nk && t0 + 32 * x + 31 >= k0 - off && t0 + 32 * x < nq) sums(n, x, t0 + 32 * x, by_rows);
     }
     lds_barrier();   // every wave is done with the tiles
   };

@@ -16,7 +16,7 @@ template <typename T, int D> struct alignas(256) FwdTiles {
   int flag;
 };
 
-template <typename T, int D> __global__ __launch_bounds__(kPackedThreads, (sizeof(T) == 4 && D == 128 ? 1 : 2)) void packed_fwd_kernel(PackedArgs a, int tiles) {
+template <typename T, int D> __global__ __launch_bounds__(kPackedThreads, (sizeof(T) == 4 && D == 128 ? 1 : D == 64 ? 3 : 2)) void packed_fwd_kernel(PackedArgs a, int tiles) {
   using P = Products<T, D>;
   constexpr int R = kFwdTile<T>, NS = R / 32, MT = D / 32, W = kPackedThreads / 64;
   using L = Tile<T, D, R>;
