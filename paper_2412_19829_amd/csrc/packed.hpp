@@ -71,6 +71,50 @@ template <int R> __device__ __forceinline__ SeqTile find_tile(const int32_t* cu,
   return {lo, (tile - lo - packed_row(cu, lo, total) / R) * R};
 }
 
+// The same with the longest work first, which evens out the end of a launch: a tile's level is how many tiles of R keys its
+// queries see (FIRST_IS_LONG: how many tiles of the sequence lie behind it, for keys, which the later queries see), and tile
+// number `rank` is taken in order of falling levels.  The sequences' tiles are counted for 64 levels at a time, in as many
+// steps as there are sequences; with more than kRanked, where no single one weighs much, the order is the tensors'.
+constexpr int kRanked = 32;
+template <int R, bool FIRST_IS_LONG>
+__device__ __forceinline__ SeqTile ranked_tile(const int32_t* cu, int total, const int32_t* cu_seen, int total_seen, int n_seqs, int rank,
+                                               int tiles, int lane) {
+  if (n_seqs > kRanked) return find_tile<R>(cu, n_seqs, total, FIRST_IS_LONG ? rank : tiles - 1 - rank, lane);
+  const int s = min(lane, n_seqs - 1);
+  int nt = 0, from = 0;   // this lane's sequence: its tiles, and the first one's level
+  if (lane < n_seqs) {
+    const int len = max(packed_row(cu, s + 1, total) - packed_row(cu, s, total), 0);
+    nt = (len + R - 1) / R;
+    if (!FIRST_IS_LONG) from = max(packed_row(cu_seen, s + 1, total_seen) - packed_row(cu_seen, s, total_seen) - len, 0) / R;
+  }
+  int lo = 0, hi = 1;
+  for (int i = 0; i < n_seqs; ++i) hi = max(hi, __builtin_amdgcn_readlane(nt, i) + __builtin_amdgcn_readlane(from, i));
+  // tiles of level l and above
+  auto above = [&](int l) {
+    int n = 0;
+    for (int i = 0; i < n_seqs; ++i) {
+      const int x = __builtin_amdgcn_readlane(nt, i);
+      n += min(max(x + __builtin_amdgcn_readlane(from, i) - l, 0), x);
+    }
+    return n;
+  };
+  do {
+    const int step = (hi - lo + 63) / 64, l = lo + lane * step;
+    const int n = __popcll(__builtin_amdgcn_ballot_w64(l < hi && above(l) > rank));
+    if (n == 0) {   // lane 0 knows all tiles: what is left are the rows behind the last sequence
+      const int all = __builtin_amdgcn_readfirstlane(above(0));
+      return {n_seqs, (rank - all) * R};
+    }
+    lo = __builtin_amdgcn_readfirstlane(lo + (n - 1) * step);
+    hi = __builtin_amdgcn_readfirstlane(min(hi, lo + step));
+  } while (hi - lo > 1);
+  uint64_t at = __builtin_amdgcn_ballot_w64(from <= lo && lo < nt + from);   // the sequences with a tile of this level
+  for (int i = rank - __builtin_amdgcn_readfirstlane(above(lo + 1)); i > 0; --i) at &= at - 1;
+  const int seq = __builtin_ctzll(at);
+  const int tile = FIRST_IS_LONG ? __builtin_amdgcn_readlane(nt, seq) - 1 - lo : lo - __builtin_amdgcn_readlane(from, seq);
+  return {seq, tile * R};
+}
+
 // Offsets of a pointer of either element type.
 template <typename T> __device__ __forceinline__ const T* rows_of(const void* p, const int64_t (&st)[2], int64_t row, int head) {
   return reinterpret_cast<const T*>(p) + row * st[0] + head * st[1];
@@ -87,14 +131,17 @@ __device__ __forceinline__ float maximum3(float a, float b, float c) {
 
 // A tile of R streamed rows in LDS: rows one behind another with no padding, as a load into LDS writes them (64 lanes, 16
 // bytes each, in lane order), the 16-byte pieces of row r at places that differ by swz(r).  swz moves bits of r about, so
-// swz(a ^ b) = swz(a) ^ swz(b), and makes both ways of reading free of bank conflicts: 16 rows at one column take the 16 pieces
-// of 256 bytes, and so do 4 neighbouring rows (8 with the other half of the wave) at two neighbouring pieces.
+// swz(a ^ b) = swz(a) ^ swz(b), and keeps both ways of reading off each other's banks (256 bytes a cycle):
+//   rows, 16 bytes a lane    lanes 0-3, 12-15, 20-23, 24-27 go together, then the others of the half: 16 different pieces
+//   transposed, bf16         a half's lanes: two neighbouring pairs of pieces in each of 4 rows, which the low bits of r set apart
+//   transposed, fp32         8 pieces of a row and of the one 4 further on, which bit 2 of r sets apart
 template <typename T, int D, int R> struct Tile {
   static constexpr int E = 16 / (int)sizeof(T), C = D / E;   // elements a piece, pieces a row
   static constexpr int RPI = 64 / C;                          // rows an instruction loads
   static constexpr int SIZE = R * D;
   __host__ __device__ static constexpr int swz(int r) {
-    return C == 8 ? (((r >> 1) & 3) << 1) | ((r >> 3) & 1) : ((r & 7) << 1) | ((r >> 3) & 1);
+    if (sizeof(T) == 4) return ((r & 7) << 1) | ((r >> 3) & 1);
+    return (C == 8 ? ((r >> 1) & 1) << 2 : (r & 3) << 2) | ((r >> 2) & 3);
   }
   static constexpr int loads(int waves) { return R / (RPI * waves); }
   // Rows r0 .. r0 + R - 1 of [rows, D] at `base`, by W waves; those past `last` are row `last`: in bounds, and masked later.

@@ -44,7 +44,7 @@ template <typename T, int D> __global__ __launch_bounds__(kPackedThreads, (kWave
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), ln = lane & 31, lh = lane >> 5;
 
   const int hh = blockIdx.x % a.H, kvh = hh % a.Hkv, h = kvh * (a.H / a.Hkv) + hh / a.Hkv;
-  const SeqTile at = find_tile<kPackedRows>(a.cu_q, a.n_seqs, a.total_q, tiles - 1 - blockIdx.x / a.H, lane);
+  const SeqTile at = ranked_tile<kPackedRows, false>(a.cu_q, a.total_q, a.cu_k, a.total_k, a.n_seqs, blockIdx.x / a.H, tiles, lane);
   if (at.first < 0) return;
   const int qbase = packed_row(a.cu_q, at.seq, a.total_q), i0 = at.first;
   if (at.seq == a.n_seqs) {
@@ -138,9 +138,8 @@ template <typename T, int D> __global__ __launch_bounds__((kPackedThreads * kStr
   auto& sm = all.stream[stream];
   const int tid = threadIdx.x % kPackedThreads, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), ln = lane & 31, lh = lane >> 5;
 
-  // first tiles first: the most queries see them
   const int kvh = blockIdx.x % a.Hkv;
-  const SeqTile at = find_tile<kPackedRows>(a.cu_k, a.n_seqs, a.total_k, blockIdx.x / a.Hkv, lane);
+  const SeqTile at = ranked_tile<kPackedRows, true>(a.cu_k, a.total_k, a.cu_q, a.total_q, a.n_seqs, blockIdx.x / a.Hkv, tiles, lane);
   if (at.first < 0) return;
   const int kbase = packed_row(a.cu_k, at.seq, a.total_k), j0 = at.first;
   if (at.seq == a.n_seqs) {

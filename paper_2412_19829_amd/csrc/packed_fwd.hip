@@ -25,9 +25,9 @@ template <typename T, int D> __global__ __launch_bounds__(kPackedThreads, (sizeo
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), ln = lane & 31, lh = lane >> 5;
 
   // Heads fastest, the heads that share keys Hkv apart: workgroups are dealt to the 8 XCDs in turn, so that those of one key
-  // head meet in few of them.  Last tiles first: they see the most keys.
+  // head meet in few of them.
   const int hh = blockIdx.x % a.H, kvh = hh % a.Hkv, h = kvh * (a.H / a.Hkv) + hh / a.Hkv;
-  const SeqTile at = find_tile<kPackedRows>(a.cu_q, a.n_seqs, a.total_q, tiles - 1 - blockIdx.x / a.H, lane);
+  const SeqTile at = ranked_tile<kPackedRows, false>(a.cu_q, a.total_q, a.cu_k, a.total_k, a.n_seqs, blockIdx.x / a.H, tiles, lane);
   if (at.first < 0) return;
   const int qbase = packed_row(a.cu_q, at.seq, a.total_q), i0 = at.first;
   if (at.seq == a.n_seqs) {
