@@ -26,6 +26,7 @@ struct PackedArgs {
   void* rest;                     // what rounding took from out, in bf16 and laid out like it; may be null
   float* lse;                     // [H, total_q], natural logarithm; may be null in the forward pass
   float* stats;                   // [2, H, total_q], workspace of the backward pass: lse in base 2, and -delta
+  float* sums;                    // [groups, 2, total_k, Hkv, d]: dk and dv of every part of the heads
   const int32_t *cu_q, *cu_k;     // [n_seqs + 1]
   int n_seqs, total_q, total_k, H, Hkv, d;
   int zero_tail;                  // rows behind the last sequence are set to zero
@@ -35,20 +36,42 @@ struct PackedArgs {
 };
 hipError_t launch_packed_fwd(const PackedArgs& a, bool bf16, hipStream_t s);
 hipError_t launch_packed_bwd(const PackedArgs& a, bool bf16, hipStream_t s);
+// What the backward pass keeps beside a query's statistics: the query heads of a key head in `groups` parts, whose dk and dv
+// are added up by a kernel of their own (1: there is none).
+int packed_head_groups(int total_k, int n_seqs, int H, int Hkv);
+inline size_t packed_stats_bytes(int total_q, int H) { return ((size_t)total_q * H * 2 * sizeof(float) + 255) / 256 * 256; }
+inline size_t packed_sums_bytes(int total_k, int n_seqs, int H, int Hkv, int d) {
+  const int groups = packed_head_groups(total_k, n_seqs, H, Hkv);
+  return groups == 1 ? 0 : (size_t)groups * total_k * Hkv * d * 2 * sizeof(float);
+}
 
 namespace {
 
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 
-constexpr int kPackedThreads = 256;
-constexpr int kPackedRows = kPackedThreads / 64 * 32;   // resident rows per workgroup
+constexpr int kPackedRows = 128;   // resident rows of a workgroup, where the streamed ones are not split over its waves
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
+// How a workgroup's waves share its work: RW of them side by side, 32 resident rows each, and S such sets ("streams") that
+// take the streamed tiles in turn and join their sums at the end.  R streamed rows a tile, BUF tiles of a stream in LDS
+// (one in use, the others on their way); registers are kept down for PER_SIMD waves on a SIMD.
+template <int RW_, int S_, int R_, int BUF_, int PER_SIMD_> struct Shape {
+  static constexpr int RW = RW_, S = S_, R = R_, BUF = BUF_, PER_SIMD = PER_SIMD_, ROWS = 32 * RW, THREADS = 64 * RW * S;
+};
 // Tiles of R rows over all sequences, none straddling two: sequence s owns tiles cu[s] / R + s up to the next
 // one's.  That is at least as many as it needs (floor(b / R) + 1 - floor(a / R) >= ceil((b - a) / R)), takes no
 // prefix sum and no look at the offsets on the host; the few tiles too many end at once.  The rows behind the last sequence
 // count as sequence n_seqs.
 inline int64_t packed_tiles(int total, int n_seqs, int rows) { return (int64_t)total / rows + n_seqs + 1; }
+
+// Whether a call has so few workgroups of kPackedRows rows that their waves are better off on different streamed rows of the
+// same resident ones.  That divides the longest workgroup's time by the streams, and loads every streamed row as many times
+// more often: worth it as long as about `limit` workgroups or fewer would leave compute units idle, or half as many where sequences
+// are short (a mean of less than 512 rows), whose joins weigh more.
+inline bool packed_splits(int rows, int heads, int n_seqs, int limit) {
+  if ((int64_t)rows < (int64_t)512 * n_seqs) limit /= 2;
+  return (int64_t)rows * heads <= (int64_t)limit * kPackedRows;
+}
 
 struct SeqTile {
   int seq;     // n_seqs: the rows behind the last sequence
@@ -469,9 +492,9 @@ __device__ __forceinline__ void put_rows(const f32x16 (&acc)[D / 32], float by, 
 }
 
 // Zeros in rows [0, rows) of a workgroup's tile.
-template <typename T, int D> __device__ __forceinline__ void zero_rows(T* to, int64_t stride, int rows, int tid) {
+template <typename T, int D> __device__ __forceinline__ void zero_rows(T* to, int64_t stride, int rows, int tid, int threads) {
   constexpr int C = D * (int)sizeof(T) / 16;
-  for (int r = tid / C; r < rows; r += kPackedThreads / C)
+  for (int r = tid / C; r < rows; r += threads / C)
     *reinterpret_cast<u32x4*>(to + r * stride + (16 / (int)sizeof(T)) * (tid % C)) = u32x4{0, 0, 0, 0};
 }
 

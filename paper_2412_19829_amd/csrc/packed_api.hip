@@ -165,7 +165,7 @@ size_t gformer_packed_attn_bwd_workspace_bytes(int total_q, int total_k, int n_s
                                                const gformer_packed_params* p) {
   PackedArgs a;
   if (check_packed(n_seqs, total_q, total_k, H, Hkv, d, p, &a) != GF_OK) return 0;
-  return ((size_t)total_q * H * 2 * sizeof(float) + 255) / 256 * 256;
+  return packed_stats_bytes(total_q, H) + packed_sums_bytes(total_k, n_seqs, H, Hkv, d);
 }
 
 gf_status gformer_packed_attn_bwd(const void* q, const void* k, const void* v, const void* out, const void* out_rest,
@@ -202,6 +202,7 @@ gf_status gformer_packed_attn_bwd(const void* q, const void* k, const void* v, c
   a.dk = dk;
   a.dv = dv;
   a.stats = static_cast<float*>(workspace);
+  a.sums = a.stats + packed_stats_bytes(total_q, H) / sizeof(float);
   a.cu_q = cu_q;
   a.cu_k = cu_k ? cu_k : cu_q;
   return status(launch_packed_bwd(a, p->dtype == GF_BF16, reinterpret_cast<hipStream_t>(hip_stream)));

@@ -5,51 +5,86 @@
 //           need no atomics, and come out in one order
 #include "packed.hpp"
 
+#include <algorithm>
+
 namespace gformer {
 namespace {
 
 // waves on a SIMD that the kernels' registers are kept down for
 template <typename T, int D> constexpr int kWaves = sizeof(T) == 4 && D == 128 ? 1 : 2;
-// keys per tile of the dq pass
-template <typename T, int D> constexpr int kKeyTile = sizeof(T) == 2 && D == 64 ? 64 : 32;
-// queries per tile of the dk, dv pass
-template <typename T, int D> constexpr int kQueryTile = sizeof(T) == 2 && D == 64 ? 64 : 32;
-// That pass's workgroups take the query tiles of their keys in this many streams, four waves each, whose sums are joined at
-// the end.  A causal sequence's first keys are seen by all its queries, its last by few, and there are only as many workgroups as
-// key tiles and key heads: the longest one decides, and with two streams it takes half as long.
-template <typename T, int D> constexpr int kStreams = kWaves<T, D>;
+
+// dq: as the forward pass; SPLIT has its waves on different keys
+template <typename T, int D, bool SPLIT> struct DqShape_;
+template <typename T, int D> struct DqShape_<T, D, false> {
+  using type = Shape<4, 1, sizeof(T) == 2 && D == 64 ? 64 : 32, 3, kWaves<T, D>>;
+};
+template <typename T, int D> struct DqShape_<T, D, true> {
+  using type = std::conditional_t<sizeof(T) == 4 && D == 128, Shape<2, 2, 32, 2, 1>, Shape<1, 4, 32, 2, sizeof(T) == 2 && D == 64 ? 2 : 1>>;
+};
+template <typename T, int D, typename F> struct alignas(256) DqTiles {
+  struct { T k[F::BUF][F::R * D], v[F::BUF][F::R * D]; } stream[F::S];
+  int flag;
+};
+
+// dk, dv: a causal sequence's first keys are seen by all its queries, its last by few, and there are only as many workgroups
+// as key tiles and key heads: the longest one decides, and with two streams it takes half as long.
+template <typename T, int D, bool SPLIT> struct KeyShape_;
+template <typename T, int D> struct KeyShape_<T, D, false> {
+  using type = Shape<4, kWaves<T, D>, sizeof(T) == 2 && D == 64 ? 64 : 32, 3, kWaves<T, D>>;
+};
+template <typename T, int D> struct KeyShape_<T, D, true> {
+  using type = Shape<2, 2 * kWaves<T, D>, 32, 2, kWaves<T, D>>;
+};
 // its value rows stay in LDS where their registers are wanted for the sums
 template <typename T, int D> constexpr bool kValuesInLds = sizeof(T) == 2 && D == 128;
-constexpr int kBuffers = 3;      // tiles in LDS: one in use, two on their way
-template <typename T, int D> struct alignas(256) DqTiles {
-  T k[kBuffers][kKeyTile<T, D> * D], v[kBuffers][kKeyTile<T, D> * D];
-  int flag;
-};
-template <typename T, int D> struct alignas(256) QueryTiles {
-  T q[kBuffers][kQueryTile<T, D> * D], g[kBuffers][kQueryTile<T, D> * D];
-  float stats[kBuffers][2 * kQueryTile<T, D>];   // in base 2: lse of the queries, then -delta
-};
-template <typename T, int D> struct alignas(256) KeyTiles {
-  QueryTiles<T, D> stream[kStreams<T, D>];
-  T v[kValuesInLds<T, D> ? kPackedRows * D : 8];
+template <typename T, int D, typename F> struct alignas(256) KeyTiles {
+  struct {
+    T q[F::BUF][F::R * D], g[F::BUF][F::R * D];
+    float stats[F::BUF][F::R == 64 ? 128 : 64];   // in base 2: lse of the queries, then -delta
+  } stream[F::S];
+  T v[kValuesInLds<T, D> ? F::ROWS * D : 8];
   int flag;
 };
 
-template <typename T, int D> __global__ __launch_bounds__(kPackedThreads, (kWaves<T, D>)) void packed_dq_kernel(PackedArgs a, int tiles) {
+// Adds the other streams' sums to the first one's, a register of 64 lanes at a time, through `own`: 64 MT 16 floats for each
+// of their waves.
+template <int S, int W, int MT> __device__ __forceinline__ void join_streams(f32x16 (&sum)[MT], float* own, int stream, int wave, int lane) {
+  auto slot = [&](int s, int r) -> float& { return own[64 * (((s - 1) * W + wave) * 16 * MT + r) + lane]; };
+  if (stream) {
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) slot(stream, 16 * mt + r) = sum[mt][r];
+  }
+  lds_barrier();
+  if (!stream) {
+#pragma unroll
+    for (int s = 1; s < S; ++s)
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sum[mt][r] += slot(s, 16 * mt + r);
+  }
+  lds_barrier();
+}
+
+template <typename T, int D, typename F> __global__ __launch_bounds__(F::THREADS, F::PER_SIMD) void packed_dq_kernel(PackedArgs a, int tiles) {
   using P = Products<T, D>;
-  constexpr int R = kKeyTile<T, D>, NS = R / 32, MT = D / 32, W = kPackedThreads / 64;
+  constexpr int R = F::R, S = F::S, ROWS = F::ROWS, BUF = F::BUF, NS = R / 32, MT = D / 32, W = F::RW;
   using L = Tile<T, D, R>;
   extern __shared__ __align__(256) unsigned char smem_raw[];
-  auto& sm = *reinterpret_cast<DqTiles<T, D>*>(smem_raw);
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), ln = lane & 31, lh = lane >> 5;
+  auto& all = *reinterpret_cast<DqTiles<T, D, F>*>(smem_raw);
+  const int tid = threadIdx.x, lane = tid & 63, ln = lane & 31, lh = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid / 64 % W), stream = __builtin_amdgcn_readfirstlane(tid / 64 / W);
+  auto& sm = all.stream[stream];
 
   const int hh = blockIdx.x % a.H, kvh = hh % a.Hkv, h = kvh * (a.H / a.Hkv) + hh / a.Hkv;
-  const SeqTile at = ranked_tile<kPackedRows, false>(a.cu_q, a.total_q, a.cu_k, a.total_k, a.n_seqs, blockIdx.x / a.H, tiles, lane);
+  const SeqTile at = ranked_tile<ROWS, false>(a.cu_q, a.total_q, a.cu_k, a.total_k, a.n_seqs, blockIdx.x / a.H, tiles, lane);
   if (at.first < 0) return;
   const int qbase = packed_row(a.cu_q, at.seq, a.total_q), i0 = at.first;
   if (at.seq == a.n_seqs) {
     if (a.zero_tail && i0 < a.total_q - qbase)
-      zero_rows<T, D>(rows_of<T>(a.dq, a.dqs, qbase + i0, h), a.dqs[0], min(kPackedRows, a.total_q - qbase - i0), tid);
+      zero_rows<T, D>(rows_of<T>(a.dq, a.dqs, qbase + i0, h), a.dqs[0], min(ROWS, a.total_q - qbase - i0), tid, F::THREADS);
     return;
   }
   const int nq = packed_row(a.cu_q, at.seq + 1, a.total_q) - qbase;
@@ -70,24 +105,24 @@ template <typename T, int D> __global__ __launch_bounds__(kPackedThreads, (kWave
   P::load(q, rows_of<T>(a.q, a.qs, qbase + ic, h), lane, a.scale < 0.f);
   const int64_t stat = (int64_t)h * a.total_q + qbase + ic;
   const float lse = a.lse[stat] * kLog2e;
-  if (i < nq) a.stats[stat + (lh ? (int64_t)a.H * a.total_q : 0)] = lh ? -delta : lse;
+  if (stream == 0 && i < nq) a.stats[stat + (lh ? (int64_t)a.H * a.total_q : 0)] = lh ? -delta : lse;
   const float sc = (a.scale == 0.f ? 1e-30f : fabsf(a.scale)) * kLog2e;
 
   f32x16 dq[MT];
 
   const T* kp = rows_of<T>(a.k, a.ks, kbase, kvh);
   const T* vp = rows_of<T>(a.v, a.vs, kbase, kvh);
-  const int last_key = min(i0 + kPackedRows, nq) - 1 + off;
+  const int last_key = min(i0 + ROWS, nq) - 1 + off;
   const int n_tiles = last_key < 0 ? 0 : last_key / R + 1;
-  auto load = [&](int t) {
-    L::template load<W>(sm.k[t % kBuffers], kp, a.ks[0], t * R, nk - 1, wave, lane);
-    L::template load<W>(sm.v[t % kBuffers], vp, a.vs[0], t * R, nk - 1, wave, lane);
+  auto load = [&](int t, int n) {   // tile t, the stream's n-th
+    L::template load<W>(sm.k[n % BUF], kp, a.ks[0], t * R, nk - 1, wave, lane);
+    L::template load<W>(sm.v[n % BUF], vp, a.vs[0], t * R, nk - 1, wave, lane);
   };
   bool odd = false;
-  auto sums = [&](int t, auto by_rows) {
+  auto sums = [&](int t, int nth, auto by_rows) {
     const int t0 = t * R;
     const bool mask = t0 + R - 1 > q0 + off;   // some query of the wave does not see the whole tile
-    const T *kt = sm.k[t % kBuffers], *vt = sm.v[t % kBuffers];
+    const T *kt = sm.k[nth % BUF], *vt = sm.v[nth % BUF];
 #pragma unroll
     for (int n = 0; n < NS; ++n) {
       const f32x16 s = P::scores(kt + 32 * n * D, q, lane), dp = P::scores(vt + 32 * n * D, g, lane);
@@ -109,44 +144,48 @@ template <typename T, int D> __global__ __launch_bounds__(kPackedThreads, (kWave
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
       for (int r = 0; r < 16; ++r) dq[mt][r] = 0.f;
-    for (int t = 0; t < kBuffers - 1; ++t)
-      if (t < n_tiles) load(t);
-    for (int t = 0; t < n_tiles; ++t) {
-      if (t + 1 < n_tiles) loads_left<2 * L::loads(W)>();
+    for (int n = 0; n < BUF - 1; ++n)
+      if (stream + S * n < n_tiles) load(stream + S * n, n);
+    for (int t = stream, n = 0; t - stream < n_tiles; t += S, ++n) {   // the streams meet at every barrier
+      if (BUF > 2 && t + S < n_tiles) loads_left<2 * L::loads(W)>();
       else loads_left<0>();
-      lds_barrier();   // tile t is there, and nobody reads tile t - 1 any more
-      if (t + kBuffers - 1 < n_tiles) load(t + kBuffers - 1);
-      if (t * R <= min(q0 + 31, nq - 1) + off) sums(t, by_rows);   // else nothing for this wave
+      lds_barrier();   // tile n is there, and nobody reads tile n - 1 any more
+      if (t + (BUF - 1) * S < n_tiles) load(t + (BUF - 1) * S, n + BUF - 1);
+      if (t < n_tiles && t * R <= min(q0 + 31, nq - 1) + off) sums(t, n, by_rows);   // else nothing for this wave
     }
     lds_barrier();   // every wave is done with the tiles
   };
   pass(std::false_type{});
-  if (any_wave(&sm.flag, odd)) pass(std::true_type{});
+  if (any_wave(&all.flag, odd)) pass(std::true_type{});
+  if constexpr (S > 1) {
+    static_assert(sizeof(DqTiles<T, D, F>) >= (S - 1) * W * 64 * 16 * MT * sizeof(float));
+    join_streams<S, W, MT>(dq, reinterpret_cast<float*>(smem_raw), stream, wave, lane);
+    if (stream) return;
+  }
   if (q0 < nq)
     put_rows<T, D>(dq, a.scale, reinterpret_cast<T*>(smem_raw) + wave * 32 * kPutRow<T, D>, rows_of<T>(a.dq, a.dqs, qbase + q0, h), a.dqs[0],
                    min(32, nq - q0), lane);
 }
 
-template <typename T, int D> __global__ __launch_bounds__((kPackedThreads * kStreams<T, D>), (kWaves<T, D>)) void packed_dkdv_kernel(PackedArgs a, int tiles) {
+template <typename T, int D, typename F> __global__ __launch_bounds__(F::THREADS, F::PER_SIMD) void packed_dkdv_kernel(PackedArgs a, int tiles, int groups) {
   using P = Products<T, D>;
-  constexpr int R = kQueryTile<T, D>, MT = D / 32, W = kPackedThreads / 64;
+  constexpr int R = F::R, S = F::S, ROWS = F::ROWS, BUF = F::BUF, MT = D / 32, W = F::RW;
   using L = Tile<T, D, R>;
   extern __shared__ __align__(256) unsigned char smem_raw[];
-  constexpr int S = kStreams<T, D>;
-  auto& all = *reinterpret_cast<KeyTiles<T, D>*>(smem_raw);
-  const int stream = __builtin_amdgcn_readfirstlane(threadIdx.x / kPackedThreads);
+  auto& all = *reinterpret_cast<KeyTiles<T, D, F>*>(smem_raw);
+  const int tid = threadIdx.x, lane = tid & 63, ln = lane & 31, lh = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid / 64 % W), stream = __builtin_amdgcn_readfirstlane(tid / 64 / W);
   auto& sm = all.stream[stream];
-  const int tid = threadIdx.x % kPackedThreads, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), ln = lane & 31, lh = lane >> 5;
 
-  const int kvh = blockIdx.x % a.Hkv;
-  const SeqTile at = ranked_tile<kPackedRows, true>(a.cu_k, a.total_k, a.cu_q, a.total_q, a.n_seqs, blockIdx.x / a.Hkv, tiles, lane);
+  const int unit = blockIdx.x % (a.Hkv * groups), kvh = unit % a.Hkv, part = unit / a.Hkv;
+  const SeqTile at = ranked_tile<ROWS, true>(a.cu_k, a.total_k, a.cu_q, a.total_q, a.n_seqs, blockIdx.x / (a.Hkv * groups), tiles, lane);
   if (at.first < 0) return;
   const int kbase = packed_row(a.cu_k, at.seq, a.total_k), j0 = at.first;
   if (at.seq == a.n_seqs) {
-    if (a.zero_tail && stream == 0 && j0 < a.total_k - kbase) {
-      const int rows = min(kPackedRows, a.total_k - kbase - j0);
-      zero_rows<T, D>(rows_of<T>(a.dk, a.dks, kbase + j0, kvh), a.dks[0], rows, tid);
-      zero_rows<T, D>(rows_of<T>(a.dv, a.dvs, kbase + j0, kvh), a.dvs[0], rows, tid);
+    if (a.zero_tail && part == 0 && j0 < a.total_k - kbase) {
+      const int rows = min(ROWS, a.total_k - kbase - j0);
+      zero_rows<T, D>(rows_of<T>(a.dk, a.dks, kbase + j0, kvh), a.dks[0], rows, tid, F::THREADS);
+      zero_rows<T, D>(rows_of<T>(a.dv, a.dvs, kbase + j0, kvh), a.dvs[0], rows, tid, F::THREADS);
     }
     return;
   }
@@ -167,16 +206,16 @@ template <typename T, int D> __global__ __launch_bounds__((kPackedThreads * kStr
 
   f32x16 dk[MT], dv[MT];
 
-  // the tiles of queries that see any of the workgroup's keys, for every head of the group in turn
+  // the tiles of queries that see any of the workgroup's keys, for every head of its part of the group in turn
   const int first_tile = max(j0 - off, 0) / R;
-  const int per_head = nq == 0 ? 0 : (nq - 1) / R + 1 - first_tile, G = a.H / a.Hkv, total = max(per_head, 0) * G;
+  const int per_head = nq == 0 ? 0 : (nq - 1) / R + 1 - first_tile, G = a.H / a.Hkv / groups, total = max(per_head, 0) * G;
   // the stream's n-th tile, queries `t` R .. of head `g` of the group; its next one
   struct Place { int g, t; };
   auto next = [&](Place& p) {
     for (p.t += S; p.t - first_tile >= per_head; p.t -= per_head) ++p.g;
   };
   auto load = [&](const Place& p, int n) {
-    const int h = kvh * G + p.g, t0 = p.t * R, to = n % kBuffers;
+    const int h = (kvh * groups + part) * G + p.g, t0 = p.t * R, to = n % BUF;
     L::template load<W>(sm.q[to], rows_of<T>(a.q, a.qs, qbase, h), a.qs[0], t0, nq - 1, wave, lane);
     L::template load<W>(sm.g[to], rows_of<T>(a.dout, a.gs, qbase, h), a.gs[0], t0, nq - 1, wave, lane);
     // one word a lane: what is left of a wave, or the other statistic; every wave brings the same
@@ -193,8 +232,8 @@ template <typename T, int D> __global__ __launch_bounds__((kPackedThreads * kStr
   auto sums = [&](int n, int part, int t0, auto by_rows) {
     // some query does not see all of the wave's keys, or is none
     const bool mask = t0 + 32 > nq || t0 < min(k0 + 31, nk - 1) - off;
-    const T *qt = sm.q[n % kBuffers] + 32 * part * D, *gt = sm.g[n % kBuffers] + 32 * part * D;
-    const float* stats = sm.stats[n % kBuffers] + 32 * part + 4 * lh;
+    const T *qt = sm.q[n % BUF] + 32 * part * D, *gt = sm.g[n % BUF] + 32 * part * D;
+    const float* stats = sm.stats[n % BUF] + 32 * part + 4 * lh;
     const int lo = from - t0, hi = nq - t0;   // rows that see this lane's key
     auto hidden = [&](int r) { return 8 * (r / 4) + 4 * lh + r % 4 < lo || 8 * (r / 4) + 4 * lh + r % 4 >= hi; };
     float p[16], ds[16];
@@ -240,16 +279,16 @@ template <typename T, int D> __global__ __launch_bounds__((kPackedThreads * kStr
     if (total == 0) return;
     Place now{0, first_tile - S + stream}, ahead = now;
     next(now);
-    for (int n = 0; n < kBuffers - 1; ++n) {
+    for (int n = 0; n < BUF - 1; ++n) {
       next(ahead);
       if (stream + S * n < total) load(ahead, n);
     }
     for (int it = stream, n = 0; it - stream < total; it += S, ++n, next(now)) {   // the streams meet at every barrier
-      if (it + S < total) loads_left<LOADS>();
+      if (BUF > 2 && it + S < total) loads_left<LOADS>();
       else loads_left<0>();
       lds_barrier();   // tile n is there, and nobody reads tile n - 1 any more
       next(ahead);
-      if (it + (kBuffers - 1) * S < total) load(ahead, n + kBuffers - 1);
+      if (it + (BUF - 1) * S < total) load(ahead, n + BUF - 1);
       const int t0 = now.t * R;
       // else no tile, no key, or none that a query of the tile sees
 #pragma unroll
@@ -261,48 +300,84 @@ template <typename T, int D> __global__ __launch_bounds__((kPackedThreads * kStr
   pass(std::false_type{});
   if (any_wave(&all.flag, odd)) pass(std::true_type{});
   if constexpr (S > 1) {
-    // the second stream's sums, a register of 64 lanes at a time
-    static_assert(S == 2 && sizeof(KeyTiles<T, D>) >= kPackedRows * D * sizeof(float));
-    float* own = reinterpret_cast<float*>(smem_raw) + wave * 32 * D + lane;
-    auto join = [&](f32x16 (&sum)[MT]) {
-#pragma unroll
-      for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (stream) own[64 * (16 * mt + r)] = sum[mt][r];
-      lds_barrier();
-#pragma unroll
-      for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (!stream) sum[mt][r] += own[64 * (16 * mt + r)];
-      lds_barrier();
-    };
-    join(dk);
-    join(dv);
+    static_assert(sizeof(all.stream) >= (S - 1) * W * 64 * 16 * MT * sizeof(float));
+    join_streams<S, W, MT>(dk, reinterpret_cast<float*>(smem_raw), stream, wave, lane);
+    join_streams<S, W, MT>(dv, reinterpret_cast<float*>(smem_raw), stream, wave, lane);
     if (stream) return;
   }
-  if (k0 < nk) {
+  if (k0 >= nk) return;
+  if (groups > 1) {
+    // this part's sums, in 32 bits
+    float* own = reinterpret_cast<float*>(smem_raw) + wave * 32 * kPutRow<float, D>;
+    const int64_t size = (int64_t)a.total_k * a.Hkv * D, row = (int64_t)a.Hkv * D;
+    float* to = a.sums + 2 * part * size + (kbase + k0) * row + kvh * D;
+    put_rows<float, D>(dk, a.scale, own, to, row, min(32, nk - k0), lane);
+    put_rows<float, D>(dv, 1.f, own, to + size, row, min(32, nk - k0), lane);
+  } else {
     T* own = reinterpret_cast<T*>(smem_raw) + wave * 32 * kPutRow<T, D>;
     put_rows<T, D>(dk, a.scale, own, rows_of<T>(a.dk, a.dks, kbase + k0, kvh), a.dks[0], min(32, nk - k0), lane);
     put_rows<T, D>(dv, 1.f, own, rows_of<T>(a.dv, a.dvs, kbase + k0, kvh), a.dvs[0], min(32, nk - k0), lane);
   }
 }
 
-template <typename T, int D> hipError_t launch(const PackedArgs& a, hipStream_t s) {
-  const size_t dq_smem = sizeof(DqTiles<T, D>), dkdv_smem = sizeof(KeyTiles<T, D>);
-  auto dq = packed_dq_kernel<T, D>;
-  auto dkdv = packed_dkdv_kernel<T, D>;
-  if (hipError_t e = allow_lds(dq, dq_smem); e != hipSuccess) return e;
-  if (hipError_t e = allow_lds(dkdv, dkdv_smem); e != hipSuccess) return e;
-  const int64_t qt = packed_tiles(a.total_q, a.n_seqs, kPackedRows), kt = packed_tiles(a.total_k, a.n_seqs, kPackedRows);
-  dq<<<dim3((unsigned)(qt * a.H)), dim3(kPackedThreads), dq_smem, s>>>(a, (int)qt);
-  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-  dkdv<<<dim3((unsigned)(kt * a.Hkv)), dim3(kPackedThreads * kStreams<T, D>), dkdv_smem, s>>>(a, (int)kt);
+// dk and dv of the sequences' rows from the sums of every part of the heads, four columns a thread.
+template <typename T, int D> __global__ __launch_bounds__(256) void packed_add_kernel(PackedArgs a, int groups) {
+  constexpr int C = D / 4;
+  const int64_t unit = ((int64_t)blockIdx.x * 256 + threadIdx.x) / C;   // (row, head), dk's and then dv's
+  const int64_t units = (int64_t)a.total_k * a.Hkv, at = unit % units;
+  const int c = 4 * (threadIdx.x % C), head = (int)(at % a.Hkv), row = (int)(at / a.Hkv);
+  if (unit >= 2 * units || row < packed_row(a.cu_k, 0, a.total_k) || row >= packed_row(a.cu_k, a.n_seqs, a.total_k)) return;
+  f32x4_t x = {0.f, 0.f, 0.f, 0.f};
+  for (int g = 0; g < groups; ++g) x += *reinterpret_cast<const f32x4_t*>(a.sums + (2 * g * units + unit) * D + c);
+  T* to = unit < units ? rows_of<T>(a.dk, a.dks, row, head) : rows_of<T>(a.dv, a.dvs, row, head);
+  Products<T, D>::put4(to + c, x[0], x[1], x[2], x[3]);
+}
+
+template <typename T, int D, bool SPLIT> hipError_t launch_dq(const PackedArgs& a, hipStream_t s) {
+  using F = typename DqShape_<T, D, SPLIT>::type;
+  constexpr size_t smem = std::max(sizeof(DqTiles<T, D, F>), F::ROWS * kPutRow<T, D> * sizeof(T));   // the rows leave through it
+  auto kern = packed_dq_kernel<T, D, F>;
+  if (hipError_t e = allow_lds(kern, smem); e != hipSuccess) return e;
+  const int64_t tiles = packed_tiles(a.total_q, a.n_seqs, F::ROWS);
+  kern<<<dim3((unsigned)(tiles * a.H)), dim3(F::THREADS), smem, s>>>(a, (int)tiles);
   return hipGetLastError();
+}
+template <typename T, int D, bool SPLIT> hipError_t launch_dkdv(const PackedArgs& a, int groups, hipStream_t s) {
+  using F = typename KeyShape_<T, D, SPLIT>::type;
+  constexpr size_t smem = std::max(sizeof(KeyTiles<T, D, F>), F::ROWS * kPutRow<float, D> * sizeof(float));
+  auto kern = packed_dkdv_kernel<T, D, F>;
+  if (hipError_t e = allow_lds(kern, smem); e != hipSuccess) return e;
+  const int64_t tiles = packed_tiles(a.total_k, a.n_seqs, F::ROWS);
+  kern<<<dim3((unsigned)(tiles * a.Hkv * groups)), dim3(F::THREADS), smem, s>>>(a, (int)tiles, groups);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || groups == 1) return e;
+  const int64_t threads = (int64_t)a.total_k * a.Hkv * 2 * (D / 4);
+  packed_add_kernel<T, D><<<dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s>>>(a, groups);
+  return hipGetLastError();
+}
+// As in the forward pass; the workgroups of dk and dv fill a compute unit each in either form.
+template <typename T, int D> hipError_t launch(const PackedArgs& a, hipStream_t s) {
+  const int units = device_compute_units(), groups = packed_head_groups(a.total_k, a.n_seqs, a.H, a.Hkv);
+  const bool dq_split = packed_splits(a.total_q, a.H, a.n_seqs, units / (sizeof(T) == 2 && D == 128 ? 2 : 1));
+  const hipError_t e = dq_split ? launch_dq<T, D, true>(a, s) : launch_dq<T, D, false>(a, s);
+  if (e != hipSuccess) return e;
+  const bool split = packed_splits(a.total_k, a.Hkv * groups, a.n_seqs, units);
+  return split ? launch_dkdv<T, D, true>(a, groups, s) : launch_dkdv<T, D, false>(a, groups, s);
 }
 
 }  // namespace
+
+// Where key heads are few, the workgroups that walk all query heads of one are few and long: the heads are parted until
+// there is a workgroup for every compute unit.
+int packed_head_groups(int total_k, int n_seqs, int H, int Hkv) {
+  const int G = H / Hkv;
+  const int64_t units = (int64_t)device_compute_units() * kPackedRows;
+  int groups = 1;
+  while (groups < G && (int64_t)total_k * Hkv * groups < units)
+    do ++groups;
+    while (G % groups != 0);
+  return groups;
+}
 
 hipError_t launch_packed_bwd(const PackedArgs& a, bool bf16, hipStream_t s) {
   if (bf16) return a.d == 128 ? launch<uint16_t, 128>(a, s) : launch<uint16_t, 64>(a, s);

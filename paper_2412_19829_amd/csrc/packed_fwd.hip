@@ -1,8 +1,8 @@
 // Forward pass of attention over packed sequences (packed.hpp has the formulas): softmax in one pass over the keys, with a
 // running maximum and sum per query.
 //
-// A workgroup holds 128 queries of one head, 32 a wave, and streams key and value tiles through two LDS buffers: the next
-// tile's rows arrive while the present one is used.
+// A workgroup holds up to 128 queries of one head, 32 a wave, and streams key and value tiles through two LDS buffers: the
+// next tile's rows arrive while the present one is used.
 #include "packed.hpp"
 
 #include <algorithm>
@@ -10,29 +10,38 @@
 namespace gformer {
 namespace {
 
-template <typename T> constexpr int kFwdTile = sizeof(T) == 2 ? 64 : 32;   // keys per tile
-template <typename T, int D> struct alignas(256) FwdTiles {
-  T k[2][kFwdTile<T> * D], v[2][kFwdTile<T> * D];
+// One stream where there are workgroups enough.  SPLIT: a few rows a workgroup, its waves on different keys.
+template <typename T, int D, bool SPLIT> struct FwdShape_;
+template <typename T, int D> struct FwdShape_<T, D, false> {
+  using type = Shape<4, 1, sizeof(T) == 2 ? 64 : 32, 2, sizeof(T) == 4 && D == 128 ? 1 : D == 64 ? 3 : 2>;
+};
+template <typename T, int D> struct FwdShape_<T, D, true> {
+  using type = std::conditional_t<sizeof(T) == 4 && D == 128, Shape<2, 2, 32, 2, 1>, Shape<1, 4, 32, 2, sizeof(T) == 2 && D == 64 ? 2 : 1>>;
+};
+template <typename T, int D, typename F> struct alignas(256) FwdTiles {
+  struct { T k[F::BUF][F::R * D], v[F::BUF][F::R * D]; } stream[F::S];
   int flag;
 };
 
-template <typename T, int D> __global__ __launch_bounds__(kPackedThreads, (sizeof(T) == 4 && D == 128 ? 1 : D == 64 ? 3 : 2)) void packed_fwd_kernel(PackedArgs a, int tiles) {
+template <typename T, int D, typename F> __global__ __launch_bounds__(F::THREADS, F::PER_SIMD) void packed_fwd_kernel(PackedArgs a, int tiles) {
   using P = Products<T, D>;
-  constexpr int R = kFwdTile<T>, NS = R / 32, MT = D / 32, W = kPackedThreads / 64;
+  constexpr int R = F::R, S = F::S, ROWS = F::ROWS, NS = R / 32, MT = D / 32, W = F::RW;
   using L = Tile<T, D, R>;
   extern __shared__ __align__(256) unsigned char smem_raw[];
-  auto& sm = *reinterpret_cast<FwdTiles<T, D>*>(smem_raw);
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), ln = lane & 31, lh = lane >> 5;
+  auto& all = *reinterpret_cast<FwdTiles<T, D, F>*>(smem_raw);
+  const int tid = threadIdx.x, lane = tid & 63, ln = lane & 31, lh = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid / 64 % W), stream = __builtin_amdgcn_readfirstlane(tid / 64 / W);
+  auto& sm = all.stream[stream];
 
   // Heads fastest, the heads that share keys Hkv apart: workgroups are dealt to the 8 XCDs in turn, so that those of one key
   // head meet in few of them.
   const int hh = blockIdx.x % a.H, kvh = hh % a.Hkv, h = kvh * (a.H / a.Hkv) + hh / a.Hkv;
-  const SeqTile at = ranked_tile<kPackedRows, false>(a.cu_q, a.total_q, a.cu_k, a.total_k, a.n_seqs, blockIdx.x / a.H, tiles, lane);
+  const SeqTile at = ranked_tile<ROWS, false>(a.cu_q, a.total_q, a.cu_k, a.total_k, a.n_seqs, blockIdx.x / a.H, tiles, lane);
   if (at.first < 0) return;
   const int qbase = packed_row(a.cu_q, at.seq, a.total_q), i0 = at.first;
   if (at.seq == a.n_seqs) {
     if (a.zero_tail && i0 < a.total_q - qbase)
-      zero_rows<T, D>(rows_of<T>(a.out, a.os, qbase + i0, h), a.os[0], min(kPackedRows, a.total_q - qbase - i0), tid);
+      zero_rows<T, D>(rows_of<T>(a.out, a.os, qbase + i0, h), a.os[0], min(ROWS, a.total_q - qbase - i0), tid, F::THREADS);
     return;
   }
   const int nq = packed_row(a.cu_q, at.seq + 1, a.total_q) - qbase;
@@ -52,17 +61,17 @@ template <typename T, int D> __global__ __launch_bounds__(kPackedThreads, (sizeo
 
   const T* kp = rows_of<T>(a.k, a.ks, kbase, kvh);
   const T* vp = rows_of<T>(a.v, a.vs, kbase, kvh);
-  const int last_key = min(i0 + kPackedRows, nq) - 1 + off;   // of the workgroup; < 0: no query sees any
+  const int last_key = min(i0 + ROWS, nq) - 1 + off;   // of the workgroup; < 0: no query sees any
   const int n_tiles = last_key < 0 ? 0 : last_key / R + 1;
-  auto load = [&](int t) {
-    L::template load<W>(sm.k[t & 1], kp, a.ks[0], t * R, nk - 1, wave, lane);
-    L::template load<W>(sm.v[t & 1], vp, a.vs[0], t * R, nk - 1, wave, lane);
+  auto load = [&](int t, int n) {   // tile t, the stream's n-th
+    L::template load<W>(sm.k[n % F::BUF], kp, a.ks[0], t * R, nk - 1, wave, lane);
+    L::template load<W>(sm.v[n % F::BUF], vp, a.vs[0], t * R, nk - 1, wave, lane);
   };
   bool odd = false;
-  auto attend = [&](int t, auto by_rows) {
+  auto attend = [&](int t, int nth, auto by_rows) {
     const int t0 = t * R;
     const bool mask = t0 + R - 1 > q0 + off;   // some query of the wave does not see the whole tile
-    const T *kt = sm.k[t & 1], *vt = sm.v[t & 1];
+    const T *kt = sm.k[nth % F::BUF], *vt = sm.v[nth % F::BUF];
     f32x16 s[NS];
 #pragma unroll
     for (int n = 0; n < NS; ++n) s[n] = P::scores(kt + 32 * n * D, q, lane);
@@ -110,17 +119,55 @@ template <typename T, int D> __global__ __launch_bounds__(kPackedThreads, (sizeo
       for (int r = 0; r < 16; ++r) o[mt][r] = 0.f;
     m = -INFINITY;
     l = 0.f;
-    if (n_tiles) load(0);
-    for (int t = 0; t < n_tiles; ++t) {
+    if (stream < n_tiles) load(stream, 0);
+    for (int t = stream, n = 0; t - stream < n_tiles; t += S, ++n) {   // the streams meet at every barrier
       loads_left<0>();
-      lds_barrier();   // tile t is there, and nobody reads tile t - 1 any more
-      if (t + 1 < n_tiles) load(t + 1);
-      if (t * R <= min(q0 + 31, nq - 1) + off) attend(t, by_rows);   // else nothing for this wave
+      lds_barrier();   // tile n is there, and nobody reads tile n - 1 any more
+      if (t + S < n_tiles) load(t + S, n + 1);
+      if (t < n_tiles && t * R <= min(q0 + 31, nq - 1) + off) attend(t, n, by_rows);   // else nothing for this wave
     }
     lds_barrier();   // every wave is done with the tiles
   };
   pass(std::false_type{});
-  if (any_wave(&sm.flag, odd)) pass(std::true_type{});
+  if (any_wave(&all.flag, odd)) pass(std::true_type{});
+  if constexpr (S > 1) {
+    // a lane's share of its query from every stream: the maximum, the sum and the registers of weighted values
+    float* at_join = reinterpret_cast<float*>(smem_raw) + lane;
+    auto slot = [&](int s, int r) -> float& { return at_join[64 * (((s - 1) * W + wave) * (16 * MT + 2) + r)]; };
+    static_assert(sizeof(FwdTiles<T, D, F>) >= (S - 1) * W * 64 * (16 * MT + 2) * sizeof(float));
+    if (stream) {
+      slot(stream, 0) = m;
+      slot(stream, 1) = l;
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) slot(stream, 2 + 16 * mt + r) = o[mt][r];
+    }
+    lds_barrier();
+    if (!stream) {
+      float up = m;
+#pragma unroll
+      for (int s = 1; s < S; ++s) up = fmaxf(up, slot(s, 0));
+      const float ref = up == -INFINITY ? 0.f : up, by = __builtin_amdgcn_exp2f(m - ref);
+      l *= by;
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[mt][r] *= by;
+#pragma unroll
+      for (int s = 1; s < S; ++s) {
+        const float by = __builtin_amdgcn_exp2f(slot(s, 0) - ref);
+        l = fmaf(slot(s, 1), by, l);
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[mt][r] = fmaf(slot(s, 2 + 16 * mt + r), by, o[mt][r]);
+      }
+      m = up;
+    }
+    lds_barrier();   // the rows leave through the same memory
+    if (stream) return;
+  }
   l = sum_over_halves(l);
   if (a.lse && lh == 0 && i < nq)
     a.lse[(int64_t)h * a.total_q + qbase + i] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
@@ -132,13 +179,21 @@ template <typename T, int D> __global__ __launch_bounds__(kPackedThreads, (sizeo
   }
 }
 
-template <typename T, int D> hipError_t launch(const PackedArgs& a, hipStream_t s) {
-  constexpr size_t smem = std::max(sizeof(FwdTiles<T, D>), kPackedRows * kPutRow<T, D> * sizeof(T));   // the rows leave through it
-  auto kern = packed_fwd_kernel<T, D>;
+template <typename T, int D, bool SPLIT> hipError_t launch(const PackedArgs& a, hipStream_t s) {
+  using F = typename FwdShape_<T, D, SPLIT>::type;
+  constexpr size_t smem = std::max(sizeof(FwdTiles<T, D, F>), F::ROWS * kPutRow<T, D> * sizeof(T));   // the rows leave through it
+  auto kern = packed_fwd_kernel<T, D, F>;
   if (hipError_t e = allow_lds(kern, smem); e != hipSuccess) return e;
-  const int64_t tiles = packed_tiles(a.total_q, a.n_seqs, kPackedRows);
-  kern<<<dim3((unsigned)(tiles * a.H)), dim3(kPackedThreads), smem, s>>>(a, (int)tiles);
+  const int64_t tiles = packed_tiles(a.total_q, a.n_seqs, F::ROWS);
+  kern<<<dim3((unsigned)(tiles * a.H)), dim3(F::THREADS), smem, s>>>(a, (int)tiles);
   return hipGetLastError();
+}
+// us, one stream against split, us (rows x heads): bf16, d = 64: 2048 x 8 35 / 19, 2048 x 16 37 / 29, 2048 x 32 39 / 49, 8 of 200 x 16 10 / 14;
+// d = 128, whose split workgroups are alone on a compute unit: 512 x 8 17 / 13, 2048 x 8 50 / 37, 512 x 32 18 / 22, 2048 x 16 53 / 70;
+// fp32, d = 64: 2048 x 8 157 / 63, 2048 x 16 162 / 116, 2048 x 32 216 / 234; d = 128: 2048 x 16 300 / 181, 2048 x 32 336 / 355.
+template <typename T, int D> hipError_t launch(const PackedArgs& a, hipStream_t s) {
+  const int limit = device_compute_units() / (sizeof(T) == 2 && D == 128 ? 2 : 1);
+  return packed_splits(a.total_q, a.H, a.n_seqs, limit) ? launch<T, D, true>(a, s) : launch<T, D, false>(a, s);
 }
 
 }  // namespace

@@ -63,7 +63,7 @@ def test_forward_refusals(kw, status):
 
 
 @pytest.mark.parametrize("kw,status", [
-    (dict(ws=0), 3), (dict(ws_bytes=255), 3), (dict(ws=A + 16), 1), (dict(dq=0), 1), (dict(lse=0), 1), (dict(dout=0), 1), (dict(dq=A), 1),
+    (dict(ws=0), 3), (dict(ws_bytes=16639), 3), (dict(ws=A + 16), 1), (dict(dq=0), 1), (dict(lse=0), 1), (dict(dout=0), 1), (dict(dq=A), 1),
     (dict(dk=9 * A, dv=9 * A), 1), (dict(dv=5 * A), 1), (dict(dk=A + 8), 1), (dict(tk=7), 1), (dict(p=wrong(dk_stride=(8, 64))), 1),
     (dict(rest=8 * A), 1), (dict(rest=12 * A, p=gb.make_packed_params(gb.GF_F32)), 1),
 ])
@@ -74,7 +74,9 @@ def test_backward_refusals(kw, status):
 def test_empty_calls():
     assert fwd(tq=0, tk=0, q=0, k=0, v=0, out=0, cu_q=0) == gb.GF_OK
     assert bwd(tq=0, tk=0) == gb.GF_OK
-    assert gb.gformer_packed_attn_bwd_workspace_bytes(10, 10, 1, 4, 2, 64) == 512
+    assert gb.gformer_packed_attn_bwd_workspace_bytes(10, 10, 1, 2, 2, 64) == 256   # two numbers a query and head
+    # and the sums of either part of the heads
+    assert gb.gformer_packed_attn_bwd_workspace_bytes(10, 10, 1, 4, 2, 64) == 512 + 2 * 10 * 2 * 64 * 2 * 4
     assert gb.gformer_packed_attn_bwd_workspace_bytes(10, 10, 1, 4, 3, 64) == 0
 
 
@@ -99,6 +101,8 @@ SHAPES = [
     ([33, 300, 65], None),
     ([1, 40, 0, 130], [77, 40, 9, 257]),       # queries behind keys that are there already
     ([20, 140, 3], [5, 0, 2]),                 # queries that see nothing
+    ([130, 5], [9000, 5]),                     # more levels of tiles than lanes
+    ([600], None),                             # long enough for waves on different keys
 ]
 
 
