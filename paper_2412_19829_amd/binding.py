@@ -1,7 +1,7 @@
 """Thin ctypes binding of libgformer_attn.so (see include/gformer.h).
 
-Argument marshalling only (a decode step's in an extension module, _decode_call.so, where that
-loads): every step of the attention forward runs in the HIP kernels behind the C ABI.  torch is used by callers for device memory and
+Argument marshalling only (a decode step's and the packed and paged calls' in an extension module,
+_decode_call.so, where that loads): every step of the attention forward runs in the HIP kernels behind the C ABI.  torch is used by callers for device memory and
 streams; this module only reads `data_ptr()` / shapes / strides from tensors.
 There is no CPU fallback: if the shared library is missing, loading raises.
 """
@@ -168,17 +168,21 @@ def lib():
         L.gformer_version.restype = ctypes.c_int
         L.gformer_version.argtypes = []
         L.decode_address = ctypes.cast(L.gformer_attn_decode, ctypes.c_void_p).value
+        L.address = {name: ctypes.cast(getattr(L, f"gformer_{name}"), ctypes.c_void_p).value for name in _NATIVE}
         _lib = L
     return _lib
 
 
 _native = None
+_module = None   # the extension module, or None where there is none
+_NATIVE = ("packed_attn_fwd", "packed_attn_bwd", "packed_attn_bwd_workspace_bytes", "paged_fill", "paged_decode",
+           "paged_decode_workspace_bytes", "pages_copy")
 
 
 def _decode_call():
     """The extension module with the host side of a decode step (host/decode_call.cpp).  Without it every step goes through
     this file's own code, which costs the host 4 us more: a warning says so, once."""
-    global _native
+    global _native, _module
     if _native is None:
         import importlib.util
 
@@ -188,6 +192,7 @@ def _decode_call():
             mod = importlib.util.module_from_spec(spec)
             spec.loader.exec_module(mod)
             _native = mod.decode
+            _module = mod
         except ImportError as e:
             warnings.warn(f"decode steps are marshalled in Python ({e}); `python -m paper_2412_19829_amd.build` builds the "
                           "module", RuntimeWarning, stacklevel=3)
@@ -608,6 +613,21 @@ def _scratch(need, workspace, like, stream):
     return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
+def _quick(function, entries, *args):
+    """Whether the extension module has made the call (host/packed_call.cpp says which ones it makes)."""
+    if _native is None:
+        _decode_call()
+    if _module is None:
+        return False
+    address = (_lib or lib()).address
+    st = getattr(_module, function)(*(address[e] for e in entries), *args)
+    if st is None:
+        return False
+    if st != GF_OK:
+        raise GformerError(st, gformer_status_string(st))
+    return True
+
+
 def make_packed_params(dtype=GF_BF16, softmax_scale=1.0, zero_tail=0, **strides) -> GformerPackedParams:
     """strides: q_stride=, k_stride=, ... as (row, head)."""
     p = GformerPackedParams(ctypes.sizeof(GformerPackedParams), int(dtype), int(zero_tail), float(softmax_scale))
@@ -639,6 +659,8 @@ def gformer_packed_attn_fwd(q, k, v, out, cu_q, cu_k=None, *, lse=None, out_rest
     (any strides with a contiguous last dimension); cu_q, cu_k int32 [n_seqs + 1] offsets (cu_k=None: the same
     sequences).  Optional and written, for the backward pass: lse, dense fp32 [H, total_q], and (bf16 only) out_rest, laid
     out like out, what rounding took from it."""
+    if _quick("packed_fwd", ("packed_attn_fwd",), q, k, v, out, cu_q, cu_k, lse, out_rest, softmax_scale, zero_tail, stream):
+        return out
     import torch
 
     dtype = _tensors(q, 3, q=q, k=k, v=v, out=out)
@@ -663,6 +685,9 @@ def gformer_packed_attn_bwd(q, k, v, out, lse, dout, dq, dk, dv, cu_q, cu_k=None
                             zero_tail=0, workspace=None, stream: Optional[int] = None):
     """Gradients of gformer_packed_attn_fwd from what it wrote (out, lse, out_rest) and the gradient dout of
     out."""
+    if _quick("packed_bwd", ("packed_attn_bwd", "packed_attn_bwd_workspace_bytes"), q, k, v, out, cu_q, cu_k, lse, dout, dq, dk, dv,
+              out_rest, softmax_scale, zero_tail, workspace, stream):
+        return dq, dk, dv
     import torch
 
     dtype = _tensors(q, 3, q=q, k=k, v=v, out=out, dout=dout, dq=dq, dk=dk, dv=dv)
@@ -707,6 +732,9 @@ def gformer_paged_decode(q, k, v, out, kpages, vpages, table, lens, *, max_len=0
     [n_pages, Hkv, page_size, d] (any strides with a contiguous last dimension); table int32 [B, table_width]; lens int32
     [B], the tokens in the cache before the call (negative: an idle row).  max_len bounds the longest
     sequence's tokens, the new one included (0: what the table holds)."""
+    if _quick("paged_decode", ("paged_decode", "paged_decode_workspace_bytes"), q, k, v, out, kpages, vpages, table, lens, max_len,
+              softmax_scale, workspace, stream):
+        return out
     if (k is None) != (v is None):
         raise ValueError("k and v come together, or neither")
     new = {} if k is None else {"k": k, "v": v}
@@ -732,6 +760,8 @@ def gformer_paged_decode(q, k, v, out, kpages, vpages, table, lens, *, max_len=0
 def gformer_paged_fill(k, v, kpages, vpages, table, start, cu, *, stream: Optional[int] = None):
     """Packed keys and values [total, Hkv, d] into a paged cache: row i of sequence s becomes its token start[s] + i.
     table int32 [n_seqs, table_width], start int32 [n_seqs], cu int32 [n_seqs + 1]."""
+    if _quick("paged_fill", ("paged_fill",), k, v, kpages, vpages, table, start, cu, stream):
+        return
     dtype = _tensors(k, 3, k=k, v=v)
     if k.shape != v.shape or cu.numel() < 1:
         raise ValueError("k and v must be [total, Hkv, d], cu [n_seqs + 1]")
@@ -748,6 +778,8 @@ def gformer_paged_fill(k, v, kpages, vpages, table, start, cu, *, stream: Option
 def gformer_pages_copy(kpages, vpages, src, dst, *, stream: Optional[int] = None):
     """Pages src[i] -> dst[i] of a paged cache (int32 device tensors), whole, keys and values; no destination may be another
     one or another's source."""
+    if _quick("pages_copy", ("pages_copy",), kpages, vpages, src, dst, stream):
+        return
     dtype = _tensors(kpages, 4, kpages=kpages, vpages=vpages)
     P, Hkv, _, d = kpages.shape
     _numbers(kpages, (None,), src=src)

@@ -14,7 +14,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OBJ_DIR = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libgformer_attn.so")
-CALL_SRC = os.path.join(HERE, "host", "decode_call.cpp")
+CALL_SRC = [os.path.join(HERE, "host", x) for x in ("decode_call.cpp", "packed_call.cpp")]
 CALL = os.path.join(HERE, "_decode_call.so")
 
 # packed-fp32 VALU forms are kept off for every device compilation unit
@@ -28,7 +28,7 @@ def sources():
 
 def _newest_input() -> float:
     deps = sources() + glob.glob(os.path.join(CSRC, "*.hpp")) + \
-        glob.glob(os.path.join(HERE, "..", "include", "*.h")) + [CALL_SRC]
+        glob.glob(os.path.join(HERE, "..", "include", "*.h")) + glob.glob(os.path.join(HERE, "host", "*"))
     return max(os.path.getmtime(p) for p in deps)
 
 
@@ -51,7 +51,7 @@ def _build_call() -> None:
     subprocess.run(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
                     f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
                     *(f"-isystem{p}" for p in [*include_paths(), sysconfig.get_paths()["include"]]),
-                    CALL_SRC, "-o", CALL, f"-L{libs}", "-ltorch_python", "-ltorch_cpu", "-lc10"], check=True)
+                    *CALL_SRC, "-o", CALL, f"-L{libs}", "-ltorch_python", "-ltorch_cpu", "-lc10"], check=True)
 
 
 def build(force: bool = True, extra_flags=(), verbose: bool = False) -> str:

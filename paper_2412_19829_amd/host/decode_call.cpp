@@ -6,48 +6,15 @@
 // returns the gf_status of the call at `address` (gformer_attn_decode), or None for anything that is not the plain,
 // well-formed call: wrapped or traced tensors, shapes or types that do not fit, numbers out of range.  The
 // binding's own code then does or refuses the call, with its own messages.
-#include <Python.h>
+#include "call.hpp"
 
-#include <ATen/core/Tensor.h>
-#include <c10/core/DispatchKeySet.h>
-#include <torch/csrc/autograd/python_variable.h>
+PyObject* gformer_host::raw_stream_getter = nullptr;
 
-#include <climits>
-#include <cstring>
-
-#include "../../include/gformer.h"
+using namespace gformer_host;
 
 namespace {
 
 using Decode = decltype(&gformer_attn_decode);
-
-// A dense tensor and nothing else: a wrapper's data pointer is not what the caller means.
-const at::Tensor* plain(PyObject* o) {
-  if (!THPVariable_CheckExact(o)) return nullptr;
-  const at::Tensor& t = THPVariable_Unpack(o);
-  if (!t.defined() || t.layout() != at::kStrided || t.is_nested() || !t.has_storage() ||
-      t.unsafeGetTensorImpl()->has_symbolic_sizes_strides() || !t.is_contiguous())
-    return nullptr;
-  constexpr c10::DispatchKeySet wrapped({
-      c10::DispatchKey::Python, c10::DispatchKey::PythonTLSSnapshot, c10::DispatchKey::Functionalize,
-      c10::DispatchKey::FuncTorchBatched, c10::DispatchKey::FuncTorchGradWrapper, c10::DispatchKey::Conjugate,
-      c10::DispatchKey::Negative, c10::DispatchKey::ZeroTensor});
-  return t.key_set().has_any(wrapped) ? nullptr : &t;
-}
-
-bool to_long(PyObject* o, int64_t lo, int64_t hi, int64_t& x) {
-  if (!PyLong_CheckExact(o)) return false;
-  int over = 0;
-  x = PyLong_AsLongLongAndOverflow(o, &over);
-  return over == 0 && x >= lo && x <= hi;
-}
-bool to_float(PyObject* o, float& x) {
-  if (!PyFloat_CheckExact(o)) return false;
-  x = (float)PyFloat_AS_DOUBLE(o);
-  return true;
-}
-
-PyObject* raw_stream_getter = nullptr;   // torch._C._cuda_getCurrentRawStream, where torch has it
 
 // What the call takes from its arguments; the stream only where it was named.
 struct Step {
@@ -113,12 +80,7 @@ PyObject* decode(PyObject*, PyObject* const* a, Py_ssize_t n) {
   }
   if (a[14] == Py_None) {
     if (!raw_stream_getter) Py_RETURN_NONE;   // the binding knows another way
-    PyObject* index = PyLong_FromLong((long)s.device);
-    PyObject* handle = index ? PyObject_CallOneArg(raw_stream_getter, index) : nullptr;
-    Py_XDECREF(index);
-    if (!handle) return nullptr;
-    s.stream = (int64_t)PyLong_AsUnsignedLongLongMask(handle);
-    Py_DECREF(handle);
+    if (!current_stream(s.device, s.stream)) return nullptr;
   }
   const Decode call = reinterpret_cast<Decode>(PyLong_AsVoidPtr(a[0]));
   if (!call) {
@@ -135,6 +97,11 @@ PyObject* decode(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 PyMethodDef methods[] = {
     {"decode", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(decode)), METH_FASTCALL, "one decode step"},
+    {"packed_fwd", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(packed_fwd)), METH_FASTCALL, "gformer_packed_attn_fwd"},
+    {"packed_bwd", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(packed_bwd)), METH_FASTCALL, "gformer_packed_attn_bwd"},
+    {"paged_fill", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(paged_fill)), METH_FASTCALL, "gformer_paged_fill"},
+    {"paged_decode", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(paged_decode)), METH_FASTCALL, "gformer_paged_decode"},
+    {"pages_copy", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(pages_copy)), METH_FASTCALL, "gformer_pages_copy"},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_decode_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -310,3 +310,30 @@ def test_captured_and_on_another_stream():
         for name, x in zip(("out", "dq", "dk", "dv", "lse"), (out, dq, dk, dv, lse)):
             assert torch.equal(x, want[name]), name     # no atomics: equal calls give equal bits
         run(q, k, v, g, lens, lens, 0.1)
+
+
+@gpu
+def test_the_extension_module_makes_the_plain_calls(monkeypatch):
+    """... with the results of the binding's own code, which makes the others."""
+    lens = [50, 90]
+    q, k, v, g = tensors(lens, lens, 4, 2, 64, "bf16", 14, layout="fused")
+    made = []
+    quick = gb._quick
+    monkeypatch.setattr(gb, "_quick", lambda *a: made.append(quick(*a)) or made[-1])
+    got = run(q, k, v, g, lens, lens, 0.2, rest=True)
+    assert made == [True, True]
+    out = torch.empty_like(q)
+    gb.gformer_packed_attn_fwd(q, k, v, out, cu(lens), softmax_scale=1, stream=torch.cuda.current_stream().cuda_stream)
+    assert made[2:] == [False]                          # a scale that is no float
+    monkeypatch.setattr(gb, "_quick", lambda *a: False)
+    again = run(q, k, v, g, lens, lens, 0.2, rest=True)
+    for name in got:
+        assert torch.equal(got[name], again[name]), name
+    with pytest.raises(ValueError, match="q's shape"):
+        gb.gformer_packed_attn_fwd(q, k, v, out[:5], cu(lens))
+    monkeypatch.setattr(gb, "_quick", quick)
+    with pytest.raises(gb.GformerError, match="status 2"):
+        gb.gformer_packed_attn_fwd(*(torch.zeros(8, 2, 32, device="cuda") for _ in range(4)), cu([8]))
+    with pytest.raises(gb.GformerError, match="status 3"):
+        gb.gformer_packed_attn_bwd(q, k, v, q, got["lse"], q, *(torch.empty_like(x) for x in (q, k, v)), cu(lens),
+                                   workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))

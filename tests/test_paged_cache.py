@@ -419,3 +419,20 @@ def test_captured_step():
         ref.check(out, *want, "replay")
         first = out.clone() if first is None else first
         assert torch.equal(out, first) and torch.equal(step(x, 0.1), first)
+
+
+@gpu
+def test_the_extension_module_makes_the_plain_calls(monkeypatch):
+    x, ks, vs = make([300, 20], 8, 2, 64, 16, "bf16", 9)
+    made, quick = [], gb._quick
+    monkeypatch.setattr(gb, "_quick", lambda *a: made.append(quick(*a)) or made[-1])
+    step(x, 0.1)
+    pages = x["kpages"].clone(), x["vpages"].clone()
+    cu, start = (torch.tensor(t, dtype=torch.int32).cuda() for t in ([0, 1, 2], [3, 5]))
+    src, dst = (x["table"][0, i:i + 1].contiguous() for i in (1, 2))
+    for pair in (pages, (x["kpages"], x["vpages"])):
+        gb.gformer_paged_fill(x["k"], x["v"], *pair, x["table"], start, cu)
+        gb.gformer_pages_copy(*pair, src, dst)
+        monkeypatch.setattr(gb, "_quick", lambda *a: False)     # the second time in Python
+    assert made == [True] * 3
+    assert all(torch.equal(a.view(torch.int16), b.view(torch.int16)) for a, b in zip(pages, (x["kpages"], x["vpages"])))
