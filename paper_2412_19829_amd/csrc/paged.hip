@@ -4,6 +4,8 @@
 // or value is read once for all of them, straight from memory into matrix operands.  A sequence is cut along its
 // length into chunks of keys, one workgroup each, whose four waves take tiles in turn; every wave keeps a softmax of
 // its own (running maximum, sum and weighted values), the waves are joined in LDS and the chunks by a second kernel.
+// Memory bounds it, and what hides its latency are waves, three on a SIMD: a tile loaded ahead in registers leaves room
+// for two only (4 sequences of up to 32768, 32 / 8 heads, d = 128: 97 us so, 88 with three, 5.4 TB/s).
 //
 // Score tile S^T = K Q^T (D = A*B, lane l, i = l % 16, g = l / 16): A row i = key i, B column i = head i, result column
 // i = head i, register r = key 4 g + r.  Those registers are the next product's B operand as they are, if its
@@ -45,7 +47,8 @@ template <int D> struct Cached<uint16_t, D> {
 #pragma unroll
     for (int s = 0; s < D / 32; ++s) k[s] = *reinterpret_cast<const u32x4*>(row + 32 * s + 8 * g);
   }
-  static __device__ __forceinline__ void load_v(Part& v, const uint16_t* row, int i) { v = *reinterpret_cast<const Part*>(row + E * i); }
+  // a value row is read whole, once, and need not stay in the caches (a key row is read in quarters, which share lines)
+  static __device__ __forceinline__ void load_v(Part& v, const uint16_t* row, int i) { v = __builtin_nontemporal_load(reinterpret_cast<const Part*>(row + E * i)); }
   static __device__ __forceinline__ f32x4 scores(const u32x4 (&k)[D / 32], const Query& q) {
     f32x4 s = kZeroF4;
 #pragma unroll
@@ -91,7 +94,7 @@ template <int D> struct Cached<float, D> {
   }
   static __device__ __forceinline__ void load_v(Part& v, const float* row, int i) {
 #pragma unroll
-    for (int hh = 0; hh < HH; ++hh) v.x[hh] = *reinterpret_cast<const f32x4*>(row + 64 * hh + 4 * i);
+    for (int hh = 0; hh < HH; ++hh) v.x[hh] = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(row + 64 * hh + 4 * i));
   }
   static __device__ __forceinline__ f32x4 scores(const f32x4 (&k)[D / 16], const Query& q) {
     f32x4 s = kZeroF4;
@@ -119,16 +122,20 @@ __device__ __forceinline__ int seen_keys(const PagedDecodeArgs& a, int b) {
   return t < 0 || t >= a.room + (a.k ? 0 : 1) ? 0 : n;
 }
 
-template <typename T, int D> __global__ __launch_bounds__(kDecodeThreads, 2) void paged_decode_kernel(PagedDecodeArgs a) {
+template <typename T, int D> __global__ __launch_bounds__(kDecodeThreads, 3) void paged_decode_kernel(PagedDecodeArgs a) {
   using C = Cached<T, D>;
   constexpr int U = C::U, R = 16 * U, NO = C::NO, E = C::E;
   __shared__ float sm_o[kDecodeWaves][kPagedHeads][D + 4], sm_m[kDecodeWaves][kPagedHeads], sm_l[kDecodeWaves][kPagedHeads];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, g = lane >> 4;
   const int G = a.H / a.Hkv, tiles = (G + kPagedHeads - 1) / kPagedHeads;
+  // Chunks slowest: workgroups are dealt to the 8 XCDs in turn, and the chunks behind short sequences' ends, which are none,
+  // would leave some XCDs without work.
   int id = blockIdx.x;
-  const int split = id % a.splits;
-  id /= a.splits;
-  const int tile = id % tiles, kvh = id / tiles % a.Hkv, b = id / tiles / a.Hkv;
+  const int tile = id % tiles;
+  id /= tiles;
+  const int kvh = id % a.Hkv;
+  id /= a.Hkv;
+  const int b = id % a.B, split = id / a.B;
   const int h0 = kvh * G + tile * kPagedHeads, heads = min(G - tile * kPagedHeads, kPagedHeads);
   const int n = seen_keys(a, b), from = split * a.chunk, to = min(n, from + a.chunk);
   if (split > 0 && from >= n) return;   // the joining kernel knows as much
@@ -191,16 +198,11 @@ template <typename T, int D> __global__ __launch_bounds__(kDecodeThreads, 2) voi
 
   const int step = kDecodeWaves * R;
   int t0 = from + wave * R;
-  Pages p_now, p_next;
-  typename C::Tile x, next;
-  if (t0 < to) {
-    p_now = pages(t0);
-    p_next = pages(t0 + step);
-    load(x, p_now, t0);
-  }
+  Pages here = pages(t0);   // looked up a tile ahead
   for (; t0 < to; t0 += step) {
-    const Pages p_after = pages(t0 + 2 * step);
-    if (t0 + step < to) load(next, p_next, t0 + step);
+    typename C::Tile x;
+    load(x, here, t0);
+    const Pages next = pages(t0 + step);
     float w[U][4];
     float top = -INFINITY;
     uint32_t in[U];
@@ -208,7 +210,7 @@ template <typename T, int D> __global__ __launch_bounds__(kDecodeThreads, 2) voi
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int key = t0 + 16 * u + i;
-      in[u] = (uint32_t)__builtin_amdgcn_ballot_w64(key < to && (there(p_now.k[u]) || key == own)) & 0xffffu;
+      in[u] = (uint32_t)__builtin_amdgcn_ballot_w64(key < to && (there(here.k[u]) || key == own)) & 0xffffu;
       whole = whole && in[u] == 0xffffu;
       const f32x4 s = C::scores(x.k[u], q);
 #pragma unroll
@@ -241,9 +243,7 @@ template <typename T, int D> __global__ __launch_bounds__(kDecodeThreads, 2) voi
 #pragma unroll
       for (int r = 0; r < 4; ++r) w[u][r] = __builtin_amdgcn_exp2f(w[u][r] - ref);
     C::product(o, x, w, l);
-    x = next;
-    p_now = p_next;
-    p_next = p_after;
+    here = next;
   }
   l = sum_over_groups(l);
 
@@ -372,10 +372,13 @@ template <typename T, int D> hipError_t decode(const PagedDecodeArgs& a, hipStre
 
 }  // namespace
 
+// Six workgroups for every compute unit if all sequences were the longest, and no chunk shorter than a tile for each wave.
+// us, 512 / 1024 / 1536 / 2048 / 4096 workgroups: 32 sequences of up to 8192, 32 / 8 heads, d = 128, 88,000 keys in all 109 / 90 / 72 / 78 / 74,
+// 4 of up to 32768 84 / 88 / 88 / 91 / 94; one of 2048, 12 heads, d = 64, by chunks of 64, 128, 256, 512: 7.8 / 7.0 / 7.9 / 10.7.
 PagedSplit paged_split(int B, int H, int Hkv, int64_t max_len) {
   const int64_t units = (int64_t)B * Hkv * ((H / Hkv + kPagedHeads - 1) / kPagedHeads);
-  int64_t chunk = (max_len * units + 1023) / 1024;
-  chunk = std::max<int64_t>(256, (chunk + 127) / 128 * 128);
+  int64_t chunk = (max_len * units + 1535) / 1536;
+  chunk = std::max<int64_t>(128, (chunk + 63) / 64 * 64);
   return {(int)chunk, (int)std::max<int64_t>(1, (max_len + chunk - 1) / chunk)};
 }
 
