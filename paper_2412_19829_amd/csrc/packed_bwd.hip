@@ -235,7 +235,12 @@ template <typename T, int D, typename F> __global__ __launch_bounds__(F::THREADS
     const T *qt = sm.q[n % BUF] + 32 * part * D, *gt = sm.g[n % BUF] + 32 * part * D;
     const float* stats = sm.stats[n % BUF] + 32 * part + 4 * lh;
     const int lo = from - t0, hi = nq - t0;   // rows that see this lane's key
-    auto hidden = [&](int r) { return 8 * (r / 4) + 4 * lh + r % 4 < lo || 8 * (r / 4) + 4 * lh + r % 4 >= hi; };
+    auto hide = [&](float (&x)[16]) {
+      int first = lo - 4 * lh;
+      asm volatile("" : "+v"(first));   // compared anew each time: 16 kept results would take 32 scalar registers
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[r] = 8 * (r / 4) + r % 4 < first || 8 * (r / 4) + r % 4 >= hi - 4 * lh ? 0.f : x[r];
+    };
     float p[16], ds[16];
     const f32x16 s = P::scores(qt, k, lane);
 #pragma unroll
@@ -244,10 +249,7 @@ template <typename T, int D, typename F> __global__ __launch_bounds__(F::THREADS
 #pragma unroll
       for (int e = 0; e < 4; ++e) p[4 * g + e] = __builtin_amdgcn_exp2f(fmaf(s[4 * g + e], sc, -l4[e]));
     }
-    if (mask) {
-#pragma unroll
-      for (int r = 0; r < 16; ++r) p[r] = hidden(r) ? 0.f : p[r];
-    }
+    if (mask) hide(p);
     const typename P::Weights wp = P::weights(p);
     if (by_rows && mask && L::odd(gt, lane)) P::product_by_rows(dv, gt, wp, lo, hi, lane);
     else P::product(dv, gt, wp, lane);
@@ -262,10 +264,7 @@ template <typename T, int D, typename F> __global__ __launch_bounds__(F::THREADS
     else dp = P::scores(gt, v, lane, dp);
 #pragma unroll
     for (int r = 0; r < 16; ++r) ds[r] = p[r] * dp[r];
-    if (mask) {
-#pragma unroll
-      for (int r = 0; r < 16; ++r) ds[r] = hidden(r) ? 0.f : ds[r];
-    }
+    if (mask) hide(ds);
     const typename P::Weights wd = P::weights(ds);
     if (by_rows && mask && L::odd(qt, lane)) P::product_by_rows(dk, qt, wd, lo, hi, lane);
     else P::product(dk, qt, wd, lane);
