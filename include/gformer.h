@@ -290,7 +290,8 @@ gf_status gformer_attn_bwd(const void* q, const void* k, const void* v, const vo
  * multiple of Hkv, query head h reads key head h / (H / Hkv); fp32 arithmetic and statistics, with bf16 only the
  * operands of the matrix products are rounded (weights, and in the backward pass the gradients of the
  * scores).  Conventions (alignment, asynchrony, errors, the device of the stream) as at the top of this file;
- * strides are multiples of 8 elements, all-zero strides mean dense, a row (token) stride may not exceed 2^20.
+ * strides are multiples of 8 elements, all-zero strides mean dense, a row (token) stride may not exceed 2^20, a
+ * packed tensor 2^30 rows.
  * Integer arrays are DEVICE pointers to int32, 4-byte aligned, and are read on the device alone: offsets,
  * lengths and page numbers out of range never make a call read or write outside the tensors it was
  * given, but what it then computes is not defined beyond what is said below.

@@ -12,7 +12,7 @@ namespace {
 
 constexpr int64_t kMaxTokenStride = 1 << 20;   // elements
 constexpr int64_t kMaxGrid = 0x7fffffff;
-constexpr int64_t kMaxCached = 1 << 30;        // tokens of one sequence
+constexpr int64_t kMaxCached = 1 << 30;        // tokens of one sequence, or rows of a packed tensor
 
 bool misaligned(uintptr_t all, unsigned bytes) { return (all & (bytes - 1)) != 0; }
 template <typename... P> uintptr_t bits(P... p) { return (0 | ... | (uintptr_t)p); }
@@ -71,6 +71,7 @@ gf_status check_packed(int n_seqs, int total_q, int total_k, int H, int Hkv, int
       (st = strides2(p->do_stride, a->gs, H, d)) != GF_OK || (st = strides2(p->dq_stride, a->dqs, H, d)) != GF_OK ||
       (st = strides2(p->dk_stride, a->dks, Hkv, d)) != GF_OK || (st = strides2(p->dv_stride, a->dvs, Hkv, d)) != GF_OK)
     return st;
+  if (total_q > kMaxCached || total_k > kMaxCached || n_seqs > kMaxCached) return GF_ERR_UNSUPPORTED;
   if (packed_tiles(total_q, n_seqs, kPackedRows) * H > kMaxGrid || packed_tiles(total_k, n_seqs, kPackedRows) * Hkv > kMaxGrid)
     return GF_ERR_UNSUPPORTED;
   a->n_seqs = n_seqs;
@@ -276,6 +277,7 @@ gf_status gformer_paged_fill(const void* k, const void* v, void* kpages, void* v
   if (st != GF_OK) return st;
   if ((st = check_table(table_width, a.shift, 0, &room)) != GF_OK) return st;
   if (n_seqs < 0 || total < 0) return GF_ERR_INVALID_ARG;
+  if (total > kMaxCached || n_seqs > kMaxCached) return GF_ERR_UNSUPPORTED;
   if ((st = strides2(p->k_stride, a.ks, Hkv, d)) != GF_OK || (st = strides2(p->v_stride, a.vs, Hkv, d)) != GF_OK) return st;
   if (packed_tiles(total, n_seqs, 32) * Hkv > kMaxGrid) return GF_ERR_UNSUPPORTED;
   if (total == 0 || n_seqs == 0 || table_width == 0 || n_pages == 0) return GF_OK;

@@ -118,8 +118,8 @@ template <int D> struct Cached<float, D> {
 // Keys that sequence b's token sees: its cached ones and, where the call brings it, its own.  A length that there
 // is no room for is an idle row: it sees nothing and writes nothing.
 __device__ __forceinline__ int seen_keys(const PagedDecodeArgs& a, int b) {
-  const int t = a.lens[b], n = a.k ? t + 1 : t;
-  return t < 0 || t >= a.room + (a.k ? 0 : 1) ? 0 : n;
+  const int t = a.lens[b], own = a.k ? 1 : 0;
+  return t < 0 || t > a.room - own ? 0 : t + own;
 }
 
 template <typename T, int D> __global__ __launch_bounds__(kDecodeThreads, 3) void paged_decode_kernel(PagedDecodeArgs a) {

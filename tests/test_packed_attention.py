@@ -160,6 +160,19 @@ def test_values_and_gradients(dtype, d, H, Hkv, shape):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("H,Hkv", [(64, 64), (128, 32)])
+@pytest.mark.parametrize("lens_q,lens_k", [([127, 129, 64, 33], None), ([1, 140, 0, 130], [77, 140, 9, 257]), ([20, 240, 3], [5, 0, 200])])
+def test_many_heads(dtype, d, H, Hkv, lens_q, lens_k):
+    """Enough workgroups for the kernels whose waves share the streamed rows (those above have waves on different ones)."""
+    lens_k = lens_k or lens_q
+    q, k, v, g = tensors(lens_q, lens_k, H, Hkv, d, dtype, H + d, layout="heads")
+    got = run(q, k, v, g, lens_q, lens_k, d ** -0.5, rest=True)
+    compare(got, ref.packed(q, k, v, g, lens_q, lens_k, d ** -0.5, dtype), lens_q, lens_k)
+
+
+@gpu
 @pytest.mark.parametrize("d", [64, 128])
 def test_what_rounding_takes_from_the_output(d):
     """out + rest is the output before its rounding, up to rest's own; dq and dk then come nearer to the formula's."""
@@ -179,7 +192,7 @@ def test_what_rounding_takes_from_the_output(d):
 
 @gpu
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("scale", [-0.2, 0.0, 1.5])
+@pytest.mark.parametrize("scale", [-0.2, 0.0, 1e-42, 1.5])
 def test_scales(dtype, scale):
     lens = [70, 200]
     q, k, v, g = tensors(lens, lens, 2, 1, 64, dtype, 5)
@@ -197,9 +210,10 @@ def test_many_short_sequences(dtype):
 @gpu
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("zero", [0, 1])
-def test_rows_behind_the_last_sequence(dtype, zero):
+@pytest.mark.parametrize("H,Hkv", [(2, 2), (4, 1), (64, 64)])
+def test_rows_behind_the_last_sequence(dtype, zero, H, Hkv):
     lens, tail = [5, 130], 300
-    q, k, v, g = tensors(lens, lens, 2, 2, 64, dtype, 7, tail=tail)
+    q, k, v, g = tensors(lens, lens, H, Hkv, 64, dtype, 7, tail=tail)
     for x in (q, k, v, g):
         x[sum(lens):] = NAN
     got = run(q, k, v, g, lens, lens, 0.125, zero_tail=zero)
@@ -212,12 +226,12 @@ def test_rows_behind_the_last_sequence(dtype, zero):
 @gpu
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("d", [64, 128])
-@pytest.mark.parametrize("bad", [NAN, INF, -INF])
-def test_what_a_row_does_not_see_has_no_part_in_it(dtype, d, bad):
+@pytest.mark.parametrize("bad,H,Hkv", [(NAN, 2, 1), (INF, 2, 1), (-INF, 2, 1), (NAN, 96, 96), (INF, 96, 48)])
+def test_what_a_row_does_not_see_has_no_part_in_it(dtype, d, bad, H, Hkv):
     # sequence 0: a key and a value that only its later queries see, and a query and a gradient that are no part of what
     # later keys get; sequence 1 sees nothing of either
     lens, at = [150, 90], 70
-    q, k, v, g = tensors(lens, lens, 2, 1, d, dtype, 8)
+    q, k, v, g = tensors(lens, lens, H, Hkv, d, dtype, 8)
     clean = ref.packed(q, k, v, g, lens, lens, 0.1, dtype)
     for name, x in (("k", k), ("v", v)):
         kept = x[at].clone()
@@ -337,3 +351,27 @@ def test_the_extension_module_makes_the_plain_calls(monkeypatch):
     with pytest.raises(gb.GformerError, match="status 3"):
         gb.gformer_packed_attn_bwd(q, k, v, q, got["lse"], q, *(torch.empty_like(x) for x in (q, k, v)), cu(lens),
                                    workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
+
+
+def test_the_tensors_device_is_current_during_the_call(monkeypatch):
+    class On:
+        device = "cuda:1"
+        def get_device(self):
+            return 1
+    current = [0]
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: current[-1])
+    class Guard:
+        def __init__(self, device):
+            assert device == "cuda:1"
+        def __enter__(self):
+            current.append(1)
+        def __exit__(self, *_):
+            current.pop()
+    monkeypatch.setattr(torch.cuda, "device", Guard)
+    seen = []
+    gb._call(lambda *a: seen.append((current[-1], a)) or gb.GF_OK, On(), 5, "x")
+    current.append(1)
+    gb._call(lambda *a: seen.append((current[-1], a)) or gb.GF_OK, On(), 6, "y")
+    assert seen == [(1, ("x", 5)), (1, ("y", 6))] and current == [0, 1]
+    with pytest.raises(gb.GformerError, match="status 2"):
+        gb._call(lambda *a: 2, On(), 5)
