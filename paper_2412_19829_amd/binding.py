@@ -628,6 +628,21 @@ def _quick(function, entries, *args):
     return True
 
 
+def packed_attention_node(q, k, v, cu_q, cu_k, softmax_scale):
+    """Packed attention with its node in torch's graph from the extension module (host/packed_grad.cpp), or None for what
+    is not its plain call."""
+    if _native is None:
+        _decode_call()
+    if _module is None:
+        return None
+    address = (_lib or lib()).address
+    out = _module.packed_attention(address["packed_attn_fwd"], address["packed_attn_bwd"], address["packed_attn_bwd_workspace_bytes"],
+                                   q, k, v, cu_q, cu_k, softmax_scale)
+    if isinstance(out, int):
+        raise GformerError(out, gformer_status_string(out))
+    return out
+
+
 def make_packed_params(dtype=GF_BF16, softmax_scale=1.0, zero_tail=0, **strides) -> GformerPackedParams:
     """strides: q_stride=, k_stride=, ... as (row, head)."""
     p = GformerPackedParams(ctypes.sizeof(GformerPackedParams), int(dtype), int(zero_tail), float(softmax_scale))

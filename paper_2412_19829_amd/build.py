@@ -14,7 +14,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OBJ_DIR = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libgformer_attn.so")
-CALL_SRC = [os.path.join(HERE, "host", x) for x in ("decode_call.cpp", "packed_call.cpp")]
+CALL_SRC = [os.path.join(HERE, "host", x) for x in ("decode_call.cpp", "packed_call.cpp", "packed_grad.cpp")]
 CALL = os.path.join(HERE, "_decode_call.so")
 
 # packed-fp32 VALU forms are kept off for every device compilation unit

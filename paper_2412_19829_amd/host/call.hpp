@@ -1,4 +1,4 @@
-// What the host sides of the calls share (decode_call.cpp, packed_call.cpp): reading Python arguments without its own
+// What the host sides of the calls share (decode_call.cpp, packed_call.cpp, packed_grad.cpp): reading Python arguments without its own
 // machinery.
 #pragma once
 
@@ -65,5 +65,7 @@ PyObject* packed_bwd(PyObject*, PyObject* const* a, Py_ssize_t n);
 PyObject* paged_fill(PyObject*, PyObject* const* a, Py_ssize_t n);
 PyObject* paged_decode(PyObject*, PyObject* const* a, Py_ssize_t n);
 PyObject* pages_copy(PyObject*, PyObject* const* a, Py_ssize_t n);
+// packed_grad.cpp
+PyObject* packed_attention(PyObject*, PyObject* const* a, Py_ssize_t n);
 
 }  // namespace gformer_host

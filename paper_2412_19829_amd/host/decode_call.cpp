@@ -102,6 +102,7 @@ PyMethodDef methods[] = {
     {"paged_fill", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(paged_fill)), METH_FASTCALL, "gformer_paged_fill"},
     {"paged_decode", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(paged_decode)), METH_FASTCALL, "gformer_paged_decode"},
     {"pages_copy", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(pages_copy)), METH_FASTCALL, "gformer_pages_copy"},
+    {"packed_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(packed_attention)), METH_FASTCALL, "packed attention as a node"},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_decode_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -375,3 +375,66 @@ def test_the_tensors_device_is_current_during_the_call(monkeypatch):
     assert seen == [(1, ("x", 5)), (1, ("y", 6))] and current == [0, 1]
     with pytest.raises(gb.GformerError, match="status 2"):
         gb._call(lambda *a: 2, On(), 5)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_the_node_of_the_extension_module_is_the_wrapper(dtype, monkeypatch):
+    from paper_2412_19829_amd import autograd
+    lens_q, lens_k, tail = [40, 0, 200, 3], [44, 9, 200, 3], 6
+    q, k, v, g = tensors(lens_q, lens_k, 4, 2, 64, dtype, 31, tail=tail)
+    q = q.transpose(0, 1).contiguous().transpose(0, 1)   # heads slowest
+    starts = cu(lens_q), cu(lens_k)
+    gradients = [g, g[:1].expand_as(g), g.transpose(0, 1).contiguous().transpose(0, 1), g.transpose(1, 2).contiguous().transpose(1, 2),
+                 torch.cat([g.flatten()[:1], g.flatten()])[1:].view_as(g)]
+    taken = []
+    made = gb.packed_attention_node
+
+    def results(gradient):
+        leaves = [x.detach().requires_grad_(True) for x in (q, k, v)]
+        out = autograd.gformer_packed_attention(*leaves, *starts, softmax_scale=0.125)
+        return [out.detach(), *torch.autograd.grad(out, leaves, gradient)]
+
+    def node(*a):
+        taken.append(made(*a))
+        return taken[-1]
+
+    for gradient in gradients:
+        with monkeypatch.context() as m:
+            m.setattr(gb, "packed_attention_node", node)
+            one = results(gradient)
+        with monkeypatch.context() as m:
+            m.setattr(gb, "packed_attention_node", lambda *a: None)
+            two = results(gradient)
+        assert taken[-1] is not None and all(torch.equal(a, b) for a, b in zip(one, two))
+
+    leaves = [x.detach().requires_grad_(True) for x in (q, k, v)]
+    out = autograd.gformer_packed_attention(*leaves, *starts, softmax_scale=0.125)
+    first = torch.autograd.grad(out, leaves, g, create_graph=True)
+    with pytest.raises(RuntimeError, match="once"):
+        first[0].float().sum().backward()
+
+    # one leaf alone, none, and a leaf changed before the backward pass
+    k1 = k.detach().requires_grad_(True)
+    again = autograd.gformer_packed_attention(q, k1, v, *starts, softmax_scale=0.125)
+    assert torch.equal(torch.autograd.grad(again, k1, g)[0], first[1].detach())
+    assert not autograd.gformer_packed_attention(q, k, v, *starts, softmax_scale=0.125).requires_grad
+    out = autograd.gformer_packed_attention(q, k1, v, *starts, softmax_scale=0.125)
+    with torch.no_grad():
+        k1.mul_(2)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        torch.autograd.grad(out, k1, g)
+
+
+@gpu
+def test_the_wrapper_refuses():
+    from paper_2412_19829_amd.autograd import gformer_packed_attention
+    q, k, v, _ = tensors([8], [8], 4, 2, 64, "bf16", 1)
+    with pytest.raises(gb.GformerError):
+        gformer_packed_attention(q[:, :3], k, v, cu([8]))          # 3 heads over 2
+    with pytest.raises(gb.GformerError):
+        gformer_packed_attention(q[..., :48], k[..., :48], v[..., :48], cu([8]))
+    for bad in ((q, k.float(), v, cu([8])), (q, k, v[:4], cu([8])), (q, k, v, cu([8]).long()), (q.cpu(), k, v, cu([8])),
+                (q[:4], k, v, cu([4])), (q, k, v, cu([8]), cu([8, 0])), (q[0], k, v, cu([8]))):
+        with pytest.raises((ValueError, gb.GformerError)):
+            gformer_packed_attention(*bad)
