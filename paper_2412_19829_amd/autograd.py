@@ -49,7 +49,8 @@ def gformer_attention(q, k, v, window: int, n_sparse_heads: int, *, phi=gb.GF_PH
 def _fits(t):
     """Whether a [rows, heads, d] tensor can be handed over as it is; a gradient may come in any layout."""
     return (t.stride(-1) == 1 and t.data_ptr() % 16 == 0 and
-            all(n == 1 or (x >= t.shape[-1] and x % 8 == 0) for n, x in zip(t.shape[:2], t.stride()[:2])))
+            all(n == 1 or (x >= t.shape[-1] and x % 8 == 0) for n, x in zip(t.shape[:2], t.stride()[:2])) and
+            (t.shape[0] == 1 or t.stride(0) <= 1 << 20))
 
 
 class _GformerPackedAttention(torch.autograd.Function):

@@ -37,7 +37,7 @@ bool strides(const at::Tensor& t, int64_t (&out)[2]) {
   if (s[2] != 1 && n[2] > 1) return false;
   out[1] = n[1] > 1 ? s[1] : n[2];
   out[0] = n[0] > 1 ? s[0] : n[2] * std::max<int64_t>(n[1], 1);
-  return out[0] >= n[2] && out[1] >= n[2] && out[0] % 8 == 0 && out[1] % 8 == 0;
+  return out[0] >= n[2] && out[1] >= n[2] && out[0] % 8 == 0 && out[1] % 8 == 0 && out[0] <= 1 << 20;
 }
 bool fits(const at::Tensor& t, int64_t (&out)[2]) { return strides(t, out) && ((uintptr_t)t.data_ptr() & 15) == 0; }
 

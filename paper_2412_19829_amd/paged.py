@@ -21,6 +21,10 @@ class PagedCache:
                  dtype=torch.bfloat16, device="cuda"):
         if min(n_pages, page_size, n_heads, d, max_seqs, max_pages, layers) < 1:
             raise ValueError("sizes must be positive")
+        if d not in (64, 128) or dtype not in (torch.bfloat16, torch.float32):
+            raise ValueError("d is 64 or 128, dtype bfloat16 or float32")
+        if not 8 <= page_size <= 65536 or page_size & (page_size - 1) or max_pages * page_size > 1 << 30:
+            raise ValueError("page_size is a power of two from 8 to 65536, a sequence has at most 2^30 tokens")
         self.page_size, self.n_heads, self.max_pages = page_size, n_heads, max_pages
         self.kpages = torch.zeros(n_pages, layers * n_heads, page_size, d, dtype=dtype, device=device)
         self.vpages = torch.zeros_like(self.kpages)

@@ -386,7 +386,8 @@ def test_the_node_of_the_extension_module_is_the_wrapper(dtype, monkeypatch):
     q = q.transpose(0, 1).contiguous().transpose(0, 1)   # heads slowest
     starts = cu(lens_q), cu(lens_k)
     gradients = [g, g[:1].expand_as(g), g.transpose(0, 1).contiguous().transpose(0, 1), g.transpose(1, 2).contiguous().transpose(1, 2),
-                 torch.cat([g.flatten()[:1], g.flatten()])[1:].view_as(g)]
+                 torch.cat([g.flatten()[:1], g.flatten()])[1:].view_as(g),
+                 torch.empty(len(g), (1 << 20) + 8, dtype=g.dtype, device="cuda")[:, :g[0].numel()].view_as(g).copy_(g)]
     taken = []
     made = gb.packed_attention_node
 

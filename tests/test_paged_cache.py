@@ -112,6 +112,13 @@ def test_bookkeeping(monkeypatch):
         c.advance([e])
 
 
+@pytest.mark.parametrize("kw", [dict(n_pages=0), dict(max_seqs=0), dict(layers=0), dict(d=80), dict(dtype=torch.float16), dict(page_size=4),
+                                dict(page_size=24), dict(page_size=1 << 17), dict(page_size=1 << 16, max_pages=(1 << 14) + 1)])
+def test_a_cache_that_the_calls_would_refuse_is_not_made(kw):
+    with pytest.raises(ValueError):
+        cache(**kw)
+
+
 def test_a_refused_call_changes_nothing(monkeypatch):
     Copies(monkeypatch)
     c = cache(n_pages=4)
