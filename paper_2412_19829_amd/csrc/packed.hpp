@@ -39,6 +39,8 @@ hipError_t launch_packed_bwd(const PackedArgs& a, bool bf16, hipStream_t s);
 // What the backward pass keeps beside a query's statistics: the query heads of a key head in `groups` parts, whose dk and dv
 // are added up by a kernel of their own (1: there is none).
 int packed_head_groups(int total_k, int n_seqs, int H, int Hkv);
+// The streams of the passes that hold queries (packed_fwd.hip has the figures).
+int packed_streams(bool fp32, int d, int total_q, int H, int n_seqs);
 inline size_t packed_stats_bytes(int total_q, int H) { return ((size_t)total_q * H * 2 * sizeof(float) + 255) / 256 * 256; }
 inline size_t packed_sums_bytes(int total_k, int n_seqs, int H, int Hkv, int d) {
   const int groups = packed_head_groups(total_k, n_seqs, H, Hkv);
@@ -63,15 +65,6 @@ template <int RW_, int S_, int R_, int BUF_, int PER_SIMD_> struct Shape {
 // prefix sum and no look at the offsets on the host; the few tiles too many end at once.  The rows behind the last sequence
 // count as sequence n_seqs.
 inline int64_t packed_tiles(int total, int n_seqs, int rows) { return (int64_t)total / rows + n_seqs + 1; }
-
-// Whether a call has so few workgroups of kPackedRows rows that their waves are better off on different streamed rows of the
-// same resident ones.  That divides the longest workgroup's time by the streams, and loads every streamed row as many times
-// more often: worth it as long as about `limit` workgroups or fewer would leave compute units idle, or half as many where sequences
-// are short (a mean of less than 512 rows), whose joins weigh more.
-inline bool packed_splits(int rows, int heads, int n_seqs, int limit) {
-  if ((int64_t)rows < (int64_t)512 * n_seqs) limit /= 2;
-  return (int64_t)rows * heads <= (int64_t)limit * kPackedRows;
-}
 
 struct SeqTile {
   int seq;     // n_seqs: the rows behind the last sequence
@@ -214,6 +207,11 @@ __device__ __forceinline__ bool any_wave(int* flag, bool x) {
 template <int N> __device__ __forceinline__ void loads_left() {
   static_assert(N < 64);
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+// A wave is done reading a tile that it alone uses: what it loads into it next comes behind.
+__device__ __forceinline__ void tile_read() {
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
 }
 
 // LDS by its byte addresses.  A tile starts at a multiple of 256 bytes, so the pieces of a row (and of the rows 16 further
@@ -441,10 +439,21 @@ template <int D> struct Products<float, D> {
   }
   static __device__ __forceinline__ void product(f32x16 (&acc)[D / 32], const T* rows, const Weights& w, int lane) {
     const uint32_t at = lds_lane(rows, turned_at(lane));
+    // some reads ahead of their products; all at once would take the registers of the sums
+    constexpr int AHEAD = 4;
 #pragma unroll
-    for (int r = 0; r < 16; ++r)
+    for (int r0 = 0; r0 < 16; r0 += AHEAD) {
+      float x[AHEAD][D / 32];
 #pragma unroll
-      for (int mt = 0; mt < D / 32; ++mt) acc[mt] = mfma(turned(at, r, mt), w.x[r], acc[mt]);
+      for (int r = 0; r < AHEAD; ++r)
+#pragma unroll
+        for (int mt = 0; mt < D / 32; ++mt) x[r][mt] = turned(at, r0 + r, mt);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int r = 0; r < AHEAD; ++r)
+#pragma unroll
+        for (int mt = 0; mt < D / 32; ++mt) acc[mt] = mfma(x[r][mt], w.x[r0 + r], acc[mt]);
+    }
   }
   static __device__ __forceinline__ void product_by_rows(f32x16 (&acc)[D / 32], const T* rows, const Weights& w, int first, int end,
                                                          int lane) {

@@ -13,13 +13,16 @@ namespace {
 // waves on a SIMD that the kernels' registers are kept down for
 template <typename T, int D> constexpr int kWaves = sizeof(T) == 4 && D == 128 ? 1 : 2;
 
-// dq: as the forward pass; SPLIT has its waves on different keys
-template <typename T, int D, bool SPLIT> struct DqShape_;
-template <typename T, int D> struct DqShape_<T, D, false> {
+// dq: as the forward pass
+template <typename T, int D, int STREAMS> struct DqShape_;
+template <typename T, int D> struct DqShape_<T, D, 1> {
   using type = Shape<4, 1, sizeof(T) == 2 && D == 64 ? 64 : 32, 3, kWaves<T, D>>;
 };
-template <typename T, int D> struct DqShape_<T, D, true> {
-  using type = std::conditional_t<sizeof(T) == 4 && D == 128, Shape<2, 2, 32, 2, 1>, Shape<1, 4, 32, 2, sizeof(T) == 2 && D == 64 ? 2 : 1>>;
+template <typename T, int D> struct DqShape_<T, D, 2> {
+  using type = Shape<2, 2, 32, 2, 1>;
+};
+template <typename T, int D> struct DqShape_<T, D, 4> {
+  using type = Shape<1, 4, 32, 1, kWaves<T, D>>;
 };
 template <typename T, int D, typename F> struct alignas(256) DqTiles {
   struct { T k[F::BUF][F::R * D], v[F::BUF][F::R * D]; } stream[F::S];
@@ -114,10 +117,15 @@ template <typename T, int D, typename F> __global__ __launch_bounds__(F::THREADS
   const T* vp = rows_of<T>(a.v, a.vs, kbase, kvh);
   const int last_key = min(i0 + ROWS, nq) - 1 + off;
   const int n_tiles = last_key < 0 ? 0 : last_key / R + 1;
-  auto load = [&](int t, int n) {   // tile t, the stream's n-th
-    L::template load<W>(sm.k[n % BUF], kp, a.ks[0], t * R, nk - 1, wave, lane);
-    L::template load<W>(sm.v[n % BUF], vp, a.vs[0], t * R, nk - 1, wave, lane);
+  // tile t, the stream's n-th
+  auto load_keys = [&](int t, int n) { L::template load<W>(sm.k[n % BUF], kp, a.ks[0], t * R, nk - 1, wave, lane); };
+  auto load_values = [&](int t, int n) { L::template load<W>(sm.v[n % BUF], vp, a.vs[0], t * R, nk - 1, wave, lane); };
+  auto load = [&](int t, int n) {
+    load_values(t, n);
+    load_keys(t, n);
   };
+  constexpr bool OWN = BUF == 1;   // as in the forward pass
+  static_assert(!OWN || W == 1);
   bool odd = false;
   auto sums = [&](int t, int nth, auto by_rows) {
     const int t0 = t * R;
@@ -125,7 +133,16 @@ template <typename T, int D, typename F> __global__ __launch_bounds__(F::THREADS
     const T *kt = sm.k[nth % BUF], *vt = sm.v[nth % BUF];
 #pragma unroll
     for (int n = 0; n < NS; ++n) {
-      const f32x16 s = P::scores(kt + 32 * n * D, q, lane), dp = P::scores(vt + 32 * n * D, g, lane);
+      if (OWN) loads_left<L::loads(W)>();
+      const f32x16 dp = P::scores(vt + 32 * n * D, g, lane);
+      if (OWN && t + S < n_tiles) {
+        tile_read();
+        load_values(t + S, nth + 1);
+        loads_left<L::loads(W)>();
+      } else if (OWN) {
+        loads_left<0>();
+      }
+      const f32x16 s = P::scores(kt + 32 * n * D, q, lane);
       float ds[16];
 #pragma unroll
       for (int r = 0; r < 16; ++r) ds[r] = __builtin_amdgcn_exp2f(fmaf(s[r], sc, -lse)) * (dp[r] - delta);
@@ -138,20 +155,28 @@ template <typename T, int D, typename F> __global__ __launch_bounds__(F::THREADS
       else P::product(dq, kt + 32 * n * D, w, lane);
       if (!by_rows && mask) odd = odd || L::odd(kt + 32 * n * D, lane);
     }
+    if (OWN && t + S < n_tiles) {
+      tile_read();
+      load_keys(t + S, nth + 1);
+    }
   };
   auto pass = [&](auto by_rows) {
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
       for (int r = 0; r < 16; ++r) dq[mt][r] = 0.f;
-    for (int n = 0; n < BUF - 1; ++n)
+    for (int n = 0; n < (OWN ? 1 : BUF - 1); ++n)
       if (stream + S * n < n_tiles) load(stream + S * n, n);
-    for (int t = stream, n = 0; t - stream < n_tiles; t += S, ++n) {   // the streams meet at every barrier
-      if (BUF > 2 && t + S < n_tiles) loads_left<2 * L::loads(W)>();
-      else loads_left<0>();
-      lds_barrier();   // tile n is there, and nobody reads tile n - 1 any more
-      if (t + (BUF - 1) * S < n_tiles) load(t + (BUF - 1) * S, n + BUF - 1);
-      if (t < n_tiles && t * R <= min(q0 + 31, nq - 1) + off) sums(t, n, by_rows);   // else nothing for this wave
+    if constexpr (OWN) {
+      for (int t = stream; t < n_tiles; t += S) sums(t, 0, by_rows);
+    } else {
+      for (int t = stream, n = 0; t - stream < n_tiles; t += S, ++n) {   // the streams meet at every barrier
+        if (BUF > 2 && t + S < n_tiles) loads_left<2 * L::loads(W)>();
+        else loads_left<0>();
+        lds_barrier();   // tile n is there, and nobody reads tile n - 1 any more
+        if (t + (BUF - 1) * S < n_tiles) load(t + (BUF - 1) * S, n + BUF - 1);
+        if (t < n_tiles && t * R <= min(q0 + 31, nq - 1) + off) sums(t, n, by_rows);   // else nothing for this wave
+      }
     }
     lds_barrier();   // every wave is done with the tiles
   };
@@ -332,8 +357,8 @@ template <typename T, int D> __global__ __launch_bounds__(256) void packed_add_k
   Products<T, D>::put4(to + c, x[0], x[1], x[2], x[3]);
 }
 
-template <typename T, int D, bool SPLIT> hipError_t launch_dq(const PackedArgs& a, hipStream_t s) {
-  using F = typename DqShape_<T, D, SPLIT>::type;
+template <typename T, int D, int STREAMS> hipError_t launch_dq(const PackedArgs& a, hipStream_t s) {
+  using F = typename DqShape_<T, D, STREAMS>::type;
   constexpr size_t smem = std::max(sizeof(DqTiles<T, D, F>), F::ROWS * kPutRow<T, D> * sizeof(T));   // the rows leave through it
   auto kern = packed_dq_kernel<T, D, F>;
   if (hipError_t e = allow_lds(kern, smem); e != hipSuccess) return e;
@@ -354,14 +379,19 @@ template <typename T, int D, bool SPLIT> hipError_t launch_dkdv(const PackedArgs
   packed_add_kernel<T, D><<<dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s>>>(a, groups);
   return hipGetLastError();
 }
-// As in the forward pass; the workgroups of dk and dv fill a compute unit each in either form.
 template <typename T, int D> hipError_t launch(const PackedArgs& a, hipStream_t s) {
-  const int units = device_compute_units(), groups = packed_head_groups(a.total_k, a.n_seqs, a.H, a.Hkv);
-  const bool dq_split = packed_splits(a.total_q, a.H, a.n_seqs, units / (sizeof(T) == 2 && D == 128 ? 2 : 1));
-  const hipError_t e = dq_split ? launch_dq<T, D, true>(a, s) : launch_dq<T, D, false>(a, s);
+  hipError_t e;
+  switch (packed_streams(sizeof(T) == 4, D, a.total_q, a.H, a.n_seqs)) {
+    case 1: e = launch_dq<T, D, 1>(a, s); break;
+    case 2: if constexpr (sizeof(T) == 4 && D == 128) { e = launch_dq<T, D, 2>(a, s); break; }
+    default: e = launch_dq<T, D, 4>(a, s);
+  }
   if (e != hipSuccess) return e;
-  const bool split = packed_splits(a.total_k, a.Hkv * groups, a.n_seqs, units);
-  return split ? launch_dkdv<T, D, true>(a, groups, s) : launch_dkdv<T, D, false>(a, groups, s);
+  const int groups = packed_head_groups(a.total_k, a.n_seqs, a.H, a.Hkv);
+  // as there, but in either form a workgroup fills a compute unit
+  int most = device_compute_units();
+  if (a.total_k < (int64_t)512 * a.n_seqs) most /= 2;
+  return (int64_t)a.total_k * a.Hkv * groups <= (int64_t)most * kPackedRows ? launch_dkdv<T, D, true>(a, groups, s) : launch_dkdv<T, D, false>(a, groups, s);
 }
 
 }  // namespace

@@ -2,7 +2,8 @@
 // running maximum and sum per query.
 //
 // A workgroup holds up to 128 queries of one head, 32 a wave, and streams key and value tiles through two LDS buffers: the
-// next tile's rows arrive while the present one is used.
+// next tile's rows arrive while the present one is used.  In calls of few rows it holds 32 queries, whose waves take every
+// fourth tile, each with one buffer of its own and no barrier.
 #include "packed.hpp"
 
 #include <algorithm>
@@ -10,13 +11,17 @@
 namespace gformer {
 namespace {
 
-// One stream where there are workgroups enough.  SPLIT: a few rows a workgroup, its waves on different keys.
-template <typename T, int D, bool SPLIT> struct FwdShape_;
-template <typename T, int D> struct FwdShape_<T, D, false> {
+// One stream where there are workgroups enough, else a few rows a workgroup and its waves on different keys: four of them, or two
+// (fp32, d = 128 only, whose four take a compute unit's LDS).
+template <typename T, int D, int STREAMS> struct FwdShape_;
+template <typename T, int D> struct FwdShape_<T, D, 1> {
   using type = Shape<4, 1, sizeof(T) == 2 ? 64 : 32, 2, sizeof(T) == 4 && D == 128 ? 1 : D == 64 ? 3 : 2>;
 };
-template <typename T, int D> struct FwdShape_<T, D, true> {
-  using type = std::conditional_t<sizeof(T) == 4 && D == 128, Shape<2, 2, 32, 2, 1>, Shape<1, 4, 32, 2, sizeof(T) == 2 && D == 64 ? 2 : 1>>;
+template <typename T, int D> struct FwdShape_<T, D, 2> {
+  using type = Shape<2, 2, 32, 2, 1>;
+};
+template <typename T, int D> struct FwdShape_<T, D, 4> {
+  using type = Shape<1, 4, 32, 1, sizeof(T) == 4 && D == 128 ? 1 : 2>;
 };
 template <typename T, int D, typename F> struct alignas(256) FwdTiles {
   struct { T k[F::BUF][F::R * D], v[F::BUF][F::R * D]; } stream[F::S];
@@ -64,18 +69,25 @@ template <typename T, int D, typename F> __global__ __launch_bounds__(F::THREADS
   const T* vp = rows_of<T>(a.v, a.vs, kbase, kvh);
   const int last_key = min(i0 + ROWS, nq) - 1 + off;   // of the workgroup; < 0: no query sees any
   const int n_tiles = last_key < 0 ? 0 : last_key / R + 1;
-  auto load = [&](int t, int n) {   // tile t, the stream's n-th
-    L::template load<W>(sm.k[n % F::BUF], kp, a.ks[0], t * R, nk - 1, wave, lane);
-    L::template load<W>(sm.v[n % F::BUF], vp, a.vs[0], t * R, nk - 1, wave, lane);
-  };
+  // tile t, the stream's n-th
+  auto load_keys = [&](int t, int n) { L::template load<W>(sm.k[n % F::BUF], kp, a.ks[0], t * R, nk - 1, wave, lane); };
+  auto load_values = [&](int t, int n) { L::template load<W>(sm.v[n % F::BUF], vp, a.vs[0], t * R, nk - 1, wave, lane); };
+  // One buffer: the wave's own, whose next keys arrive while it weights the values, and the other way round.
+  constexpr bool OWN = F::BUF == 1;
+  static_assert(!OWN || W == 1);
   bool odd = false;
   auto attend = [&](int t, int nth, auto by_rows) {
     const int t0 = t * R;
     const bool mask = t0 + R - 1 > q0 + off;   // some query of the wave does not see the whole tile
     const T *kt = sm.k[nth % F::BUF], *vt = sm.v[nth % F::BUF];
     f32x16 s[NS];
+    if (OWN) loads_left<L::loads(W)>();
 #pragma unroll
     for (int n = 0; n < NS; ++n) s[n] = P::scores(kt + 32 * n * D, q, lane);
+    if (OWN && t + S < n_tiles) {
+      tile_read();
+      load_keys(t + S, nth + 1);
+    }
     if (mask) {
 #pragma unroll
       for (int n = 0; n < NS; ++n)
@@ -99,6 +111,10 @@ template <typename T, int D, typename F> __global__ __launch_bounds__(F::THREADS
         for (int r = 0; r < 16; ++r) o[mt][r] *= by;
     }
     const float ref = m == -INFINITY ? 0.f : m;
+    if (OWN) {
+      if (t + S < n_tiles) loads_left<L::loads(W)>();
+      else loads_left<0>();
+    }
 #pragma unroll
     for (int n = 0; n < NS; ++n) {
       float p[16];
@@ -112,6 +128,10 @@ template <typename T, int D, typename F> __global__ __launch_bounds__(F::THREADS
       else P::product(o, vt + 32 * n * D, w, lane);
       if (!by_rows && mask) odd = odd || L::odd(vt + 32 * n * D, lane);
     }
+    if (OWN && t + S < n_tiles) {
+      tile_read();
+      load_values(t + S, nth + 1);
+    }
   };
   auto pass = [&](auto by_rows) {
 #pragma unroll
@@ -120,12 +140,22 @@ template <typename T, int D, typename F> __global__ __launch_bounds__(F::THREADS
       for (int r = 0; r < 16; ++r) o[mt][r] = 0.f;
     m = -INFINITY;
     l = 0.f;
-    if (stream < n_tiles) load(stream, 0);
-    for (int t = stream, n = 0; t - stream < n_tiles; t += S, ++n) {   // the streams meet at every barrier
-      loads_left<0>();
-      lds_barrier();   // tile n is there, and nobody reads tile n - 1 any more
-      if (t + S < n_tiles) load(t + S, n + 1);
-      if (t < n_tiles && t * R <= min(q0 + 31, nq - 1) + off) attend(t, n, by_rows);   // else nothing for this wave
+    if (stream < n_tiles) {
+      load_keys(stream, 0);
+      load_values(stream, 0);
+    }
+    if constexpr (OWN) {
+      for (int t = stream; t < n_tiles; t += S) attend(t, 0, by_rows);
+    } else {
+      for (int t = stream, n = 0; t - stream < n_tiles; t += S, ++n) {   // the streams meet at every barrier
+        loads_left<0>();
+        lds_barrier();   // tile n is there, and nobody reads tile n - 1 any more
+        if (t + S < n_tiles) {
+          load_keys(t + S, n + 1);
+          load_values(t + S, n + 1);
+        }
+        if (t < n_tiles && t * R <= min(q0 + 31, nq - 1) + off) attend(t, n, by_rows);   // else nothing for this wave
+      }
     }
     lds_barrier();   // every wave is done with the tiles
   };
@@ -180,8 +210,8 @@ template <typename T, int D, typename F> __global__ __launch_bounds__(F::THREADS
   }
 }
 
-template <typename T, int D, bool SPLIT> hipError_t launch(const PackedArgs& a, hipStream_t s) {
-  using F = typename FwdShape_<T, D, SPLIT>::type;
+template <typename T, int D, int STREAMS> hipError_t launch(const PackedArgs& a, hipStream_t s) {
+  using F = typename FwdShape_<T, D, STREAMS>::type;
   constexpr size_t smem = std::max(sizeof(FwdTiles<T, D, F>), F::ROWS * kPutRow<T, D> * sizeof(T));   // the rows leave through it
   auto kern = packed_fwd_kernel<T, D, F>;
   if (hipError_t e = allow_lds(kern, smem); e != hipSuccess) return e;
@@ -189,15 +219,30 @@ template <typename T, int D, bool SPLIT> hipError_t launch(const PackedArgs& a, 
   kern<<<dim3((unsigned)(tiles * a.H)), dim3(F::THREADS), smem, s>>>(a, (int)tiles);
   return hipGetLastError();
 }
-// us, one stream against split, us (rows x heads): bf16, d = 64: 2048 x 8 35 / 19, 2048 x 16 37 / 29, 2048 x 32 39 / 49, 8 of 200 x 16 10 / 14;
-// d = 128, whose split workgroups are alone on a compute unit: 512 x 8 17 / 13, 2048 x 8 50 / 37, 512 x 32 18 / 22, 2048 x 16 53 / 70;
-// fp32, d = 64: 2048 x 8 157 / 63, 2048 x 16 162 / 116, 2048 x 32 216 / 234; d = 128: 2048 x 16 300 / 181, 2048 x 32 336 / 355.
+// us, one stream / two / four (rows x heads): bf16, d = 64: 2048 x 8 35 / - / 19, 2048 x 16 37 / - / 24, 4096 x 16 67 / - / 65, 4000 x 12 67 / - / 52,
+// 2048 x 32 38 / - / 39, 8 of 200 x 16 10 / - / 12; d = 128: 512 x 8 17 / - / 12, 2048 x 8 50 / - / 27, 512 x 32 18 / - / 13, 2048 x 16 52 / - / 41,
+// 4000 x 12 95 / - / 90, 4096 x 16 101 / - / 120; fp32, d = 64: 2048 x 8 157 / - / 63, 2048 x 16 162 / - / 98, 4096 x 16 415 / - / 317, 4096 x 32 578 / - / 577;
+// d = 128: 1024 x 16 - / 85 / 65, 2048 x 8 - / 161 / 106, 2048 x 16 300 / 178 / 209, 4000 x 12 570 / 523 / 548, 4096 x 16 633 / 650 / -.
 template <typename T, int D> hipError_t launch(const PackedArgs& a, hipStream_t s) {
-  const int limit = device_compute_units() / (sizeof(T) == 2 && D == 128 ? 2 : 1);
-  return packed_splits(a.total_q, a.H, a.n_seqs, limit) ? launch<T, D, true>(a, s) : launch<T, D, false>(a, s);
+  switch (packed_streams(sizeof(T) == 4, D, a.total_q, a.H, a.n_seqs)) {
+    case 1: return launch<T, D, 1>(a, s);
+    case 2: if constexpr (sizeof(T) == 4 && D == 128) return launch<T, D, 2>(a, s);
+    default: return launch<T, D, 4>(a, s);
+  }
 }
 
 }  // namespace
+
+// Streams divide the longest workgroup's time, and load every streamed row as many times more often.  Four of them leave room for
+// two workgroups on a compute unit (fp32, d = 128: one), so up to two rounds of the unsplit workgroups are better split; at
+// d = 128, whose values cost more to join, one and a half; a quarter of that where sequences are short (a mean of less than
+// 512 rows) and the joins weigh more.
+int packed_streams(bool fp32, int d, int total_q, int H, int n_seqs) {
+  const int units = device_compute_units();
+  const int64_t workgroups = (int64_t)total_q * H / kPackedRows, most = units * (d == 64 ? 4 : 3) / 2;
+  if (workgroups > (total_q < (int64_t)512 * n_seqs ? most / 4 : most)) return 1;
+  return fp32 && d == 128 && workgroups > units / 2 ? 2 : 4;
+}
 
 hipError_t launch_packed_fwd(const PackedArgs& a, bool bf16, hipStream_t s) {
   if (bf16) return a.d == 128 ? launch<uint16_t, 128>(a, s) : launch<uint16_t, 64>(a, s);

@@ -173,6 +173,23 @@ def test_many_heads(dtype, d, H, Hkv, lens_q, lens_k):
 
 
 @gpu
+@pytest.mark.parametrize("lens_q,lens_k", [([600], [600]), ([513, 555], [1100, 400])])
+def test_single_precision_in_two_streams(lens_q, lens_k):
+    """d = 128, with more workgroups than compute units can hold of four streams each; a key that some rows do not see is no number."""
+    q, k, v, g = tensors(lens_q, lens_k, 32, 8, 128, "f32", 71, layout="heads")
+    want = ref.packed(q, k, v, g, lens_q, lens_k, 0.1, "f32")
+    got = run(q, k, v, g, lens_q, lens_k, 0.1)
+    compare(got, want, lens_q, lens_k)
+    k, v = k.clone(), v.clone()
+    last = lens_k[0] - 1                       # the first sequence's last key: its last query alone sees it
+    k[last], v[last] = float("nan"), float("inf")
+    bad = run(q, k, v, g, lens_q, lens_k, 0.1)
+    rows = [i for i in range(sum(lens_q)) if i != lens_q[0] - 1]
+    assert torch.equal(bad["out"][rows], got["out"][rows]) and torch.equal(bad["dq"][rows], got["dq"][rows])
+    assert bad["out"][lens_q[0] - 1].isnan().all()
+
+
+@gpu
 @pytest.mark.parametrize("d", [64, 128])
 def test_what_rounding_takes_from_the_output(d):
     """out + rest is the output before its rounding, up to rest's own; dq and dk then come nearer to the formula's."""
