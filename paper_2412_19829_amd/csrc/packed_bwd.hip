@@ -3,6 +3,13 @@
 //   dq      queries resident, keys and values streamed; also leaves both statistics of a query for the other pass
 //   dk, dv  keys resident, the queries of every head that shares them streamed, one head after another: their sums
 //           need no atomics, and come out in one order
+// One pass for all three would save two of nine products and need atomics, whose order changes the sums.
+//
+// Bound like the forward pass.  4096 + 3001 + 1095 tokens, 32 / 8 heads, d = 128, bf16: dq 375 us, dk and dv 607 (matrix units busy 47 and
+// 39 %, waves waiting 31 and 44 %: dk and dv leave one workgroup of eight waves on a compute unit); 8192 tokens in 8 documents, 16 heads,
+// d = 64: 63 and 111; fp32, 1024 + 300 + 700 tokens, 12 heads, d = 64: 57 and 83.  What did not help: two blocks of 32 rows a wave
+// (d = 64: dq 64 -> 91), three workgroups' worth of registers (dk, dv 111 -> 114 to 187), wave priorities (607 -> 627 and more), and all
+// transposed reads of a product in one statement (d = 128 spills: 852).
 #include "packed.hpp"
 
 #include <algorithm>
@@ -344,7 +351,8 @@ template <typename T, int D, typename F> __global__ __launch_bounds__(F::THREADS
   }
 }
 
-// dk and dv of the sequences' rows from the sums of every part of the heads, four columns a thread.
+// dk and dv of the sequences' rows from the sums of every part of the heads, four columns a thread.  Bound by memory, and small:
+// the heads are parted only where there are few rows (at most 128 a compute unit, of all key heads).
 template <typename T, int D> __global__ __launch_bounds__(256) void packed_add_kernel(PackedArgs a, int groups) {
   constexpr int C = D / 4;
   const int64_t unit = ((int64_t)blockIdx.x * 256 + threadIdx.x) / C;   // (row, head), dk's and then dv's

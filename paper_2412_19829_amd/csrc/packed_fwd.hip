@@ -4,6 +4,12 @@
 // A workgroup holds up to 128 queries of one head, 32 a wave, and streams key and value tiles through two LDS buffers: the
 // next tile's rows arrive while the present one is used.  In calls of few rows it holds 32 queries, whose waves take every
 // fourth tile, each with one buffer of its own and no barrier.
+//
+// Bound by the matrix units and the vector work between the products of a tile (exponentials, the maximum, packing of the weights):
+// 8192 tokens, 32 / 8 heads, d = 128, bf16 549 us, 1.0 PFLOP/s where a plain product of 8192 x 8192 matrices reaches 1.32; the matrix
+// units are busy 49 % of the time, the waves wait 24 %, LDS conflicts 1 % of its cycles.  fp32, 4096 tokens, 32 / 8 heads, d = 64:
+// 577 us, 119 TFLOP/s of 154.  Two blocks of 32 queries a wave halve the reads of LDS and cost a workgroup (d = 64, 49 -> 66 us);
+// raised wave priorities around the products cost 7 %.
 #include "packed.hpp"
 
 #include <algorithm>

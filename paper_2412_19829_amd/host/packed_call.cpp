@@ -1,6 +1,6 @@
 // The host sides of the packed and paged calls, for the functions of the same names in binding.py: checking and marshalling in
 // Python takes 10 to 15 us a call, and the smallest ones 3 to 9 us on the device (a prompt of 128 tokens of 12 heads and its way
-// into the cache: 31 us among others, 12 with this; a token of one user over 2047: 26 and 12).
+// into the cache: 31 us among others, 9 with this; a token of one user over 2047: 26 and 9).
 //
 // Every function takes the library's entry points by address, the binding's arguments and the stream (or None), and returns
 // the gf_status of the call, or None for anything that is not the plain, well-formed call: wrapped tensors, shapes, types or
