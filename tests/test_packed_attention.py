@@ -456,3 +456,39 @@ def test_the_wrapper_refuses():
                 (q[:4], k, v, cu([4])), (q, k, v, cu([8]), cu([8, 0])), (q[0], k, v, cu([8]))):
         with pytest.raises((ValueError, gb.GformerError)):
             gformer_packed_attention(*bad)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_captured_training_step(dtype):
+    from paper_2412_19829_amd.autograd import gformer_packed_attention
+    lens = [70, 1, 200]
+    q, k, v, g = tensors(lens, lens, 8, 2, 64, dtype, 41, tail=9)
+    offs = cu(lens)
+    leaves = [x.clone().requires_grad_(True) for x in (q, k, v)]
+
+    def step():
+        out = gformer_packed_attention(*leaves, offs, softmax_scale=0.125)
+        return [out.detach(), *torch.autograd.grad(out, leaves, g)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        want = [x.clone() for x in step()]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        got = step()
+    for i in range(3):
+        for x in got:
+            x.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), i
+        assert all(torch.equal(a, b) for a, b in zip(step(), want)), i   # the program's own, between the replays
+    # other values in the same places
+    with torch.no_grad():
+        for x in leaves:
+            x.mul_(0.5)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, step()))
