@@ -6,9 +6,9 @@
 // One pass for all three would save two of nine products and need atomics, whose order changes the sums.
 //
 // Bound like the forward pass.  4096 + 3001 + 1095 tokens, 32 / 8 heads, d = 128, bf16: dq 375 us, dk and dv 607 (matrix units busy 47 and
-// 39 %, waves waiting 31 and 44 %: dk and dv leave one workgroup of eight waves on a compute unit); 8192 tokens in 8 documents, 16 heads,
-// d = 64: 63 and 111; fp32, 1024 + 300 + 700 tokens, 12 heads, d = 64: 57 and 83.  What did not help: two blocks of 32 rows a wave
-// (d = 64: dq 64 -> 91), three workgroups' worth of registers (dk, dv 111 -> 114 to 187), wave priorities (607 -> 627 and more), and all
+// 39 %, waves waiting 31 and 44 %: dk and dv are one workgroup of eight waves on a compute unit there); 8192 tokens in 8 documents, 16 heads,
+// d = 64: 63 and 93; fp32, 1024 + 300 + 700 tokens, 12 heads, d = 64: 57 and 83.  What did not help: two blocks of 32 rows a wave
+// (d = 64: dq 64 -> 91), three waves on a SIMD (dk, dv of the second 114 to 187 where two took 111), wave priorities (607 -> 627 and more), and all
 // transposed reads of a product in one statement (d = 128 spills: 852).
 #include "packed.hpp"
 
@@ -37,12 +37,17 @@ template <typename T, int D, typename F> struct alignas(256) DqTiles {
 };
 
 // dk, dv: a causal sequence's first keys are seen by all its queries, its last by few, and there are only as many workgroups
-// as key tiles and key heads: the longest one decides, and with two streams it takes half as long.
-template <typename T, int D, bool SPLIT> struct KeyShape_;
-template <typename T, int D> struct KeyShape_<T, D, false> {
+// as key tiles and key heads.  MANY: one stream, two workgroups on a compute unit, neither of which waits for the other.  SOME: the
+// longest workgroup decides, and with two streams and a compute unit of its own it takes half as long.  FEW: shorter ones yet.
+enum { MANY, SOME, FEW };
+template <typename T, int D, int CALL> struct KeyShape_;
+template <typename T, int D> struct KeyShape_<T, D, MANY> {
+  using type = Shape<4, 1, sizeof(T) == 2 && D == 64 ? 64 : 32, sizeof(T) == 2 && D == 128 ? 2 : 3, kWaves<T, D>>;
+};
+template <typename T, int D> struct KeyShape_<T, D, SOME> {
   using type = Shape<4, kWaves<T, D>, sizeof(T) == 2 && D == 64 ? 64 : 32, 3, kWaves<T, D>>;
 };
-template <typename T, int D> struct KeyShape_<T, D, true> {
+template <typename T, int D> struct KeyShape_<T, D, FEW> {
   using type = Shape<2, 2 * kWaves<T, D>, 32, 2, kWaves<T, D>>;
 };
 // its value rows stay in LDS where their registers are wanted for the sums
@@ -374,8 +379,8 @@ template <typename T, int D, int STREAMS> hipError_t launch_dq(const PackedArgs&
   kern<<<dim3((unsigned)(tiles * a.H)), dim3(F::THREADS), smem, s>>>(a, (int)tiles);
   return hipGetLastError();
 }
-template <typename T, int D, bool SPLIT> hipError_t launch_dkdv(const PackedArgs& a, int groups, hipStream_t s) {
-  using F = typename KeyShape_<T, D, SPLIT>::type;
+template <typename T, int D, int CALL> hipError_t launch_dkdv(const PackedArgs& a, int groups, hipStream_t s) {
+  using F = typename KeyShape_<T, D, CALL>::type;
   constexpr size_t smem = std::max(sizeof(KeyTiles<T, D, F>), F::ROWS * kPutRow<float, D> * sizeof(float));
   auto kern = packed_dkdv_kernel<T, D, F>;
   if (hipError_t e = allow_lds(kern, smem); e != hipSuccess) return e;
@@ -387,6 +392,9 @@ template <typename T, int D, bool SPLIT> hipError_t launch_dkdv(const PackedArgs
   packed_add_kernel<T, D><<<dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s>>>(a, groups);
   return hipGetLastError();
 }
+// dk, dv in two streams / one, us of the whole pass (keys x key heads): bf16, d = 64: 4 of 1000 x 32 118 / 104, 16 of 100 x 32 38 / 30, 4096 x 16 175 / 202,
+// 8 of 200 x 16 34 / 36; d = 128: 4 of 1000 x 32 205 / 182, 16 of 100 x 32 61 / 49, 4096 x 16 304 / 346; fp32, d = 64: 4 of 1000 x 32 583 / 579,
+// 16 of 100 x 32 103 / 88, 4096 x 16 1016 / 1213.
 template <typename T, int D> hipError_t launch(const PackedArgs& a, hipStream_t s) {
   hipError_t e;
   switch (packed_streams(sizeof(T) == 4, D, a.total_q, a.H, a.n_seqs)) {
@@ -396,10 +404,11 @@ template <typename T, int D> hipError_t launch(const PackedArgs& a, hipStream_t 
   }
   if (e != hipSuccess) return e;
   const int groups = packed_head_groups(a.total_k, a.n_seqs, a.H, a.Hkv);
-  // as there, but in either form a workgroup fills a compute unit
-  int most = device_compute_units();
-  if (a.total_k < (int64_t)512 * a.n_seqs) most /= 2;
-  return (int64_t)a.total_k * a.Hkv * groups <= (int64_t)most * kPackedRows ? launch_dkdv<T, D, true>(a, groups, s) : launch_dkdv<T, D, false>(a, groups, s);
+  const int units = device_compute_units();
+  const bool brief = a.total_k < (int64_t)512 * a.n_seqs;   // short sequences have no long workgroups
+  const int64_t workgroups = (int64_t)a.total_k * a.Hkv * groups / kPackedRows;
+  if (workgroups <= (brief ? units / 2 : units)) return launch_dkdv<T, D, FEW>(a, groups, s);
+  return workgroups > (brief ? units : 3 * units) ? launch_dkdv<T, D, MANY>(a, groups, s) : launch_dkdv<T, D, SOME>(a, groups, s);
 }
 
 }  // namespace

@@ -162,7 +162,7 @@ def test_values_and_gradients(dtype, d, H, Hkv, shape):
 @gpu
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("d", [64, 128])
-@pytest.mark.parametrize("H,Hkv", [(64, 64), (128, 32)])
+@pytest.mark.parametrize("H,Hkv", [(64, 64), (128, 32), (128, 128)])
 @pytest.mark.parametrize("lens_q,lens_k", [([127, 129, 64, 33], None), ([1, 140, 0, 130], [77, 140, 9, 257]), ([20, 240, 3], [5, 0, 200])])
 def test_many_heads(dtype, d, H, Hkv, lens_q, lens_k):
     """Enough workgroups for the kernels whose waves share the streamed rows (those above have waves on different ones)."""
