@@ -402,7 +402,7 @@ template <typename T, int D> hipError_t launch(const PackedArgs& a, hipStream_t 
     case 2: if constexpr (sizeof(T) == 4 && D == 128) { e = launch_dq<T, D, 2>(a, s); break; }
     default: e = launch_dq<T, D, 4>(a, s);
   }
-  if (e != hipSuccess) return e;
+  if (e != hipSuccess || a.total_k == 0) return e;
   const int groups = packed_head_groups(a.total_k, a.n_seqs, a.H, a.Hkv);
   const int units = device_compute_units();
   const bool brief = a.total_k < (int64_t)512 * a.n_seqs;   // short sequences have no long workgroups
