@@ -38,12 +38,12 @@ hipError_t launch_packed_fwd(const PackedArgs& a, bool bf16, hipStream_t s);
 hipError_t launch_packed_bwd(const PackedArgs& a, bool bf16, hipStream_t s);
 // What the backward pass keeps beside a query's statistics: the query heads of a key head in `groups` parts, whose dk and dv
 // are added up by a kernel of their own (1: there is none).
-int packed_head_groups(int total_k, int n_seqs, int H, int Hkv);
+int packed_head_groups(int total_k, int H, int Hkv);
 // The streams of the passes that hold queries (packed_fwd.hip has the figures).
 int packed_streams(bool fp32, int d, int total_q, int H, int n_seqs);
 inline size_t packed_stats_bytes(int total_q, int H) { return ((size_t)total_q * H * 2 * sizeof(float) + 255) / 256 * 256; }
-inline size_t packed_sums_bytes(int total_k, int n_seqs, int H, int Hkv, int d) {
-  const int groups = packed_head_groups(total_k, n_seqs, H, Hkv);
+inline size_t packed_sums_bytes(int total_k, int H, int Hkv, int d) {
+  const int groups = packed_head_groups(total_k, H, Hkv);
   return groups == 1 ? 0 : (size_t)groups * total_k * Hkv * d * 2 * sizeof(float);
 }
 

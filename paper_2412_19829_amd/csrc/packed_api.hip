@@ -166,7 +166,7 @@ size_t gformer_packed_attn_bwd_workspace_bytes(int total_q, int total_k, int n_s
                                                const gformer_packed_params* p) {
   PackedArgs a;
   if (check_packed(n_seqs, total_q, total_k, H, Hkv, d, p, &a) != GF_OK) return 0;
-  return packed_stats_bytes(total_q, H) + packed_sums_bytes(total_k, n_seqs, H, Hkv, d);
+  return packed_stats_bytes(total_q, H) + packed_sums_bytes(total_k, H, Hkv, d);
 }
 
 gf_status gformer_packed_attn_bwd(const void* q, const void* k, const void* v, const void* out, const void* out_rest,

@@ -403,7 +403,7 @@ template <typename T, int D> hipError_t launch(const PackedArgs& a, hipStream_t 
     default: e = launch_dq<T, D, 4>(a, s);
   }
   if (e != hipSuccess || a.total_k == 0) return e;
-  const int groups = packed_head_groups(a.total_k, a.n_seqs, a.H, a.Hkv);
+  const int groups = packed_head_groups(a.total_k, a.H, a.Hkv);
   const int units = device_compute_units();
   const bool brief = a.total_k < (int64_t)512 * a.n_seqs;   // short sequences have no long workgroups
   const int64_t workgroups = (int64_t)a.total_k * a.Hkv * groups / kPackedRows;
@@ -414,14 +414,18 @@ template <typename T, int D> hipError_t launch(const PackedArgs& a, hipStream_t 
 }  // namespace
 
 // Where key heads are few, the workgroups that walk all query heads of one are few and long: the heads are parted until
-// there is a workgroup for every compute unit.
-int packed_head_groups(int total_k, int n_seqs, int H, int Hkv) {
+// there is a workgroup for every compute unit.  Parts divide a group evenly; where the next number of them that does would make
+// more than four for every compute unit (seven heads, say, and nearly enough rows), whose sums cost more than idle units, it is not taken.
+int packed_head_groups(int total_k, int H, int Hkv) {
   const int G = H / Hkv;
-  const int64_t units = (int64_t)device_compute_units() * kPackedRows;
+  const int64_t rows = (int64_t)total_k * Hkv, enough = (int64_t)device_compute_units() * kPackedRows;
   int groups = 1;
-  while (groups < G && (int64_t)total_k * Hkv * groups < units)
-    do ++groups;
-    while (G % groups != 0);
+  while (groups < G && rows * groups < enough) {
+    int next = groups + 1;
+    while (G % next != 0) ++next;
+    if (rows * next > 4 * enough) break;
+    groups = next;
+  }
   return groups;
 }
 

@@ -507,3 +507,13 @@ def test_calls_with_nothing_to_do(lens_q, lens_k, tail, node, monkeypatch):
     grads = torch.autograd.grad(out, leaves, g)
     assert out.shape == q.shape and all(a.shape == b.shape for a, b in zip(grads, leaves))
     assert not out.any() and not any(x.any() for x in grads)
+
+
+def test_the_backward_workspace_stays_bounded():
+    """Parts of the query heads never take more sums than four 128-row workgroups for each of a card's compute units hold."""
+    for H, Hkv in ((127, 1), (7, 1), (28, 4), (64, 1), (1024, 1), (48, 2), (16, 16)):
+        for total in (1, 100, 5000, 20000, 40000, 1 << 20):
+            for d in (64, 128):
+                p = gb.make_packed_params()
+                sums = gb.gformer_packed_attn_bwd_workspace_bytes(0, total, 1, H, Hkv, d, p)
+                assert sums <= 4 * 512 * 128 * d * 8
