@@ -335,6 +335,16 @@ template <int D> struct Products<uint16_t, D> {
     }
     return w;
   }
+  // what rounding took from them
+  static __device__ __forceinline__ Weights rests(const float (&p)[16], const Weights& w) {
+    float x[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const uint32_t y = as_u32x4(w.x[i / 8])[i % 8 / 2];
+      x[i] = p[i] - (i % 2 ? bf16_hi(y) : bf16_lo(y));
+    }
+    return weights(x);
+  }
   // acc += rows^T weights
   static __device__ __forceinline__ void product(f32x16 (&acc)[D / 32], const T* rows, const Weights& w, int lane) {
     const uint32_t at = lds_lane(rows, turned_at(lane));

@@ -3,11 +3,15 @@
 //   dq      queries resident, keys and values streamed; also leaves both statistics of a query for the other pass
 //   dk, dv  keys resident, the queries of every head that shares them streamed, one head after another: their sums
 //           need no atomics, and come out in one order
+// The gradients of the scores are rounded to bf16 for their products, which costs dq and dk as much as their own rounding, and
+// more where a row has few keys and a few weights decide.  In tiles that some rows see in part, short sequences' all, both
+// parts of them go in: the value rounded, and what that took (the error of dq and dk over that of one rounding, 70 batches of 1 to 20
+// sequences: 1.43 to 1.51 without, 1.05 to 1.34 with; dq and dk, dv at d = 64 66 and 94 us in place of 64 and 92).
 // One pass for all three would save two of nine products and need atomics, whose order changes the sums.
 //
 // Bound like the forward pass.  4096 + 3001 + 1095 tokens, 32 / 8 heads, d = 128, bf16: dq 375 us, dk and dv 607 (matrix units busy 47 and
 // 39 %, waves waiting 31 and 44 %: dk and dv are one workgroup of eight waves on a compute unit there); 8192 tokens in 8 documents, 16 heads,
-// d = 64: 63 and 93; fp32, 1024 + 300 + 700 tokens, 12 heads, d = 64: 57 and 83.  What did not help: two blocks of 32 rows a wave
+// d = 64: 66 and 94; fp32, 1024 + 300 + 700 tokens, 12 heads, d = 64: 57 and 83.  What did not help: two blocks of 32 rows a wave
 // (d = 64: dq 64 -> 91), three waves on a SIMD (dk, dv of the second 114 to 187 where two took 111), wave priorities (607 -> 627 and more), and all
 // transposed reads of a product in one statement (d = 128 spills: 852).
 #include "packed.hpp"
@@ -23,13 +27,13 @@ template <typename T, int D> constexpr int kWaves = sizeof(T) == 4 && D == 128 ?
 // dq: as the forward pass
 template <typename T, int D, int STREAMS> struct DqShape_;
 template <typename T, int D> struct DqShape_<T, D, 1> {
-  using type = Shape<4, 1, sizeof(T) == 2 && D == 64 ? 64 : 32, 3, kWaves<T, D>>;
+  using type = Shape<4, 1, sizeof(T) == 2 && D == 64 ? 64 : 32, 3, sizeof(T) == 2 && D == 64 ? 3 : kWaves<T, D>>;
 };
 template <typename T, int D> struct DqShape_<T, D, 2> {
   using type = Shape<2, 2, 32, 2, 1>;
 };
 template <typename T, int D> struct DqShape_<T, D, 4> {
-  using type = Shape<1, 4, 32, 1, kWaves<T, D>>;
+  using type = Shape<1, 4, 32, 1, sizeof(T) == 2 && D == 64 ? 3 : kWaves<T, D>>;
 };
 template <typename T, int D, typename F> struct alignas(256) DqTiles {
   struct { T k[F::BUF][F::R * D], v[F::BUF][F::R * D]; } stream[F::S];
@@ -165,6 +169,12 @@ template <typename T, int D, typename F> __global__ __launch_bounds__(F::THREADS
       const typename P::Weights w = P::weights(ds);
       if (by_rows && mask && L::odd(kt + 32 * n * D, lane)) P::product_by_rows(dq, kt + 32 * n * D, w, 0, seen + 1 - t0 - 32 * n, lane);
       else P::product(dq, kt + 32 * n * D, w, lane);
+      if constexpr (sizeof(T) == 2)
+        if (mask) {   // both parts of the gradients of the scores
+          const typename P::Weights rest = P::rests(ds, w);
+          if (by_rows && L::odd(kt + 32 * n * D, lane)) P::product_by_rows(dq, kt + 32 * n * D, rest, 0, seen + 1 - t0 - 32 * n, lane);
+          else P::product(dq, kt + 32 * n * D, rest, lane);
+        }
       if (!by_rows && mask) odd = odd || L::odd(kt + 32 * n * D, lane);
     }
     if (OWN && t + S < n_tiles) {
@@ -305,6 +315,12 @@ template <typename T, int D, typename F> __global__ __launch_bounds__(F::THREADS
     const typename P::Weights wd = P::weights(ds);
     if (by_rows && mask && L::odd(qt, lane)) P::product_by_rows(dk, qt, wd, lo, hi, lane);
     else P::product(dk, qt, wd, lane);
+    if constexpr (sizeof(T) == 2)
+      if (mask) {
+        const typename P::Weights rest = P::rests(ds, wd);
+        if (by_rows && L::odd(qt, lane)) P::product_by_rows(dk, qt, rest, lo, hi, lane);
+        else P::product(dk, qt, rest, lane);
+      }
     if (!by_rows && mask) odd = odd || L::odd(qt, lane) || L::odd(gt, lane);
   };
   auto pass = [&](auto by_rows) {

@@ -208,6 +208,28 @@ def test_what_rounding_takes_from_the_output(d):
 
 
 @gpu
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("H,Hkv", [(8, 2), (128, 128)])
+def test_short_sequences_are_rounded_once(d, H, Hkv):
+    """Sequences inside one tile: both parts of the scores' gradients go into dq and dk, so that next to their own rounding, of
+    relative error r in the mean, only the weights' rounding in the forward pass is left, which delta sees through the output.
+    It puts an error of r sqrt(sum_j p_j^2 dp_j^2) into delta, and of that times p_j into every score's gradient p_j (dp_j - delta):
+    with independent values, of r sqrt(sum_j p_j^2) times a row of dq.  Scores of variance 1 have sum_j p_j^2 = e / n for n keys (0.6 for two),
+    and rows weigh as much in dq's norm; over rows of 2 to n keys the weighted mean is (0.36 + 7.4 sum 1 / n^2) / (0.6 + 2.7 sum 1 / n),
+    sums from 3: 0.44 for n = 32, 0.6 for n = 5.  So dq and dk are off by at most sqrt(1 + 0.6) = 1.27 times one rounding, and by
+    sqrt(2) and more with another one."""
+    lens = [5, 16, 31, 28, 2, 9, 32]
+    q, k, v, g = tensors(lens, lens, H, Hkv, d, "bf16", 51)
+    want = ref.packed(q, k, v, g, lens, lens, d ** -0.5, "bf16")
+    got = run(q, k, v, g, lens, lens, d ** -0.5, rest=True)
+    compare(got, want, lens, lens)
+    for name in ("dq", "dk"):
+        exact = want[name][0].double()
+        off = lambda x: float((x.double().to(exact.device) - exact).norm())
+        assert off(got[name]) < 1.27 * off(exact.to(torch.bfloat16)), name
+
+
+@gpu
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("scale", [-0.2, 0.0, 1e-42, 1.5])
 def test_scales(dtype, scale):
