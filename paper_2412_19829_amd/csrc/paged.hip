@@ -379,10 +379,12 @@ template <typename T, int D> hipError_t decode(const PagedDecodeArgs& a, hipStre
 // Six workgroups for every compute unit if all sequences were the longest, and no chunk shorter than a tile for each wave.
 // us, 512 / 1024 / 1536 / 2048 / 4096 workgroups: 32 sequences of up to 8192, 32 / 8 heads, d = 128, 88,000 keys in all 109 / 90 / 72 / 78 / 74,
 // 4 of up to 32768 84 / 88 / 88 / 91 / 94; one of 2048, 12 heads, d = 64, by chunks of 64, 128, 256, 512: 7.8 / 7.0 / 7.9 / 10.7.
+// Short of that many workgroups without a cut, a chunk is no longer than max_len (at most 2^30); from there on there is none to make.
 PagedSplit paged_split(int B, int H, int Hkv, int64_t max_len) {
-  const int64_t units = (int64_t)B * Hkv * ((H / Hkv + kPagedHeads - 1) / kPagedHeads);
-  int64_t chunk = (max_len * units + 1535) / 1536;
-  chunk = std::max<int64_t>(128, (chunk + 63) / 64 * 64);
+  constexpr int64_t kWorkgroups = 1536;
+  const int64_t units = (int64_t)B * Hkv * (((int64_t)H / Hkv + kPagedHeads - 1) / kPagedHeads);
+  const int64_t share = units < kWorkgroups ? (max_len * units + kWorkgroups - 1) / kWorkgroups : max_len;
+  const int64_t chunk = std::max<int64_t>(128, (share + 63) / 64 * 64);
   return {(int)chunk, (int)std::max<int64_t>(1, (max_len + chunk - 1) / chunk)};
 }
 

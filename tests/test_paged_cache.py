@@ -443,3 +443,51 @@ def test_the_extension_module_makes_the_plain_calls(monkeypatch):
         monkeypatch.setattr(gb, "_quick", lambda *a: False)     # the second time in Python
     assert made == [True] * 3
     assert all(torch.equal(a.view(torch.int16), b.view(torch.int16)) for a, b in zip(pages, (x["kpages"], x["vpages"])))
+
+
+# ---- calls whose sequences may be long, and whose rows are many --------------------------------------
+
+class Split(ctypes.Structure):
+    _fields_ = [("chunk", ctypes.c_int), ("splits", ctypes.c_int)]
+
+
+def test_chunks_cover_every_length():
+    """The library's own cut of a sequence, from one row to more than any launch has, and up to the longest sequence."""
+    cut = getattr(gb.lib(), "_ZN7gformer11paged_splitEiiil")
+    cut.restype, cut.argtypes = Split, [ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int64]
+    for B in (1, 2, 32, 191, 192, 193, 1535, 1536, 1537, 8192, 1 << 20, 2 ** 31 - 1):
+        for H, Hkv in ((1, 1), (8, 8), (32, 8), (40, 2), (32, 32), (2 ** 31 - 1, 1), (2 ** 31 - 1, 2 ** 31 - 1)):
+            for room in (0, 1, 63, 64, 129, 5000, 1 << 20, 1 << 24, (1 << 29) - 1, 1 << 30):
+                s = cut(B, H, Hkv, room)
+                what = (B, H, Hkv, room, s.chunk, s.splits)
+                assert 128 <= s.chunk <= max(128, -(-room // 64) * 64) and s.chunk % 64 == 0, what
+                assert s.splits >= 1 and s.chunk * s.splits >= room and s.chunk * (s.splits - 1) <= max(room - 1, 0), what
+                assert s.splits == 1 or B * Hkv * -(-(H // Hkv) // 16) * s.splits < 2 * 1536, what
+
+
+@gpu
+def test_many_rows_over_a_table_of_many_pages():
+    """Room for 2^28 tokens in each of 1600 rows of 8 key heads; three of them are in use."""
+    B, H, Hkv, d, page, width = 1600, 8, 8, 64, 65536, 4096
+    gen = torch.Generator().manual_seed(12)
+    rnd = lambda *s: torch.randn(*s, generator=gen).bfloat16()
+    lens = {0: 40, 801: 0, 1599: 700}
+    table = torch.full((B, width), -1, dtype=torch.int32, device="cuda")
+    kp, vp = (torch.full((3, Hkv, page, d), NAN, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    held = torch.full((B,), -1, dtype=torch.int32)
+    ks, vs = [], []
+    for place, (b, n) in enumerate(lens.items()):
+        table[b, 0], held[b] = 2 - place, n
+        ks.append(rnd(n, Hkv, d))
+        vs.append(rnd(n, Hkv, d))
+        kp[2 - place, :, :n], vp[2 - place, :, :n] = ks[-1].transpose(0, 1).cuda(), vs[-1].transpose(0, 1).cuda()
+    rows = list(lens)
+    x = dict(q=rnd(B, H, d).cuda(), k=rnd(B, Hkv, d).cuda(), v=rnd(B, Hkv, d).cuda(), kpages=kp, vpages=vp, table=table, lens=held.cuda())
+    got = step(x, 0.125)
+    want = expect({**x, **{n: x[n][rows] for n in "qkv"}, "lens": held[rows]}, ks, vs, 0.125, "bf16")
+    ref.check(got[rows], *want, "out")
+    idle = torch.ones(B, dtype=torch.bool)
+    idle[rows] = False
+    assert not got[idle.cuda()].any()
+    for place, (b, n) in enumerate(lens.items()):        # the new token is in its slot
+        assert torch.equal(kp[2 - place, :, n], x["k"][b]) and torch.equal(vp[2 - place, :, n], x["v"][b])
