@@ -291,7 +291,9 @@ gf_status gformer_attn_bwd(const void* q, const void* k, const void* v, const vo
  * operands of the matrix products are rounded (weights, and in the backward pass the gradients of the
  * scores).  Conventions (alignment, asynchrony, errors, the device of the stream) as at the top of this file;
  * strides are multiples of 8 elements, all-zero strides mean dense, a row (token) stride may not exceed 2^20, a
- * packed tensor 2^30 rows.
+ * packed tensor 2^30 rows.  A call that would take a launch of 2^32 threads or more (a sequence, a page or a token of a
+ * sequence takes 256 or 512 for every head, or for the heads that share a key head) gives GF_ERR_UNSUPPORTED
+ * before anything is launched.
  * Integer arrays are DEVICE pointers to int32, 4-byte aligned, and are read on the device alone: offsets,
  * lengths and page numbers out of range never make a call read or write outside the tensors it was
  * given, but what it then computes is not defined beyond what is said below.

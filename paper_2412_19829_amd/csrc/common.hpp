@@ -229,6 +229,8 @@ constexpr int kMfmaWindowRows = 128;    // query rows per workgroup, MFMA window
 constexpr int kMfmaWindowThreads = 256;
 int mfma_linear_threads(int d, int query_halves);   // of a read-out's workgroup
 int device_compute_units();   // of the current device; 256 (MI355X) in a process without one
+// Workgroups of `threads` that one launch may have: its threads are counted in 32 bits.
+constexpr int64_t most_workgroups(int threads) { return 0xffffffffll / threads; }
 // The device a call works on; an error where the stream is another one's.
 hipError_t call_device(hipStream_t s, int* dev);
 

@@ -41,6 +41,9 @@ hipError_t launch_packed_bwd(const PackedArgs& a, bool bf16, hipStream_t s);
 int packed_head_groups(int total_k, int H, int Hkv);
 // The streams of the passes that hold queries (packed_fwd.hip has the figures).
 int packed_streams(bool fp32, int d, int total_q, int H, int n_seqs);
+// Whether the launches of the passes that hold queries, and of the pass that holds keys, are within what one may have.
+bool packed_queries_fit(bool fp32, int d, int total_q, int H, int n_seqs);
+bool packed_keys_fit(bool fp32, int d, int total_k, int H, int Hkv, int n_seqs);
 inline size_t packed_stats_bytes(int total_q, int H) { return ((size_t)total_q * H * 2 * sizeof(float) + 255) / 256 * 256; }
 inline size_t packed_sums_bytes(int total_k, int H, int Hkv, int d) {
   const int groups = packed_head_groups(total_k, H, Hkv);
@@ -60,6 +63,9 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 template <int RW_, int S_, int R_, int BUF_, int PER_SIMD_> struct Shape {
   static constexpr int RW = RW_, S = S_, R = R_, BUF = BUF_, PER_SIMD = PER_SIMD_, ROWS = 32 * RW, THREADS = 64 * RW * S;
 };
+// Of a workgroup that holds queries, by its streams.
+constexpr int kQueryThreads = 256;
+constexpr int query_rows(int streams) { return kPackedRows / streams; }
 // Tiles of R rows over all sequences, none straddling two: sequence s owns tiles cu[s] / R + s up to the next
 // one's.  That is at least as many as it needs (floor(b / R) + 1 - floor(a / R) >= ceil((b - a) / R)), takes no
 // prefix sum and no look at the offsets on the host; the few tiles too many end at once.  The rows behind the last sequence

@@ -11,7 +11,6 @@ namespace gformer {
 namespace {
 
 constexpr int64_t kMaxTokenStride = 1 << 20;   // elements
-constexpr int64_t kMaxGrid = 0x7fffffff;
 constexpr int64_t kMaxCached = 1 << 30;        // tokens of one sequence, or rows of a packed tensor
 
 bool misaligned(uintptr_t all, unsigned bytes) { return (all & (bytes - 1)) != 0; }
@@ -59,7 +58,8 @@ gf_status check_heads(int dtype, int H, int Hkv, int d) {
   return d == 64 || d == 128 ? GF_OK : GF_ERR_UNSUPPORTED;
 }
 
-gf_status check_packed(int n_seqs, int total_q, int total_k, int H, int Hkv, int d, const gformer_packed_params* p, PackedArgs* a) {
+gf_status check_packed(bool backward, int n_seqs, int total_q, int total_k, int H, int Hkv, int d, const gformer_packed_params* p,
+                       PackedArgs* a) {
   if (!p || p->struct_size != sizeof(gformer_packed_params)) return GF_ERR_INVALID_ARG;
   if (n_seqs < 0 || total_q < 0 || total_k < 0 || !isfinite(p->softmax_scale) || (p->zero_tail != 0 && p->zero_tail != 1))
     return GF_ERR_INVALID_ARG;
@@ -72,7 +72,8 @@ gf_status check_packed(int n_seqs, int total_q, int total_k, int H, int Hkv, int
       (st = strides2(p->dk_stride, a->dks, Hkv, d)) != GF_OK || (st = strides2(p->dv_stride, a->dvs, Hkv, d)) != GF_OK)
     return st;
   if (total_q > kMaxCached || total_k > kMaxCached || n_seqs > kMaxCached) return GF_ERR_UNSUPPORTED;
-  if (packed_tiles(total_q, n_seqs, kPackedRows) * H > kMaxGrid || packed_tiles(total_k, n_seqs, kPackedRows) * Hkv > kMaxGrid)
+  const bool fp32 = p->dtype == GF_F32;
+  if (!packed_queries_fit(fp32, d, total_q, H, n_seqs) || (backward && total_k > 0 && !packed_keys_fit(fp32, d, total_k, H, Hkv, n_seqs)))
     return GF_ERR_UNSUPPORTED;
   a->n_seqs = n_seqs;
   a->total_q = total_q;
@@ -141,7 +142,7 @@ gf_status gformer_packed_attn_fwd(const void* q, const void* k, const void* v, v
                                   const int32_t* cu_q, const int32_t* cu_k, int n_seqs, int total_q, int total_k, int H, int Hkv, int d,
                                   const gformer_packed_params* p, void* hip_stream) {
   PackedArgs a;
-  gf_status st = check_packed(n_seqs, total_q, total_k, H, Hkv, d, p, &a);
+  gf_status st = check_packed(false, n_seqs, total_q, total_k, H, Hkv, d, p, &a);
   if (st != GF_OK) return st;
   if (total_q == 0) return GF_OK;
   if (!q || !out || !cu_q || (total_k > 0 && (!k || !v))) return GF_ERR_INVALID_ARG;
@@ -165,7 +166,7 @@ gf_status gformer_packed_attn_fwd(const void* q, const void* k, const void* v, v
 size_t gformer_packed_attn_bwd_workspace_bytes(int total_q, int total_k, int n_seqs, int H, int Hkv, int d,
                                                const gformer_packed_params* p) {
   PackedArgs a;
-  if (check_packed(n_seqs, total_q, total_k, H, Hkv, d, p, &a) != GF_OK) return 0;
+  if (check_packed(true, n_seqs, total_q, total_k, H, Hkv, d, p, &a) != GF_OK) return 0;
   return packed_stats_bytes(total_q, H) + packed_sums_bytes(total_k, H, Hkv, d);
 }
 
@@ -174,7 +175,7 @@ gf_status gformer_packed_attn_bwd(const void* q, const void* k, const void* v, c
                                   int total_k, int H, int Hkv, int d, const gformer_packed_params* p, void* workspace,
                                   size_t workspace_bytes, void* hip_stream) {
   PackedArgs a;
-  gf_status st = check_packed(n_seqs, total_q, total_k, H, Hkv, d, p, &a);
+  gf_status st = check_packed(true, n_seqs, total_q, total_k, H, Hkv, d, p, &a);
   if (st != GF_OK) return st;
   if (total_q == 0 && total_k == 0) return GF_OK;
   if (!cu_q || (total_q > 0 && (!q || !out || !lse || !dout || !dq)) || (total_k > 0 && (!k || !v || !dk || !dv))) return GF_ERR_INVALID_ARG;
@@ -235,12 +236,12 @@ gf_status gformer_paged_decode(const void* q, const void* k, const void* v, void
       (st = strides2(p->v_stride, a.vs, Hkv, d)) != GF_OK || (st = strides2(p->o_stride, a.os, H, d)) != GF_OK)
     return st;
   if (B == 0) return GF_OK;
+  const PagedSplit s = paged_split(B, H, Hkv, a.room);
+  if (!paged_decode_fits(B, H, Hkv, s)) return GF_ERR_UNSUPPORTED;
   if (n_pages < 1) return GF_ERR_INVALID_ARG;
   if (!q || !out || !kpages || !vpages || (!table && table_width > 0) || !lens || !k != !v) return GF_ERR_INVALID_ARG;
   if (misaligned(bits(q, k, v, out, kpages, vpages), 16) || misaligned(bits(table, lens), 4)) return GF_ERR_INVALID_ARG;
   if (out == q || out == k || out == v || out == kpages || out == vpages || kpages == vpages) return GF_ERR_INVALID_ARG;
-  const PagedSplit s = paged_split(B, H, Hkv, a.room);
-  if ((int64_t)B * H * s.splits > kMaxGrid) return GF_ERR_UNSUPPORTED;   // no fewer than the workgroups of either launch
   const size_t need = decode_bytes(B, H, Hkv, d, a.room);
   if (need > 0 && (!workspace || workspace_bytes < need)) return GF_ERR_WORKSPACE;
   if (need > 0 && misaligned(bits(workspace), 256)) return GF_ERR_INVALID_ARG;
@@ -279,7 +280,7 @@ gf_status gformer_paged_fill(const void* k, const void* v, void* kpages, void* v
   if (n_seqs < 0 || total < 0) return GF_ERR_INVALID_ARG;
   if (total > kMaxCached || n_seqs > kMaxCached) return GF_ERR_UNSUPPORTED;
   if ((st = strides2(p->k_stride, a.ks, Hkv, d)) != GF_OK || (st = strides2(p->v_stride, a.vs, Hkv, d)) != GF_OK) return st;
-  if (packed_tiles(total, n_seqs, 32) * Hkv > kMaxGrid) return GF_ERR_UNSUPPORTED;
+  if (!paged_fill_fits(total, n_seqs, Hkv)) return GF_ERR_UNSUPPORTED;
   if (total == 0 || n_seqs == 0 || table_width == 0 || n_pages == 0) return GF_OK;
   if (!k || !v || !kpages || !vpages || !table || !start || !cu) return GF_ERR_INVALID_ARG;
   if (misaligned(bits(k, v, kpages, vpages), 16) || misaligned(bits(table, start, cu), 4)) return GF_ERR_INVALID_ARG;
@@ -309,7 +310,7 @@ gf_status gformer_pages_copy(void* kpages, void* vpages, const int32_t* src, con
   gf_status st = check_paged(Hkv, d, n_pages, p, &shift, a.kps, a.vps);
   if (st != GF_OK) return st;
   if (n_copies < 0) return GF_ERR_INVALID_ARG;
-  if ((int64_t)n_copies * Hkv > kMaxGrid) return GF_ERR_UNSUPPORTED;
+  if ((int64_t)n_copies * Hkv > most_workgroups(kPagedThreads)) return GF_ERR_UNSUPPORTED;
   if (n_copies == 0) return GF_OK;
   if (!kpages || !vpages || !src || !dst || kpages == vpages) return GF_ERR_INVALID_ARG;
   if (misaligned(bits(kpages, vpages), 16) || misaligned(bits(src, dst), 4)) return GF_ERR_INVALID_ARG;

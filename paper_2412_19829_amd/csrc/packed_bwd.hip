@@ -44,6 +44,16 @@ template <typename T, int D, typename F> struct alignas(256) DqTiles {
 // as key tiles and key heads.  MANY: one stream, two workgroups on a compute unit, neither of which waits for the other.  SOME: the
 // longest workgroup decides, and with two streams and a compute unit of its own it takes half as long.  FEW: shorter ones yet.
 enum { MANY, SOME, FEW };
+int key_call(int total_k, int Hkv, int n_seqs, int groups) {
+  const int units = device_compute_units();
+  const bool brief = total_k < (int64_t)512 * n_seqs;   // short sequences have no long workgroups
+  const int64_t workgroups = (int64_t)total_k * Hkv * groups / kPackedRows;
+  if (workgroups <= (brief ? units / 2 : units)) return FEW;
+  return workgroups > (brief ? units : 3 * units) ? MANY : SOME;
+}
+// rows and threads of a workgroup
+constexpr int key_rows(int call) { return call == FEW ? 64 : kPackedRows; }
+constexpr int key_threads(bool fp32, int d, int call) { return call == MANY || (fp32 && d == 128) ? 256 : 512; }
 template <typename T, int D, int CALL> struct KeyShape_;
 template <typename T, int D> struct KeyShape_<T, D, MANY> {
   using type = Shape<4, 1, sizeof(T) == 2 && D == 64 ? 64 : 32, sizeof(T) == 2 && D == 128 ? 2 : 3, kWaves<T, D>>;
@@ -386,8 +396,11 @@ template <typename T, int D> __global__ __launch_bounds__(256) void packed_add_k
   Products<T, D>::put4(to + c, x[0], x[1], x[2], x[3]);
 }
 
+int64_t add_workgroups(int total_k, int Hkv, int d) { return ((int64_t)total_k * Hkv * 2 * (d / 4) + 255) / 256; }
+
 template <typename T, int D, int STREAMS> hipError_t launch_dq(const PackedArgs& a, hipStream_t s) {
   using F = typename DqShape_<T, D, STREAMS>::type;
+  static_assert(F::ROWS == query_rows(STREAMS) && F::THREADS == kQueryThreads);
   constexpr size_t smem = std::max(sizeof(DqTiles<T, D, F>), F::ROWS * kPutRow<T, D> * sizeof(T));   // the rows leave through it
   auto kern = packed_dq_kernel<T, D, F>;
   if (hipError_t e = allow_lds(kern, smem); e != hipSuccess) return e;
@@ -397,6 +410,7 @@ template <typename T, int D, int STREAMS> hipError_t launch_dq(const PackedArgs&
 }
 template <typename T, int D, int CALL> hipError_t launch_dkdv(const PackedArgs& a, int groups, hipStream_t s) {
   using F = typename KeyShape_<T, D, CALL>::type;
+  static_assert(F::ROWS == key_rows(CALL) && F::THREADS == key_threads(sizeof(T) == 4, D, CALL));
   constexpr size_t smem = std::max(sizeof(KeyTiles<T, D, F>), F::ROWS * kPutRow<float, D> * sizeof(float));
   auto kern = packed_dkdv_kernel<T, D, F>;
   if (hipError_t e = allow_lds(kern, smem); e != hipSuccess) return e;
@@ -404,8 +418,7 @@ template <typename T, int D, int CALL> hipError_t launch_dkdv(const PackedArgs& 
   kern<<<dim3((unsigned)(tiles * a.Hkv * groups)), dim3(F::THREADS), smem, s>>>(a, (int)tiles, groups);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || groups == 1) return e;
-  const int64_t threads = (int64_t)a.total_k * a.Hkv * 2 * (D / 4);
-  packed_add_kernel<T, D><<<dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s>>>(a, groups);
+  packed_add_kernel<T, D><<<dim3((unsigned)add_workgroups(a.total_k, a.Hkv, D)), dim3(256), 0, s>>>(a, groups);
   return hipGetLastError();
 }
 // dk, dv in two streams / one, us of the whole pass (keys x key heads): bf16, d = 64: 4 of 1000 x 32 118 / 104, 16 of 100 x 32 38 / 30, 4096 x 16 175 / 202,
@@ -420,11 +433,11 @@ template <typename T, int D> hipError_t launch(const PackedArgs& a, hipStream_t 
   }
   if (e != hipSuccess || a.total_k == 0) return e;
   const int groups = packed_head_groups(a.total_k, a.H, a.Hkv);
-  const int units = device_compute_units();
-  const bool brief = a.total_k < (int64_t)512 * a.n_seqs;   // short sequences have no long workgroups
-  const int64_t workgroups = (int64_t)a.total_k * a.Hkv * groups / kPackedRows;
-  if (workgroups <= (brief ? units / 2 : units)) return launch_dkdv<T, D, FEW>(a, groups, s);
-  return workgroups > (brief ? units : 3 * units) ? launch_dkdv<T, D, MANY>(a, groups, s) : launch_dkdv<T, D, SOME>(a, groups, s);
+  switch (key_call(a.total_k, a.Hkv, a.n_seqs, groups)) {
+    case FEW: return launch_dkdv<T, D, FEW>(a, groups, s);
+    case SOME: return launch_dkdv<T, D, SOME>(a, groups, s);
+    default: return launch_dkdv<T, D, MANY>(a, groups, s);
+  }
 }
 
 }  // namespace
@@ -443,6 +456,12 @@ int packed_head_groups(int total_k, int H, int Hkv) {
     groups = next;
   }
   return groups;
+}
+
+bool packed_keys_fit(bool fp32, int d, int total_k, int H, int Hkv, int n_seqs) {
+  const int groups = packed_head_groups(total_k, H, Hkv), call = key_call(total_k, Hkv, n_seqs, groups);
+  return packed_tiles(total_k, n_seqs, key_rows(call)) * Hkv * groups <= most_workgroups(key_threads(fp32, d, call)) &&
+         (groups == 1 || add_workgroups(total_k, Hkv, d) <= most_workgroups(256));
 }
 
 hipError_t launch_packed_bwd(const PackedArgs& a, bool bf16, hipStream_t s) {

@@ -221,6 +221,7 @@ template <typename T, int D, int STREAMS> hipError_t launch(const PackedArgs& a,
   constexpr size_t smem = std::max(sizeof(FwdTiles<T, D, F>), F::ROWS * kPutRow<T, D> * sizeof(T));   // the rows leave through it
   auto kern = packed_fwd_kernel<T, D, F>;
   if (hipError_t e = allow_lds(kern, smem); e != hipSuccess) return e;
+  static_assert(F::ROWS == query_rows(STREAMS) && F::THREADS == kQueryThreads);
   const int64_t tiles = packed_tiles(a.total_q, a.n_seqs, F::ROWS);
   kern<<<dim3((unsigned)(tiles * a.H)), dim3(F::THREADS), smem, s>>>(a, (int)tiles);
   return hipGetLastError();
@@ -248,6 +249,10 @@ int packed_streams(bool fp32, int d, int total_q, int H, int n_seqs) {
   const int64_t workgroups = (int64_t)total_q * H / kPackedRows, most = units * (d == 64 ? 4 : 3) / 2;
   if (workgroups > (total_q < (int64_t)512 * n_seqs ? most / 4 : most)) return 1;
   return fp32 && d == 128 && workgroups > units / 2 ? 2 : 4;
+}
+
+bool packed_queries_fit(bool fp32, int d, int total_q, int H, int n_seqs) {
+  return packed_tiles(total_q, n_seqs, query_rows(packed_streams(fp32, d, total_q, H, n_seqs))) * H <= most_workgroups(kQueryThreads);
 }
 
 hipError_t launch_packed_fwd(const PackedArgs& a, bool bf16, hipStream_t s) {

@@ -24,7 +24,7 @@
 namespace gformer {
 namespace {
 
-constexpr int kDecodeThreads = 256, kDecodeWaves = 4;
+constexpr int kDecodeWaves = kPagedThreads / 64;
 
 __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
@@ -124,7 +124,7 @@ __device__ __forceinline__ int seen_keys(const PagedDecodeArgs& a, int b) {
   return t < 0 || t > a.room - own ? 0 : t + own;
 }
 
-template <typename T, int D> __global__ __launch_bounds__(kDecodeThreads, 3) void paged_decode_kernel(PagedDecodeArgs a) {
+template <typename T, int D> __global__ __launch_bounds__(kPagedThreads, 3) void paged_decode_kernel(PagedDecodeArgs a) {
   using C = Cached<T, D>;
   constexpr int U = C::U, R = 16 * U, NO = C::NO, E = C::E;
   __shared__ float sm_o[kDecodeWaves][kPagedHeads][D + 4], sm_m[kDecodeWaves][kPagedHeads], sm_l[kDecodeWaves][kPagedHeads];
@@ -260,7 +260,7 @@ template <typename T, int D> __global__ __launch_bounds__(kDecodeThreads, 3) voi
     for (int r = 0; r < 4; ++r) sm_o[wave][i][64 * (e / E) + E * (4 * g + r) + e % E] = o[e][r];
   __syncthreads();
   const int c = tid % D;
-  for (int h = tid / D; h < heads; h += kDecodeThreads / D) {
+  for (int h = tid / D; h < heads; h += kPagedThreads / D) {
     float top = -INFINITY, sum = 0.f, acc = 0.f;
 #pragma unroll
     for (int x = 0; x < kDecodeWaves; ++x) top = fmaxf(top, sm_m[x][h]);
@@ -284,9 +284,9 @@ template <typename T, int D> __global__ __launch_bounds__(kDecodeThreads, 3) voi
   }
 }
 
-// Joins the chunks of one head: a workgroup's threads take 4 columns of every (256 / (D / 4))-th chunk.  Latency: 3 to 4 us.
-template <typename T, int D> __global__ __launch_bounds__(256) void paged_join_kernel(PagedDecodeArgs a) {
-  constexpr int C4 = D / 4, GROUPS = 256 / C4;
+// Joins the chunks of one head: a workgroup's threads take 4 columns of every (kPagedThreads / (D / 4))-th chunk.  Latency: 3 to 4 us.
+template <typename T, int D> __global__ __launch_bounds__(kPagedThreads) void paged_join_kernel(PagedDecodeArgs a) {
+  constexpr int C4 = D / 4, GROUPS = kPagedThreads / C4;
   __shared__ float sm_top[4];
   __shared__ f32x4 sm_o[GROUPS][C4];
   __shared__ float sm_l[GROUPS];
@@ -294,7 +294,7 @@ template <typename T, int D> __global__ __launch_bounds__(256) void paged_join_k
   const int n = seen_keys(a, b), used = max(1, (n + a.chunk - 1) / a.chunk);
   const int64_t at = ((int64_t)b * a.H + h) * a.splits;
   float top = -INFINITY;
-  for (int s = tid; s < used; s += 256) top = fmaxf(top, a.stats[2 * (at + s)]);
+  for (int s = tid; s < used; s += kPagedThreads) top = fmaxf(top, a.stats[2 * (at + s)]);
 #pragma unroll
   for (int x = 32; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor(top, x, 64));
   if ((tid & 63) == 0) sm_top[tid >> 6] = top;
@@ -325,14 +325,14 @@ template <typename T, int D> __global__ __launch_bounds__(256) void paged_join_k
 // Packed rows into their slots: a workgroup moves 32 rows of one head.  Memory: 8192 tokens of 8 heads, d = 128, bf16 (67 MB read and
 // written) 11.2 us, 6.0 TB/s with part of them in the caches; 128 tokens of 12 heads, d = 64: 2.6.
 constexpr int kFillRows = 32;
-template <typename T, int D> __global__ __launch_bounds__(256) void paged_fill_kernel(PagedFillArgs a) {
+template <typename T, int D> __global__ __launch_bounds__(kPagedThreads) void paged_fill_kernel(PagedFillArgs a) {
   constexpr int C = D * (int)sizeof(T) / 16, E = 16 / (int)sizeof(T);
   const int tid = threadIdx.x, head = blockIdx.x % a.Hkv;
   const SeqTile at = find_tile<kFillRows>(a.cu, a.n_seqs, a.total, blockIdx.x / a.Hkv, tid & 63);
   if (at.first < 0 || at.seq == a.n_seqs) return;
   const int base = packed_row(a.cu, at.seq, a.total), n = packed_row(a.cu, at.seq + 1, a.total) - base;
   const int64_t room = (int64_t)a.width << a.shift;
-  for (int r = tid / C; r < kFillRows; r += 256 / C) {
+  for (int r = tid / C; r < kFillRows; r += kPagedThreads / C) {
     const int row = at.first + r;
     const int64_t pos = (int64_t)a.start[at.seq] + row;
     if (row >= n || pos < 0 || pos >= room) continue;
@@ -348,8 +348,8 @@ template <typename T, int D> __global__ __launch_bounds__(256) void paged_fill_k
 
 // Whole pages: a workgroup copies one head of one page, keys and values.  Memory: 1024 pages of 64 tokens, 8 heads, d = 128, bf16 (537 MB
 // read and written) 102 us, 5.3 TB/s; 16 pages 3.4.
-template <typename T, int D> __global__ __launch_bounds__(256) void pages_copy_kernel(PagesCopyArgs a) {
-  constexpr int C = D * (int)sizeof(T) / 16, E = 16 / (int)sizeof(T), STEP = 256 / C;
+template <typename T, int D> __global__ __launch_bounds__(kPagedThreads) void pages_copy_kernel(PagesCopyArgs a) {
+  constexpr int C = D * (int)sizeof(T) / 16, E = 16 / (int)sizeof(T), STEP = kPagedThreads / C;
   const int copy = blockIdx.x / a.Hkv, head = blockIdx.x % a.Hkv;
   const int src = a.src[copy], dst = a.dst[copy];
   if ((unsigned)src >= (unsigned)a.n_pages || (unsigned)dst >= (unsigned)a.n_pages || src == dst) return;
@@ -365,12 +365,15 @@ template <typename T, int D> __global__ __launch_bounds__(256) void pages_copy_k
   }
 }
 
+// Workgroups of an uncut call: 16 query heads of one key head of one sequence each.
+int64_t decode_units(int B, int H, int Hkv) { return (int64_t)B * Hkv * (((int64_t)H / Hkv + kPagedHeads - 1) / kPagedHeads); }
+
 template <typename T, int D> hipError_t decode(const PagedDecodeArgs& a, hipStream_t s) {
-  const int tiles = (a.H / a.Hkv + kPagedHeads - 1) / kPagedHeads;
-  paged_decode_kernel<T, D><<<dim3((unsigned)((int64_t)a.B * a.Hkv * tiles * a.splits)), dim3(kDecodeThreads), 0, s>>>(a);
+  const unsigned workgroups = (unsigned)(decode_units(a.B, a.H, a.Hkv) * a.splits);
+  paged_decode_kernel<T, D><<<dim3(workgroups), dim3(kPagedThreads), 0, s>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.splits == 1) return e;
-  paged_join_kernel<T, D><<<dim3((unsigned)((int64_t)a.B * a.H)), dim3(256), 0, s>>>(a);
+  paged_join_kernel<T, D><<<dim3((unsigned)((int64_t)a.B * a.H)), dim3(kPagedThreads), 0, s>>>(a);
   return hipGetLastError();
 }
 
@@ -382,11 +385,17 @@ template <typename T, int D> hipError_t decode(const PagedDecodeArgs& a, hipStre
 // Short of that many workgroups without a cut, a chunk is no longer than max_len (at most 2^30); from there on there is none to make.
 PagedSplit paged_split(int B, int H, int Hkv, int64_t max_len) {
   constexpr int64_t kWorkgroups = 1536;
-  const int64_t units = (int64_t)B * Hkv * (((int64_t)H / Hkv + kPagedHeads - 1) / kPagedHeads);
+  const int64_t units = decode_units(B, H, Hkv);
   const int64_t share = units < kWorkgroups ? (max_len * units + kWorkgroups - 1) / kWorkgroups : max_len;
   const int64_t chunk = std::max<int64_t>(128, (share + 63) / 64 * 64);
   return {(int)chunk, (int)std::max<int64_t>(1, (max_len + chunk - 1) / chunk)};
 }
+
+bool paged_decode_fits(int B, int H, int Hkv, PagedSplit s) {
+  return decode_units(B, H, Hkv) * s.splits <= most_workgroups(kPagedThreads) &&
+         (s.splits == 1 || (int64_t)B * H <= most_workgroups(kPagedThreads));
+}
+bool paged_fill_fits(int total, int n_seqs, int Hkv) { return packed_tiles(total, n_seqs, kFillRows) * Hkv <= most_workgroups(kPagedThreads); }
 
 hipError_t launch_paged_decode(const PagedDecodeArgs& a, bool bf16, hipStream_t s) {
   if (bf16) return a.d == 128 ? decode<uint16_t, 128>(a, s) : decode<uint16_t, 64>(a, s);
@@ -395,15 +404,15 @@ hipError_t launch_paged_decode(const PagedDecodeArgs& a, bool bf16, hipStream_t 
 
 hipError_t launch_paged_fill(const PagedFillArgs& a, bool bf16, hipStream_t s) {
   const dim3 grid((unsigned)(packed_tiles(a.total, a.n_seqs, kFillRows) * a.Hkv));
-  if (bf16) a.d == 128 ? paged_fill_kernel<uint16_t, 128><<<grid, 256, 0, s>>>(a) : paged_fill_kernel<uint16_t, 64><<<grid, 256, 0, s>>>(a);
-  else a.d == 128 ? paged_fill_kernel<float, 128><<<grid, 256, 0, s>>>(a) : paged_fill_kernel<float, 64><<<grid, 256, 0, s>>>(a);
+  if (bf16) a.d == 128 ? paged_fill_kernel<uint16_t, 128><<<grid, kPagedThreads, 0, s>>>(a) : paged_fill_kernel<uint16_t, 64><<<grid, kPagedThreads, 0, s>>>(a);
+  else a.d == 128 ? paged_fill_kernel<float, 128><<<grid, kPagedThreads, 0, s>>>(a) : paged_fill_kernel<float, 64><<<grid, kPagedThreads, 0, s>>>(a);
   return hipGetLastError();
 }
 
 hipError_t launch_pages_copy(const PagesCopyArgs& a, bool bf16, hipStream_t s) {
   const dim3 grid((unsigned)((int64_t)a.n_copies * a.Hkv));
-  if (bf16) a.d == 128 ? pages_copy_kernel<uint16_t, 128><<<grid, 256, 0, s>>>(a) : pages_copy_kernel<uint16_t, 64><<<grid, 256, 0, s>>>(a);
-  else a.d == 128 ? pages_copy_kernel<float, 128><<<grid, 256, 0, s>>>(a) : pages_copy_kernel<float, 64><<<grid, 256, 0, s>>>(a);
+  if (bf16) a.d == 128 ? pages_copy_kernel<uint16_t, 128><<<grid, kPagedThreads, 0, s>>>(a) : pages_copy_kernel<uint16_t, 64><<<grid, kPagedThreads, 0, s>>>(a);
+  else a.d == 128 ? pages_copy_kernel<float, 128><<<grid, kPagedThreads, 0, s>>>(a) : pages_copy_kernel<float, 64><<<grid, kPagedThreads, 0, s>>>(a);
   return hipGetLastError();
 }
 

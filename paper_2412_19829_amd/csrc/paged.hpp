@@ -37,7 +37,11 @@ struct PagedSplit {
   int chunk, splits;
 };
 constexpr int kPagedHeads = 16;        // query heads of one key head that a workgroup takes
+constexpr int kPagedThreads = 256;     // of a workgroup, in all of these kernels
 PagedSplit paged_split(int B, int H, int Hkv, int64_t max_len);
+// Whether the launches are within what one may have.
+bool paged_decode_fits(int B, int H, int Hkv, PagedSplit s);
+bool paged_fill_fits(int total, int n_seqs, int Hkv);
 hipError_t launch_paged_decode(const PagedDecodeArgs& a, bool bf16, hipStream_t s);
 hipError_t launch_paged_fill(const PagedFillArgs& a, bool bf16, hipStream_t s);
 hipError_t launch_pages_copy(const PagesCopyArgs& a, bool bf16, hipStream_t s);

@@ -539,3 +539,34 @@ def test_the_backward_workspace_stays_bounded():
                 p = gb.make_packed_params()
                 sums = gb.gformer_packed_attn_bwd_workspace_bytes(0, total, 1, H, Hkv, d, p)
                 assert sums <= 4 * 512 * 128 * d * 8
+
+
+# The refusals below come before the pointers are looked at, so that a call of the largest size, with a null pointer in it, is
+# refused for the pointer.
+@pytest.mark.parametrize("dtype,d,few", [(gb.GF_BF16, 64, 512), (gb.GF_BF16, 128, 512), (gb.GF_F32, 64, 512), (gb.GF_F32, 128, 256)])
+@pytest.mark.parametrize("H,Hkv", [(32, 32), (32, 8), (5, 1)])
+def test_launches_stay_within_what_one_may_have(dtype, d, few, H, Hkv):
+    """A launch has less than 2^32 threads; 8 rows of n sequences take n + 1 tiles a head, of 256 threads for queries and of `few` for keys
+    (a workgroup for every part of the query heads that share them)."""
+    p = gb.make_packed_params(dtype)
+    most = (2 ** 32 - 1) // 256 // H - 1
+    assert fwd(p=p, q=0, n=most, H=H, Hkv=Hkv, d=d) == gb.GF_ERR_INVALID_ARG
+    assert fwd(p=p, q=0, n=most + 1, H=H, Hkv=Hkv, d=d) == gb.GF_ERR_UNSUPPORTED
+    need = lambda n: gb.gformer_packed_attn_bwd_workspace_bytes(8, 8, n, H, Hkv, d, p)
+    groups = max(1, round((need(1) - 256 * -(-8 * H * 8 // 256)) / (8 * Hkv * d * 8)))   # parts of the query heads, by their sums
+    keys = (2 ** 32 - 1) // few // (Hkv * groups) - 1
+    assert need(min(most, keys)) > 0 and need(min(most, keys) + 1) == 0
+    call = lambda n: gb.lib().gformer_packed_attn_bwd(0, 2 * A, 3 * A, 4 * A, 0, 5 * A, 11 * A, 8 * A, 9 * A, 10 * A, 6 * A, 0, n, 8, 8, H, Hkv, d,
+                                                      ctypes.byref(p), 7 * A, 1 << 20, None)
+    assert call(min(most, keys)) == gb.GF_ERR_INVALID_ARG and call(min(most, keys) + 1) == gb.GF_ERR_UNSUPPORTED
+
+
+def test_long_launches_stay_within_what_one_may_have():
+    """Long sequences: tiles of 128 rows."""
+    p = gb.make_packed_params()
+    rows = 1 << 30
+    H = ((2 ** 32 - 1) // 256) // (rows // 128 + 2)
+    for heads, status in ((H, gb.GF_ERR_INVALID_ARG), (H + 1, gb.GF_ERR_UNSUPPORTED), (2 ** 31 - 1, gb.GF_ERR_UNSUPPORTED)):
+        assert fwd(p=p, q=0, n=1, tq=rows, tk=rows, H=heads, Hkv=heads) == status
+        assert gb.lib().gformer_packed_attn_bwd(0, 2 * A, 3 * A, 4 * A, 0, 5 * A, 11 * A, 8 * A, 9 * A, 10 * A, 6 * A, 0, 1, rows, rows, heads, heads,
+                                                64, ctypes.byref(p), 7 * A, 1 << 20, None) == status

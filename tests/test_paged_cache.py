@@ -491,3 +491,22 @@ def test_many_rows_over_a_table_of_many_pages():
     assert not got[idle.cuda()].any()
     for place, (b, n) in enumerate(lens.items()):        # the new token is in its slot
         assert torch.equal(kp[2 - place, :, n], x["k"][b]) and torch.equal(vp[2 - place, :, n], x["v"][b])
+
+
+def test_launches_stay_within_what_one_may_have():
+    """A launch has less than 2^32 threads, of which a workgroup has 256; a decode step has one for every 16 query heads of a key head (two for
+    20, so four a row with two key heads).  The largest call of each kind is refused for its null
+    pointer alone."""
+    most = (2 ** 32 - 1) // 256
+    for B, H, Hkv, status in ((most // 32, 32, 32, 1), (most // 32 + 1, 32, 32, 2), (most // 8, 32, 8, 1), (most // 8 + 1, 32, 8, 2), (most // 4, 40, 2, 1),
+                              (most // 4 + 1, 40, 2, 2), (2 ** 31 - 1, 2 ** 31 - 1, 1, 2), (2 ** 31 - 1, 2 ** 31 - 1, 2 ** 31 - 1, 2)):
+        assert decode(q=0, B=B, H=H, Hkv=Hkv) == status, (B, H, Hkv)
+    p = gb.make_paged_params()
+    fill = lambda n, total, heads: gb.lib().gformer_paged_fill(0, *(i * A for i in range(2, 8)), n, total, heads, 64, 9, 4, ctypes.byref(p), None)
+    for n, total, heads in ((most // 32 - 1, 8, 32), (most - 1, 8, 1), (1, 1 << 28, most // ((1 << 28) // 32 + 2))):
+        assert fill(n, total, heads) == gb.GF_ERR_INVALID_ARG
+    for n, total, heads in ((most // 32, 8, 32), (most, 8, 1), (1, 1 << 28, most // ((1 << 28) // 32 + 2) + 1), (1 << 30, 8, 2 ** 31 - 1)):
+        assert fill(n, total, heads) == gb.GF_ERR_UNSUPPORTED
+    copy = lambda n, heads: gb.lib().gformer_pages_copy(0, 2 * A, 3 * A, 4 * A, n, heads, 64, 9, ctypes.byref(p), None)
+    assert copy(most // 256, 256) == copy(most, 1) == gb.GF_ERR_INVALID_ARG
+    assert copy(most // 256 + 1, 256) == copy(most + 1, 1) == copy(2 ** 31 - 1, 2 ** 31 - 1) == gb.GF_ERR_UNSUPPORTED
