@@ -21,7 +21,7 @@ gf_status strides2(const int64_t* in, int64_t* out, int heads, int d) {
   if (in[0] == 0 && in[1] == 0) {
     out[0] = (int64_t)heads * d;
     out[1] = d;
-    return GF_OK;
+    return out[0] > kMaxTokenStride ? GF_ERR_UNSUPPORTED : GF_OK;
   }
   for (int i = 0; i < 2; ++i) {
     if (in[i] < 0 || in[i] % 8 != 0) return GF_ERR_INVALID_ARG;

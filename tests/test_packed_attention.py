@@ -570,3 +570,15 @@ def test_long_launches_stay_within_what_one_may_have():
         assert fwd(p=p, q=0, n=1, tq=rows, tk=rows, H=heads, Hkv=heads) == status
         assert gb.lib().gformer_packed_attn_bwd(0, 2 * A, 3 * A, 4 * A, 0, 5 * A, 11 * A, 8 * A, 9 * A, 10 * A, 6 * A, 0, 1, rows, rows, heads, heads,
                                                 64, ctypes.byref(p), 7 * A, 1 << 20, None) == status
+
+
+def test_dense_rows_are_as_long_as_strided_ones_may_be():
+    """Rows of 2^20 elements at most, whether the strides are named or left to the library."""
+    for d in (64, 128):
+        heads = (1 << 20) // d
+        for h, status in ((heads, gb.GF_ERR_INVALID_ARG), (heads + 1, gb.GF_ERR_UNSUPPORTED), ((1 << 26) // d, gb.GF_ERR_UNSUPPORTED)):
+            for p in (wrong(), wrong(**{f"{x}_stride": (h * d, d) for x in ("q", "k", "v", "o")})):
+                assert fwd(p=p, q=0, tq=3, tk=3, H=h, Hkv=h, d=d) == status   # where the length is fine, for the null pointer
+    p = gb.make_packed_params()
+    assert gb.gformer_packed_attn_bwd_workspace_bytes(3, 3, 1, 1 << 14, 1 << 14, 64, p) > 0
+    assert gb.gformer_packed_attn_bwd_workspace_bytes(3, 3, 1, (1 << 14) + 1, (1 << 14) + 1, 64, p) == 0

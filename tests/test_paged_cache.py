@@ -510,3 +510,12 @@ def test_launches_stay_within_what_one_may_have():
     copy = lambda n, heads: gb.lib().gformer_pages_copy(0, 2 * A, 3 * A, 4 * A, n, heads, 64, 9, ctypes.byref(p), None)
     assert copy(most // 256, 256) == copy(most, 1) == gb.GF_ERR_INVALID_ARG
     assert copy(most // 256 + 1, 256) == copy(most + 1, 1) == copy(2 ** 31 - 1, 2 ** 31 - 1) == gb.GF_ERR_UNSUPPORTED
+
+
+def test_dense_rows_are_as_long_as_strided_ones_may_be():
+    p = gb.make_paged_params()
+    for d in (64, 128):
+        heads = (1 << 20) // d
+        for h, status in ((heads, gb.GF_ERR_INVALID_ARG), (heads + 1, gb.GF_ERR_UNSUPPORTED)):
+            assert decode(q=0, H=h, Hkv=1, d=d) == decode(q=0, H=h, Hkv=h, d=d) == status
+            assert gb.lib().gformer_paged_fill(0, *(i * A for i in range(2, 8)), 2, 5, h, d, 9, 4, ctypes.byref(p), None) == status
