@@ -157,6 +157,8 @@ __device__ __forceinline__ float maximum3(float a, float b, float c) {
 //   rows, 16 bytes a lane    lanes 0-3, 12-15, 20-23, 24-27 go together, then the others of the half: 16 different pieces
 //   transposed, bf16         a half's lanes: two neighbouring pairs of pieces in each of 4 rows, which the low bits of r set apart
 //   transposed, fp32         8 pieces of a row and of the one 4 further on, which bit 2 of r sets apart
+template <typename T, int D> constexpr size_t kTileAlign = D * sizeof(T);   // a row's bytes (lds_lane())
+constexpr size_t kLdsAlign = 512;                                           // the longest row's
 template <typename T, int D, int R> struct Tile {
   static constexpr int E = 16 / (int)sizeof(T), C = D / E;   // elements a piece, pieces a row
   static constexpr int RPI = 64 / C;                          // rows an instruction loads
@@ -220,8 +222,8 @@ __device__ __forceinline__ void tile_read() {
   __builtin_amdgcn_sched_barrier(0);
 }
 
-// LDS by its byte addresses.  A tile starts at a multiple of 256 bytes, so the pieces of a row (and of the rows 16 further
-// on) differ from a lane's first one by an exclusive or: one instruction a read, where addresses kept ready would take
+// LDS by its byte addresses.  A tile starts at a multiple of a row's bytes (kTileAlign), so the pieces of a row (and of the rows
+// 16 further on) differ from a lane's first one by an exclusive or: one instruction a read, where addresses kept ready would take
 // the registers of the sums.  lds_lane() keeps the compiler from doing that.
 __device__ __forceinline__ uint32_t lds_lane(const void* tile, int bytes) {
   uint32_t at = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)tile + bytes;

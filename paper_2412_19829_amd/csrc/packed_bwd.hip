@@ -35,8 +35,8 @@ template <typename T, int D> struct DqShape_<T, D, 2> {
 template <typename T, int D> struct DqShape_<T, D, 4> {
   using type = Shape<1, 4, 32, 1, sizeof(T) == 2 && D == 64 ? 3 : kWaves<T, D>>;
 };
-template <typename T, int D, typename F> struct alignas(256) DqTiles {
-  struct { T k[F::BUF][F::R * D], v[F::BUF][F::R * D]; } stream[F::S];
+template <typename T, int D, typename F> struct alignas(kLdsAlign) DqTiles {
+  struct { alignas(kTileAlign<T, D>) T k[F::BUF][F::R * D], v[F::BUF][F::R * D]; } stream[F::S];
   int flag;
 };
 
@@ -66,12 +66,12 @@ template <typename T, int D> struct KeyShape_<T, D, FEW> {
 };
 // its value rows stay in LDS where their registers are wanted for the sums
 template <typename T, int D> constexpr bool kValuesInLds = sizeof(T) == 2 && D == 128;
-template <typename T, int D, typename F> struct alignas(256) KeyTiles {
+template <typename T, int D, typename F> struct alignas(kLdsAlign) KeyTiles {
   struct {
-    T q[F::BUF][F::R * D], g[F::BUF][F::R * D];
+    alignas(kTileAlign<T, D>) T q[F::BUF][F::R * D], g[F::BUF][F::R * D];
     float stats[F::BUF][F::R == 64 ? 128 : 64];   // in base 2: lse of the queries, then -delta
   } stream[F::S];
-  T v[kValuesInLds<T, D> ? F::ROWS * D : 8];
+  alignas(kTileAlign<T, D>) T v[kValuesInLds<T, D> ? F::ROWS * D : 8];
   int flag;
 };
 
@@ -101,7 +101,8 @@ template <typename T, int D, typename F> __global__ __launch_bounds__(F::THREADS
   using P = Products<T, D>;
   constexpr int R = F::R, S = F::S, ROWS = F::ROWS, BUF = F::BUF, NS = R / 32, MT = D / 32, W = F::RW;
   using L = Tile<T, D, R>;
-  extern __shared__ __align__(256) unsigned char smem_raw[];
+  extern __shared__ __align__(kLdsAlign) unsigned char smem_raw[];
+  static_assert(F::R * D * sizeof(T) % kTileAlign<T, D> == 0, "the tiles behind the first");
   auto& all = *reinterpret_cast<DqTiles<T, D, F>*>(smem_raw);
   const int tid = threadIdx.x, lane = tid & 63, ln = lane & 31, lh = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64 % W), stream = __builtin_amdgcn_readfirstlane(tid / 64 / W);
@@ -228,7 +229,8 @@ template <typename T, int D, typename F> __global__ __launch_bounds__(F::THREADS
   using P = Products<T, D>;
   constexpr int R = F::R, S = F::S, ROWS = F::ROWS, BUF = F::BUF, MT = D / 32, W = F::RW;
   using L = Tile<T, D, R>;
-  extern __shared__ __align__(256) unsigned char smem_raw[];
+  extern __shared__ __align__(kLdsAlign) unsigned char smem_raw[];
+  static_assert(F::R * D * sizeof(T) % kTileAlign<T, D> == 0, "the tiles behind the first");
   auto& all = *reinterpret_cast<KeyTiles<T, D, F>*>(smem_raw);
   const int tid = threadIdx.x, lane = tid & 63, ln = lane & 31, lh = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64 % W), stream = __builtin_amdgcn_readfirstlane(tid / 64 / W);

@@ -29,8 +29,8 @@ template <typename T, int D> struct FwdShape_<T, D, 2> {
 template <typename T, int D> struct FwdShape_<T, D, 4> {
   using type = Shape<1, 4, 32, 1, sizeof(T) == 4 && D == 128 ? 1 : 2>;
 };
-template <typename T, int D, typename F> struct alignas(256) FwdTiles {
-  struct { T k[F::BUF][F::R * D], v[F::BUF][F::R * D]; } stream[F::S];
+template <typename T, int D, typename F> struct alignas(kLdsAlign) FwdTiles {
+  struct { alignas(kTileAlign<T, D>) T k[F::BUF][F::R * D], v[F::BUF][F::R * D]; } stream[F::S];
   int flag;
 };
 
@@ -38,7 +38,8 @@ template <typename T, int D, typename F> __global__ __launch_bounds__(F::THREADS
   using P = Products<T, D>;
   constexpr int R = F::R, S = F::S, ROWS = F::ROWS, NS = R / 32, MT = D / 32, W = F::RW;
   using L = Tile<T, D, R>;
-  extern __shared__ __align__(256) unsigned char smem_raw[];
+  extern __shared__ __align__(kLdsAlign) unsigned char smem_raw[];
+  static_assert(F::R * D * sizeof(T) % kTileAlign<T, D> == 0, "the tiles behind the first");
   auto& all = *reinterpret_cast<FwdTiles<T, D, F>*>(smem_raw);
   const int tid = threadIdx.x, lane = tid & 63, ln = lane & 31, lh = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64 % W), stream = __builtin_amdgcn_readfirstlane(tid / 64 / W);
