@@ -62,10 +62,15 @@ class PagedCache:
                 return s
         raise RuntimeError("the cache holds as many sequences as it can")
 
-    def _take(self, n):
+    def _next(self, n):
+        """The pages that _take() would take."""
         if n > len(self._free):
             raise RuntimeError(f"the cache is full: {n} pages wanted, {len(self._free)} free")
-        taken = [self._free.pop() for _ in range(n)]
+        return self._free[len(self._free) - n:][::-1]
+
+    def _take(self, n):
+        taken = self._next(n)
+        del self._free[len(self._free) - n:]
         for p in taken:
             self._held[p] = 1
         return taken
@@ -98,9 +103,9 @@ class PagedCache:
         full = len(mine)
         if partly or full * self.page_size > self._len[seq]:
             full = self._len[seq] // self.page_size
-        own = self._take(1 if partly else 0)
         if partly:
-            self._copy([(mine[full], own[0])])
+            self._copy([(mine[full], self._next(1)[0])])   # may fail, and so comes first
+        own = self._take(1 if partly else 0)
         for p in mine[:full]:
             self._held[p] += 1
         self._pages[new], self._len[new] = mine[:full] + own, self._len[seq]

@@ -519,3 +519,17 @@ def test_dense_rows_are_as_long_as_strided_ones_may_be():
         for h, status in ((heads, gb.GF_ERR_INVALID_ARG), (heads + 1, gb.GF_ERR_UNSUPPORTED)):
             assert decode(q=0, H=h, Hkv=1, d=d) == decode(q=0, H=h, Hkv=h, d=d) == status
             assert gb.lib().gformer_paged_fill(0, *(i * A for i in range(2, 8)), 2, 5, h, d, 9, 4, ctypes.byref(p), None) == status
+
+
+def test_a_fork_whose_copy_fails_changes_nothing(monkeypatch):
+    def fail(*_):
+        raise gb.GformerError(4, "no device")
+    c = cache()
+    a = c.open(13)
+    before = (list(c._held), list(c._free), [list(p or []) for p in c._pages], list(c._len))
+    monkeypatch.setattr(gb, "gformer_pages_copy", fail)
+    with pytest.raises(gb.GformerError):
+        c.fork(a)
+    assert before == (c._held, c._free, [list(p or []) for p in c._pages], c._len)
+    Copies(monkeypatch)
+    assert c.pages(c.fork(a)) == [0, 2]
