@@ -4,7 +4,9 @@ entry points take (device).
 A sequence's row of `table` lists its pages, `lens` its tokens.  Pages are counted by the sequences that hold them: a
 fork shares the full ones, which nobody writes again, and takes a copy of the last one if that is partly filled.
 Every change of the bookkeeping is checked before it is made, so a refused call leaves the cache as it was.
-The copies run on torch's current stream; `table` and `lens` are uploaded in order with it.
+The copies run on torch's current stream, in order with what changes of `table` and `lens`; no call waits for the stream.
+reserve() and advance() for one token of every sequence take the host, us, without a new page / with one for each: 32 sequences 32 / 100, 256 152 / 240,
+however many pages a row has (with the whole table sent each time, 256 rows of 2048 took 12500 / 25000).
 """
 from __future__ import annotations
 
@@ -75,14 +77,29 @@ class PagedCache:
             self._held[p] = 1
         return taken
 
-    def _upload(self):
-        rows = [(p or []) + [-1] * (self.max_pages - len(p or [])) for p in self._pages]
-        self.table.copy_(torch.tensor(rows, dtype=torch.int32))
-        self.lens.copy_(torch.tensor(self._len, dtype=torch.int32))
+    def _send(self, numbers, dtype):
+        """Numbers on the device, from memory of their own that a copy on its way keeps."""
+        t = torch.tensor(numbers, dtype=dtype, pin_memory=self.table.is_cuda)
+        return t.to(self.table.device, non_blocking=True)
+
+    def _update(self, lens, pages=()):
+        """`lens` {sequence: tokens} and `pages` [(sequence, place in its row, page)], on the device and then in the books of lengths:
+        where there is no memory for it, nothing has changed."""
+        new = list(self._len)
+        for s, n in lens.items():
+            new[s] = n
+        if pages:
+            at = self._send([s * self.max_pages + i for s, i, _ in pages], torch.int64)
+            values = self._send([p for _, _, p in pages], torch.int32)
+        if lens:
+            self.lens.copy_(torch.tensor(new, dtype=torch.int32, pin_memory=self.lens.is_cuda), non_blocking=True)
+        if pages:
+            self.table.view(-1).scatter_(0, at, values)
+        self._len = new
 
     def _copy(self, pairs):
         if pairs:
-            src, dst = torch.tensor(pairs, dtype=torch.int32).t().contiguous().to(self.table.device)
+            src, dst = self._send(list(zip(*pairs)), torch.int32)
             gb.gformer_pages_copy(self.kpages, self.vpages, src, dst)
 
     def open(self, tokens: int = 0) -> int:
@@ -91,8 +108,8 @@ class PagedCache:
         if tokens < 0 or n > self.max_pages:
             raise ValueError(f"a sequence has 0 to {self.max_pages * self.page_size} tokens")
         seq = self._slot()
-        self._pages[seq], self._len[seq] = self._take(n), tokens
-        self._upload()
+        self._update({seq: tokens}, [(seq, i, p) for i, p in enumerate(self._next(n))])
+        self._pages[seq] = self._take(n)
         return seq
 
     def fork(self, seq: int) -> int:
@@ -103,25 +120,27 @@ class PagedCache:
         full = len(mine)
         if partly or full * self.page_size > self._len[seq]:
             full = self._len[seq] // self.page_size
+        own = self._next(1 if partly else 0)
         if partly:
-            self._copy([(mine[full], self._next(1)[0])])   # may fail, and so comes first
-        own = self._take(1 if partly else 0)
+            self._copy([(mine[full], own[0])])
+        pages = mine[:full] + own
+        self._update({new: self._len[seq]}, [(new, i, p) for i, p in enumerate(pages)])
+        self._take(len(own))
         for p in mine[:full]:
             self._held[p] += 1
-        self._pages[new], self._len[new] = mine[:full] + own, self._len[seq]
-        self._upload()
+        self._pages[new] = pages
         return new
 
     def free(self, seq: int) -> None:
         """Gives a sequence's pages back, as far as no other holds them."""
         self._check(seq)
+        self._update({seq: -1}, [(seq, i, -1) for i in range(len(self._pages[seq]))])
         for p in self._pages[seq]:
             self._held[p] -= 1
             if self._held[p] == 0:
                 self._free.append(p)
         self._free.sort(reverse=True)
-        self._pages[seq], self._len[seq] = None, -1
-        self._upload()
+        self._pages[seq] = None
 
     def reserve(self, seqs) -> None:
         """A slot for the next token of each of `seqs`: what a step needs before it writes."""
@@ -132,9 +151,11 @@ class PagedCache:
                 raise ValueError(f"sequence {s} is as long as it can be")
         short = [s for s in seqs if len(self._pages[s]) * self.page_size == self._len[s]]
         if short:
-            for s, p in zip(short, self._take(len(short))):
+            new = list(zip(short, self._next(len(short))))
+            self._update({}, [(s, len(self._pages[s]), p) for s, p in new])
+            self._take(len(short))
+            for s, p in new:
                 self._pages[s].append(p)
-            self._upload()
 
     def advance(self, seqs) -> None:
         """After a step that wrote one token of each of `seqs` in every layer."""
@@ -143,9 +164,7 @@ class PagedCache:
             self._check(s)
             if len(self._pages[s]) * self.page_size <= self._len[s]:
                 raise ValueError(f"sequence {s} has no slot for the token: reserve() comes first")
-        for s in seqs:
-            self._len[s] += 1
-        self._upload()
+        self._update({s: self._len[s] + 1 for s in seqs})
 
     def compact(self) -> int:
         """Moves the pages in use to the cache's front; returns how many were moved."""
@@ -153,11 +172,11 @@ class PagedCache:
         holes = [p for p in range(len(used)) if not self._held[p]]
         moved = dict(zip(used[len(used) - len(holes):], holes))
         self._copy(list(moved.items()))
+        self._update({}, [(s, i, moved[p]) for s, pages in enumerate(self._pages) for i, p in enumerate(pages or ()) if p in moved])
         for old, new in moved.items():
             self._held[new], self._held[old] = self._held[old], 0
         for pages in self._pages:
             if pages:
                 pages[:] = [moved.get(p, p) for p in pages]
         self._free = [p for p in range(len(self._held) - 1, -1, -1) if not self._held[p]]
-        self._upload()
         return len(moved)

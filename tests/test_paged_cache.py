@@ -533,3 +533,98 @@ def test_a_fork_whose_copy_fails_changes_nothing(monkeypatch):
     assert before == (c._held, c._free, [list(p or []) for p in c._pages], c._len)
     Copies(monkeypatch)
     assert c.pages(c.fork(a)) == [0, 2]
+
+
+# ---- what the books send to the device ---------------------------------------------------------------
+
+def rows(c):
+    return [(p or []) + [-1] * (c.max_pages - len(p or [])) for p in c._pages]
+
+
+def test_table_and_lengths_follow_the_books(monkeypatch):
+    Copies(monkeypatch)
+    rng, c, live = random.Random(11), cache(n_pages=24, max_seqs=7), []
+    for _ in range(600):
+        try:
+            what = rng.choice(["open", "fork", "free", "reserve", "step", "step", "compact"])
+            if what == "open":
+                live.append(c.open(rng.randint(0, 40)))
+            elif what == "fork" and live:
+                live.append(c.fork(rng.choice(live)))
+            elif what == "free" and live:
+                c.free(live.pop(rng.randrange(len(live))))
+            elif what in ("reserve", "step") and live:
+                some = rng.sample(live, rng.randint(1, len(live)))
+                c.reserve(some)
+                if what == "step":
+                    c.advance(some)
+            elif what == "compact":
+                c.compact()
+        except (RuntimeError, ValueError):
+            pass
+        assert c.table.tolist() == rows(c) and c.lens.tolist() == c._len
+
+
+def test_a_change_sends_what_changed(monkeypatch):
+    """The rows of other sequences, marked here, are not written again."""
+    Copies(monkeypatch)
+    c = cache()
+    a, b = c.open(15), c.open(9)
+    mark = 77
+    c.table[a] = mark
+    c.reserve([b])
+    c.advance([b])
+    c.free(c.fork(b))
+    for _ in range(7):
+        c.reserve([b])                                   # the last one takes a page
+        c.advance([b])
+    assert c.table[a].tolist() == [mark] * 5 and c.table[b].tolist() == c.pages(b) + [-1] * 2 and c.length(b) == 17
+    sent = []
+    monkeypatch.setattr(c, "_send", lambda numbers, dtype, send=c._send: sent.append(len(numbers)) or send(numbers, dtype))
+    c.advance([a])
+    c.reserve([b])
+    assert sent == []                                    # lengths alone
+    c.reserve([a])
+    assert sent == [1, 1] and c.table[a].tolist() == [mark, mark, c.pages(a)[2], mark, mark]
+
+
+def test_a_change_that_the_device_has_no_memory_for_is_none(monkeypatch):
+    Copies(monkeypatch)
+    c = cache()
+    a, b = c.open(16), c.open(3)
+    before = (list(c._held), list(c._free), [list(p or []) for p in c._pages], list(c._len), c.table.tolist(), c.lens.tolist())
+
+    def fail(*_):
+        raise torch.OutOfMemoryError("none left")
+    monkeypatch.setattr(c, "_send", fail)
+    for call in (lambda: c.open(9), lambda: c.fork(a), lambda: c.fork(b), lambda: c.reserve([a, b]), lambda: c.free(a)):
+        with pytest.raises(torch.OutOfMemoryError):
+            call()
+        assert before == (c._held, c._free, [list(p or []) for p in c._pages], c._len, c.table.tolist(), c.lens.tolist())
+
+
+@gpu
+def test_a_step_waits_for_nothing():
+    """Bookkeeping behind 50 large products returns while they run, and takes its place behind them."""
+    c = PagedCache(300, 8, 2, 64, 40, 512)
+    seqs = [c.open(7) for _ in range(32)]
+    x = torch.randn(8192, 8192, device="cuda", dtype=torch.bfloat16)
+    y = torch.empty_like(x)
+    torch.mm(x, x, out=y)
+    c.advance(seqs)
+    c.free(seqs.pop())
+    torch.cuda.synchronize()
+    done = torch.cuda.Event()
+    for _ in range(50):
+        torch.mm(x, x, out=y)
+    done.record()
+    was = c.table.clone(), c.lens.clone()                # read behind the products, in front of the changes
+    c.reserve(seqs)
+    c.advance(seqs)
+    new = c.open(20)
+    c.fork(new)
+    c.free(seqs.pop(0))
+    assert not done.query()
+    torch.cuda.synchronize()
+    assert was[0][1].tolist() == [1] + [-1] * 511 and was[1].tolist() == [8] * 31 + [-1] * 9
+    assert c.table.tolist() == rows(c) and c.lens.tolist() == c._len and c._len[new] == 20
