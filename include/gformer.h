@@ -308,7 +308,7 @@ typedef struct gformer_packed_params {
   int32_t dtype;          /* gf_dtype of all tensors but lse                                 */
   int32_t zero_tail;      /* 0: rows behind the last sequence (of out; dq; dk, dv) are left  */
                           /* as they were.  1: they are set to zero (lse never is)           */
-  float softmax_scale;    /* multiplies q.k; any finite value                                */
+  float softmax_scale;    /* multiplies q.k; of magnitude 2^127 at most                      */
   int64_t q_stride[2], k_stride[2], v_stride[2], o_stride[2]; /* (row, head) element strides  */
   int64_t do_stride[2], dq_stride[2], dk_stride[2], dv_stride[2]; /* gformer_packed_attn_bwd */
 } gformer_packed_params;
@@ -351,7 +351,7 @@ typedef struct gformer_paged_params {
   uint32_t struct_size;   /* = sizeof(gformer_paged_params)                                  */
   int32_t dtype;          /* gf_dtype of all tensors                                         */
   int32_t page_size;      /* tokens per page                                                 */
-  float softmax_scale;    /* gformer_paged_decode: multiplies q.k; any finite value          */
+  float softmax_scale;    /* gformer_paged_decode: multiplies q.k; 2^127 at most, as above   */
   int64_t q_stride[2], o_stride[2]; /* (sequence, head); gformer_paged_decode                */
   int64_t k_stride[2], v_stride[2]; /* (sequence, head) or, in gformer_paged_fill, (row, head) */
   int64_t kpage_stride[3], vpage_stride[3]; /* (page, head, token)                           */

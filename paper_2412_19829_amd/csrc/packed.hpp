@@ -137,6 +137,10 @@ __device__ __forceinline__ SeqTile ranked_tile(const int32_t* cu, int total, con
   return {seq, tile * R};
 }
 
+// What scores are multiplied by for base-2 exponents, without the scale's sign.  Not let down to zero, where a masked score (-infinity)
+// would lose its weight of zero: the smallest number in its place changes no exponent by more than 5e-7.
+__device__ __forceinline__ float base2_scale(float scale) { return fmaxf(fabsf(scale) * kLog2e, 0x1p-149f); }
+
 // Offsets of a pointer of either element type.
 template <typename T> __device__ __forceinline__ const T* rows_of(const void* p, const int64_t (&st)[2], int64_t row, int head) {
   return reinterpret_cast<const T*>(p) + row * st[0] + head * st[1];

@@ -13,6 +13,8 @@ namespace {
 constexpr int64_t kMaxTokenStride = 1 << 20;   // elements
 constexpr int64_t kMaxCached = 1 << 30;        // tokens of one sequence, or rows of a packed tensor
 
+// Scales that stay finite as factors of base-2 exponents.
+bool scale_fits(float scale) { return fabsf(scale) <= 0x1p127f; }
 bool misaligned(uintptr_t all, unsigned bytes) { return (all & (bytes - 1)) != 0; }
 template <typename... P> uintptr_t bits(P... p) { return (0 | ... | (uintptr_t)p); }
 
@@ -61,7 +63,7 @@ gf_status check_heads(int dtype, int H, int Hkv, int d) {
 gf_status check_packed(bool backward, int n_seqs, int total_q, int total_k, int H, int Hkv, int d, const gformer_packed_params* p,
                        PackedArgs* a) {
   if (!p || p->struct_size != sizeof(gformer_packed_params)) return GF_ERR_INVALID_ARG;
-  if (n_seqs < 0 || total_q < 0 || total_k < 0 || !isfinite(p->softmax_scale) || (p->zero_tail != 0 && p->zero_tail != 1))
+  if (n_seqs < 0 || total_q < 0 || total_k < 0 || !scale_fits(p->softmax_scale) || (p->zero_tail != 0 && p->zero_tail != 1))
     return GF_ERR_INVALID_ARG;
   gf_status st = check_heads(p->dtype, H, Hkv, d);
   if (st != GF_OK) return st;
@@ -230,7 +232,7 @@ gf_status gformer_paged_decode(const void* q, const void* k, const void* v, void
   gf_status st = check_paged(Hkv, d, n_pages, p, &a.shift, a.kps, a.vps);
   if (st != GF_OK) return st;
   if ((st = check_heads(p->dtype, H, Hkv, d)) != GF_OK) return st;
-  if (B < 0 || !isfinite(p->softmax_scale)) return GF_ERR_INVALID_ARG;
+  if (B < 0 || !scale_fits(p->softmax_scale)) return GF_ERR_INVALID_ARG;
   if ((st = check_table(table_width, a.shift, max_len, &a.room)) != GF_OK) return st;
   if ((st = strides2(p->q_stride, a.qs, H, d)) != GF_OK || (st = strides2(p->k_stride, a.ks, Hkv, d)) != GF_OK ||
       (st = strides2(p->v_stride, a.vs, Hkv, d)) != GF_OK || (st = strides2(p->o_stride, a.os, H, d)) != GF_OK)

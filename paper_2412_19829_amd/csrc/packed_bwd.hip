@@ -136,7 +136,7 @@ template <typename T, int D, typename F> __global__ __launch_bounds__(F::THREADS
   const int64_t stat = (int64_t)h * a.total_q + qbase + ic;
   const float lse = a.lse[stat] * kLog2e;
   if (stream == 0 && i < nq) a.stats[stat + (lh ? (int64_t)a.H * a.total_q : 0)] = lh ? -delta : lse;
-  const float sc = fmaxf(fabsf(a.scale), 1e-30f) * kLog2e;
+  const float sc = base2_scale(a.scale);
 
   f32x16 dq[MT];
 
@@ -261,7 +261,7 @@ template <typename T, int D, typename F> __global__ __launch_bounds__(F::THREADS
   T* const own_v = all.v + (kValuesInLds<T, D> ? wave * 32 * D : 0);
   if constexpr (kValuesInLds<T, D>)
     if (stream == 0) P::to_lds(v, own_v, lane);   // read behind the first barrier
-  const float sc = fmaxf(fabsf(a.scale), 1e-30f) * kLog2e;
+  const float sc = base2_scale(a.scale);
 
   f32x16 dk[MT], dv[MT];
 

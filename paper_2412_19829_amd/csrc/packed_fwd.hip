@@ -65,9 +65,8 @@ template <typename T, int D, typename F> __global__ __launch_bounds__(F::THREADS
   const int i = q0 + ln, seen = min(i, nq - 1) + off;   // this lane's query sees keys 0 .. seen
   typename P::Resident q;
   P::load(q, rows_of<T>(a.q, a.qs, qbase + min(i, nq - 1), h), lane, a.scale < 0.f);
-  // base-2 exponents are score * sc, the scale's sign is in q; which is not let down to zero, where a masked
-  // score would lose its weight of zero
-  const float sc = fmaxf(fabsf(a.scale), 1e-30f) * kLog2e;
+  // base-2 exponents are score * sc, the scale's sign is in q
+  const float sc = base2_scale(a.scale);
 
   f32x16 o[MT];
   float m, l;   // running maximum (base 2) and this half's share of the sum

@@ -582,3 +582,27 @@ def test_dense_rows_are_as_long_as_strided_ones_may_be():
     p = gb.make_packed_params()
     assert gb.gformer_packed_attn_bwd_workspace_bytes(3, 3, 1, 1 << 14, 1 << 14, 64, p) > 0
     assert gb.gformer_packed_attn_bwd_workspace_bytes(3, 3, 1, (1 << 14) + 1, (1 << 14) + 1, 64, p) == 0
+
+
+def test_scales_that_overflow_are_refused():
+    for x in (3e38, -3e38, NAN, -INF):
+        assert fwd(p=wrong(softmax_scale=x)) == bwd(p=wrong(softmax_scale=x), ws=0) == gb.GF_ERR_INVALID_ARG
+    for x in (2.0 ** 127, -2.0 ** 127, 0.0, 1e-40):      # refused for the workspace alone
+        assert bwd(p=wrong(softmax_scale=x), ws=0) == 3
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("H", [2, 96])
+def test_small_scales_of_large_scores(dtype, d, H):
+    """Powers of two move from the scale to the queries and keys: the same exponents, so the same bits, and gradients
+    that are those times a power of two."""
+    lens, by = [70, 200], 2.0 ** 57
+    q, k, v, g = tensors(lens, lens, H, H, d, dtype, 61)
+    want = run(q, k, v, g, lens, lens, 0.125)
+    got = run(q * by, k * by, v, g, lens, lens, 0.125 / by / by)
+    for name in ("out", "lse", "dv"):
+        assert torch.equal(got[name], want[name]), name
+    for name in ("dq", "dk"):
+        assert torch.equal(got[name].float() * by, want[name].float()), name

@@ -628,3 +628,19 @@ def test_a_step_waits_for_nothing():
     torch.cuda.synchronize()
     assert was[0][1].tolist() == [1] + [-1] * 511 and was[1].tolist() == [8] * 31 + [-1] * 9
     assert c.table.tolist() == rows(c) and c.lens.tolist() == c._len and c._len[new] == 20
+
+
+def test_scales_that_overflow_are_refused():
+    assert all(decode(p=wrong(softmax_scale=x), width=64, ws=0) == 1 for x in (3e38, -3e38, NAN, float("inf")))
+    assert all(decode(p=wrong(softmax_scale=x), width=64, ws=0) == 3 for x in (2.0 ** 127, -2.0 ** 127, 0.0, 1e-40))
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_small_scales_of_large_scores(dtype):
+    x, _, _ = make([40, 300], 4, 2, 64, 16, dtype, 3, fill=0.0)
+    y = {n: t.clone() for n, t in x.items()}             # each step writes its token into pages of its own
+    want, by = step(x, 0.125), 2.0 ** 57
+    for n in ("q", "k", "kpages"):
+        y[n] = y[n] * by
+    assert torch.equal(step(y, 0.125 / by / by), want)
