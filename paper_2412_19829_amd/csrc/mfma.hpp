@@ -61,18 +61,14 @@ __device__ __forceinline__ float dot2_ones_bf16(uint32_t a, float acc) {
   return dot2_bf16(a, kOnesBf16x2, acc);
 }
 
-// max(a, b, c) / min(a, b, c) in one instruction.  The library forms never see a NaN here (scores
-// are finite or the infinity a mask put there), and written this way the compiler does not add
-// the quieting moves it puts in front of every fmaxf / fminf.
+// max(a, b, c) / min(a, b, c) in one instruction (v_maximum3_f32, v_minimum3_f32: what is no number stays none), without the quieting
+// moves that the compiler puts in front of every fmaxf / fminf.  Not as asm statements: the compiler, which knows how long
+// after a matrix instruction its result may be read, does not see the reader there.
 __device__ __forceinline__ float max3(float a, float b, float c) {
-  float r;
-  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-  return r;
+  return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c);
 }
 __device__ __forceinline__ float min3(float a, float b, float c) {
-  float r;
-  asm("v_min3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-  return r;
+  return __builtin_elementwise_minimum(__builtin_elementwise_minimum(a, b), c);
 }
 
 // Lanes l and l^32 exchange a value (v_permlane32_swap): `a` and `b` come back as the lane's own
