@@ -543,6 +543,13 @@ def _row_strides(name, t):
     return out[::-1]
 
 
+def _sizes(**sizes):
+    """Numbers that the library takes as int: ctypes would hand over what is left of larger ones."""
+    for name, n in sizes.items():
+        if not -1 << 31 <= n < 1 << 31:
+            raise ValueError(f"{name}: {n} does not fit 32 bits")
+
+
 def _tensors(like, n_dims, **tensors):
     """Device tensors of one type, one device and `n_dims` dimensions."""
     import torch
@@ -550,6 +557,7 @@ def _tensors(like, n_dims, **tensors):
     if like.dtype not in (torch.bfloat16, torch.float32):
         raise ValueError(f"unsupported dtype {like.dtype}")
     for name, t in tensors.items():
+        _sizes(**{name: max(t.shape, default=0)})
         if not t.is_cuda:
             raise ValueError(f"{name} must be a device tensor: there is no CPU path")
         if t.dtype != like.dtype or t.device != like.device:
@@ -564,6 +572,7 @@ def _numbers(like, shape, **tensors):
     import torch
 
     for name, t in tensors.items():
+        _sizes(**{name: max(t.shape, default=0)})
         if not t.is_cuda or t.device != like.device or t.dtype != torch.int32 or not t.is_contiguous():
             raise ValueError(f"{name} must be a dense int32 tensor on the device of the others")
         if t.dim() != len(shape) or any(n is not None and n != x for n, x in zip(shape, t.shape)):
@@ -692,6 +701,7 @@ def gformer_packed_attn_fwd(q, k, v, out, cu_q, cu_k=None, *, lse=None, out_rest
 
 
 def gformer_packed_attn_bwd_workspace_bytes(total_q, total_k, n_seqs, H, Hkv, d, params=None) -> int:
+    _sizes(total_q=total_q, total_k=total_k, n_seqs=n_seqs, H=H, Hkv=Hkv, d=d)
     return int(lib().gformer_packed_attn_bwd_workspace_bytes(total_q, total_k, n_seqs, H, Hkv, d,
                                                              ctypes.byref(params or make_packed_params())))
 
@@ -729,6 +739,7 @@ def gformer_paged_decode_workspace_bytes(B, H, Hkv, d, max_len, params=None, tab
     p = params or make_paged_params()
     if table_width is None:
         table_width = -(-max_len // p.page_size)
+    _sizes(B=B, H=H, Hkv=Hkv, d=d, max_len=max_len, table_width=table_width)
     return int(lib().gformer_paged_decode_workspace_bytes(B, H, Hkv, d, table_width, max_len, ctypes.byref(p)))
 
 

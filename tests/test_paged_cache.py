@@ -644,3 +644,26 @@ def test_small_scales_of_large_scores(dtype):
     for n in ("q", "k", "kpages"):
         y[n] = y[n] * by
     assert torch.equal(step(y, 0.125 / by / by), want)
+
+
+def test_numbers_past_32_bits_are_refused():
+    """... not cut to what is left of them: a bound of 2^32 + 5 tokens, say, to one of 5."""
+    b = gb.gformer_paged_decode_workspace_bytes
+    for kw in (dict(max_len=2 ** 32 + 5, table_width=4), dict(max_len=-2 ** 32, table_width=4), dict(max_len=5, table_width=2 ** 32 + 4)):
+        with pytest.raises(ValueError, match="32 bits"):
+            b(1, 4, 2, 64, **kw)
+    with pytest.raises(ValueError, match="n_seqs"):
+        gb.gformer_packed_attn_bwd_workspace_bytes(8, 8, 2 ** 32 + 1, 2, 2, 64)
+    meta = lambda *shape, dtype=torch.int32: torch.empty(*shape, dtype=dtype, device="meta")
+    with pytest.raises(ValueError, match="table"):
+        gb._numbers(meta(1), (1, None), table=meta(1, 2 ** 32 + 4))
+    with pytest.raises(ValueError, match="kpages"):
+        gb._tensors(meta(1, dtype=torch.bfloat16), 4, kpages=meta(2 ** 31, 1, 8, 64, dtype=torch.bfloat16))
+
+
+@gpu
+def test_a_bound_past_32_bits_is_refused():
+    x, _, _ = make([40], 4, 2, 64, 16, "bf16", 3)
+    for bound in (2 ** 32, 2 ** 32 + 5):
+        with pytest.raises(ValueError, match="max_len"):
+            step(x, 0.125, max_len=bound)
