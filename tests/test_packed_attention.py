@@ -606,3 +606,24 @@ def test_small_scales_of_large_scores(dtype, d, H):
         assert torch.equal(got[name], want[name]), name
     for name in ("dq", "dk"):
         assert torch.equal(got[name].float() * by, want[name].float()), name
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("H,Hkv", [(4, 2), (128, 32)])
+@pytest.mark.parametrize("n", [32, 33, 90])
+def test_long_sequences_among_many_short_ones(dtype, H, Hkv, n):
+    """Up to 32 sequences are taken in order of falling work, more in the tensors' order: tiles behind a sequence's first in both, at
+    either end and in the middle, with prompts that go on behind keys and rows behind the last one."""
+    lens_q = [(3 * i) % 4 for i in range(n)]
+    lens_q[0], lens_q[n // 2], lens_q[n - 2], lens_q[n - 1] = 300, 513, 129, 65
+    lens_k = list(lens_q)
+    lens_k[1], lens_k[n // 2], lens_k[n // 3], lens_k[n - 2] = 400, 700, 260, 90
+    q, k, v, g = tensors(lens_q, lens_k, H, Hkv, 128, dtype, n + H, tail=150)
+    for x, rows in ((q, sum(lens_q)), (g, sum(lens_q)), (k, sum(lens_k)), (v, sum(lens_k))):
+        x[rows:] = NAN
+    got = run(q, k, v, g, lens_q, lens_k, 0.09, zero_tail=1, rest=True)
+    nq, nk = sum(lens_q), sum(lens_k)
+    compare(got, ref.packed(q[:nq], k[:nk], v[:nk], g[:nq], lens_q, lens_k, 0.09, dtype), lens_q, lens_k)
+    for name, rows in (("out", nq), ("dq", nq), ("dk", nk), ("dv", nk)):
+        assert not got[name][rows:].any(), name
