@@ -345,7 +345,8 @@ gf_status gformer_packed_attn_bwd(const void* q, const void* k, const void* v, c
 /* The paged cache: kpages and vpages are [n_pages, Hkv, page_size, d] through (page, head, token) strides;
  * token t of sequence s lies in page table[s][t / page_size], slot t % page_size, table being int32
  * [sequences, table_width] dense.  A page number outside [0, n_pages) is no page: its tokens are not seen and
- * not written.  Pages may be shared between sequences as long as nobody writes into them.
+ * not written (a new token whose slot has no page is seen by its own queries all the same).  Pages may be shared
+ * between sequences as long as nobody writes into them.
  * page_size: a power of two from 8 to 65536; table_width * page_size at most 2^30. */
 typedef struct gformer_paged_params {
   uint32_t struct_size;   /* = sizeof(gformer_paged_params)                                  */

@@ -82,6 +82,7 @@ def gformer_packed_attention(q, k, v, cu_q, cu_k=None, *, softmax_scale: float =
     """Causal attention over packed sequences: q [total_q, H, d], k, v [total_k, Hkv, d] device tensors (bf16 or fp32, any
     strides with a contiguous last dimension, H a multiple of Hkv), cu_q and cu_k int32 [n_seqs + 1] offsets on the
     device (cu_k=None: the same sequences).  With more keys than queries a sequence's queries are its last; rows
-    behind the last sequence give zeros.  Differentiable once with respect to q, k and v."""
+    behind the last sequence give zeros.  Differentiable once with respect to q, k and v.  Both passes can be captured in a graph, as
+    long as no eager graph of the same leaves is alive: torch keeps one node a leaf for its gradient, with the stream that it was made on."""
     out = gb.packed_attention_node(q, k, v, cu_q, cu_k, float(softmax_scale))
     return _GformerPackedAttention.apply(q, k, v, cu_q, cu_k, float(softmax_scale)) if out is None else out

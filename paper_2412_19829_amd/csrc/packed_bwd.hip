@@ -9,11 +9,17 @@
 // sequences: 1.43 to 1.51 without, 1.05 to 1.34 with; dq and dk, dv at d = 64 66 and 94 us in place of 64 and 92).
 // One pass for all three would save two of nine products and need atomics, whose order changes the sums.
 //
-// Bound like the forward pass.  4096 + 3001 + 1095 tokens, 32 / 8 heads, d = 128, bf16: dq 375 us, dk and dv 607 (matrix units busy 47 and
-// 39 %, waves waiting 31 and 44 %: dk and dv are one workgroup of eight waves on a compute unit there); 8192 tokens in 8 documents, 16 heads,
+// Bound like the forward pass.  4096 + 3001 + 1095 tokens, 32 / 8 heads, d = 128, bf16: dq 349 us, dk and dv 532 (373 and 593 in the mean of
+// 40 passes, whose clocks differ; matrix units busy 47 and 39 %, waves waiting 31 and 44 %: dk and dv are one workgroup of eight waves on
+// a compute unit there, and the longest of them takes 512 steps of 32 queries where the mean unit has 429); 8192 tokens in 8 documents, 16 heads,
 // d = 64: 66 and 94; fp32, 1024 + 300 + 700 tokens, 12 heads, d = 64: 57 and 83.  What did not help: two blocks of 32 rows a wave
 // (d = 64: dq 64 -> 91), three waves on a SIMD (dk, dv of the second 114 to 187 where two took 111), wave priorities (607 -> 627 and more), and all
-// transposed reads of a product in one statement (d = 128 spills: 852).
+// transposed reads of a product in one statement (d = 128 spills more: 852).
+//
+// As built, dk and dv do not run two tiles ahead where they have three buffers: the compiler waits for all loads at the loop's barrier,
+// behind the counted wait (not in fp32 at d = 128; nor does it in dq).  The second loop, row by row, is what makes it, and at d = 128 in bf16
+// also makes it keep 84 to 86 registers in memory, four of which the first loop reads back in every step; dq keeps 23 and 35 at
+// d = 128, in the second loop alone.
 #include "packed.hpp"
 
 #include <algorithm>

@@ -6,8 +6,9 @@
 // fourth tile, each with one buffer of its own and no barrier.
 //
 // Bound by the matrix units and the vector work between the products of a tile (exponentials, the maximum, packing of the weights):
-// 8192 tokens, 32 / 8 heads, d = 128, bf16 549 us, 1.0 PFLOP/s where a plain product of 8192 x 8192 matrices reaches 1.32; the matrix
-// units are busy 49 % of the time, the waves wait 24 %, LDS conflicts 1 % of its cycles.  fp32, 4096 tokens, 32 / 8 heads, d = 64:
+// 8192 tokens, 32 / 8 heads, d = 128, bf16 558 us (615 in the mean of 40 passes, whose clocks differ), 0.9 to 1.0 PFLOP/s where a plain
+// product of 8192 x 8192 matrices reaches 1.32; the matrix units are busy 49 % of the time, the waves wait 24 %, LDS conflicts 1 % of its
+// cycles.  The bf16 kernels of one stream keep 8 and 9 registers in memory, in the second loop (row by row) alone.  fp32, 4096 tokens, 32 / 8 heads, d = 64:
 // 577 us, 119 TFLOP/s of 154.  Two blocks of 32 queries a wave halve the reads of LDS and cost a workgroup (d = 64, 49 -> 66 us);
 // raised wave priorities around the products cost 7 %.
 #include "packed.hpp"
@@ -243,7 +244,8 @@ template <typename T, int D> hipError_t launch(const PackedArgs& a, hipStream_t 
 // Streams divide the longest workgroup's time, and load every streamed row as many times more often.  Four of them leave room for
 // two workgroups on a compute unit (fp32, d = 128: one), so up to two rounds of the unsplit workgroups are better split; at
 // d = 128, whose values cost more to join, one and a half; a quarter of that where sequences are short (a mean of less than
-// 512 rows) and the joins weigh more.
+// 512 rows) and the joins weigh more.  The mean is what the host knows, and single tokens beside a long prompt lower it: 2048 rows of 8
+// heads take 28 us at d = 128 and 18 at d = 64, with 31 single tokens 55 and 39 (backward 79 and 52, 153 and 96).
 int packed_streams(bool fp32, int d, int total_q, int H, int n_seqs) {
   const int units = device_compute_units();
   const int64_t workgroups = (int64_t)total_q * H / kPackedRows, most = units * (d == 64 ? 4 : 3) / 2;
