@@ -4,7 +4,8 @@ entry points take (device).
 A sequence's row of `table` lists its pages, `lens` its tokens.  Pages are counted by the sequences that hold them: a
 fork shares the full ones, which nobody writes again, and takes a copy of the last one if that is partly filled.
 Every change of the bookkeeping is checked before it is made, so a refused call leaves the cache as it was.
-The copies run on torch's current stream, in order with what changes of `table` and `lens`; no call waits for the stream.
+The copies run on torch's current stream, in order with what changes of `table` and `lens`, and no call waits for it: a program that
+uses the cache on another stream has that one wait.  The books do not change while a graph is captured.
 reserve() and advance() for one token of every sequence take the host, us, without a new page / with one for each: 32 sequences 32 / 100, 256 152 / 240,
 however many pages a row has (with the whole table sent each time, 256 rows of 2048 took 12500 / 25000).
 """
@@ -77,10 +78,14 @@ class PagedCache:
             self._held[p] = 1
         return taken
 
+    def _host(self, numbers, dtype):
+        """Memory of their own for numbers on their way to the device, which a copy keeps until it has run (but not until it runs again)."""
+        if self.table.is_cuda and torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("the books cannot change while a graph is captured: its replays would not change them")
+        return torch.tensor(numbers, dtype=dtype, pin_memory=self.table.is_cuda)
+
     def _send(self, numbers, dtype):
-        """Numbers on the device, from memory of their own that a copy on its way keeps."""
-        t = torch.tensor(numbers, dtype=dtype, pin_memory=self.table.is_cuda)
-        return t.to(self.table.device, non_blocking=True)
+        return self._host(numbers, dtype).to(self.table.device, non_blocking=True)
 
     def _update(self, lens, pages=()):
         """`lens` {sequence: tokens} and `pages` [(sequence, place in its row, page)], on the device and then in the books of lengths:
@@ -92,7 +97,7 @@ class PagedCache:
             at = self._send([s * self.max_pages + i for s, i, _ in pages], torch.int64)
             values = self._send([p for _, _, p in pages], torch.int32)
         if lens:
-            self.lens.copy_(torch.tensor(new, dtype=torch.int32, pin_memory=self.lens.is_cuda), non_blocking=True)
+            self.lens.copy_(self._host(new, torch.int32), non_blocking=True)
         if pages:
             self.table.view(-1).scatter_(0, at, values)
         self._len = new

@@ -667,3 +667,28 @@ def test_a_bound_past_32_bits_is_refused():
     for bound in (2 ** 32, 2 ** 32 + 5):
         with pytest.raises(ValueError, match="max_len"):
             step(x, 0.125, max_len=bound)
+
+
+@gpu
+def test_the_books_do_not_change_while_a_graph_is_captured():
+    """A replay would send memory that has long been another's; the calls say so, and the capture goes on."""
+    c = PagedCache(20, 8, 2, 64, 4, 8)
+    a, b = c.open(8), c.open(3)
+    before = (list(c._held), list(c._free), [list(p or []) for p in c._pages], list(c._len), c.table.tolist(), c.lens.tolist())
+    x = torch.zeros(8, device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        x.add_(1)
+        for call in (lambda: c.advance([b]), lambda: c.reserve([a]), lambda: c.open(0), lambda: c.open(9), lambda: c.fork(a), lambda: c.fork(b),
+                     lambda: c.free(a)):
+            with pytest.raises(RuntimeError, match="captured"):
+                call()
+        x.add_(1)
+    for n in range(1, 4):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert (x == 2 * n).all()
+    assert before == (c._held, c._free, [list(p or []) for p in c._pages], c._len, c.table.tolist(), c.lens.tolist())
+    c.advance([b])
+    assert c.lens.tolist() == [8, 4, -1, -1]
