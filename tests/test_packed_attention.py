@@ -627,3 +627,35 @@ def test_long_sequences_among_many_short_ones(dtype, H, Hkv, n):
     compare(got, ref.packed(q[:nq], k[:nk], v[:nk], g[:nq], lens_q, lens_k, 0.09, dtype), lens_q, lens_k)
     for name, rows in (("out", nq), ("dq", nq), ("dk", nk), ("dv", nk)):
         assert not got[name][rows:].any(), name
+
+
+@gpu
+def test_the_largest_launch():
+    """One-token sequences, as many as a launch of 32 heads holds (n tiles, n / 128 and 1 for those that straddle, 32 heads, 256 threads): a row
+    gives its value, and a value's gradient is its row's.  The next one is refused."""
+    H, d, n = 32, 64, 520222
+    assert (n + n // 128 + 1) * H * 256 < 2 ** 32 <= (n + 1 + (n + 1) // 128 + 1) * H * 256
+    gen = torch.Generator("cuda").manual_seed(81)
+    q, k, v, g = (torch.randn(n + 1, H, d, device="cuda", generator=gen, dtype=torch.bfloat16) for _ in range(4))
+    out, rest, dq, dk, dv = (torch.full_like(q, 7.0) for _ in range(5))
+    lse = torch.empty(H, n, device="cuda")
+    starts = torch.arange(n + 2, dtype=torch.int32, device="cuda")
+    cut = [x[:n] for x in (q, k, v, out)]
+    gb.gformer_packed_attn_fwd(*cut, starts[:n + 1], lse=lse, out_rest=rest[:n], softmax_scale=0.125)
+    gb.gformer_packed_attn_bwd(*cut, lse, g[:n], dq[:n], dk[:n], dv[:n], starts[:n + 1], out_rest=rest[:n], softmax_scale=0.125)
+    torch.cuda.synchronize()
+    assert torch.equal(out[:n], v[:n]) and torch.equal(dv[:n], g[:n])
+    # The one weight is exp2(x - m), m the rounding of the same x: 1 but for half a step of x in base 2, which is |score| U of the weight, and
+    # exp2's own step.  The product sees it rounded to bf16, 1, the sum as it is: out is v / sum, whose reciprocal, product and
+    # difference to v add a step each, and rest rounds what is left
+    score = 0.125 * (q[:n].float() * k[:n].float()).sum(-1, keepdim=True).abs()
+    assert (rest[:n].float().abs() <= ref.U * (score + 8) * v[:n].float().abs()).all()
+    del score
+    # a score of 64 products: 68 roundings and the exponent's few, against fp64 on some rows
+    at = torch.tensor([0, 1, 77777, n - 2, n - 1], device="cuda")
+    s = 0.125 * (q[at].double() * k[at].double()).sum(-1)
+    bound = ref.U * (68 * 0.125 * (q[at].double() * k[at].double()).abs().sum(-1) + 8 * s.abs() + 16)
+    assert ((lse[:, at].T.double() - s).abs() <= bound).all()
+    assert all((x[n:] == 7.0).all() for x in (out, rest, dq, dk, dv))
+    with pytest.raises(gb.GformerError, match="status 2"):
+        gb.gformer_packed_attn_fwd(q, k, v, out, starts, softmax_scale=0.125)

@@ -692,3 +692,26 @@ def test_the_books_do_not_change_while_a_graph_is_captured():
     assert before == (c._held, c._free, [list(p or []) for p in c._pages], c._len, c.table.tolist(), c.lens.tolist())
     c.advance([b])
     assert c.lens.tolist() == [8, 4, -1, -1]
+
+
+@gpu
+def test_the_largest_launch():
+    """As many rows of 32 heads as a launch holds, three of them in use."""
+    H, d, page, B = 32, 64, 8, (2 ** 32 - 1) // 256 // 32
+    gen = torch.Generator("cuda").manual_seed(82)
+    q, k, v = (torch.randn(B, H, d, device="cuda", generator=gen, dtype=torch.bfloat16) for _ in range(3))
+    kp, vp = (torch.randn(3, H, page, d, device="cuda", generator=gen, dtype=torch.bfloat16) for _ in range(2))
+    rows, lens = [0, 300000, B - 1], [0, 7, 4]
+    table = torch.full((B, 1), -1, dtype=torch.int32, device="cuda")
+    held = torch.full((B,), -1, dtype=torch.int32, device="cuda")
+    for i, (b, n) in enumerate(zip(rows, lens)):
+        table[b, 0], held[b] = i, n
+    ks, vs = ([x[i, :, :n].transpose(0, 1).cpu() for i, n in enumerate(lens)] for x in (kp, vp))
+    out = torch.full_like(q, 7.0)
+    gb.gformer_paged_decode(q, k, v, out, kp, vp, table, held, softmax_scale=0.125)
+    torch.cuda.synchronize()
+    ref.check(out[rows], *expect(dict(q=q[rows], k=k[rows], v=v[rows], lens=held[rows].cpu()), ks, vs, 0.125, "bf16"), "out")
+    out[rows] = 0
+    assert not out.any()
+    for i, (b, n) in enumerate(zip(rows, lens)):
+        assert torch.equal(kp[i, :, n], k[b]) and torch.equal(vp[i, :, n], v[b])
