@@ -394,6 +394,74 @@ gf_status gformer_pages_copy(void* kpages, void* vpages, const int32_t* src, con
                              int n_copies, int Hkv, int d, int n_pages, const gformer_paged_params* p,
                              void* hip_stream);
 
+/* The paged cache in 4 bits a value (5 with what goes beside them): pages, table, starts and lengths as above, but a row (one token of
+ * one head) is d / 2 + d / 8 bytes: first the codes, channel c in bits 4 (c % 2) .. 4 (c % 2) + 3 of byte c / 2, then for each 32
+ * channels a scale s and a lowest value l, both bf16.  Code n stands for l + s n.  Of a group's values x
+ *     l = the largest bf16 <= min x (zero: +0),   s = the smallest bf16 >= (max x - l) / 15,   n = the integer nearest (x - l) / s
+ * (of two as near the even one; n = 0 where s = 0), so that no value is off by more than s / 2.  A group with a value that is not finite, or
+ * of magnitude 2^127 or more, stands for values that are no number.  These calls take gformer_paged_params too:
+ * dtype is that of q, k, v and out; kpage_stride and vpage_stride are in BYTES, multiples of d / 8, all zero for dense
+ * [n_pages, Hkv, page_size, d / 2 + d / 8]. */
+
+/* gformer_paged_fill, quantising the rows. */
+gf_status gformer_paged_fill_q4(const void* k, const void* v, void* kpages, void* vpages,
+                                const int32_t* table, const int32_t* start, const int32_t* cu, int n_seqs,
+                                int total, int Hkv, int d, int n_pages, int table_width,
+                                const gformer_paged_params* p, void* hip_stream);
+
+/* The way back: row i of sequence s of k and v [total, Hkv, d] becomes what token start[s] + i stands for, rounded to dtype
+ * once (what a prompt that goes on behind cached tokens reads before gformer_packed_attn_fwd).  Tokens in front of 0, behind the
+ * table's end or of no page give zeros; rows behind the last sequence are left as they were. */
+gf_status gformer_paged_read_q4(const void* kpages, const void* vpages, void* k, void* v,
+                                const int32_t* table, const int32_t* start, const int32_t* cu, int n_seqs,
+                                int total, int Hkv, int d, int n_pages, int table_width,
+                                const gformer_paged_params* p, void* hip_stream);
+
+/* gformer_paged_decode over this cache.  The new token is seen as its slot holds it, quantised.  Scores and sums take the values
+ * that codes stand for unrounded; bf16 calls round the weights, times the values' scales, to bf16. */
+size_t gformer_paged_decode_q4_workspace_bytes(int B, int H, int Hkv, int d, int table_width, int max_len,
+                                               const gformer_paged_params* p);
+gf_status gformer_paged_decode_q4(const void* q, const void* k, const void* v, void* out, void* kpages,
+                                  void* vpages, const int32_t* table, const int32_t* lens, int B, int H,
+                                  int Hkv, int d, int n_pages, int table_width, int max_len,
+                                  const gformer_paged_params* p, void* workspace, size_t workspace_bytes,
+                                  void* hip_stream);
+
+/* gformer_pages_copy of this cache's pages. */
+gf_status gformer_pages_copy_q4(void* kpages, void* vpages, const int32_t* src, const int32_t* dst,
+                                int n_copies, int Hkv, int d, int n_pages, const gformer_paged_params* p,
+                                void* hip_stream);
+
+/* Rotary positions: pairs (a, b) of a head's first `rot` channels turn by the row's position,
+ *     (a, b) -> factor (a cos x - b sin x, b cos x + a sin x),   x = position * freqs[pair],
+ * the channels behind them are taken over.  Angles are taken in 64 bits (of magnitude 2^50 at most), products in 32, results are
+ * rounded once.  Conventions of the packed calls.
+ *   q, q_out : device [total, H, d], read / written; q_out may be q itself, with the same strides (in place)
+ *   k, k_out : device [total, Hkv, d], likewise; k NULL: queries alone (Hkv = 0)
+ *   freqs    : device fp32 [rot / 2], dense: any base and any stretching of the context is in them
+ *   positions: device int32 [total], the row's position, any number; or NULL for packed sequences:
+ *   cu, start: row i of sequence s, cu[s] .. cu[s+1]-1, is at start[s] + i (start NULL: i).  Rows behind the last
+ *              sequence are left as they were, or zero_tail = 1: set to zero.  NULL both where there are positions */
+typedef struct gformer_rotary_params {
+  uint32_t struct_size;   /* = sizeof(gformer_rotary_params)                                 */
+  int32_t dtype;          /* gf_dtype of q, k and their outputs                              */
+  int32_t rot;            /* channels that turn: a multiple of 16 from 16 to d               */
+  int32_t interleaved;    /* 0: pair i is channels i and i + rot / 2;  1: 2i and 2i + 1      */
+  int32_t inverse;        /* 1: by -x (with the same factor: the gradient's way back)        */
+  int32_t zero_tail;
+  float factor;           /* finite                                                          */
+  int32_t reserved0;      /* 0                                                               */
+  int64_t q_stride[2], k_stride[2], q_out_stride[2], k_out_stride[2]; /* (row, head)          */
+} gformer_rotary_params;
+
+/* struct_size set, dtype = GF_BF16, rot = 64, factor = 1, the rest zero */
+void gformer_rotary_params_init(gformer_rotary_params* p);
+
+gf_status gformer_rotary(const void* q, const void* k, void* q_out, void* k_out, const float* freqs,
+                         const int32_t* positions, const int32_t* cu, const int32_t* start, int n_seqs,
+                         int total, int H, int Hkv, int d, const gformer_rotary_params* p,
+                         void* hip_stream);
+
 /* Positive random features as a pre-map of Q or K for the linear heads.  Section III-A names
  * "positive orthogonal random features" for the linear part and Algorithm 1 "random feature
  * maps"; neither prints them, so the formula is the construction of the work they cite:

@@ -1,5 +1,5 @@
-"""The layer as a differentiable PyTorch operation (gformer_attn_fwd in forward, gformer_attn_bwd in backward), and
-attention over packed sequences likewise (gformer_packed_attn_fwd, gformer_packed_attn_bwd).
+"""The layer as a differentiable PyTorch operation (gformer_attn_fwd in forward, gformer_attn_bwd in backward), attention over
+packed sequences likewise (gformer_packed_attn_fwd, gformer_packed_attn_bwd), and rotary positions (gformer_rotary both ways).
 
 Plumbing only: tensors are allocated here (PyTorch is used for device memory and streams) and
 every arithmetic step runs in the HIP kernels behind the C ABI.  There is no CPU path.
@@ -86,3 +86,36 @@ def gformer_packed_attention(q, k, v, cu_q, cu_k=None, *, softmax_scale: float =
     long as no eager graph of the same leaves is alive: torch keeps one node a leaf for its gradient, with the stream that it was made on."""
     out = gb.packed_attention_node(q, k, v, cu_q, cu_k, float(softmax_scale))
     return _GformerPackedAttention.apply(q, k, v, cu_q, cu_k, float(softmax_scale)) if out is None else out
+
+
+class _GformerRotary(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, freqs, positions, cu, start, interleaved, inverse, factor):
+        ctx.save_for_backward(freqs, positions, cu, start)
+        ctx.set_materialize_grads(False)
+        ctx.how = (interleaved, inverse, factor)
+        # gradients may come in any layout, and one of the two not at all
+        x = [t if t is None or _fits(t) else t.clone(memory_format=torch.contiguous_format) for t in (q, k)]
+        out = [None if t is None else torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in x]
+        if x[0] is None:
+            gb.gformer_rotary(x[1], None, out[1], None, freqs, positions=positions, cu=cu, start=start, interleaved=interleaved,
+                              inverse=inverse, factor=factor, zero_tail=1)
+        else:
+            gb.gformer_rotary(x[0], x[1], out[0], out[1], freqs, positions=positions, cu=cu, start=start, interleaved=interleaved,
+                              inverse=inverse, factor=factor, zero_tail=1)
+        return tuple(out)
+
+    @staticmethod
+    def backward(ctx, dq, dk):
+        interleaved, inverse, factor = ctx.how
+        if dq is None and dk is None:
+            return (None,) * 9
+        dq, dk = _GformerRotary.apply(dq, dk, *ctx.saved_tensors, interleaved, 1 - inverse, factor)
+        return (dq, dk) + (None,) * 7
+
+
+def gformer_rotary_positions(q, k, freqs, *, positions=None, cu=None, start=None, interleaved: int = 0, factor: float = 1.0):
+    """Queries [total, H, d] and keys [total, Hkv, d] (None: queries alone) turned by their positions, as new tensors: see
+    binding.gformer_rotary for freqs and for positions, or cu and start.  Rows behind the last sequence give zeros.  Differentiable with
+    respect to q and k, any number of times: the gradients turn back.  Both ways can be captured in a graph."""
+    return _GformerRotary.apply(q, k, freqs, positions, cu, start, int(interleaved), 0, float(factor))

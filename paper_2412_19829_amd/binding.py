@@ -32,6 +32,8 @@ EXPORTS = ("gformer_params_init", "gformer_attn_workspace_bytes", "gformer_attn_
            "gformer_packed_params_init", "gformer_packed_attn_fwd", "gformer_packed_attn_bwd_workspace_bytes",
            "gformer_packed_attn_bwd", "gformer_paged_params_init", "gformer_paged_decode_workspace_bytes",
            "gformer_paged_decode", "gformer_paged_fill", "gformer_pages_copy",
+           "gformer_paged_fill_q4", "gformer_paged_read_q4", "gformer_paged_decode_q4_workspace_bytes", "gformer_paged_decode_q4",
+           "gformer_pages_copy_q4", "gformer_rotary_params_init", "gformer_rotary",
            "gformer_partition_balance", "gformer_partition_heads",
            "gformer_status_string", "gformer_version")
 
@@ -77,6 +79,13 @@ class GformerPagedParams(ctypes.Structure):
                 ("softmax_scale", ctypes.c_float),
                 *((f"{x}_stride", ctypes.c_int64 * 2) for x in ("q", "o", "k", "v")),
                 *((f"{x}_stride", ctypes.c_int64 * 3) for x in ("kpage", "vpage"))]
+
+
+class GformerRotaryParams(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("dtype", ctypes.c_int32), ("rot", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32), ("inverse", ctypes.c_int32), ("zero_tail", ctypes.c_int32),
+                ("factor", ctypes.c_float), ("reserved0", ctypes.c_int32)] + \
+        [(f"{n}_stride", ctypes.c_int64 * 2) for n in ("q", "k", "q_out", "k_out")]
 
 
 class GformerPartitionInputs(ctypes.Structure):
@@ -147,15 +156,22 @@ def lib():
         L.gformer_packed_attn_bwd.restype = ctypes.c_int
         L.gformer_packed_attn_bwd.argtypes = [ctypes.c_void_p] * 12 + [ctypes.c_int] * 6 + \
             [PP, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]
-        L.gformer_paged_decode_workspace_bytes.restype = ctypes.c_size_t
-        L.gformer_paged_decode_workspace_bytes.argtypes = [ctypes.c_int] * 6 + [GP]
-        L.gformer_paged_decode.restype = ctypes.c_int
-        L.gformer_paged_decode.argtypes = [ctypes.c_void_p] * 8 + [ctypes.c_int] * 7 + \
-            [GP, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]
-        L.gformer_paged_fill.restype = ctypes.c_int
-        L.gformer_paged_fill.argtypes = [ctypes.c_void_p] * 7 + [ctypes.c_int] * 6 + [GP, ctypes.c_void_p]
-        L.gformer_pages_copy.restype = ctypes.c_int
-        L.gformer_pages_copy.argtypes = [ctypes.c_void_p] * 4 + [ctypes.c_int] * 4 + [GP, ctypes.c_void_p]
+        for name, restype, argtypes in (
+                ("paged_decode{}_workspace_bytes", ctypes.c_size_t, [ctypes.c_int] * 6 + [GP]),
+                ("paged_decode{}", ctypes.c_int, [ctypes.c_void_p] * 8 + [ctypes.c_int] * 7 +
+                 [GP, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
+                ("paged_fill{}", ctypes.c_int, [ctypes.c_void_p] * 7 + [ctypes.c_int] * 6 + [GP, ctypes.c_void_p]),
+                ("pages_copy{}", ctypes.c_int, [ctypes.c_void_p] * 4 + [ctypes.c_int] * 4 + [GP, ctypes.c_void_p])):
+            for kind in ("", "_q4"):
+                entry = getattr(L, "gformer_" + name.format(kind))
+                entry.restype, entry.argtypes = restype, argtypes
+        L.gformer_paged_read_q4.restype = ctypes.c_int
+        L.gformer_paged_read_q4.argtypes = L.gformer_paged_fill_q4.argtypes
+        RP = ctypes.POINTER(GformerRotaryParams)
+        L.gformer_rotary_params_init.restype = None
+        L.gformer_rotary_params_init.argtypes = [RP]
+        L.gformer_rotary.restype = ctypes.c_int
+        L.gformer_rotary.argtypes = [ctypes.c_void_p] * 8 + [ctypes.c_int] * 5 + [RP, ctypes.c_void_p]
         L.gformer_partition_balance.restype = ctypes.c_int
         L.gformer_partition_balance.argtypes = [ctypes.POINTER(GformerPartitionInputs),
                                                 ctypes.POINTER(ctypes.c_double),
@@ -176,7 +192,8 @@ def lib():
 _native = None
 _module = None   # the extension module, or None where there is none
 _NATIVE = ("packed_attn_fwd", "packed_attn_bwd", "packed_attn_bwd_workspace_bytes", "paged_fill", "paged_decode",
-           "paged_decode_workspace_bytes", "pages_copy")
+           "paged_decode_workspace_bytes", "pages_copy", "paged_fill_q4", "paged_read_q4", "paged_decode_q4",
+           "paged_decode_q4_workspace_bytes", "pages_copy_q4", "rotary")
 
 
 def _decode_call():
@@ -734,13 +751,17 @@ def gformer_packed_attn_bwd(q, k, v, out, lse, dout, dq, dk, dv, cu_q, cu_k=None
     return dq, dk, dv
 
 
-def gformer_paged_decode_workspace_bytes(B, H, Hkv, d, max_len, params=None, table_width=None) -> int:
-    """For sequences of up to max_len tokens, the new one included (0: what a table of table_width pages holds)."""
+def _decode_bytes(entry, B, H, Hkv, d, max_len, params, table_width):
     p = params or make_paged_params()
     if table_width is None:
         table_width = -(-max_len // p.page_size)
     _sizes(B=B, H=H, Hkv=Hkv, d=d, max_len=max_len, table_width=table_width)
-    return int(lib().gformer_paged_decode_workspace_bytes(B, H, Hkv, d, table_width, max_len, ctypes.byref(p)))
+    return int(entry(B, H, Hkv, d, table_width, max_len, ctypes.byref(p)))
+
+
+def gformer_paged_decode_workspace_bytes(B, H, Hkv, d, max_len, params=None, table_width=None) -> int:
+    """For sequences of up to max_len tokens, the new one included (0: what a table of table_width pages holds)."""
+    return _decode_bytes(lib().gformer_paged_decode_workspace_bytes, B, H, Hkv, d, max_len, params, table_width)
 
 
 def _paged(like, kpages, vpages, Hkv, d):
@@ -751,16 +772,20 @@ def _paged(like, kpages, vpages, Hkv, d):
             "vpage_stride": _row_strides("vpages", vpages)}
 
 
-def gformer_paged_decode(q, k, v, out, kpages, vpages, table, lens, *, max_len=0, softmax_scale=1.0, workspace=None,
-                         stream: Optional[int] = None):
-    """One new token of every sequence over a paged cache, on device tensors: q, out [B, H, d]; k, v [B, Hkv, d], the new
-    keys and values, which go to their slots (both None: they are there already); kpages, vpages
-    [n_pages, Hkv, page_size, d] (any strides with a contiguous last dimension); table int32 [B, table_width]; lens int32
-    [B], the tokens in the cache before the call (negative: an idle row).  max_len bounds the longest
-    sequence's tokens, the new one included (0: what the table holds)."""
-    if _quick("paged_decode", ("paged_decode", "paged_decode_workspace_bytes"), q, k, v, out, kpages, vpages, table, lens, max_len,
-              softmax_scale, workspace, stream):
-        return out
+def _paged_q4(like, kpages, vpages, Hkv, d):
+    import torch
+
+    for name, t in (("kpages", kpages), ("vpages", vpages)):
+        _sizes(**{name: max(t.shape, default=0)})
+        if not t.is_cuda or t.device != like.device or t.dtype != torch.uint8:
+            raise ValueError(f"{name} must be an uint8 tensor on the device of the others")
+    if kpages.dim() != 4 or kpages.shape != vpages.shape or kpages.shape[1] != Hkv or kpages.shape[3] != d // 2 + d // 8:
+        raise ValueError("kpages and vpages must be [n_pages, Hkv, page_size, d / 2 + d / 8]")
+    return {"page_size": kpages.shape[2], "kpage_stride": _row_strides("kpages", kpages),
+            "vpage_stride": _row_strides("vpages", vpages)}
+
+
+def _paged_decode(entry, workspace_bytes, of_pages, q, k, v, out, kpages, vpages, table, lens, max_len, softmax_scale, workspace, stream):
     if (k is None) != (v is None):
         raise ValueError("k and v come together, or neither")
     new = {} if k is None else {"k": k, "v": v}
@@ -773,21 +798,18 @@ def gformer_paged_decode(q, k, v, out, kpages, vpages, table, lens, *, max_len=0
     _numbers(q, (B,), lens=lens)
     strides = {f"{n}_stride": _row_strides(n, t) for n, t in {"q": q, **new}.items()}
     p = make_paged_params(dtype, softmax_scale=softmax_scale, o_stride=_row_strides("out", out), **strides,
-                          **_paged(q, kpages, vpages, Hkv, d))
+                          **of_pages(q, kpages, vpages, Hkv, d))
     width = table.shape[1]
-    need = gformer_paged_decode_workspace_bytes(B, H, Hkv, d, max_len, p, width)
+    need = _decode_bytes(workspace_bytes, B, H, Hkv, d, max_len, p, width)
     workspace, at, held = _scratch(need, workspace, q, stream)
-    _call(lib().gformer_paged_decode, q, stream, q.data_ptr(), None if k is None else k.data_ptr(),
+    _call(entry, q, stream, q.data_ptr(), None if k is None else k.data_ptr(),
           None if v is None else v.data_ptr(), out.data_ptr(), kpages.data_ptr(), vpages.data_ptr(), table.data_ptr(),
           lens.data_ptr(), B, H, Hkv, d, kpages.shape[0], width, int(max_len), ctypes.byref(p), at, held)
     return out
 
 
-def gformer_paged_fill(k, v, kpages, vpages, table, start, cu, *, stream: Optional[int] = None):
-    """Packed keys and values [total, Hkv, d] into a paged cache: row i of sequence s becomes its token start[s] + i.
-    table int32 [n_seqs, table_width], start int32 [n_seqs], cu int32 [n_seqs + 1]."""
-    if _quick("paged_fill", ("paged_fill",), k, v, kpages, vpages, table, start, cu, stream):
-        return
+def _paged_rows(entry, of_pages, k, v, kpages, vpages, table, start, cu, stream, *tensors):
+    """A call that moves packed rows into pages or out of them; `tensors`: the four in the entry point's order."""
     dtype = _tensors(k, 3, k=k, v=v)
     if k.shape != v.shape or cu.numel() < 1:
         raise ValueError("k and v must be [total, Hkv, d], cu [n_seqs + 1]")
@@ -796,9 +818,31 @@ def gformer_paged_fill(k, v, kpages, vpages, table, start, cu, *, stream: Option
     _numbers(k, (n + 1,), cu=cu)
     _numbers(k, (n, None), table=table)
     _numbers(k, (n,), start=start)
-    p = make_paged_params(dtype, k_stride=_row_strides("k", k), v_stride=_row_strides("v", v), **_paged(k, kpages, vpages, Hkv, d))
-    _call(lib().gformer_paged_fill, k, stream, k.data_ptr(), v.data_ptr(), kpages.data_ptr(), vpages.data_ptr(), table.data_ptr(),
-          start.data_ptr(), cu.data_ptr(), n, T, Hkv, d, kpages.shape[0], table.shape[1], ctypes.byref(p))
+    p = make_paged_params(dtype, k_stride=_row_strides("k", k), v_stride=_row_strides("v", v), **of_pages(k, kpages, vpages, Hkv, d))
+    _call(entry, k, stream, *(x.data_ptr() for x in tensors), table.data_ptr(), start.data_ptr(), cu.data_ptr(), n, T, Hkv, d,
+          kpages.shape[0], table.shape[1], ctypes.byref(p))
+
+
+def gformer_paged_decode(q, k, v, out, kpages, vpages, table, lens, *, max_len=0, softmax_scale=1.0, workspace=None,
+                         stream: Optional[int] = None):
+    """One new token of every sequence over a paged cache, on device tensors: q, out [B, H, d]; k, v [B, Hkv, d], the new
+    keys and values, which go to their slots (both None: they are there already); kpages, vpages
+    [n_pages, Hkv, page_size, d] (any strides with a contiguous last dimension); table int32 [B, table_width]; lens int32
+    [B], the tokens in the cache before the call (negative: an idle row).  max_len bounds the longest
+    sequence's tokens, the new one included (0: what the table holds)."""
+    if _quick("paged_decode", ("paged_decode", "paged_decode_workspace_bytes"), q, k, v, out, kpages, vpages, table, lens, max_len,
+              softmax_scale, workspace, stream):
+        return out
+    return _paged_decode(lib().gformer_paged_decode, lib().gformer_paged_decode_workspace_bytes, _paged, q, k, v, out, kpages, vpages,
+                         table, lens, max_len, softmax_scale, workspace, stream)
+
+
+def gformer_paged_fill(k, v, kpages, vpages, table, start, cu, *, stream: Optional[int] = None):
+    """Packed keys and values [total, Hkv, d] into a paged cache: row i of sequence s becomes its token start[s] + i.
+    table int32 [n_seqs, table_width], start int32 [n_seqs], cu int32 [n_seqs + 1]."""
+    if _quick("paged_fill", ("paged_fill",), k, v, kpages, vpages, table, start, cu, stream):
+        return
+    _paged_rows(lib().gformer_paged_fill, _paged, k, v, kpages, vpages, table, start, cu, stream, k, v, kpages, vpages)
 
 
 def gformer_pages_copy(kpages, vpages, src, dst, *, stream: Optional[int] = None):
@@ -813,6 +857,103 @@ def gformer_pages_copy(kpages, vpages, src, dst, *, stream: Optional[int] = None
     p = make_paged_params(dtype, **_paged(kpages, kpages, vpages, Hkv, d))
     _call(lib().gformer_pages_copy, kpages, stream, kpages.data_ptr(), vpages.data_ptr(), src.data_ptr(), dst.data_ptr(),
           src.numel(), Hkv, d, P, ctypes.byref(p))
+
+
+# ---- the paged cache in 4 bits a value, and rotary positions -----------------------------------
+
+def gformer_paged_fill_q4(k, v, kpages, vpages, table, start, cu, *, stream: Optional[int] = None):
+    """gformer_paged_fill into a cache of 4 bits a value: kpages, vpages uint8 [n_pages, Hkv, page_size, d / 2 + d / 8] (any strides
+    that are multiples of d / 8, with a contiguous last dimension), whose rows include/gformer.h describes."""
+    if _quick("paged_fill_q4", ("paged_fill_q4",), k, v, kpages, vpages, table, start, cu, stream):
+        return
+    _paged_rows(lib().gformer_paged_fill_q4, _paged_q4, k, v, kpages, vpages, table, start, cu, stream, k, v, kpages, vpages)
+
+
+def gformer_paged_read_q4(kpages, vpages, k, v, table, start, cu, *, stream: Optional[int] = None):
+    """The way back: row i of sequence s of k and v [total, Hkv, d], written, becomes what its token start[s] + i stands for (zeros
+    where there is no page); rows behind the last sequence are left as they were."""
+    if _quick("paged_read_q4", ("paged_read_q4",), kpages, vpages, k, v, table, start, cu, stream):
+        return k, v
+    _paged_rows(lib().gformer_paged_read_q4, _paged_q4, k, v, kpages, vpages, table, start, cu, stream, kpages, vpages, k, v)
+    return k, v
+
+
+def gformer_paged_decode_q4_workspace_bytes(B, H, Hkv, d, max_len, params=None, table_width=None) -> int:
+    """As gformer_paged_decode_workspace_bytes."""
+    return _decode_bytes(lib().gformer_paged_decode_q4_workspace_bytes, B, H, Hkv, d, max_len, params, table_width)
+
+
+def gformer_paged_decode_q4(q, k, v, out, kpages, vpages, table, lens, *, max_len=0, softmax_scale=1.0, workspace=None,
+                            stream: Optional[int] = None):
+    """gformer_paged_decode over a cache of 4 bits a value (kpages, vpages as in gformer_paged_fill_q4).  The new token is seen as
+    its slot holds it, quantised."""
+    if _quick("paged_decode_q4", ("paged_decode_q4", "paged_decode_q4_workspace_bytes"), q, k, v, out, kpages, vpages, table, lens,
+              max_len, softmax_scale, workspace, stream):
+        return out
+    return _paged_decode(lib().gformer_paged_decode_q4, lib().gformer_paged_decode_q4_workspace_bytes, _paged_q4, q, k, v, out, kpages,
+                         vpages, table, lens, max_len, softmax_scale, workspace, stream)
+
+
+def gformer_pages_copy_q4(kpages, vpages, src, dst, *, stream: Optional[int] = None):
+    """gformer_pages_copy of a cache of 4 bits a value."""
+    if _quick("pages_copy_q4", ("pages_copy_q4",), kpages, vpages, src, dst, stream):
+        return
+    P, Hkv = kpages.shape[:2] if kpages.dim() == 4 else (0, 0)
+    d = kpages.shape[-1] * 8 // 5 if kpages.dim() == 4 else 0
+    p = make_paged_params(**_paged_q4(kpages, kpages, vpages, Hkv, d))
+    _numbers(kpages, (None,), src=src)
+    _numbers(kpages, (src.numel(),), dst=dst)
+    _call(lib().gformer_pages_copy_q4, kpages, stream, kpages.data_ptr(), vpages.data_ptr(), src.data_ptr(), dst.data_ptr(),
+          src.numel(), Hkv, d, P, ctypes.byref(p))
+
+
+def make_rotary_params(dtype=GF_BF16, rot=64, interleaved=0, inverse=0, zero_tail=0, factor=1.0, **strides) -> GformerRotaryParams:
+    """strides: q_stride=, ... as (row, head)."""
+    p = GformerRotaryParams(ctypes.sizeof(GformerRotaryParams), int(dtype), int(rot), int(interleaved), int(inverse), int(zero_tail),
+                            float(factor), 0)
+    for name, val in strides.items():
+        setattr(p, name, _Int64x2(*val))
+    return p
+
+
+def gformer_rotary(q, k, q_out, k_out, freqs, *, positions=None, cu=None, start=None, interleaved=0, inverse=0, factor=1.0,
+                   zero_tail=0, stream: Optional[int] = None):
+    """Queries and keys turned by their positions: q, q_out [total, H, d], k, k_out [total, Hkv, d] (k and k_out None: queries alone;
+    an output may be its input, in place); freqs fp32 [rot / 2], the angle per position of each pair of a head's first rot channels (pair i:
+    channels i and i + rot / 2, interleaved=1: 2i and 2i + 1).  Positions: int32 [total], or those of packed
+    sequences, cu int32 [n_seqs + 1] and start int32 [n_seqs], row i of sequence s at start[s] + i (start None: i).  inverse=1 turns back."""
+    if _quick("rotary", ("rotary",), q, k, q_out, k_out, freqs, positions, cu, start, interleaved, inverse, factor, zero_tail, stream):
+        return q_out, k_out
+    import torch
+
+    if (k is None) != (k_out is None):
+        raise ValueError("k and k_out come together, or neither")
+    both = {"q": (q, q_out)} if k is None else {"q": (q, q_out), "k": (k, k_out)}
+    dtype = _tensors(q, 3, **{n: x for n, (x, _) in both.items()}, **{f"{n}_out": y for n, (_, y) in both.items()})
+    T, H, d = q.shape
+    if any(x.shape != y.shape for x, y in both.values()) or (k is not None and (k.shape[0] != T or k.shape[2] != d)):
+        raise ValueError("q and q_out must be [total, H, d], k and k_out [total, Hkv, d]")
+    _sizes(freqs=2 * max(freqs.shape, default=0))
+    if freqs.device != q.device or freqs.dtype != torch.float32 or freqs.dim() != 1 or not freqs.is_contiguous():
+        raise ValueError("freqs must be dense fp32 [rot / 2] on the device of the others")
+    n = 0
+    if positions is not None:
+        if cu is not None or start is not None:
+            raise ValueError("positions come by row, or from cu and start")
+        _numbers(q, (T,), positions=positions)
+    elif cu is None or cu.numel() < 1:
+        raise ValueError("positions, or cu with n_seqs + 1 offsets, must be given")
+    else:
+        n = cu.numel() - 1
+        _numbers(q, (n + 1,), cu=cu)
+        if start is not None:
+            _numbers(q, (n,), start=start)
+    strides = {f"{name}{end}_stride": _row_strides(name + end, t) for name, pair in both.items() for end, t in zip(("", "_out"), pair)}
+    p = make_rotary_params(dtype, 2 * freqs.numel(), interleaved, inverse, zero_tail, factor, **strides)
+    ptr = lambda t: None if t is None else t.data_ptr()
+    _call(lib().gformer_rotary, q, stream, q.data_ptr(), ptr(k), q_out.data_ptr(), ptr(k_out), freqs.data_ptr(), ptr(positions), ptr(cu),
+          ptr(start), n, T, H, 0 if k is None else k.shape[1], d, ctypes.byref(p))
+    return q_out, k_out
 
 
 def gformer_partition_balance(p, size, flops_per0, flops_per1, perf0, perf1):

@@ -1,11 +1,14 @@
-// C ABI of packed attention and the paged cache: argument validation and dispatch (include/gformer.h).
+// C ABI of packed attention, the paged caches and rotary positions: argument validation and dispatch (include/gformer.h).
 #include "../../include/gformer.h"
 
+#include <float.h>
 #include <math.h>
 #include <string.h>
 
 #include "packed.hpp"
 #include "paged.hpp"
+#include "paged_q4.hpp"
+#include "rotary.hpp"
 
 namespace gformer {
 namespace {
@@ -33,8 +36,8 @@ gf_status strides2(const int64_t* in, int64_t* out, int heads, int d) {
   return in[0] > kMaxTokenStride ? GF_ERR_UNSUPPORTED : GF_OK;
 }
 
-// (page, head, token) strides of [pages, heads, page, d]
-gf_status strides3(const int64_t* in, int64_t* out, int heads, int page, int d) {
+// (page, head, token) strides of [pages, heads, page, d], multiples of `unit`
+gf_status strides3(const int64_t* in, int64_t* out, int heads, int page, int d, int unit) {
   if (in[0] == 0 && in[1] == 0 && in[2] == 0) {
     out[0] = (int64_t)heads * page * d;
     out[1] = (int64_t)page * d;
@@ -42,7 +45,7 @@ gf_status strides3(const int64_t* in, int64_t* out, int heads, int page, int d) 
     return GF_OK;
   }
   for (int i = 0; i < 3; ++i) {
-    if (in[i] < 0 || in[i] % 8 != 0) return GF_ERR_INVALID_ARG;
+    if (in[i] < 0 || in[i] % unit != 0) return GF_ERR_INVALID_ARG;
     out[i] = in[i];
   }
   if (in[0] < d || in[2] < d || (heads > 1 && in[1] < d)) return GF_ERR_INVALID_ARG;
@@ -88,15 +91,16 @@ gf_status check_packed(bool backward, int n_seqs, int total_q, int total_k, int 
   return GF_OK;
 }
 
-gf_status check_paged(int Hkv, int d, int n_pages, const gformer_paged_params* p, int* shift, int64_t* kps, int64_t* vps) {
+gf_status check_paged(int Hkv, int d, int n_pages, const gformer_paged_params* p, int* shift, int64_t* kps, int64_t* vps, bool q4 = false) {
   if (!p || p->struct_size != sizeof(gformer_paged_params)) return GF_ERR_INVALID_ARG;
   gf_status st = check_heads(p->dtype, Hkv, Hkv, d);
   if (st != GF_OK) return st;
   if (n_pages < 0 || p->page_size < 1) return GF_ERR_INVALID_ARG;
   if (p->page_size < 8 || p->page_size > 65536 || (p->page_size & (p->page_size - 1))) return GF_ERR_UNSUPPORTED;
   for (*shift = 3; (1 << *shift) < p->page_size;) ++*shift;
-  if ((st = strides3(p->kpage_stride, kps, Hkv, p->page_size, d)) != GF_OK) return st;
-  return strides3(p->vpage_stride, vps, Hkv, p->page_size, d);
+  const int row = q4 ? q4_row(d) : d, unit = q4 ? q4_piece(d) : 8;
+  if ((st = strides3(p->kpage_stride, kps, Hkv, p->page_size, row, unit)) != GF_OK) return st;
+  return strides3(p->vpage_stride, vps, Hkv, p->page_size, row, unit);
 }
 
 // Whether the table's sequences can be numbered, and how many keys one may have.
@@ -108,13 +112,139 @@ gf_status check_table(int width, int shift, int max_len, int* room) {
   return GF_OK;
 }
 
-size_t decode_bytes(int B, int H, int Hkv, int d, int room) {
-  const PagedSplit s = paged_split(B, H, Hkv, room);
+PagedSplit split_of(bool q4, int B, int H, int Hkv, int d, int room) {
+  return q4 ? paged_q4_split(B, H, Hkv, d, room) : paged_split(B, H, Hkv, room);
+}
+size_t decode_bytes(bool q4, int B, int H, int Hkv, int d, int room) {
+  const PagedSplit s = split_of(q4, B, H, Hkv, d, room);
   if (s.splits == 1) return 0;
   return ((size_t)B * H * s.splits * (d + 2) * sizeof(float) + 255) / 256 * 256;
 }
 
 gf_status status(hipError_t e) { return e == hipSuccess ? GF_OK : GF_ERR_DEVICE; }
+
+// The calls over both kinds of paged cache, rows of d elements and (q4) of codes.
+size_t decode_workspace(bool q4, int B, int H, int Hkv, int d, int table_width, int max_len,
+                        const gformer_paged_params* p) {
+  int shift, room;
+  int64_t kps[3], vps[3];
+  if (!p || B < 1 || check_heads(p->dtype, H, Hkv, d) != GF_OK || check_paged(Hkv, d, 1, p, &shift, kps, vps, q4) != GF_OK ||
+      check_table(table_width, shift, max_len, &room) != GF_OK)
+    return 0;
+  return decode_bytes(q4, B, H, Hkv, d, room);
+}
+
+gf_status decode_step(bool q4, const void* q, const void* k, const void* v, void* out, void* kpages, void* vpages,
+                      const int32_t* table, const int32_t* lens, int B, int H, int Hkv, int d, int n_pages,
+                      int table_width, int max_len, const gformer_paged_params* p, void* workspace,
+                      size_t workspace_bytes, void* hip_stream) {
+  PagedDecodeArgs a;
+  memset(&a, 0, sizeof(a));
+  if (!p) return GF_ERR_INVALID_ARG;
+  gf_status st = check_paged(Hkv, d, n_pages, p, &a.shift, a.kps, a.vps, q4);
+  if (st != GF_OK) return st;
+  if ((st = check_heads(p->dtype, H, Hkv, d)) != GF_OK) return st;
+  if (B < 0 || !scale_fits(p->softmax_scale)) return GF_ERR_INVALID_ARG;
+  if ((st = check_table(table_width, a.shift, max_len, &a.room)) != GF_OK) return st;
+  if ((st = strides2(p->q_stride, a.qs, H, d)) != GF_OK || (st = strides2(p->k_stride, a.ks, Hkv, d)) != GF_OK ||
+      (st = strides2(p->v_stride, a.vs, Hkv, d)) != GF_OK || (st = strides2(p->o_stride, a.os, H, d)) != GF_OK)
+    return st;
+  if (B == 0) return GF_OK;
+  const PagedSplit s = split_of(q4, B, H, Hkv, d, a.room);
+  if (!(q4 ? paged_q4_decode_fits(B, H, Hkv, d, s) : paged_decode_fits(B, H, Hkv, s))) return GF_ERR_UNSUPPORTED;
+  if (n_pages < 1) return GF_ERR_INVALID_ARG;
+  if (!q || !out || !kpages || !vpages || (!table && table_width > 0) || !lens || !k != !v) return GF_ERR_INVALID_ARG;
+  if (misaligned(bits(q, k, v, out, kpages, vpages), 16) || misaligned(bits(table, lens), 4)) return GF_ERR_INVALID_ARG;
+  if (out == q || out == k || out == v || out == kpages || out == vpages || kpages == vpages) return GF_ERR_INVALID_ARG;
+  const size_t need = decode_bytes(q4, B, H, Hkv, d, a.room);
+  if (need > 0 && (!workspace || workspace_bytes < need)) return GF_ERR_WORKSPACE;
+  if (need > 0 && misaligned(bits(workspace), 256)) return GF_ERR_INVALID_ARG;
+  if ((st = check_device(hip_stream)) != GF_OK) return st;
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.out = out;
+  a.kpages = kpages;
+  a.vpages = vpages;
+  a.table = table;
+  a.lens = lens;
+  a.B = B;
+  a.H = H;
+  a.Hkv = Hkv;
+  a.d = d;
+  a.n_pages = n_pages;
+  a.width = table_width;
+  a.chunk = s.chunk;
+  a.splits = s.splits;
+  a.scale = p->softmax_scale;
+  a.sums = static_cast<float*>(workspace);
+  if (s.splits > 1) a.stats = a.sums + (size_t)B * H * s.splits * d;
+  const bool bf16 = p->dtype == GF_BF16;
+  const hipStream_t on = reinterpret_cast<hipStream_t>(hip_stream);
+  return status(q4 ? launch_paged_q4_decode(a, bf16, on) : launch_paged_decode(a, bf16, on));
+}
+
+gf_status fill(bool q4, const void* k, const void* v, void* kpages, void* vpages, const int32_t* table, const int32_t* start,
+               const int32_t* cu, int n_seqs, int total, int Hkv, int d, int n_pages, int table_width,
+               const gformer_paged_params* p, void* hip_stream) {
+  PagedFillArgs a;
+  memset(&a, 0, sizeof(a));
+  int room;
+  gf_status st = check_paged(Hkv, d, n_pages, p, &a.shift, a.kps, a.vps, q4);
+  if (st != GF_OK) return st;
+  if ((st = check_table(table_width, a.shift, 0, &room)) != GF_OK) return st;
+  if (n_seqs < 0 || total < 0) return GF_ERR_INVALID_ARG;
+  if (total > kMaxCached || n_seqs > kMaxCached) return GF_ERR_UNSUPPORTED;
+  if ((st = strides2(p->k_stride, a.ks, Hkv, d)) != GF_OK || (st = strides2(p->v_stride, a.vs, Hkv, d)) != GF_OK) return st;
+  if (!(q4 ? paged_q4_rows_fit(total, n_seqs, Hkv) : paged_fill_fits(total, n_seqs, Hkv))) return GF_ERR_UNSUPPORTED;
+  if (total == 0 || n_seqs == 0 || table_width == 0 || n_pages == 0) return GF_OK;
+  if (!k || !v || !kpages || !vpages || !table || !start || !cu) return GF_ERR_INVALID_ARG;
+  if (misaligned(bits(k, v, kpages, vpages), 16) || misaligned(bits(table, start, cu), 4)) return GF_ERR_INVALID_ARG;
+  if (kpages == vpages) return GF_ERR_INVALID_ARG;
+  if ((st = check_device(hip_stream)) != GF_OK) return st;
+  a.k = k;
+  a.v = v;
+  a.kpages = kpages;
+  a.vpages = vpages;
+  a.table = table;
+  a.start = start;
+  a.cu = cu;
+  a.n_seqs = n_seqs;
+  a.total = total;
+  a.Hkv = Hkv;
+  a.d = d;
+  a.n_pages = n_pages;
+  a.width = table_width;
+  const bool bf16 = p->dtype == GF_BF16;
+  const hipStream_t on = reinterpret_cast<hipStream_t>(hip_stream);
+  return status(q4 ? launch_paged_q4_fill(a, bf16, on) : launch_paged_fill(a, bf16, on));
+}
+
+gf_status copy_pages(bool q4, void* kpages, void* vpages, const int32_t* src, const int32_t* dst, int n_copies, int Hkv, int d,
+                     int n_pages, const gformer_paged_params* p, void* hip_stream) {
+  PagesCopyArgs a;
+  memset(&a, 0, sizeof(a));
+  int shift;
+  gf_status st = check_paged(Hkv, d, n_pages, p, &shift, a.kps, a.vps, q4);
+  if (st != GF_OK) return st;
+  if (n_copies < 0) return GF_ERR_INVALID_ARG;
+  if ((int64_t)n_copies * Hkv > most_workgroups(kPagedThreads)) return GF_ERR_UNSUPPORTED;
+  if (n_copies == 0) return GF_OK;
+  if (!kpages || !vpages || !src || !dst || kpages == vpages) return GF_ERR_INVALID_ARG;
+  if (misaligned(bits(kpages, vpages), 16) || misaligned(bits(src, dst), 4)) return GF_ERR_INVALID_ARG;
+  if ((st = check_device(hip_stream)) != GF_OK) return st;
+  a.kpages = kpages;
+  a.vpages = vpages;
+  a.src = src;
+  a.dst = dst;
+  a.n_copies = n_copies;
+  a.Hkv = Hkv;
+  a.d = d;
+  a.n_pages = n_pages;
+  a.page = p->page_size;
+  const hipStream_t on = reinterpret_cast<hipStream_t>(hip_stream);
+  return status(q4 ? launch_pages_q4_copy(a, on) : launch_pages_copy(a, p->dtype == GF_BF16, on));
+}
 
 }  // namespace
 }  // namespace gformer
@@ -214,84 +344,65 @@ gf_status gformer_packed_attn_bwd(const void* q, const void* k, const void* v, c
 
 size_t gformer_paged_decode_workspace_bytes(int B, int H, int Hkv, int d, int table_width, int max_len,
                                             const gformer_paged_params* p) {
-  int shift, room;
-  int64_t kps[3], vps[3];
-  if (!p || B < 1 || check_heads(p->dtype, H, Hkv, d) != GF_OK || check_paged(Hkv, d, 1, p, &shift, kps, vps) != GF_OK ||
-      check_table(table_width, shift, max_len, &room) != GF_OK)
-    return 0;
-  return decode_bytes(B, H, Hkv, d, room);
+  return decode_workspace(false, B, H, Hkv, d, table_width, max_len, p);
+}
+
+size_t gformer_paged_decode_q4_workspace_bytes(int B, int H, int Hkv, int d, int table_width, int max_len,
+                                               const gformer_paged_params* p) {
+  return decode_workspace(true, B, H, Hkv, d, table_width, max_len, p);
 }
 
 gf_status gformer_paged_decode(const void* q, const void* k, const void* v, void* out, void* kpages, void* vpages,
                                const int32_t* table, const int32_t* lens, int B, int H, int Hkv, int d, int n_pages,
                                int table_width, int max_len, const gformer_paged_params* p, void* workspace,
                                size_t workspace_bytes, void* hip_stream) {
-  PagedDecodeArgs a;
-  memset(&a, 0, sizeof(a));
-  if (!p) return GF_ERR_INVALID_ARG;
-  gf_status st = check_paged(Hkv, d, n_pages, p, &a.shift, a.kps, a.vps);
-  if (st != GF_OK) return st;
-  if ((st = check_heads(p->dtype, H, Hkv, d)) != GF_OK) return st;
-  if (B < 0 || !scale_fits(p->softmax_scale)) return GF_ERR_INVALID_ARG;
-  if ((st = check_table(table_width, a.shift, max_len, &a.room)) != GF_OK) return st;
-  if ((st = strides2(p->q_stride, a.qs, H, d)) != GF_OK || (st = strides2(p->k_stride, a.ks, Hkv, d)) != GF_OK ||
-      (st = strides2(p->v_stride, a.vs, Hkv, d)) != GF_OK || (st = strides2(p->o_stride, a.os, H, d)) != GF_OK)
-    return st;
-  if (B == 0) return GF_OK;
-  const PagedSplit s = paged_split(B, H, Hkv, a.room);
-  if (!paged_decode_fits(B, H, Hkv, s)) return GF_ERR_UNSUPPORTED;
-  if (n_pages < 1) return GF_ERR_INVALID_ARG;
-  if (!q || !out || !kpages || !vpages || (!table && table_width > 0) || !lens || !k != !v) return GF_ERR_INVALID_ARG;
-  if (misaligned(bits(q, k, v, out, kpages, vpages), 16) || misaligned(bits(table, lens), 4)) return GF_ERR_INVALID_ARG;
-  if (out == q || out == k || out == v || out == kpages || out == vpages || kpages == vpages) return GF_ERR_INVALID_ARG;
-  const size_t need = decode_bytes(B, H, Hkv, d, a.room);
-  if (need > 0 && (!workspace || workspace_bytes < need)) return GF_ERR_WORKSPACE;
-  if (need > 0 && misaligned(bits(workspace), 256)) return GF_ERR_INVALID_ARG;
-  if ((st = check_device(hip_stream)) != GF_OK) return st;
-  a.q = q;
-  a.k = k;
-  a.v = v;
-  a.out = out;
-  a.kpages = kpages;
-  a.vpages = vpages;
-  a.table = table;
-  a.lens = lens;
-  a.B = B;
-  a.H = H;
-  a.Hkv = Hkv;
-  a.d = d;
-  a.n_pages = n_pages;
-  a.width = table_width;
-  a.chunk = s.chunk;
-  a.splits = s.splits;
-  a.scale = p->softmax_scale;
-  a.sums = static_cast<float*>(workspace);
-  if (s.splits > 1) a.stats = a.sums + (size_t)B * H * s.splits * d;
-  return status(launch_paged_decode(a, p->dtype == GF_BF16, reinterpret_cast<hipStream_t>(hip_stream)));
+  return decode_step(false, q, k, v, out, kpages, vpages, table, lens, B, H, Hkv, d, n_pages, table_width, max_len, p, workspace,
+                     workspace_bytes, hip_stream);
+}
+
+gf_status gformer_paged_decode_q4(const void* q, const void* k, const void* v, void* out, void* kpages, void* vpages,
+                                  const int32_t* table, const int32_t* lens, int B, int H, int Hkv, int d, int n_pages,
+                                  int table_width, int max_len, const gformer_paged_params* p, void* workspace,
+                                  size_t workspace_bytes, void* hip_stream) {
+  return decode_step(true, q, k, v, out, kpages, vpages, table, lens, B, H, Hkv, d, n_pages, table_width, max_len, p, workspace,
+                     workspace_bytes, hip_stream);
 }
 
 gf_status gformer_paged_fill(const void* k, const void* v, void* kpages, void* vpages, const int32_t* table, const int32_t* start,
                              const int32_t* cu, int n_seqs, int total, int Hkv, int d, int n_pages, int table_width,
                              const gformer_paged_params* p, void* hip_stream) {
-  PagedFillArgs a;
+  return fill(false, k, v, kpages, vpages, table, start, cu, n_seqs, total, Hkv, d, n_pages, table_width, p, hip_stream);
+}
+
+gf_status gformer_paged_fill_q4(const void* k, const void* v, void* kpages, void* vpages, const int32_t* table, const int32_t* start,
+                                const int32_t* cu, int n_seqs, int total, int Hkv, int d, int n_pages, int table_width,
+                                const gformer_paged_params* p, void* hip_stream) {
+  return fill(true, k, v, kpages, vpages, table, start, cu, n_seqs, total, Hkv, d, n_pages, table_width, p, hip_stream);
+}
+
+gf_status gformer_paged_read_q4(const void* kpages, const void* vpages, void* k, void* v, const int32_t* table, const int32_t* start,
+                                const int32_t* cu, int n_seqs, int total, int Hkv, int d, int n_pages, int table_width,
+                                const gformer_paged_params* p, void* hip_stream) {
+  PagedReadArgs a;
   memset(&a, 0, sizeof(a));
   int room;
-  gf_status st = check_paged(Hkv, d, n_pages, p, &a.shift, a.kps, a.vps);
+  gf_status st = check_paged(Hkv, d, n_pages, p, &a.shift, a.kps, a.vps, true);
   if (st != GF_OK) return st;
   if ((st = check_table(table_width, a.shift, 0, &room)) != GF_OK) return st;
   if (n_seqs < 0 || total < 0) return GF_ERR_INVALID_ARG;
   if (total > kMaxCached || n_seqs > kMaxCached) return GF_ERR_UNSUPPORTED;
   if ((st = strides2(p->k_stride, a.ks, Hkv, d)) != GF_OK || (st = strides2(p->v_stride, a.vs, Hkv, d)) != GF_OK) return st;
-  if (!paged_fill_fits(total, n_seqs, Hkv)) return GF_ERR_UNSUPPORTED;
-  if (total == 0 || n_seqs == 0 || table_width == 0 || n_pages == 0) return GF_OK;
-  if (!k || !v || !kpages || !vpages || !table || !start || !cu) return GF_ERR_INVALID_ARG;
+  if (!paged_q4_rows_fit(total, n_seqs, Hkv)) return GF_ERR_UNSUPPORTED;
+  if (total == 0 || n_seqs == 0) return GF_OK;
+  // a table or cache of no pages: its tokens are zeros, and nothing of it is read
+  if (!k || !v || (!table && table_width > 0) || !start || !cu || (n_pages > 0 && (!kpages || !vpages))) return GF_ERR_INVALID_ARG;
   if (misaligned(bits(k, v, kpages, vpages), 16) || misaligned(bits(table, start, cu), 4)) return GF_ERR_INVALID_ARG;
-  if (kpages == vpages) return GF_ERR_INVALID_ARG;
+  if (k == v || k == kpages || k == vpages || v == kpages || v == vpages) return GF_ERR_INVALID_ARG;
   if ((st = check_device(hip_stream)) != GF_OK) return st;
-  a.k = k;
-  a.v = v;
   a.kpages = kpages;
   a.vpages = vpages;
+  a.k = k;
+  a.v = v;
   a.table = table;
   a.start = start;
   a.cu = cu;
@@ -301,32 +412,72 @@ gf_status gformer_paged_fill(const void* k, const void* v, void* kpages, void* v
   a.d = d;
   a.n_pages = n_pages;
   a.width = table_width;
-  return status(launch_paged_fill(a, p->dtype == GF_BF16, reinterpret_cast<hipStream_t>(hip_stream)));
+  return status(launch_paged_q4_read(a, p->dtype == GF_BF16, reinterpret_cast<hipStream_t>(hip_stream)));
 }
 
 gf_status gformer_pages_copy(void* kpages, void* vpages, const int32_t* src, const int32_t* dst, int n_copies, int Hkv, int d,
                              int n_pages, const gformer_paged_params* p, void* hip_stream) {
-  PagesCopyArgs a;
+  return copy_pages(false, kpages, vpages, src, dst, n_copies, Hkv, d, n_pages, p, hip_stream);
+}
+
+gf_status gformer_pages_copy_q4(void* kpages, void* vpages, const int32_t* src, const int32_t* dst, int n_copies, int Hkv, int d,
+                                int n_pages, const gformer_paged_params* p, void* hip_stream) {
+  return copy_pages(true, kpages, vpages, src, dst, n_copies, Hkv, d, n_pages, p, hip_stream);
+}
+
+void gformer_rotary_params_init(gformer_rotary_params* p) {
+  if (!p) return;
+  memset(p, 0, sizeof(*p));
+  p->struct_size = sizeof(*p);
+  p->dtype = GF_BF16;
+  p->rot = 64;
+  p->factor = 1.f;
+}
+
+gf_status gformer_rotary(const void* q, const void* k, void* q_out, void* k_out, const float* freqs, const int32_t* positions,
+                         const int32_t* cu, const int32_t* start, int n_seqs, int total, int H, int Hkv, int d,
+                         const gformer_rotary_params* p, void* hip_stream) {
+  if (!p || p->struct_size != sizeof(gformer_rotary_params)) return GF_ERR_INVALID_ARG;
+  if (p->dtype != GF_F32 && p->dtype != GF_BF16) return GF_ERR_INVALID_ARG;
+  const auto flag = [](int x) { return x == 0 || x == 1; };
+  if (total < 0 || n_seqs < 0 || H < 1 || Hkv < 0 || d < 1 || p->reserved0 != 0 || !flag(p->interleaved) || !flag(p->inverse) ||
+      !flag(p->zero_tail) || !(fabsf(p->factor) <= FLT_MAX) || p->rot < 1 || p->rot > d)
+    return GF_ERR_INVALID_ARG;
+  if ((d != 64 && d != 128) || p->rot % 16 != 0) return GF_ERR_UNSUPPORTED;
+  RotaryArgs a;
   memset(&a, 0, sizeof(a));
-  int shift;
-  gf_status st = check_paged(Hkv, d, n_pages, p, &shift, a.kps, a.vps);
-  if (st != GF_OK) return st;
-  if (n_copies < 0) return GF_ERR_INVALID_ARG;
-  if ((int64_t)n_copies * Hkv > most_workgroups(kPagedThreads)) return GF_ERR_UNSUPPORTED;
-  if (n_copies == 0) return GF_OK;
-  if (!kpages || !vpages || !src || !dst || kpages == vpages) return GF_ERR_INVALID_ARG;
-  if (misaligned(bits(kpages, vpages), 16) || misaligned(bits(src, dst), 4)) return GF_ERR_INVALID_ARG;
+  gf_status st;
+  if ((st = strides2(p->q_stride, a.qs, H, d)) != GF_OK || (st = strides2(p->k_stride, a.ks, Hkv, d)) != GF_OK ||
+      (st = strides2(p->q_out_stride, a.qos, H, d)) != GF_OK || (st = strides2(p->k_out_stride, a.kos, Hkv, d)) != GF_OK)
+    return st;
+  if (total > kMaxCached || n_seqs > kMaxCached || !rotary_fits(total, H, Hkv, d)) return GF_ERR_UNSUPPORTED;
+  if (total == 0) return GF_OK;
+  if (!q || !q_out || !freqs || !k != !k_out || !k != (Hkv == 0)) return GF_ERR_INVALID_ARG;
+  if (positions ? cu || start || n_seqs != 0 : !cu) return GF_ERR_INVALID_ARG;
+  if (misaligned(bits(q, k, q_out, k_out), 16) || misaligned(bits(freqs, positions, cu, start), 4)) return GF_ERR_INVALID_ARG;
+  if (q_out == k || q_out == k_out || (k && k_out == q)) return GF_ERR_INVALID_ARG;
+  // in place, or apart
+  if ((q_out == q && memcmp(a.qs, a.qos, sizeof(a.qs))) || (k && k_out == k && memcmp(a.ks, a.kos, sizeof(a.ks)))) return GF_ERR_INVALID_ARG;
   if ((st = check_device(hip_stream)) != GF_OK) return st;
-  a.kpages = kpages;
-  a.vpages = vpages;
-  a.src = src;
-  a.dst = dst;
-  a.n_copies = n_copies;
+  a.q = q;
+  a.k = k;
+  a.q_out = q_out;
+  a.k_out = k_out;
+  a.freqs = freqs;
+  a.positions = positions;
+  a.cu = cu;
+  a.start = start;
+  a.n_seqs = n_seqs;
+  a.total = total;
+  a.H = H;
   a.Hkv = Hkv;
   a.d = d;
-  a.n_pages = n_pages;
-  a.page = p->page_size;
-  return status(launch_pages_copy(a, p->dtype == GF_BF16, reinterpret_cast<hipStream_t>(hip_stream)));
+  a.rot = p->rot;
+  a.interleaved = p->interleaved;
+  a.inverse = p->inverse;
+  a.zero_tail = p->zero_tail;
+  a.factor = p->factor;
+  return status(launch_rotary(a, p->dtype == GF_BF16, reinterpret_cast<hipStream_t>(hip_stream)));
 }
 
 }  // extern "C"

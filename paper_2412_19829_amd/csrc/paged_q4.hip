@@ -1,0 +1,511 @@
+// The paged cache in 4 bits a value: what writes its rows, reads them back and moves its pages, and one new token of every sequence
+// over it.
+//
+// decode: with codes n, scales s and lowest values l of the keys' groups g of 32 channels c, and Q_g the sum of a query's channels there,
+//   q.k_j = sum_g ( s_jg sum_c q_c n_jc + l_jg Q_g ),   sum_j p_j v_jc = sum_j (p_j s_jg) n_jc + sum_j p_j l_jg
+// so that codes are the matrix operands, which bf16 holds exactly, and scales meet 16 x 16 tiles.  The tiles' columns are pairs
+// (query head, group): a column's query is zero outside its group, its scores' parts are added over the columns of a head,
+// which leaves them in every one of them, and there a weight takes its own group's scale for the second product, whose rows (channels) count
+// in their own group's columns alone.  16 columns are 4 heads of 128 channels, or 8 of 64.
+// A code becomes an operand by way of fp8: the byte n is n 2^-9 for n < 16, two of which one instruction converts.
+#include "paged_q4.hpp"
+
+#include "f32_mfma.hpp"
+#include "mfma.hpp"
+#include "packed.hpp"
+
+#include <algorithm>
+
+namespace gformer {
+namespace {
+
+constexpr int kWaves = kPagedThreads / 64;
+constexpr uint32_t kNibbles = 0x0f0f0f0fu;
+
+__device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+
+// A value of the lane whose number differs in bit 0 or bit 1.
+template <int BIT> __device__ __forceinline__ uint32_t beside(uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, BIT == 1 ? 0xb1 : 0x4e, 0xf, 0xf, true);
+}
+template <int BIT> __device__ __forceinline__ float beside(float x) { return __uint_as_float(beside<BIT>(__float_as_uint(x))); }
+
+// ---- rows -------------------------------------------------------------------------------------------
+
+// Codes of 8 of 32 values that four neighbouring lanes hold, and the group's (scale, lowest value).
+struct Codes {
+  uint32_t n, pair;
+};
+__device__ __forceinline__ Codes quantised(const float (&x)[8]) {
+  float lo = INFINITY, hi = -INFINITY;
+  uint32_t sound = 1;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    lo = fminf(lo, x[i]);
+    hi = fmaxf(hi, x[i]);
+    sound &= fabsf(x[i]) < 0x1p127f ? 1u : 0u;
+  }
+  lo = fminf(lo, beside<1>(lo));
+  lo = fminf(lo, beside<2>(lo));
+  hi = fmaxf(hi, beside<1>(hi));
+  hi = fmaxf(hi, beside<2>(hi));
+  sound &= beside<1>(sound);
+  sound &= beside<2>(sound);
+  if (!sound) return {0u, 0x7fc07fc0u};
+  uint32_t low = __float_as_uint(lo + 0.f);   // zero without its sign
+  low = (low & 0xffff0000u) + ((low & 0x8000ffffu) > 0x80000000u ? 0x10000u : 0u);   // negative with bits behind: one step away from zero
+  const double l = (double)__uint_as_float(low), range = (double)(hi + 0.f) - l;
+  // the quotient's first guess may be a step short of what reaches the range, or two where the guess itself was rounded down
+  uint32_t scale = __float_as_uint((float)(range * (1.0 / 15.0))) & 0xffff0000u;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) scale += 15.0 * (double)__uint_as_float(scale) < range ? 0x10000u : 0u;
+  const double s = (double)__uint_as_float(scale), half = 0.5 * s, by = scale ? __builtin_amdgcn_rcp(s) : 0.0;
+  uint32_t codes = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const double at = (double)x[i] - l;
+    const double n = rint(at * by), rest = fma(-n, s, at);   // exact: s has 8 bits
+    int k = (int)n;
+    if (rest > half || (rest == half && (k & 1))) ++k;
+    else if (rest < -half || (rest == -half && (k & 1))) --k;
+    codes |= (uint32_t)k << (4 * i);
+  }
+  return {codes, low | scale >> 16};
+}
+
+template <typename T> __device__ __forceinline__ void load8(float (&x)[8], const T* p);
+template <> __device__ __forceinline__ void load8(float (&x)[8], const uint16_t* p) {
+  const u32x4 w = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = bf16_lo(w[i]);
+    x[2 * i + 1] = bf16_hi(w[i]);
+  }
+}
+template <> __device__ __forceinline__ void load8(float (&x)[8], const float* p) {
+  const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[i] = a[i];
+    x[4 + i] = b[i];
+  }
+}
+__device__ __forceinline__ void store8(uint16_t* p, const float (&x)[8]) {
+  *reinterpret_cast<u32x4*>(p) = u32x4{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])};
+}
+__device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
+  *reinterpret_cast<f32x4*>(p) = f32x4{x[0], x[1], x[2], x[3]};
+  *reinterpret_cast<f32x4*>(p + 4) = f32x4{x[4], x[5], x[6], x[7]};
+}
+
+// Lane c of a row's D / 8 puts its codes, and the first of four the group's pair.
+template <int D> __device__ __forceinline__ void put_codes(uint32_t* row, int c, Codes x) {
+  row[c] = x.n;
+  if (c % 4 == 0) row[D / 8 + c / 4] = x.pair;
+}
+
+// Packed rows into their slots, or out of them: a workgroup takes 32 rows of one head, a lane 8 channels of a row at a time.
+constexpr int kRows = 32;
+template <typename T, int D> __global__ __launch_bounds__(kPagedThreads) void q4_fill_kernel(PagedFillArgs a) {
+  constexpr int C = D / 8;
+  const int tid = threadIdx.x, head = blockIdx.x % a.Hkv, c = tid % C;
+  const SeqTile at = find_tile<kRows>(a.cu, a.n_seqs, a.total, blockIdx.x / a.Hkv, tid & 63);
+  if (at.first < 0 || at.seq == a.n_seqs) return;
+  const int base = packed_row(a.cu, at.seq, a.total), n = packed_row(a.cu, at.seq + 1, a.total) - base;
+  const int64_t room = (int64_t)a.width << a.shift;
+  for (int r = tid / C; r < kRows; r += kPagedThreads / C) {
+    const int row = at.first + r;
+    const int64_t pos = (int64_t)a.start[at.seq] + row;
+    if (row >= n || pos < 0 || pos >= room) continue;
+    const int page = a.table[(int64_t)at.seq * a.width + (pos >> a.shift)];
+    if ((unsigned)page >= (unsigned)a.n_pages) continue;
+    const int slot = (int)pos & ((1 << a.shift) - 1);
+    float k[8], v[8];
+    load8(k, rows_of<T>(a.k, a.ks, base + row, head) + 8 * c);
+    load8(v, rows_of<T>(a.v, a.vs, base + row, head) + 8 * c);
+    put_codes<D>(reinterpret_cast<uint32_t*>(reinterpret_cast<char*>(a.kpages) + page * a.kps[0] + head * a.kps[1] + slot * a.kps[2]), c, quantised(k));
+    put_codes<D>(reinterpret_cast<uint32_t*>(reinterpret_cast<char*>(a.vpages) + page * a.vps[0] + head * a.vps[1] + slot * a.vps[2]), c, quantised(v));
+  }
+}
+
+template <int D> __device__ __forceinline__ void values8(float (&x)[8], const uint32_t* row, int c) {
+  const uint32_t n = row[c], pair = row[D / 8 + c / 4];
+  const float s = bf16_lo(pair), l = bf16_hi(pair);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = fmaf(s, (float)(n >> (4 * i) & 15u), l);
+}
+template <typename T, int D> __global__ __launch_bounds__(kPagedThreads) void q4_read_kernel(PagedReadArgs a) {
+  constexpr int C = D / 8;
+  const int tid = threadIdx.x, head = blockIdx.x % a.Hkv, c = tid % C;
+  const SeqTile at = find_tile<kRows>(a.cu, a.n_seqs, a.total, blockIdx.x / a.Hkv, tid & 63);
+  if (at.first < 0 || at.seq == a.n_seqs) return;
+  const int base = packed_row(a.cu, at.seq, a.total), n = packed_row(a.cu, at.seq + 1, a.total) - base;
+  const int64_t room = (int64_t)a.width << a.shift;
+  for (int r = tid / C; r < kRows; r += kPagedThreads / C) {
+    const int row = at.first + r;
+    if (row >= n) continue;
+    const int64_t pos = (int64_t)a.start[at.seq] + row;
+    const int page = pos < 0 || pos >= room ? -1 : a.table[(int64_t)at.seq * a.width + (pos >> a.shift)];
+    float k[8] = {}, v[8] = {};
+    if ((unsigned)page < (unsigned)a.n_pages) {
+      const int slot = (int)pos & ((1 << a.shift) - 1);
+      values8<D>(k, reinterpret_cast<const uint32_t*>(reinterpret_cast<const char*>(a.kpages) + page * a.kps[0] + head * a.kps[1] + slot * a.kps[2]), c);
+      values8<D>(v, reinterpret_cast<const uint32_t*>(reinterpret_cast<const char*>(a.vpages) + page * a.vps[0] + head * a.vps[1] + slot * a.vps[2]), c);
+    }
+    store8(rows_of<T>(a.k, a.ks, base + row, head) + 8 * c, k);
+    store8(rows_of<T>(a.v, a.vs, base + row, head) + 8 * c, v);
+  }
+}
+
+// Whole pages: a workgroup copies one head of one page, keys and values, in five pieces a row.
+template <int D> __global__ __launch_bounds__(kPagedThreads) void q4_copy_kernel(PagesCopyArgs a) {
+  typedef typename std::conditional<D == 128, u32x4, u32x2>::type Piece;
+  const int copy = blockIdx.x / a.Hkv, head = blockIdx.x % a.Hkv;
+  const int src = a.src[copy], dst = a.dst[copy];
+  if ((unsigned)src >= (unsigned)a.n_pages || (unsigned)dst >= (unsigned)a.n_pages || src == dst) return;
+  const char* ks = reinterpret_cast<const char*>(a.kpages) + src * a.kps[0] + head * a.kps[1];
+  const char* vs = reinterpret_cast<const char*>(a.vpages) + src * a.vps[0] + head * a.vps[1];
+  char* kd = reinterpret_cast<char*>(a.kpages) + dst * a.kps[0] + head * a.kps[1];
+  char* vd = reinterpret_cast<char*>(a.vpages) + dst * a.vps[0] + head * a.vps[1];
+  for (int i = threadIdx.x; i < 5 * a.page; i += kPagedThreads) {
+    const int r = i / 5, c = (int)sizeof(Piece) * (i % 5);
+    const Piece k = *reinterpret_cast<const Piece*>(ks + r * a.kps[2] + c), v = *reinterpret_cast<const Piece*>(vs + r * a.vps[2] + c);
+    *reinterpret_cast<Piece*>(kd + r * a.kps[2] + c) = k;
+    *reinterpret_cast<Piece*>(vd + r * a.vps[2] + c) = v;
+  }
+}
+
+// ---- the decode step --------------------------------------------------------------------------------
+
+template <int D> struct Shape4 {
+  static constexpr int GR = D / kQ4Group, HC = 16 / GR;   // groups of a row, query heads of a workgroup
+  static constexpr int ST = D / 32;                       // products of a score tile: lane group L takes channels D / 4 L ..
+  static constexpr int E = D / 16;                        // channels of a value row that a lane takes: E i ..
+  typedef typename std::conditional<D == 128, u32x4, u32x2>::type KeyCodes;
+  typedef typename std::conditional<D == 128, uint32_t, uint16_t>::type ValueCodes;
+};
+constexpr int q4_heads(int d) { return d == 128 ? Shape4<128>::HC : Shape4<64>::HC; }
+
+// Parts in bf16 that a factor of the products is taken in: bf16 queries are one, their weights are rounded to one (as a bf16
+// cache's are); fp32 takes the three that hold its 24 bits.
+template <typename T> constexpr int kParts = sizeof(T) == 2 ? 1 : 3;
+
+// x's first bf16 part, two at a time; what it leaves stays in a and b.
+__device__ __forceinline__ uint32_t take_part(float& a, float& b) {
+  const uint32_t w = pack_bf16(a, b);
+  a -= bf16_lo(w);
+  b -= bf16_hi(w);
+  return w;
+}
+
+__device__ __forceinline__ uint32_t codes_bf16(uint32_t bytes, bool upper) {
+  return __builtin_bit_cast(uint32_t, upper ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(bytes, 512.f, true)
+                                            : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(bytes, 512.f, false));
+}
+
+__device__ __forceinline__ int seen_tokens(const PagedDecodeArgs& a, int b) {
+  const int t = a.lens[b], own = a.k ? 1 : 0;
+  return t < 0 || t > a.room - own ? 0 : t + own;
+}
+
+template <typename T, int D> __global__ __launch_bounds__(kPagedThreads) void q4_decode_kernel(PagedDecodeArgs a) {
+  using S = Shape4<D>;
+  typedef typename S::KeyCodes KeyCodes;
+  constexpr int GR = S::GR, HC = S::HC, ST = S::ST, E = S::E, PARTS = kParts<T>, ROW = q4_row(D), U = 2, R = 16 * U;
+  __shared__ float sm_o[kWaves][HC][D + 4], sm_m[kWaves][HC], sm_l[kWaves][HC];
+  __shared__ __align__(16) uint32_t sm_new[2][ROW / 4];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, L = lane >> 4;
+  const int G = a.H / a.Hkv, tiles = (G + HC - 1) / HC;
+  int id = blockIdx.x;   // chunks slowest, as in the other cache's step
+  const int tile = id % tiles;
+  id /= tiles;
+  const int kvh = id % a.Hkv;
+  id /= a.Hkv;
+  const int b = id % a.B, split = id / a.B;
+  const int h0 = kvh * G + tile * HC, heads = min(G - tile * HC, HC);
+  const int n = seen_tokens(a, b), from = split * a.chunk, to = min(n, from + a.chunk);
+  if (split > 0 && from >= n) return;   // the joining kernel knows as much
+
+  const int own = a.k && n > 0 ? n - 1 : -1;   // the new token's position
+  const char* kc = reinterpret_cast<const char*>(a.kpages) + kvh * a.kps[1];
+  const char* vc = reinterpret_cast<const char*>(a.vpages) + kvh * a.vps[1];
+  const int32_t* table = a.table + (int64_t)b * a.width;
+  const int in_page = (1 << a.shift) - 1;
+
+  // the new token's row, for its slot and for the tile that sees it: nobody reads the slot in this call
+  if (own >= from && own < to) {
+    const int c = lane % (D / 8);
+    if (wave < 2 && lane < D / 8) {
+      float x[8];
+      load8(x, (wave == 0 ? rows_of<T>(a.k, a.ks, b, kvh) : rows_of<T>(a.v, a.vs, b, kvh)) + 8 * c);
+      const Codes y = quantised(x);
+      put_codes<D>(sm_new[wave], c, y);
+      const int page = table[own >> a.shift];
+      if (tile == 0 && (unsigned)page < (unsigned)a.n_pages) {
+        char* row = wave == 0 ? reinterpret_cast<char*>(a.kpages) + page * a.kps[0] + kvh * a.kps[1] + (own & in_page) * a.kps[2]
+                              : reinterpret_cast<char*>(a.vpages) + page * a.vps[0] + kvh * a.vps[1] + (own & in_page) * a.vps[2];
+        put_codes<D>(reinterpret_cast<uint32_t*>(row), c, y);
+      }
+    }
+    __syncthreads();
+  }
+
+  // column i: query head i / GR, group i % GR
+  const int h = i / GR, g = i % GR, mine = L * GR / 4;   // mine: the group of this lane's channels
+  bf16x8 q[PARTS][ST];
+  float qsum = 0.f;
+#pragma unroll
+  for (int t = 0; t < ST; ++t) {
+    float x[8] = {};
+    if (h < heads && g == mine) load8(x, rows_of<T>(a.q, a.qs, b, h0 + h) + D / 4 * L + 8 * t);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) qsum += x[e];
+#pragma unroll
+    for (int p = 0; p < PARTS; ++p) {
+      u32x4 w;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int e = j < 2 ? 4 * j : 4 * j - 7;   // the order that codes_bf16 leaves them in: 0 2 4 6 1 3 5 7
+        w[j] = take_part(x[e], x[e + 2]);
+      }
+      q[p][t] = as_bf16x8(w);
+    }
+  }
+  qsum = sum_over_groups(qsum);
+  const float sc = a.scale * kLog2e;
+  f32x4 o[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) o[e] = kZeroF4;
+  float m = -INFINITY, l = 0.f, low = 0.f;
+
+  struct Pages { int k[U], v[U]; };
+  auto pages = [&](int t0) {
+    Pages p;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      p.k[u] = t0 + 16 * u + i < to ? table[(t0 + 16 * u + i) >> a.shift] : -1;
+      p.v[u] = t0 + 16 * u + 4 * L < to ? table[(t0 + 16 * u + 4 * L) >> a.shift] : -1;
+    }
+    return p;
+  };
+  auto there = [&](int page) { return (unsigned)page < (unsigned)a.n_pages; };
+  struct Tile {
+    KeyCodes k[U];
+    uint32_t v[U][4], kp[U][4], vp[U][4];   // value codes and the pairs of keys and values of tokens 4 L + r
+  };
+  // rows that are not there are read from page 0: in bounds, and masked
+  auto load = [&](Tile& x, const Pages& p, int t0) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int key = t0 + 16 * u + i, four = t0 + 16 * u + 4 * L;
+      x.k[u] = *reinterpret_cast<const KeyCodes*>(kc + (there(p.k[u]) ? p.k[u] * a.kps[0] + (key & in_page) * a.kps[2] : 0) + q4_piece(D) * L);
+      const char* ks = kc + (there(p.v[u]) ? p.v[u] * a.kps[0] + (four & in_page) * a.kps[2] : 0);
+      const char* vs = vc + (there(p.v[u]) ? p.v[u] * a.vps[0] + (four & in_page) * a.vps[2] : 0);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        x.kp[u][r] = reinterpret_cast<const uint32_t*>(ks + r * a.kps[2])[D / 8 + g];
+        x.vp[u][r] = reinterpret_cast<const uint32_t*>(vs + r * a.vps[2])[D / 8 + g];
+        x.v[u][r] = reinterpret_cast<const typename S::ValueCodes*>(vs + r * a.vps[2])[i];
+      }
+    }
+  };
+
+  const int step = kWaves * R;
+  int t0 = from + wave * R;
+  Pages here = pages(t0);   // looked up a tile ahead
+  for (; t0 < to; t0 += step) {
+    Tile x;
+    load(x, here, t0);
+    const Pages next = pages(t0 + step);
+    if ((unsigned)(own - t0) < (unsigned)R) {   // this tile holds the new token
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (t0 + 16 * u + i == own) x.k[u] = *reinterpret_cast<const KeyCodes*>(reinterpret_cast<const char*>(sm_new[0]) + q4_piece(D) * L);
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (t0 + 16 * u + 4 * L + r == own) {
+            x.kp[u][r] = sm_new[0][D / 8 + g];
+            x.vp[u][r] = sm_new[1][D / 8 + g];
+            x.v[u][r] = reinterpret_cast<const typename S::ValueCodes*>(sm_new[1])[i];
+          }
+      }
+    }
+    float w[U][4];
+    uint32_t in[U];
+    bool whole = true;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int key = t0 + 16 * u + i;
+      in[u] = (uint32_t)__builtin_amdgcn_ballot_w64(key < to && (there(here.k[u]) || key == own)) & 0xffffu;
+      whole = whole && in[u] == 0xffffu;
+      f32x4 s = kZeroF4;
+#pragma unroll
+      for (int t = 0; t < ST; ++t) {
+        const uint32_t even = x.k[u][t] & kNibbles, odd = x.k[u][t] >> 4 & kNibbles;
+        const bf16x8 codes = as_bf16x8(u32x4{codes_bf16(even, false), codes_bf16(even, true), codes_bf16(odd, false), codes_bf16(odd, true)});
+#pragma unroll
+        for (int p = PARTS - 1; p >= 0; --p) s = mfma16(codes, q[p][t], s);
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        float y = fmaf(bf16_lo(x.kp[u][r]), s[r], bf16_hi(x.kp[u][r]) * qsum);
+        y += beside<1>(y);
+        if (GR == 4) y += beside<2>(y);
+        w[u][r] = y * sc;
+      }
+    }
+    if (!whole) {
+      // what is not there gets no weight, and its values, which may be anything, become zero
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (!(in[u] >> (4 * L + r) & 1u)) {
+            w[u][r] = -INFINITY;
+            x.vp[u][r] = 0u;
+          }
+    }
+    float top = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < U; ++u) top = fmaxf(top, fmaxf(fmaxf(w[u][0], w[u][1]), fmaxf(w[u][2], w[u][3])));
+    top = max_over_groups(top);
+    if (__builtin_amdgcn_ballot_w64(top > m + 8.f) != 0) {   // weights stay below 2^8 (packed_fwd.hip)
+      const float up = fmaxf(m, top), by = __builtin_amdgcn_exp2f(m - (up == -INFINITY ? 0.f : up));
+      m = up;
+      l *= by;
+      low *= by;
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] *= by;
+    }
+    const float ref = m == -INFINITY ? 0.f : m;
+    u32x4 weights[PARTS];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int r = 0; r < 4; r += 2) {
+        float y[2];
+#pragma unroll
+        for (int z = 0; z < 2; ++z) {
+          const float p = __builtin_amdgcn_exp2f(w[u][r + z] - ref);
+          l += p;
+          low = fmaf(p, bf16_hi(x.vp[u][r + z]), low);
+          y[z] = p * bf16_lo(x.vp[u][r + z]);
+        }
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) weights[p][2 * u + r / 2] = take_part(y[0], y[1]);
+      }
+    // channels of the same byte's half and parity at a time: a byte of each of two tokens, then one of the next
+#pragma unroll
+    for (int half = 0; half < E / 4; ++half) {
+      uint32_t two[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        two[j] = __builtin_amdgcn_perm(x.v[j / 2][2 * (j % 2) + 1], x.v[j / 2][2 * (j % 2)], half ? 0x07030602u : 0x05010400u);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        u32x4 codes;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) codes[j] = codes_bf16(two[j] >> (4 * (e % 2)) & kNibbles, e >= 2);
+#pragma unroll
+        for (int p = PARTS - 1; p >= 0; --p) o[4 * half + e] = mfma16(as_bf16x8(codes), as_bf16x8(weights[p]), o[4 * half + e]);
+      }
+    }
+    here = next;
+  }
+  l = sum_over_groups(l);
+  low = sum_over_groups(low);
+
+  // join the waves: a channel counts in its own group's column
+  if (L == 0 && g == 0) {
+    sm_m[wave][h] = m;
+    sm_l[wave][h] = l;
+  }
+  if (g == mine) {
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sm_o[wave][h][E * (4 * L + r) + e] = o[e][r] + low;
+  }
+  __syncthreads();
+  const int c = tid % D;
+  for (int x = tid / D; x < heads; x += kPagedThreads / D) {
+    float top = -INFINITY, sum = 0.f, acc = 0.f;
+#pragma unroll
+    for (int y = 0; y < kWaves; ++y) top = fmaxf(top, sm_m[y][x]);
+    const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+    for (int y = 0; y < kWaves; ++y) {
+      const float by = __builtin_amdgcn_exp2f(sm_m[y][x] - ref);
+      sum = fmaf(sm_l[y][x], by, sum);
+      acc = fmaf(sm_o[y][x][c], by, acc);
+    }
+    if (a.splits == 1) {
+      Storage<T>::store(rows_of<T>(a.out, a.os, b, h0 + x), c, sum == 0.f ? 0.f : acc / sum);
+    } else {
+      const int64_t at = ((int64_t)b * a.H + h0 + x) * a.splits + split;
+      a.sums[at * D + c] = acc;
+      if (c == 0) {
+        a.stats[2 * at] = top;
+        a.stats[2 * at + 1] = sum;
+      }
+    }
+  }
+}
+
+// Workgroups of an uncut call.
+int64_t decode_units(int B, int H, int Hkv, int d) {
+  const int hc = q4_heads(d);
+  return (int64_t)B * Hkv * (((int64_t)H / Hkv + hc - 1) / hc);
+}
+
+template <typename T, int D> hipError_t decode(const PagedDecodeArgs& a, hipStream_t s) {
+  const unsigned workgroups = (unsigned)(decode_units(a.B, a.H, a.Hkv, D) * a.splits);
+  q4_decode_kernel<T, D><<<dim3(workgroups), dim3(kPagedThreads), 0, s>>>(a);
+  const hipError_t e = hipGetLastError();
+  return e != hipSuccess || a.splits == 1 ? e : launch_paged_join(a, sizeof(T) == 2, s);
+}
+
+unsigned row_groups(int total, int n_seqs, int Hkv) { return (unsigned)(packed_tiles(total, n_seqs, kRows) * Hkv); }
+
+}  // namespace
+
+PagedSplit paged_q4_split(int B, int H, int Hkv, int d, int64_t max_len) {
+  constexpr int64_t kWorkgroups = 1536;
+  const int64_t units = decode_units(B, H, Hkv, d);
+  const int64_t share = units < kWorkgroups ? (max_len * units + kWorkgroups - 1) / kWorkgroups : max_len;
+  const int64_t chunk = std::max<int64_t>(128, (share + 63) / 64 * 64);
+  return {(int)chunk, (int)std::max<int64_t>(1, (max_len + chunk - 1) / chunk)};
+}
+
+bool paged_q4_decode_fits(int B, int H, int Hkv, int d, PagedSplit s) {
+  return decode_units(B, H, Hkv, d) * s.splits <= most_workgroups(kPagedThreads) &&
+         (s.splits == 1 || (int64_t)B * H <= most_workgroups(kPagedThreads));
+}
+bool paged_q4_rows_fit(int total, int n_seqs, int Hkv) { return packed_tiles(total, n_seqs, kRows) * Hkv <= most_workgroups(kPagedThreads); }
+
+hipError_t launch_paged_q4_decode(const PagedDecodeArgs& a, bool bf16, hipStream_t s) {
+  if (bf16) return a.d == 128 ? decode<uint16_t, 128>(a, s) : decode<uint16_t, 64>(a, s);
+  return a.d == 128 ? decode<float, 128>(a, s) : decode<float, 64>(a, s);
+}
+
+hipError_t launch_paged_q4_fill(const PagedFillArgs& a, bool bf16, hipStream_t s) {
+  const dim3 grid(row_groups(a.total, a.n_seqs, a.Hkv));
+  if (bf16) a.d == 128 ? q4_fill_kernel<uint16_t, 128><<<grid, kPagedThreads, 0, s>>>(a) : q4_fill_kernel<uint16_t, 64><<<grid, kPagedThreads, 0, s>>>(a);
+  else a.d == 128 ? q4_fill_kernel<float, 128><<<grid, kPagedThreads, 0, s>>>(a) : q4_fill_kernel<float, 64><<<grid, kPagedThreads, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_paged_q4_read(const PagedReadArgs& a, bool bf16, hipStream_t s) {
+  const dim3 grid(row_groups(a.total, a.n_seqs, a.Hkv));
+  if (bf16) a.d == 128 ? q4_read_kernel<uint16_t, 128><<<grid, kPagedThreads, 0, s>>>(a) : q4_read_kernel<uint16_t, 64><<<grid, kPagedThreads, 0, s>>>(a);
+  else a.d == 128 ? q4_read_kernel<float, 128><<<grid, kPagedThreads, 0, s>>>(a) : q4_read_kernel<float, 64><<<grid, kPagedThreads, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_pages_q4_copy(const PagesCopyArgs& a, hipStream_t s) {
+  const dim3 grid((unsigned)((int64_t)a.n_copies * a.Hkv));
+  a.d == 128 ? q4_copy_kernel<128><<<grid, kPagedThreads, 0, s>>>(a) : q4_copy_kernel<64><<<grid, kPagedThreads, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace gformer

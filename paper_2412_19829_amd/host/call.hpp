@@ -65,6 +65,11 @@ PyObject* packed_bwd(PyObject*, PyObject* const* a, Py_ssize_t n);
 PyObject* paged_fill(PyObject*, PyObject* const* a, Py_ssize_t n);
 PyObject* paged_decode(PyObject*, PyObject* const* a, Py_ssize_t n);
 PyObject* pages_copy(PyObject*, PyObject* const* a, Py_ssize_t n);
+PyObject* paged_fill_q4(PyObject*, PyObject* const* a, Py_ssize_t n);
+PyObject* paged_read_q4(PyObject*, PyObject* const* a, Py_ssize_t n);
+PyObject* paged_decode_q4(PyObject*, PyObject* const* a, Py_ssize_t n);
+PyObject* pages_copy_q4(PyObject*, PyObject* const* a, Py_ssize_t n);
+PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n);
 // packed_grad.cpp
 PyObject* packed_attention(PyObject*, PyObject* const* a, Py_ssize_t n);
 

@@ -102,6 +102,11 @@ PyMethodDef methods[] = {
     {"paged_fill", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(paged_fill)), METH_FASTCALL, "gformer_paged_fill"},
     {"paged_decode", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(paged_decode)), METH_FASTCALL, "gformer_paged_decode"},
     {"pages_copy", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(pages_copy)), METH_FASTCALL, "gformer_pages_copy"},
+    {"paged_fill_q4", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(paged_fill_q4)), METH_FASTCALL, "gformer_paged_fill_q4"},
+    {"paged_read_q4", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(paged_read_q4)), METH_FASTCALL, "gformer_paged_read_q4"},
+    {"paged_decode_q4", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(paged_decode_q4)), METH_FASTCALL, "gformer_paged_decode_q4"},
+    {"pages_copy_q4", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(pages_copy_q4)), METH_FASTCALL, "gformer_pages_copy_q4"},
+    {"rotary", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(rotary)), METH_FASTCALL, "gformer_rotary"},
     {"packed_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(packed_attention)), METH_FASTCALL, "packed attention as a node"},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_decode_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

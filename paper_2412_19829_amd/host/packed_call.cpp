@@ -147,21 +147,29 @@ struct Packed {
   }
 };
 
-struct Pages {
+// Pages of rows of d elements, or of 4 bits a value (bytes).
+template <bool Q4> struct Pages {
   const at::Tensor *k, *v;
   bool of(Call& c, PyObject* ko, PyObject* vo, gformer_paged_params& p) {
     k = strided(ko), v = strided(vo);
-    if (!c.tensors({k, v}, 4) || k->sizes() != v->sizes()) return false;
+    if (!(Q4 ? bytes(k) && bytes(v) : c.tensors({k, v}, 4)) || k->sizes() != v->sizes()) return false;
     std::memset(&p, 0, sizeof(p));
     p.struct_size = sizeof(p);
-    p.dtype = c.dtype();
+    if (Q4 && !c.like) c.like = k;   // pages of codes alone, which are of neither type
+    p.dtype = c.like->scalar_type() == at::kFloat ? GF_F32 : GF_BF16;
     p.page_size = (int32_t)k->size(2);
     p.softmax_scale = 1.f;
     return row_strides(*k, p.kpage_stride) && row_strides(*v, p.vpage_stride);
   }
+  static bool bytes(const at::Tensor* t) {
+    if (!t || t->dim() != 4 || t->scalar_type() != at::kByte || (t->size(3) != 40 && t->size(3) != 80)) return false;
+    for (const int64_t n : t->sizes())
+      if (!fits_int(n)) return false;
+    return true;
+  }
   int count() const { return (int)k->size(0); }
   int heads() const { return (int)k->size(1); }
-  int d() const { return (int)k->size(3); }
+  int d() const { return Q4 ? (int)k->size(3) / 5 * 8 : (int)k->size(3); }
 };
 
 }  // namespace
@@ -224,39 +232,41 @@ PyObject* packed_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// address, k, v, kpages, vpages, table, start, cu, stream
-PyObject* paged_fill(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (n != 9) return wrong_count("paged_fill takes 9 arguments");
+namespace {
+
+// A call that moves packed rows into pages or out of them, its four tensors in the entry point's order: address, four tensors, table,
+// start, cu, stream.
+template <bool Q4, bool OUT, typename F> PyObject* rows_call(PyObject* const* a, F call) {
   Call c;
-  Pages x;
+  Pages<Q4> x;
   gformer_paged_params p;
   const at::Tensor *k = nullptr, *v = nullptr, *table = nullptr, *start = nullptr, *cu = nullptr;
-  const auto call = address<decltype(&gformer_paged_fill)>(a[0]);
+  const int rows = OUT ? 3 : 1, pages = OUT ? 1 : 3;
   return run(c, [&] {
-    k = strided(a[1]), v = strided(a[2]);
+    k = strided(a[rows]), v = strided(a[rows + 1]);
     table = numbers(a[5], 2), start = numbers(a[6], 1), cu = numbers(a[7], 1);
-    return call && c.tensors({k, v}, 3) && x.of(c, a[3], a[4], p) && k->sizes() == v->sizes() && k->size(1) == x.heads() &&
+    return call && c.tensors({k, v}, 3) && x.of(c, a[pages], a[pages + 1], p) && k->sizes() == v->sizes() && k->size(1) == x.heads() &&
            k->size(2) == x.d() && row_strides(*k, p.k_stride) && row_strides(*v, p.v_stride) && table && start && cu &&
            cu->numel() >= 1 && fits_int(cu->numel()) && table->size(0) == cu->numel() - 1 && fits_int(table->size(1)) &&
            start->numel() == cu->numel() - 1 && c.stream_of(a[8]) && c.device({k, v, x.k, x.v, table, start, cu});
   }, [&](void* s) {
-    return call(at_of(k), at_of(v), at_of(x.k), at_of(x.v), ints(table), ints(start), ints(cu), (int)cu->numel() - 1, (int)k->size(0),
-                x.heads(), x.d(), x.count(), (int)table->size(1), &p, s);
+    const at::Tensor* at[4] = {OUT ? x.k : k, OUT ? x.v : v, OUT ? k : x.k, OUT ? v : x.v};
+    return call(at_of(at[0]), at_of(at[1]), at_of(at[2]), at_of(at[3]), ints(table), ints(start), ints(cu), (int)cu->numel() - 1,
+                (int)k->size(0), x.heads(), x.d(), x.count(), (int)table->size(1), &p, s);
   });
 }
 
 // address, address of the workspace's size, q, k, v, out, kpages, vpages, table, lens, max_len, softmax_scale, workspace, stream
-PyObject* paged_decode(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (n != 14) return wrong_count("paged_decode takes 14 arguments");
+template <bool Q4> PyObject* decode_call(PyObject* const* a) {
   Call c;
-  Pages x;
+  Pages<Q4> x;
   gformer_paged_params p;
   const at::Tensor *q = nullptr, *k = nullptr, *v = nullptr, *out = nullptr, *table = nullptr, *lens = nullptr;
   int64_t max_len = 0;
   void* ws = nullptr;
   size_t bytes = 0;
   at::Tensor own;
-  const auto call = address<decltype(&gformer_paged_decode)>(a[0]);
+  const auto call = address<decltype(&gformer_paged_decode)>(a[0]);   // the other cache's is of the same type
   const auto size = address<decltype(&gformer_paged_decode_workspace_bytes)>(a[1]);
   return run(c, [&] {
     bool ok = call && size && (a[3] == Py_None) == (a[4] == Py_None);
@@ -282,10 +292,9 @@ PyObject* paged_decode(PyObject*, PyObject* const* a, Py_ssize_t n) {
 }
 
 // address, kpages, vpages, src, dst, stream
-PyObject* pages_copy(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (n != 6) return wrong_count("pages_copy takes 6 arguments");
+template <bool Q4> PyObject* copy_call(PyObject* const* a) {
   Call c;
-  Pages x;
+  Pages<Q4> x;
   gformer_paged_params p;
   const at::Tensor *src = nullptr, *dst = nullptr;
   const auto call = address<decltype(&gformer_pages_copy)>(a[0]);
@@ -295,6 +304,80 @@ PyObject* pages_copy(PyObject*, PyObject* const* a, Py_ssize_t n) {
            c.device({x.k, x.v, src, dst});
   }, [&](void* s) {
     return call(at_of(x.k), at_of(x.v), ints(src), ints(dst), (int)src->numel(), x.heads(), x.d(), x.count(), &p, s);
+  });
+}
+
+}  // namespace
+
+// address, k, v, kpages, vpages, table, start, cu, stream
+PyObject* paged_fill(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 9) return wrong_count("paged_fill takes 9 arguments");
+  return rows_call<false, false>(a, address<decltype(&gformer_paged_fill)>(a[0]));
+}
+PyObject* paged_fill_q4(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 9) return wrong_count("paged_fill_q4 takes 9 arguments");
+  return rows_call<true, false>(a, address<decltype(&gformer_paged_fill_q4)>(a[0]));
+}
+// address, kpages, vpages, k, v, table, start, cu, stream
+PyObject* paged_read_q4(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 9) return wrong_count("paged_read_q4 takes 9 arguments");
+  return rows_call<true, true>(a, address<decltype(&gformer_paged_read_q4)>(a[0]));
+}
+PyObject* paged_decode(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return n == 14 ? decode_call<false>(a) : wrong_count("paged_decode takes 14 arguments");
+}
+PyObject* paged_decode_q4(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return n == 14 ? decode_call<true>(a) : wrong_count("paged_decode_q4 takes 14 arguments");
+}
+PyObject* pages_copy(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return n == 6 ? copy_call<false>(a) : wrong_count("pages_copy takes 6 arguments");
+}
+PyObject* pages_copy_q4(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return n == 6 ? copy_call<true>(a) : wrong_count("pages_copy_q4 takes 6 arguments");
+}
+
+// address, q, k, q_out, k_out, freqs, positions, cu, start, interleaved, inverse, factor, zero_tail, stream
+PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 14) return wrong_count("rotary takes 14 arguments");
+  Call c;
+  gformer_rotary_params p;
+  const at::Tensor *q = nullptr, *k = nullptr, *qo = nullptr, *ko = nullptr, *freqs = nullptr, *positions = nullptr, *cu = nullptr, *start = nullptr;
+  const auto call = address<decltype(&gformer_rotary)>(a[0]);
+  return run(c, [&] {
+    bool ok = call && (a[2] == Py_None) == (a[4] == Py_None);
+    q = strided(a[1]), k = optional(a[2], ok), qo = strided(a[3]), ko = optional(a[4], ok), freqs = plain(a[5]);
+    if (!ok || !c.tensors({q, qo}, 3) || q->sizes() != qo->sizes() ||
+        (k && (!c.tensors({k, ko}, 3) || k->sizes() != ko->sizes() || k->size(0) != q->size(0) || k->size(2) != q->size(2))) || !freqs ||
+        freqs->scalar_type() != at::kFloat || freqs->dim() != 1 || !fits_int(2 * freqs->numel()))
+      return false;
+    std::memset(&p, 0, sizeof(p));
+    if (a[6] != Py_None) {
+      positions = numbers(a[6], 1);
+      if (!positions || positions->numel() != q->size(0) || a[7] != Py_None || a[8] != Py_None) return false;
+    } else {
+      cu = numbers(a[7], 1);
+      if (!cu || cu->numel() < 1 || !fits_int(cu->numel())) return false;
+      if (a[8] != Py_None) {
+        start = numbers(a[8], 1);
+        if (!start || start->numel() != cu->numel() - 1) return false;
+      }
+    }
+    int64_t interleaved, inverse, zero;
+    if (!to_long(a[9], INT_MIN, INT_MAX, interleaved) || !to_long(a[10], INT_MIN, INT_MAX, inverse) || !to_float(a[11], p.factor) ||
+        !to_long(a[12], INT_MIN, INT_MAX, zero) || !row_strides(*q, p.q_stride) || !row_strides(*qo, p.q_out_stride) ||
+        (k && (!row_strides(*k, p.k_stride) || !row_strides(*ko, p.k_out_stride))) || !c.stream_of(a[13]) ||
+        !c.device({q, qo, k, ko, freqs, positions, cu, start}))
+      return false;
+    p.struct_size = sizeof(p);
+    p.dtype = c.dtype();
+    p.rot = (int32_t)(2 * freqs->numel());
+    p.interleaved = (int32_t)interleaved;
+    p.inverse = (int32_t)inverse;
+    p.zero_tail = (int32_t)zero;
+    return true;
+  }, [&](void* s) {
+    return call(at_of(q), at_of(k), at_of(qo), at_of(ko), static_cast<const float*>(at_of(freqs)), ints(positions), ints(cu), ints(start),
+                cu ? (int)cu->numel() - 1 : 0, (int)q->size(0), (int)q->size(1), k ? (int)k->size(1) : 0, (int)q->size(2), &p, s);
   });
 }
 

@@ -18,18 +18,22 @@ from . import binding as gb
 
 class PagedCache:
     """Room for `n_pages` pages of `page_size` tokens, for up to `max_seqs` sequences of up to `max_pages` pages, `n_heads` key
-    heads of size `d` in each of `layers` layers."""
+    heads of size `d` in each of `layers` layers.  bits=4: pages of 4 bits a value, for gformer_paged_fill_q4 and the calls beside it,
+    whose rows may be of either type."""
 
     def __init__(self, n_pages: int, page_size: int, n_heads: int, d: int, max_seqs: int, max_pages: int, *, layers: int = 1,
-                 dtype=torch.bfloat16, device="cuda"):
+                 dtype=torch.bfloat16, device="cuda", bits: int = 0):
         if min(n_pages, page_size, n_heads, d, max_seqs, max_pages, layers) < 1:
             raise ValueError("sizes must be positive")
         if d not in (64, 128) or dtype not in (torch.bfloat16, torch.float32):
             raise ValueError("d is 64 or 128, dtype bfloat16 or float32")
+        if bits not in (0, 4):
+            raise ValueError("bits is 4, or 0 for dtype's own")
         if not 8 <= page_size <= 65536 or page_size & (page_size - 1) or max_pages * page_size > 1 << 30:
             raise ValueError("page_size is a power of two from 8 to 65536, a sequence has at most 2^30 tokens")
         self.page_size, self.n_heads, self.max_pages = page_size, n_heads, max_pages
-        self.kpages = torch.zeros(n_pages, layers * n_heads, page_size, d, dtype=dtype, device=device)
+        row, dtype = (d // 2 + d // 8, torch.uint8) if bits == 4 else (d, dtype)
+        self.kpages = torch.zeros(n_pages, layers * n_heads, page_size, row, dtype=dtype, device=device)
         self.vpages = torch.zeros_like(self.kpages)
         self.table = torch.full((max_seqs, max_pages), -1, dtype=torch.int32, device=device)
         self.lens = torch.full((max_seqs,), -1, dtype=torch.int32, device=device)   # -1: an idle row
@@ -105,10 +109,11 @@ class PagedCache:
     def _copy(self, pairs):
         if pairs:
             src, dst = self._send(list(zip(*pairs)), torch.int32)
-            gb.gformer_pages_copy(self.kpages, self.vpages, src, dst)
+            copy = gb.gformer_pages_copy_q4 if self.kpages.dtype == torch.uint8 else gb.gformer_pages_copy
+            copy(self.kpages, self.vpages, src, dst)
 
     def open(self, tokens: int = 0) -> int:
-        """A new sequence of `tokens` tokens, whose keys and values the caller writes (gformer_paged_fill)."""
+        """A new sequence of `tokens` tokens, whose keys and values the caller writes (gformer_paged_fill, gformer_paged_fill_q4)."""
         n = -(-tokens // self.page_size)
         if tokens < 0 or n > self.max_pages:
             raise ValueError(f"a sequence has 0 to {self.max_pages * self.page_size} tokens")

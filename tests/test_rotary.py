@@ -1,0 +1,241 @@
+"""Rotary positions and their gradients."""
+from __future__ import annotations
+
+import ctypes
+import math
+
+import pytest
+import torch
+
+from paper_2412_19829_amd import binding as gb
+from paper_2412_19829_amd.autograd import gformer_packed_attention, gformer_rotary_positions
+from paper_2412_19829_amd.rotary import rotary_factor, rotary_frequencies
+from tests import packed_reference as pref
+
+gpu = pytest.mark.gpu
+A = 1 << 20
+U = pref.U
+
+
+# ---- refusals and frequencies (CPU) ----------------------------------------------------------------
+
+def wrong(**kw):
+    p = gb.make_rotary_params()
+    for name, val in kw.items():
+        setattr(p, name, val if not isinstance(val, tuple) else (ctypes.c_int64 * len(val))(*val))
+    return p
+
+
+def rotary(p=None, q=A, k=2 * A, qo=3 * A, ko=4 * A, freqs=5 * A, positions=0, cu=6 * A, start=7 * A, n=2, total=5, H=4, Hkv=2, d=64):
+    return gb.lib().gformer_rotary(q, k, qo, ko, freqs, positions, cu, start, n, total, H, Hkv, d, ctypes.byref(p or gb.make_rotary_params()), None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(total=0), 0), (dict(q=0), 1), (dict(k=0), 1), (dict(qo=0), 1), (dict(ko=0), 1), (dict(freqs=0), 1), (dict(cu=0), 1),
+    (dict(positions=8 * A), 1), (dict(k=0, ko=0), 1), (dict(Hkv=0), 1), (dict(positions=8 * A, cu=0, start=0), 1),       # n stays 2
+    (dict(qo=2 * A), 1), (dict(ko=A), 1), (dict(ko=3 * A), 1), (dict(q=A + 8), 1), (dict(cu=A + 2), 1), (dict(freqs=A + 2), 1),
+    (dict(n=-1), 1), (dict(total=-1), 1), (dict(H=0), 1), (dict(Hkv=-1), 1), (dict(d=0), 1), (dict(d=96), 2), (dict(d=32, p=wrong(rot=32)), 2),
+    (dict(p=wrong(rot=0)), 1), (dict(p=wrong(rot=24)), 2), (dict(p=wrong(rot=80)), 1), (dict(p=wrong(rot=-16)), 1), (dict(p=wrong(interleaved=2)), 1),
+    (dict(p=wrong(inverse=-1)), 1), (dict(p=wrong(zero_tail=2)), 1), (dict(p=wrong(factor=math.nan)), 1), (dict(p=wrong(factor=math.inf)), 1),
+    (dict(p=wrong(reserved0=1)), 1), (dict(p=wrong(struct_size=8)), 1), (dict(p=wrong(dtype=2)), 1), (dict(p=wrong(q_stride=(256, 60))), 1),
+    (dict(p=wrong(q_out_stride=(32, 64))), 1), (dict(p=wrong(k_out_stride=((1 << 20) + 8, 64))), 2), (dict(H=1 << 15, total=1), 2),
+    (dict(qo=A, p=wrong(q_out_stride=(512, 64))), 1), (dict(ko=2 * A, p=wrong(k_stride=(512, 64))), 1),       # in place, but elsewhere
+    (dict(total=1 << 30, H=64, d=128), 2), (dict(total=(1 << 30) + 1), 2),
+])
+def test_refusals(kw, status):
+    assert rotary(**kw) == status
+
+
+def test_binding_refuses():
+    z = torch.zeros
+    q, k, f = z(3, 4, 64), z(3, 2, 64), z(32)
+    with pytest.raises(ValueError, match="device"):
+        gb.gformer_rotary(q, k, z(3, 4, 64), z(3, 2, 64), f, positions=z(3, dtype=torch.int32))
+    with pytest.raises(ValueError, match="together"):
+        gb.gformer_rotary(q, k, z(3, 4, 64), None, f, positions=z(3, dtype=torch.int32))
+    for bad in (lambda: rotary_frequencies(0, device="cpu"), lambda: rotary_frequencies(7, device="cpu"), lambda: rotary_frequencies(64, -1.0, device="cpu"),
+                lambda: rotary_frequencies(64, stretch=0.5, device="cpu"), lambda: rotary_frequencies(64, slow=4.0, fast=2.0, device="cpu"),
+                lambda: rotary_frequencies(64, trained=-1, device="cpu"), lambda: rotary_factor(0.5)):
+        with pytest.raises(ValueError):
+            bad()
+
+
+def test_frequencies():
+    f = rotary_frequencies(64, device="cpu")
+    assert f.dtype == torch.float32 and f.shape == (32,) and f[0] == 1.0
+    assert torch.equal(f, torch.tensor([10000.0 ** (-i / 32) for i in range(32)], dtype=torch.float64).float())
+    assert torch.equal(rotary_frequencies(64, stretch=4.0, device="cpu"), f / 4)
+    g = rotary_frequencies(64, stretch=4.0, trained=4096, device="cpu")
+    turns = 4096 * f.double() / (2 * math.pi)
+    assert torch.equal(g[turns >= 32], f[turns >= 32]) and torch.equal(g[turns <= 1], f[turns <= 1] / 4)
+    mid = (turns > 1) & (turns < 32)
+    assert mid.any() and bool((g[mid] < f[mid]).all()) and bool((g[mid] > f[mid] / 4).all())
+    assert rotary_factor(1.0) == 1.0 and rotary_factor(math.e) == pytest.approx(1.1)
+
+
+# ---- against 64 bits (GPU) -------------------------------------------------------------------------
+
+def turned(x, freqs, positions, rot, interleaved, factor, dtype, inverse=0):
+    """(value, bound) of [rows, heads, d] in 64 bits.  The cosine and sine are off by three half steps of 1 (the angle's remainder and the
+    series), the factor, the products and the sum by one each; then the result's rounding."""
+    x = x.detach().double().cpu()
+    angle = positions.double()[:, None] * freqs.double().cpu()
+    cos, sin = factor * torch.cos(angle)[:, None], (-1 if inverse else 1) * factor * torch.sin(angle)[:, None]
+    first, second = (slice(0, rot, 2), slice(1, rot, 2)) if interleaved else (slice(0, rot // 2), slice(rot // 2, rot))
+    y, bound = x.clone(), torch.zeros_like(x)
+    a, b = x[..., first], x[..., second]
+    y[..., first], y[..., second] = a * cos - b * sin, b * cos + a * sin
+    far = 2.0 ** -52 * angle.abs()[:, None]                              # the product of position and frequency in 64 bits
+    for half in (first, second):
+        bound[..., half] = (6 * U + far) * abs(factor) * (a.abs() + b.abs()) + pref.HALF[dtype] * y[..., half].abs()
+    return y, bound
+
+
+def ints(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def inputs(gen, dtype, rows, H, Hkv, d, wide):
+    T = pref.TYPES[dtype]
+    qkv = torch.randn(rows, H + 2 * Hkv, d, generator=gen).to(T).cuda()
+    q, k = qkv[:, :H], qkv[:, H:H + Hkv]
+    return (q, k) if wide else (q.contiguous(), k.contiguous())
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("interleaved", [0, 1])
+@pytest.mark.parametrize("H,Hkv,d,rot,wide", [(1, 1, 64, 64, False), (12, 12, 64, 16, True), (8, 2, 128, 128, True), (7, 1, 128, 48, False),
+                                              (33, 3, 64, 48, False), (4, 4, 128, 80, True)])
+def test_positions_by_row(dtype, interleaved, H, Hkv, d, rot, wide):
+    gen = torch.Generator().manual_seed(H + d + rot)
+    pos = [0, 1, -1, 7, 2047, 131071, 1 << 20, (1 << 31) - 1, -(1 << 31), 5, 6, 1000003, 12345678, 3, 4, 99, 40]
+    q, k = inputs(gen, dtype, len(pos), H, Hkv, d, wide)
+    freqs = rotary_frequencies(rot)
+    for factor, inverse in ((1.0, 0), (1.5, 1)):
+        qo, ko = torch.full(q.shape, 7.0, dtype=q.dtype, device="cuda"), torch.full(k.shape, 7.0, dtype=k.dtype, device="cuda")
+        gb.gformer_rotary(q, k, qo, ko, freqs, positions=ints(pos), interleaved=interleaved, factor=factor, inverse=inverse)
+        for got, x in ((qo, q), (ko, k)):
+            want, bound = turned(x, freqs, torch.tensor(pos), rot, interleaved, factor, dtype, inverse)
+            pref.check(got, want, bound, f"{factor}")
+    # queries alone, in place
+    want = torch.empty_like(q, memory_format=torch.contiguous_format)
+    gb.gformer_rotary(q, None, want, None, freqs, positions=ints(pos), interleaved=interleaved)
+    rest = k.clone()
+    gb.gformer_rotary(q, None, q, None, freqs, positions=ints(pos), interleaved=interleaved)
+    assert torch.equal(q, want) and torch.equal(k, rest)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lens,start", [([5], [0]), ([1], [100]), ([0, 3, 0, 0, 70, 1, 0], [9, 4000, 3, 1, 0, 1 << 30, 2]), ([33] * 40, None),
+                                        ([300, 31, 32, 33], [0, 1, 2, 3]), ([], [])])
+@pytest.mark.parametrize("tail", [0, 9])
+def test_packed(dtype, lens, start, tail):
+    gen = torch.Generator().manual_seed(len(lens) + tail)
+    H, Hkv, d, rows = 8, 2, 64, sum(lens) + tail
+    q, k = inputs(gen, dtype, rows, H, Hkv, d, True)
+    freqs = rotary_frequencies(d, stretch=4.0, trained=2048)
+    pos = torch.cat([torch.arange(n) + (0 if start is None else start[s]) for s, n in enumerate(lens)] + [torch.zeros(0, dtype=torch.long)])
+    for zero in (0, 1):
+        qo, ko = torch.full(q.shape, 7.0, dtype=q.dtype, device="cuda"), torch.full(k.shape, 7.0, dtype=k.dtype, device="cuda")
+        gb.gformer_rotary(q, k, qo, ko, freqs, cu=ints(pref.offsets(lens)), start=None if start is None else ints(start), zero_tail=zero)
+        for got, x in ((qo, q), (ko, k)):
+            want, bound = turned(x[:sum(lens)], freqs, pos, d, 0, 1.0, dtype)
+            pref.check(got[:sum(lens)], want, bound, "rows")
+            assert bool((got[sum(lens):] == (0.0 if zero else 7.0)).all())
+    before = q[sum(lens):].clone()
+    gb.gformer_rotary(q, k, q, k, freqs, cu=ints(pref.offsets(lens)), start=None if start is None else ints(start))
+    assert torch.equal(q[sum(lens):], before) and torch.equal(q[:sum(lens)], qo[:sum(lens)]) and torch.equal(k[:sum(lens)], ko[:sum(lens)])
+
+
+@gpu
+def test_what_is_no_number_stays_in_its_pair():
+    x = torch.ones(2, 1, 64, device="cuda")
+    x[0, 0, 5], x[1, 0, 40] = math.nan, math.inf
+    out = torch.zeros_like(x)
+    gb.gformer_rotary(x, None, out, None, rotary_frequencies(32), positions=ints([3, 4]))
+    bad = ~torch.isfinite(out).cpu()
+    want = torch.zeros(2, 1, 64, dtype=torch.bool)
+    want[0, 0, 5] = want[0, 0, 21] = want[1, 0, 40] = True
+    assert torch.equal(bad, want)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("interleaved,rot", [(0, 64), (1, 32)])
+def test_gradients(dtype, interleaved, rot):
+    gen = torch.Generator().manual_seed(rot)
+    lens, start, H, Hkv, d, factor = [9, 0, 30], [0, 5, 1000], 4, 2, 64, 1.25
+    rows = sum(lens) + 4
+    q, k = (x.clone().requires_grad_(True) for x in inputs(gen, dtype, rows, H, Hkv, d, False))
+    freqs = rotary_frequencies(rot)
+    pos = torch.cat([torch.arange(n) + start[s] for s, n in enumerate(lens)])
+    qo, ko = gformer_rotary_positions(q, k, freqs, cu=ints(pref.offsets(lens)), start=ints(start), interleaved=interleaved, factor=factor)
+    assert bool((qo[sum(lens):] == 0).all())
+    # a gradient in a layout that is handed on as a copy, and one that is broadcast
+    gq = torch.randn(rows, d, H, generator=gen).to(q.dtype).cuda().transpose(1, 2)
+    gk = torch.randn(1, 1, d, generator=gen).to(q.dtype).cuda().expand(rows, Hkv, d)
+    dq, dk = torch.autograd.grad((qo, ko), (q, k), (gq, gk), retain_graph=True)
+    for got, g in ((dq, gq), (dk, gk)):
+        want, bound = turned(g[:sum(lens)], freqs, pos, rot, interleaved, factor, dtype, inverse=1)
+        pref.check(got[:sum(lens)], want, bound, "gradient")
+        assert bool((got[sum(lens):] == 0).all())
+    # one of the two alone
+    assert torch.equal(torch.autograd.grad(ko, k, gk, retain_graph=True)[0], dk)
+    assert torch.equal(torch.autograd.grad(qo, q, gq)[0], dq)
+
+
+@gpu
+def test_gradient_against_differences_and_again():
+    gen = torch.Generator().manual_seed(2)
+    q = torch.randn(5, 2, 64, generator=gen).cuda().requires_grad_(True)
+    freqs, pos = rotary_frequencies(64), ints([0, 3, 77, 1000, 4])
+    f = lambda x: gformer_rotary_positions(x, None, freqs, positions=pos)[0]
+    w, u = torch.randn(5, 2, 64, generator=gen).cuda(), torch.randn(5, 2, 64, generator=gen).cuda()
+    (g,) = torch.autograd.grad((f(q) * w).sum(), q)
+    with torch.no_grad():      # linear: a difference of any width is the derivative, but for 640 sums' and values' roundings
+        diff = ((f(q + u).double() - f(q - u).double()) / 2 * w.double()).sum()
+    size = float((w.double().abs() * (u.double().abs() + q.detach().double().abs()) * 2).sum())
+    assert abs(float(diff) - float((g.double() * u.double()).sum())) <= 16 * U * size
+    # twice: the gradient of |f(q)|^2 / 2 is q for a factor of 1, and its own gradient along u is u
+    (g,) = torch.autograd.grad(0.5 * (f(q) ** 2).sum(), q, create_graph=True)
+    (gg,) = torch.autograd.grad((g * u).sum(), q)
+    for got, want in ((g, q), (gg, u)):
+        pair = want.detach().double().abs()
+        pair = pair + pair.roll(32, -1)
+        assert bool(((got.double() - want.double()).abs() <= 2 * 8 * U * 2 * pair).all())
+
+
+@gpu
+def test_a_captured_training_step():
+    """Turning, packed attention and the way back in one graph, replayed with other inputs."""
+    gen = torch.Generator().manual_seed(1)
+    lens, H, Hkv, d = [40, 0, 23, 1], 4, 2, 64
+    rows = sum(lens) + 8
+    cu, freqs = ints(pref.offsets(lens)), rotary_frequencies(d)
+    rand = lambda h: torch.randn(rows, h, d, generator=gen).bfloat16().cuda()
+    q, k, v, g = rand(H).requires_grad_(True), rand(Hkv).requires_grad_(True), rand(Hkv).requires_grad_(True), rand(H)
+
+    def step(q, k, v):
+        a, b = gformer_rotary_positions(q, k, freqs, cu=cu)
+        out = gformer_packed_attention(a, b, v, cu, softmax_scale=0.125)
+        return (out, *torch.autograd.grad(out, (q, k, v), g))
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(q, k, v)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            held = step(q, k, v)
+    torch.cuda.current_stream().wait_stream(side)
+    for _ in range(3):
+        with torch.no_grad():
+            for t in (q, k, v, g):
+                t.copy_(torch.randn(t.shape, generator=gen))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [x.detach().clone() for x in held]
+        eager = step(*(x.detach().clone().requires_grad_(True) for x in (q, k, v)))
+        assert all(torch.equal(a, b) for a, b in zip(got, eager))
