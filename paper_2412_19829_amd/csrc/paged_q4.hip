@@ -186,9 +186,14 @@ template <int D> struct Shape4 {
 };
 constexpr int q4_heads(int d) { return d == 128 ? Shape4<128>::HC : Shape4<64>::HC; }
 
-// Parts in bf16 that a factor of the products is taken in: bf16 queries are one, their weights are rounded to one (as a bf16
-// cache's are); fp32 takes the three that hold its 24 bits.
-template <typename T> constexpr int kParts = sizeof(T) == 2 ? 1 : 3;
+// Parts in bf16 that a factor of the products is taken in.  Queries: bf16 is one, fp32 the three that hold its 24 bits.  Weights times scales: two
+// for bf16 calls and three for fp32.  In one part their rounding meets codes from 0 to 15, whose sum the lowest values' cancels nearly:
+// the output of 2048 to 32768 random tokens is then off by 1.8 to 2.4 times one rounding of it, in two by one.
+template <typename T> constexpr int kQueryParts = sizeof(T) == 2 ? 1 : 3;
+template <typename T> constexpr int kWeightParts = sizeof(T) == 2 ? 2 : 3;
+// fp32 sums would lose bits to that cancelling too: there the first part meets codes less kMiddle, which goes to the lowest values.
+constexpr float kMiddle = 7.5f;
+constexpr uint32_t kMinusMiddle = 0xc0f0c0f0u;
 
 // x's first bf16 part, two at a time; what it leaves stays in a and b.
 __device__ __forceinline__ uint32_t take_part(float& a, float& b) {
@@ -211,7 +216,7 @@ __device__ __forceinline__ int seen_tokens(const PagedDecodeArgs& a, int b) {
 template <typename T, int D> __global__ __launch_bounds__(kPagedThreads) void q4_decode_kernel(PagedDecodeArgs a) {
   using S = Shape4<D>;
   typedef typename S::KeyCodes KeyCodes;
-  constexpr int GR = S::GR, HC = S::HC, ST = S::ST, E = S::E, PARTS = kParts<T>, ROW = q4_row(D), U = 2, R = 16 * U;
+  constexpr int GR = S::GR, HC = S::HC, ST = S::ST, E = S::E, PARTS = kQueryParts<T>, WPARTS = kWeightParts<T>, ROW = q4_row(D), U = 2, R = 16 * U;
   __shared__ float sm_o[kWaves][HC][D + 4], sm_m[kWaves][HC], sm_l[kWaves][HC];
   __shared__ __align__(16) uint32_t sm_new[2][ROW / 4];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, L = lane >> 4;
@@ -378,7 +383,7 @@ template <typename T, int D> __global__ __launch_bounds__(kPagedThreads) void q4
       for (int e = 0; e < E; ++e) o[e] *= by;
     }
     const float ref = m == -INFINITY ? 0.f : m;
-    u32x4 weights[PARTS];
+    u32x4 weights[WPARTS];
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -392,7 +397,8 @@ template <typename T, int D> __global__ __launch_bounds__(kPagedThreads) void q4
           y[z] = p * bf16_lo(x.vp[u][r + z]);
         }
 #pragma unroll
-        for (int p = 0; p < PARTS; ++p) weights[p][2 * u + r / 2] = take_part(y[0], y[1]);
+        for (int p = 0; p < WPARTS; ++p) weights[p][2 * u + r / 2] = take_part(y[0], y[1]);
+        if (sizeof(T) == 4) low = fmaf(kMiddle, bf16_lo(weights[0][2 * u + r / 2]), fmaf(kMiddle, bf16_hi(weights[0][2 * u + r / 2]), low));
       }
     // channels of the same byte's half and parity at a time: a byte of each of two tokens, then one of the next
 #pragma unroll
@@ -406,8 +412,10 @@ template <typename T, int D> __global__ __launch_bounds__(kPagedThreads) void q4
         u32x4 codes;
 #pragma unroll
         for (int j = 0; j < 4; ++j) codes[j] = codes_bf16(two[j] >> (4 * (e % 2)) & kNibbles, e >= 2);
+        if (sizeof(T) == 4)
+          o[4 * half + e] = mfma16(as_bf16x8(u32x4{kMinusMiddle, kMinusMiddle, kMinusMiddle, kMinusMiddle}), as_bf16x8(weights[0]), o[4 * half + e]);
 #pragma unroll
-        for (int p = PARTS - 1; p >= 0; --p) o[4 * half + e] = mfma16(as_bf16x8(codes), as_bf16x8(weights[p]), o[4 * half + e]);
+        for (int p = WPARTS - 1; p >= 0; --p) o[4 * half + e] = mfma16(as_bf16x8(codes), as_bf16x8(weights[p]), o[4 * half + e]);
       }
     }
     here = next;
