@@ -108,6 +108,7 @@ class _GformerRotary(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dq, dk):
         interleaved, inverse, factor = ctx.how
+        dq, dk = (g if need else None for g, need in zip((dq, dk), ctx.needs_input_grad))
         if dq is None and dk is None:
             return (None,) * 9
         dq, dk = _GformerRotary.apply(dq, dk, *ctx.saved_tensors, interleaved, 1 - inverse, factor)
@@ -118,4 +119,5 @@ def gformer_rotary_positions(q, k, freqs, *, positions=None, cu=None, start=None
     """Queries [total, H, d] and keys [total, Hkv, d] (None: queries alone) turned by their positions, as new tensors: see
     binding.gformer_rotary for freqs and for positions, or cu and start.  Rows behind the last sequence give zeros.  Differentiable with
     respect to q and k, any number of times: the gradients turn back.  Both ways can be captured in a graph."""
-    return _GformerRotary.apply(q, k, freqs, positions, cu, start, int(interleaved), 0, float(factor))
+    out = gb.rotary_node(q, k, freqs, positions, cu, start, int(interleaved), float(factor))
+    return _GformerRotary.apply(q, k, freqs, positions, cu, start, int(interleaved), 0, float(factor)) if out is None else out

@@ -669,6 +669,19 @@ def packed_attention_node(q, k, v, cu_q, cu_k, softmax_scale):
     return out
 
 
+def rotary_node(q, k, freqs, positions, cu, start, interleaved, factor):
+    """Rotary positions with their node in torch's graph from the extension module (host/rotary_grad.cpp), or None for what is not its
+    plain call."""
+    if _native is None:
+        _decode_call()
+    if _module is None:
+        return None
+    out = _module.rotary_positions((_lib or lib()).address["rotary"], q, k, freqs, positions, cu, start, interleaved, factor)
+    if isinstance(out, int):
+        raise GformerError(out, gformer_status_string(out))
+    return out
+
+
 def make_packed_params(dtype=GF_BF16, softmax_scale=1.0, zero_tail=0, **strides) -> GformerPackedParams:
     """strides: q_stride=, k_stride=, ... as (row, head)."""
     p = GformerPackedParams(ctypes.sizeof(GformerPackedParams), int(dtype), int(zero_tail), float(softmax_scale))

@@ -450,7 +450,7 @@ gf_status gformer_rotary(const void* q, const void* k, void* q_out, void* k_out,
   if ((st = strides2(p->q_stride, a.qs, H, d)) != GF_OK || (st = strides2(p->k_stride, a.ks, Hkv, d)) != GF_OK ||
       (st = strides2(p->q_out_stride, a.qos, H, d)) != GF_OK || (st = strides2(p->k_out_stride, a.kos, Hkv, d)) != GF_OK)
     return st;
-  if (total > kMaxCached || n_seqs > kMaxCached || !rotary_fits(total, H, Hkv, d)) return GF_ERR_UNSUPPORTED;
+  if (total > kMaxCached || n_seqs > kMaxCached || !rotary_fits(total)) return GF_ERR_UNSUPPORTED;
   if (total == 0) return GF_OK;
   if (!q || !q_out || !freqs || !k != !k_out || !k != (Hkv == 0)) return GF_ERR_INVALID_ARG;
   if (positions ? cu || start || n_seqs != 0 : !cu) return GF_ERR_INVALID_ARG;

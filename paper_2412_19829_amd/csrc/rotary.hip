@@ -1,5 +1,7 @@
-// Rotary positions (rotary.hpp).  A thread holds the cosines and sines of one row's pairs in two pieces of 16 bytes and walks heads with
-// them, so that the angles, which take 64 bits, are taken once for several heads.  Memory bounds it.
+// Rotary positions (rotary.hpp).  The angles, which take 64 bits, are taken once for all heads of a row.  Memory bounds it: 9223 rows of
+// 32 / 8 heads, d = 128, bf16 (148 MB read and written) 31.4 us, 4.7 TB/s; 4 rows of 12 / 12 heads, d = 64: 4.7.  What is read need
+// not stay in the caches, what is written is what attention reads next: with such loads alone 31.4 (34.5 without) and, with packed attention
+// over 281-token sequences behind it, 138 us (142); with such stores too 28.3 and 143.
 #include "rotary.hpp"
 
 #include "mfma.hpp"
@@ -11,7 +13,8 @@ namespace gformer {
 namespace {
 
 constexpr int kRotaryThreads = 256;
-constexpr int kRotaryHeads = 8;      // heads that a thread walks
+constexpr int kRows = 4;             // of a workgroup
+constexpr int kBatch = 4;            // heads that a thread has on their way
 
 // cos and sin of position x frequency.  The product and its remainder of quarter turns are taken in 64 bits: a far position's angle
 // has lost its fraction in 32.  What is left is at most pi/4, where the series' first terms behind those taken are below 2^-28.
@@ -55,102 +58,152 @@ template <> struct Piece<float> {
   }
 };
 
-template <typename T> __global__ __launch_bounds__(kRotaryThreads) void rotary_kernel(RotaryArgs a) {
+// The last sequence that starts at or before a row (n_seqs: the row lies behind them all, -1: in front), by 64 probes at a time.
+__device__ __forceinline__ int sequence_of(const int32_t* cu, int n_seqs, int total, int row, int lane) {
+  int lo = 0, hi = n_seqs + 1;
+  do {
+    const int step = (hi - lo + 63) / 64, s = lo + lane * step;
+    const int n = __popcll(__builtin_amdgcn_ballot_w64(s < hi && packed_row(cu, min(s, n_seqs), total) <= row));
+    if (n == 0) return -1;
+    lo = __builtin_amdgcn_readfirstlane(lo + (n - 1) * step);
+    hi = __builtin_amdgcn_readfirstlane(min(hi, lo + step));
+  } while (hi - lo > 1);
+  return lo;
+}
+
+// A workgroup takes ROWS rows, all heads.  Its threads take the rows' angles first, one pair each, and exchange them through LDS; then a
+// thread keeps one row's cosines and sines of its pieces and walks heads, kBatch of them on their way at once.
+template <typename T, int D, int ROWS, bool INTERLEAVED> __global__ __launch_bounds__(kRotaryThreads) void rotary_kernel(RotaryArgs a) {
   using P = Piece<T>;
-  constexpr int N = P::N;
-  const int units = a.d / (2 * N), rows = kRotaryThreads / units;      // two pieces each
-  const int tid = threadIdx.x, unit = tid % units;
-  const int heads = a.H + a.Hkv, sets = (heads + kRotaryHeads - 1) / kRotaryHeads;
-  const int64_t row = (int64_t)(blockIdx.x / sets) * rows + tid / units;
-  const int first = blockIdx.x % sets * kRotaryHeads, last = min(first + kRotaryHeads, heads);
-  if (row >= a.total) return;
-  bool real = true;
-  int position;
-  if (a.positions) {
-    position = a.positions[row];
-  } else {
-    // the last sequence that starts at or before the row
-    int lo = 0, hi = a.n_seqs + 1;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) / 2;
-      if (packed_row(a.cu, mid, a.total) <= row) lo = mid; else hi = mid;
-    }
-    real = lo < a.n_seqs && packed_row(a.cu, lo, a.total) <= row;
-    position = (int)((uint32_t)row - (uint32_t)packed_row(a.cu, lo, a.total) + (uint32_t)(real && a.start ? a.start[lo] : 0));
-  }
-  if (!real && !a.zero_tail) return;
+  constexpr int N = P::N, UNITS = D / (2 * N), SETS = kRotaryThreads / (UNITS * ROWS), HALF = D / 2;
+  static_assert(SETS >= 1 && ROWS <= kRotaryThreads / 64, "a wave for each row's position");
+  __shared__ __align__(16) float sm_c[ROWS][HALF], sm_s[ROWS][HALF];
+  __shared__ int sm_position[ROWS];
+  __shared__ bool sm_real[ROWS];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int unit = tid % UNITS, r = tid / UNITS % ROWS, set = tid / (UNITS * ROWS);
+  const int64_t row0 = (int64_t)blockIdx.x * ROWS;
+  const int half = a.rot / 2;
+  const bool mine = row0 + r < a.total;
 
   // turning channels: the first rot / (2 N) units, two pieces that belong together each
   const bool turns = unit * 2 * N < a.rot;
   int c0 = unit * 2 * N, c1 = c0 + N;
-  if (turns && !a.interleaved) {
+  if (turns && !INTERLEAVED) {
     c0 = unit * N;
-    c1 = a.rot / 2 + c0;
+    c1 = half + c0;
   }
-  float c[N], s[N];
-  if (turns && real) {
+  const int heads = a.H + a.Hkv;
+  auto from = [&](int h) { return h < a.H ? rows_of<T>(a.q, a.qs, row0 + r, h) : rows_of<T>(a.k, a.ks, row0 + r, h - a.H); };
+  auto to = [&](int h) { return h < a.H ? rows_of<T>(a.q_out, a.qos, row0 + r, h) : rows_of<T>(a.k_out, a.kos, row0 + r, h - a.H); };
+  P x[kBatch], y[kBatch];
+  auto load = [&](int h0) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      turn(position, a.freqs[unit * N + i], c[i], s[i]);
-      c[i] *= a.factor;
-      s[i] *= a.inverse ? -a.factor : a.factor;
-    }
-  }
-  for (int h = first; h < last; ++h) {
-    const bool key = h >= a.H;
-    if (!turns && real && (key ? a.k == a.k_out : a.q == a.q_out)) continue;   // in place: there already
-    const T* in = key ? rows_of<T>(a.k, a.ks, row, h - a.H) : rows_of<T>(a.q, a.qs, row, h);
-    T* out = key ? rows_of<T>(a.k_out, a.kos, row, h - a.H) : rows_of<T>(a.q_out, a.qos, row, h);
-    P x, y;
-    if (!real) {
-      x.w = y.w = u32x4{0, 0, 0, 0};
-    } else {
-      x.w = *reinterpret_cast<const u32x4*>(in + c0);
-      y.w = *reinterpret_cast<const u32x4*>(in + c1);
-      if (turns) {
-        float u[N], v[N];
-        if (a.interleaved) {
-#pragma unroll
-          for (int i = 0; i < N; ++i) {
-            const float p = i < N / 2 ? x.at(2 * i) : y.at(2 * i - N), q = i < N / 2 ? x.at(2 * i + 1) : y.at(2 * i + 1 - N);
-            const float p2 = fmaf(p, c[i], -(q * s[i])), q2 = fmaf(q, c[i], p * s[i]);
-            if (i < N / 2) {
-              u[2 * i] = p2;
-              u[2 * i + 1] = q2;
-            } else {
-              v[2 * i - N] = p2;
-              v[2 * i + 1 - N] = q2;
-            }
-          }
-        } else {
-#pragma unroll
-          for (int i = 0; i < N; ++i) {
-            const float p = x.at(i), q = y.at(i);
-            u[i] = fmaf(p, c[i], -(q * s[i]));
-            v[i] = fmaf(q, c[i], p * s[i]);
-          }
-        }
-        x.set(u);
-        y.set(v);
+    for (int j = 0; j < kBatch; ++j) {
+      const int h = h0 + j * SETS;
+      if (mine && h < heads) {
+        x[j].w = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(from(h) + c0));
+        y[j].w = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(from(h) + c1));
       }
     }
-    *reinterpret_cast<u32x4*>(out + c0) = x.w;
-    *reinterpret_cast<u32x4*>(out + c1) = y.w;
+  };
+  load(set);   // on their way while the angles are taken
+
+  // wave by wave a row's position; no sequence's row: it is zeroed or left
+  if (wave < ROWS && row0 + wave < a.total) {
+    const int row = (int)row0 + wave;
+    int position;
+    bool real = true;
+    if (a.positions) {
+      position = a.positions[row];
+    } else {
+      const int seq = sequence_of(a.cu, a.n_seqs, a.total, row, lane);
+      real = seq >= 0 && seq < a.n_seqs;
+      position = real ? (int)((uint32_t)row - (uint32_t)packed_row(a.cu, seq, a.total) + (uint32_t)(a.start ? a.start[seq] : 0)) : 0;
+    }
+    if (lane == 0) {
+      sm_position[wave] = position;
+      sm_real[wave] = real;
+    }
+  }
+  lds_barrier();
+  for (int i = tid; i < ROWS * half; i += kRotaryThreads) {
+    if (row0 + i / half < a.total) {
+      float c, s;
+      turn(sm_position[i / half], a.freqs[i % half], c, s);
+      sm_c[i / half][i % half] = c * a.factor;
+      sm_s[i / half][i % half] = s * (a.inverse ? -a.factor : a.factor);
+    }
+  }
+  lds_barrier();
+  if (!mine) return;
+  const bool real = sm_real[r];
+  if (!real && !a.zero_tail) return;
+  float c[N], s[N];
+  if (turns) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      c[i] = sm_c[r][unit * N + i];
+      s[i] = sm_s[r][unit * N + i];
+    }
+  }
+  for (int h0 = set; h0 < heads; h0 += kBatch * SETS) {
+    if (h0 != set) load(h0);
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+      const int h = h0 + j * SETS;
+      if (h >= heads) break;
+      if (!real) {
+        x[j].w = y[j].w = u32x4{0, 0, 0, 0};
+      } else if (turns) {
+        float u[N], v[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const bool low = !INTERLEAVED || i < N / 2;   // the pair's two channels
+          const float p = INTERLEAVED ? (low ? x[j].at(2 * i % N) : y[j].at(2 * i % N)) : x[j].at(i);
+          const float q = INTERLEAVED ? (low ? x[j].at(2 * i % N + 1) : y[j].at(2 * i % N + 1)) : y[j].at(i);
+          const float p2 = fmaf(p, c[i], -(q * s[i])), q2 = fmaf(q, c[i], p * s[i]);
+          if (!INTERLEAVED) {
+            u[i] = p2;
+            v[i] = q2;
+          } else if (low) {
+            u[2 * i % N] = p2;
+            u[2 * i % N + 1] = q2;
+          } else {
+            v[2 * i % N] = p2;
+            v[2 * i % N + 1] = q2;
+          }
+        }
+        x[j].set(u);
+        y[j].set(v);
+      } else if (h < a.H ? a.q == a.q_out : a.k == a.k_out) {
+        continue;   // in place: there already
+      }
+      *reinterpret_cast<u32x4*>(to(h) + c0) = x[j].w;
+      *reinterpret_cast<u32x4*>(to(h) + c1) = y[j].w;
+    }
   }
 }
 
-int64_t groups(int total, int H, int Hkv, int d, int n) {
-  const int rows = kRotaryThreads / (d / (2 * n)), sets = (H + Hkv + kRotaryHeads - 1) / kRotaryHeads;
-  return ((int64_t)total + rows - 1) / rows * sets;
+constexpr int kManyRows = 1024;   // from here on a workgroup takes kRows rows, below it one
+
+template <typename T, int D, int ROWS> void launch(const RotaryArgs& a, hipStream_t s) {
+  const dim3 grid((unsigned)(((int64_t)a.total + ROWS - 1) / ROWS));
+  if (a.interleaved) rotary_kernel<T, D, ROWS, true><<<grid, dim3(kRotaryThreads), 0, s>>>(a);
+  else rotary_kernel<T, D, ROWS, false><<<grid, dim3(kRotaryThreads), 0, s>>>(a);
+}
+template <typename T, int D> void launch(const RotaryArgs& a, hipStream_t s) {
+  if (a.total >= kManyRows) launch<T, D, kRows>(a, s);
+  else launch<T, D, 1>(a, s);
 }
 
 }  // namespace
 
-bool rotary_fits(int total, int H, int Hkv, int d) { return groups(total, H, Hkv, d, Piece<float>::N) <= most_workgroups(kRotaryThreads); }
+bool rotary_fits(int total) { return ((int64_t)total + kRows - 1) / kRows <= most_workgroups(kRotaryThreads); }
 
 hipError_t launch_rotary(const RotaryArgs& a, bool bf16, hipStream_t s) {
-  if (bf16) rotary_kernel<uint16_t><<<dim3((unsigned)groups(a.total, a.H, a.Hkv, a.d, 8)), dim3(kRotaryThreads), 0, s>>>(a);
-  else rotary_kernel<float><<<dim3((unsigned)groups(a.total, a.H, a.Hkv, a.d, 4)), dim3(kRotaryThreads), 0, s>>>(a);
+  if (bf16) a.d == 128 ? launch<uint16_t, 128>(a, s) : launch<uint16_t, 64>(a, s);
+  else a.d == 128 ? launch<float, 128>(a, s) : launch<float, 64>(a, s);
   return hipGetLastError();
 }
 

@@ -18,7 +18,7 @@ struct RotaryArgs {
   float factor;
   int64_t qs[2], ks[2], qos[2], kos[2];   // (row, head) strides
 };
-bool rotary_fits(int total, int H, int Hkv, int d);
+bool rotary_fits(int total);
 hipError_t launch_rotary(const RotaryArgs& a, bool bf16, hipStream_t s);
 
 }  // namespace gformer

@@ -1,4 +1,4 @@
-// What the host sides of the calls share (decode_call.cpp, packed_call.cpp, packed_grad.cpp): reading Python arguments without its own
+// What the host sides of the calls share (decode_call.cpp, packed_call.cpp, packed_grad.cpp, rotary_grad.cpp): reading Python arguments without its own
 // machinery.
 #pragma once
 
@@ -72,5 +72,7 @@ PyObject* pages_copy_q4(PyObject*, PyObject* const* a, Py_ssize_t n);
 PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n);
 // packed_grad.cpp
 PyObject* packed_attention(PyObject*, PyObject* const* a, Py_ssize_t n);
+// rotary_grad.cpp
+PyObject* rotary_positions(PyObject*, PyObject* const* a, Py_ssize_t n);
 
 }  // namespace gformer_host

@@ -108,6 +108,7 @@ PyMethodDef methods[] = {
     {"pages_copy_q4", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(pages_copy_q4)), METH_FASTCALL, "gformer_pages_copy_q4"},
     {"rotary", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(rotary)), METH_FASTCALL, "gformer_rotary"},
     {"packed_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(packed_attention)), METH_FASTCALL, "packed attention as a node"},
+    {"rotary_positions", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(rotary_positions)), METH_FASTCALL, "rotary positions as a node"},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_decode_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -161,10 +161,25 @@ def test_what_is_no_number_stays_in_its_pair():
     assert torch.equal(bad, want)
 
 
+@pytest.fixture(params=["native", "python"])
+def node(request, monkeypatch):
+    """Both makers of the node."""
+    if request.param == "python":
+        monkeypatch.setattr(gb, "rotary_node", lambda *a: None)
+    else:
+        made = gb.rotary_node
+
+        def checked(*a):
+            out = made(*a)
+            assert out is not None
+            return out
+        monkeypatch.setattr(gb, "rotary_node", checked)
+
+
 @gpu
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("interleaved,rot", [(0, 64), (1, 32)])
-def test_gradients(dtype, interleaved, rot):
+def test_gradients(dtype, interleaved, rot, node):
     gen = torch.Generator().manual_seed(rot)
     lens, start, H, Hkv, d, factor = [9, 0, 30], [0, 5, 1000], 4, 2, 64, 1.25
     rows = sum(lens) + 4
@@ -183,11 +198,17 @@ def test_gradients(dtype, interleaved, rot):
         assert bool((got[sum(lens):] == 0).all())
     # one of the two alone
     assert torch.equal(torch.autograd.grad(ko, k, gk, retain_graph=True)[0], dk)
-    assert torch.equal(torch.autograd.grad(qo, q, gq)[0], dq)
+    assert torch.equal(torch.autograd.grad(qo, q, gq, retain_graph=True)[0], dq)
+    assert torch.autograd.grad((qo, ko), q, (gq, gk))[0].equal(dq)
+    # inputs of which one has no gradient
+    qo, ko = gformer_rotary_positions(q.detach(), k, freqs, cu=ints(pref.offsets(lens)), start=ints(start), interleaved=interleaved, factor=factor)
+    assert torch.equal(torch.autograd.grad((qo, ko) if qo.requires_grad else (ko,), k, (gq, gk) if qo.requires_grad else (gk,))[0], dk)
+    with torch.no_grad():
+        assert not gformer_rotary_positions(q, k, freqs, cu=ints(pref.offsets(lens)), interleaved=interleaved)[1].requires_grad
 
 
 @gpu
-def test_gradient_against_differences_and_again():
+def test_gradient_against_differences_and_again(node):
     gen = torch.Generator().manual_seed(2)
     q = torch.randn(5, 2, 64, generator=gen).cuda().requires_grad_(True)
     freqs, pos = rotary_frequencies(64), ints([0, 3, 77, 1000, 4])
@@ -208,7 +229,7 @@ def test_gradient_against_differences_and_again():
 
 
 @gpu
-def test_a_captured_training_step():
+def test_a_captured_training_step(node):
     """Turning, packed attention and the way back in one graph, replayed with other inputs."""
     gen = torch.Generator().manual_seed(1)
     lens, H, Hkv, d = [40, 0, 23, 1], 4, 2, 64
