@@ -196,7 +196,7 @@ gf_status fill(bool q4, const void* k, const void* v, void* kpages, void* vpages
   if (n_seqs < 0 || total < 0) return GF_ERR_INVALID_ARG;
   if (total > kMaxCached || n_seqs > kMaxCached) return GF_ERR_UNSUPPORTED;
   if ((st = strides2(p->k_stride, a.ks, Hkv, d)) != GF_OK || (st = strides2(p->v_stride, a.vs, Hkv, d)) != GF_OK) return st;
-  if (!(q4 ? paged_q4_rows_fit(total, n_seqs, Hkv) : paged_fill_fits(total, n_seqs, Hkv))) return GF_ERR_UNSUPPORTED;
+  if (!(q4 ? paged_q4_rows_fit(total, n_seqs, Hkv, d) : paged_fill_fits(total, n_seqs, Hkv))) return GF_ERR_UNSUPPORTED;
   if (total == 0 || n_seqs == 0 || table_width == 0 || n_pages == 0) return GF_OK;
   if (!k || !v || !kpages || !vpages || !table || !start || !cu) return GF_ERR_INVALID_ARG;
   if (misaligned(bits(k, v, kpages, vpages), 16) || misaligned(bits(table, start, cu), 4)) return GF_ERR_INVALID_ARG;
@@ -392,7 +392,7 @@ gf_status gformer_paged_read_q4(const void* kpages, const void* vpages, void* k,
   if (n_seqs < 0 || total < 0) return GF_ERR_INVALID_ARG;
   if (total > kMaxCached || n_seqs > kMaxCached) return GF_ERR_UNSUPPORTED;
   if ((st = strides2(p->k_stride, a.ks, Hkv, d)) != GF_OK || (st = strides2(p->v_stride, a.vs, Hkv, d)) != GF_OK) return st;
-  if (!paged_q4_rows_fit(total, n_seqs, Hkv)) return GF_ERR_UNSUPPORTED;
+  if (!paged_q4_rows_fit(total, n_seqs, Hkv, d)) return GF_ERR_UNSUPPORTED;
   if (total == 0 || n_seqs == 0) return GF_OK;
   // a table or cache of no pages: its tokens are zeros, and nothing of it is read
   if (!k || !v || (!table && table_width > 0) || !start || !cu || (n_pages > 0 && (!kpages || !vpages))) return GF_ERR_INVALID_ARG;

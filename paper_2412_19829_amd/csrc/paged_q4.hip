@@ -36,30 +36,17 @@ template <int BIT> __device__ __forceinline__ float beside(float x) { return __u
 struct Codes {
   uint32_t n, pair;
 };
-__device__ __forceinline__ Codes quantised(const float (&x)[8]) {
-  float lo = INFINITY, hi = -INFINITY;
-  uint32_t sound = 1;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    lo = fminf(lo, x[i]);
-    hi = fmaxf(hi, x[i]);
-    sound &= fabsf(x[i]) < 0x1p127f ? 1u : 0u;
-  }
-  lo = fminf(lo, beside<1>(lo));
-  lo = fminf(lo, beside<2>(lo));
-  hi = fmaxf(hi, beside<1>(hi));
-  hi = fmaxf(hi, beside<2>(hi));
-  sound &= beside<1>(sound);
-  sound &= beside<2>(sound);
-  if (!sound) return {0u, 0x7fc07fc0u};
-  uint32_t low = __float_as_uint(lo + 0.f);   // zero without its sign
-  low = (low & 0xffff0000u) + ((low & 0x8000ffffu) > 0x80000000u ? 0x10000u : 0u);   // negative with bits behind: one step away from zero
-  const double l = (double)__uint_as_float(low), range = (double)(hi + 0.f) - l;
+
+// What the scale and codes are by their definition, in 64 bits, for any sound values: x - l and the quotients are exact or nearly.
+__device__ __forceinline__ uint32_t scale_of(double range) {
   // the quotient's first guess may be a step short of what reaches the range, or two where the guess itself was rounded down
   uint32_t scale = __float_as_uint((float)(range * (1.0 / 15.0))) & 0xffff0000u;
 #pragma unroll
   for (int i = 0; i < 2; ++i) scale += 15.0 * (double)__uint_as_float(scale) < range ? 0x10000u : 0u;
-  const double s = (double)__uint_as_float(scale), half = 0.5 * s, by = scale ? __builtin_amdgcn_rcp(s) : 0.0;
+  return scale;
+}
+__device__ __forceinline__ uint32_t careful_codes(const float (&x)[8], float low, uint32_t scale) {
+  const double l = (double)low, s = (double)__uint_as_float(scale), half = 0.5 * s, by = scale ? __builtin_amdgcn_rcp(s) : 0.0;
   uint32_t codes = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
@@ -70,32 +57,92 @@ __device__ __forceinline__ Codes quantised(const float (&x)[8]) {
     else if (rest < -half || (rest == -half && (k & 1))) --k;
     codes |= (uint32_t)k << (4 * i);
   }
-  return {codes, low | scale >> 16};
+  return codes;
 }
 
-template <typename T> __device__ __forceinline__ void load8(float (&x)[8], const T* p);
-template <> __device__ __forceinline__ void load8(float (&x)[8], const uint16_t* p) {
-  const u32x4 w = *reinterpret_cast<const u32x4*>(p);
+// In 32 bits where that gives the same.  Differences of bf16 values are exact where none is below 2^-15 of the largest, and then
+// so is a quotient that is half way between two codes: the guess's remainder is exact (at most 9 bits), and the corrected quotient is off by
+// 2^-45 of it before its rounding.  An fp32 difference is rounded, so that quotients within 2^-18 of half way are not told from it.  Those
+// waves, and ones of steps or ranges near the ends of the exponents, take 64 bits for all of their values.
+template <typename T> __device__ __forceinline__ Codes quantised(const float (&x)[8]) {
+  constexpr bool BF16 = sizeof(T) == 2;
+  float lo = min3(x[0], x[1], x[2]), hi = max3(x[0], x[1], x[2]);   // no number stays none
+  float least = min3(fabsf(x[0]), fabsf(x[1]), fabsf(x[2]));
+#pragma unroll
+  for (int i = 3; i < 7; i += 2) {
+    lo = min3(lo, x[i], x[i + 1]);
+    hi = max3(hi, x[i], x[i + 1]);
+    if (BF16) least = min3(least, fabsf(x[i]), fabsf(x[i + 1]));
+  }
+  lo = min3(lo, x[7], beside<1>(min3(lo, x[7], x[7])));
+  lo = min3(lo, beside<2>(lo), lo);
+  hi = max3(hi, x[7], beside<1>(max3(hi, x[7], x[7])));
+  hi = max3(hi, beside<2>(hi), hi);
+  if (BF16) {
+    least = min3(least, fabsf(x[7]), beside<1>(min3(least, fabsf(x[7]), fabsf(x[7]))));
+    least = min3(least, beside<2>(least), least);
+  }
+  const float most = max3(fabsf(lo), fabsf(hi), fabsf(hi));
+  const bool sound = most < 0x1p127f;
+  uint32_t low = __float_as_uint(lo + 0.f);             // zero without its sign
+  if (!BF16) low = (low & 0xffff0000u) + ((low & 0x8000ffffu) > 0x80000000u ? 0x10000u : 0u);   // negative with bits behind: one step away from zero
+  const float l = __uint_as_float(low), top = hi + 0.f;
+  bool careful = !(most < 0x1p126f) || (BF16 && least < most * 0x1p-15f);
+  uint32_t scale;
+  if (BF16) {
+    const float range = top - l;
+    scale = __float_as_uint(range * (1.f / 15.f)) & 0xffff0000u;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) scale += 15.f * __uint_as_float(scale) < range ? 0x10000u : 0u;
+  } else {
+    scale = scale_of((double)top - (double)l);
+  }
+  const float s = __uint_as_float(scale), by = __builtin_amdgcn_rcpf(s);
+  careful = (careful && lo != hi) || s < 0x1p-100f;     // a step of zero among them
+  uint32_t codes = 0;
+  float nearest = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float at = x[i] - l, guess = at * by, quotient = fmaf(fmaf(-guess, s, at), by, guess), n = rintf(quotient);
+    if (!BF16) nearest = max3(nearest, fabsf(quotient - n), nearest);
+    codes |= (uint32_t)n << (4 * i);
+  }
+  careful = careful || (!BF16 && !(nearest < 0.5f - 0x1p-18f));
+  if (__builtin_amdgcn_ballot_w64(careful && sound)) {
+    if (BF16) scale = scale_of((double)top - (double)l);
+    codes = careful_codes(x, l, scale);
+  }
+  return sound ? Codes{codes, low | scale >> 16} : Codes{0u, 0x7fc07fc0u};
+}
+
+// 8 values of a row; what a kernel reads or writes for the last time may pass the caches by.
+template <bool ONCE = false, typename V> __device__ __forceinline__ V get(const V* p) { return ONCE ? __builtin_nontemporal_load(p) : *p; }
+template <typename V> __device__ __forceinline__ void put(V* p, V x, bool once) {
+  if (once) __builtin_nontemporal_store(x, p);
+  else *p = x;
+}
+template <bool ONCE = false> __device__ __forceinline__ void load8(float (&x)[8], const uint16_t* p) {
+  const u32x4 w = get<ONCE>(reinterpret_cast<const u32x4*>(p));
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     x[2 * i] = bf16_lo(w[i]);
     x[2 * i + 1] = bf16_hi(w[i]);
   }
 }
-template <> __device__ __forceinline__ void load8(float (&x)[8], const float* p) {
-  const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
+template <bool ONCE = false> __device__ __forceinline__ void load8(float (&x)[8], const float* p) {
+  const f32x4 a = get<ONCE>(reinterpret_cast<const f32x4*>(p)), b = get<ONCE>(reinterpret_cast<const f32x4*>(p + 4));
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     x[i] = a[i];
     x[4 + i] = b[i];
   }
 }
-__device__ __forceinline__ void store8(uint16_t* p, const float (&x)[8]) {
-  *reinterpret_cast<u32x4*>(p) = u32x4{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])};
+__device__ __forceinline__ void store8(uint16_t* p, const float (&x)[8], bool once) {
+  put(reinterpret_cast<u32x4*>(p), u32x4{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])}, once);
 }
-__device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
-  *reinterpret_cast<f32x4*>(p) = f32x4{x[0], x[1], x[2], x[3]};
-  *reinterpret_cast<f32x4*>(p + 4) = f32x4{x[4], x[5], x[6], x[7]};
+__device__ __forceinline__ void store8(float* p, const float (&x)[8], bool once) {
+  put(reinterpret_cast<f32x4*>(p), f32x4{x[0], x[1], x[2], x[3]}, once);
+  put(reinterpret_cast<f32x4*>(p + 4), f32x4{x[4], x[5], x[6], x[7]}, once);
 }
 
 // Lane c of a row's D / 8 puts its codes, and the first of four the group's pair.
@@ -104,57 +151,97 @@ template <int D> __device__ __forceinline__ void put_codes(uint32_t* row, int c,
   if (c % 4 == 0) row[D / 8 + c / 4] = x.pair;
 }
 
-// Packed rows into their slots, or out of them: a workgroup takes 32 rows of one head, a lane 8 channels of a row at a time.
-constexpr int kRows = 32;
-template <typename T, int D> __global__ __launch_bounds__(kPagedThreads) void q4_fill_kernel(PagedFillArgs a) {
-  constexpr int C = D / 8;
-  const int tid = threadIdx.x, head = blockIdx.x % a.Hkv, c = tid % C;
-  const SeqTile at = find_tile<kRows>(a.cu, a.n_seqs, a.total, blockIdx.x / a.Hkv, tid & 63);
-  if (at.first < 0 || at.seq == a.n_seqs) return;
-  const int base = packed_row(a.cu, at.seq, a.total), n = packed_row(a.cu, at.seq + 1, a.total) - base;
-  const int64_t room = (int64_t)a.width << a.shift;
-  for (int r = tid / C; r < kRows; r += kPagedThreads / C) {
-    const int row = at.first + r;
-    const int64_t pos = (int64_t)a.start[at.seq] + row;
-    if (row >= n || pos < 0 || pos >= room) continue;
-    const int page = a.table[(int64_t)at.seq * a.width + (pos >> a.shift)];
-    if ((unsigned)page >= (unsigned)a.n_pages) continue;
-    const int slot = (int)pos & ((1 << a.shift) - 1);
-    float k[8], v[8];
-    load8(k, rows_of<T>(a.k, a.ks, base + row, head) + 8 * c);
-    load8(v, rows_of<T>(a.v, a.vs, base + row, head) + 8 * c);
-    put_codes<D>(reinterpret_cast<uint32_t*>(reinterpret_cast<char*>(a.kpages) + page * a.kps[0] + head * a.kps[1] + slot * a.kps[2]), c, quantised(k));
-    put_codes<D>(reinterpret_cast<uint32_t*>(reinterpret_cast<char*>(a.vpages) + page * a.vps[0] + head * a.vps[1] + slot * a.vps[2]), c, quantised(v));
+// Packed rows into their slots, or out of them: a workgroup takes ROWS rows of kHeads heads, a lane 8 channels of two of them.
+constexpr int kHeads = 4;
+template <int D> struct RowShape {
+  static constexpr int C = D / 8, STEP = kPagedThreads / C, N = 2, ROWS = N * STEP / kHeads;   // lanes a row; rows of all lanes, of one
+};
+// Where a lane's rows are: rows of the packed tensors (negative: none), and their slots (page negative: none).
+template <int D> struct Slots {
+  int row[RowShape<D>::N], head[RowShape<D>::N], page[RowShape<D>::N], slot[RowShape<D>::N];
+  template <typename A> __device__ __forceinline__ bool find(const A& a, int block, int tid) {
+    using S = RowShape<D>;
+    const int sets = (a.Hkv + kHeads - 1) / kHeads;
+    const SeqTile at = find_tile<S::ROWS>(a.cu, a.n_seqs, a.total, block / sets, tid & 63);
+    if (at.first < 0 || at.seq == a.n_seqs) return false;
+    const int base = packed_row(a.cu, at.seq, a.total), n = packed_row(a.cu, at.seq + 1, a.total) - base;
+    const int64_t room = (int64_t)a.width << a.shift, from = a.start[at.seq];
+    const int32_t* table = a.table + (int64_t)at.seq * a.width;
+#pragma unroll
+    for (int i = 0; i < S::N; ++i) {
+      const int u = tid / S::C + i * S::STEP, r = at.first + u / kHeads;
+      const int64_t pos = from + r;
+      head[i] = block % sets * kHeads + u % kHeads;
+      const bool real = r < n && head[i] < a.Hkv;
+      row[i] = real ? base + r : -1;
+      page[i] = real && pos >= 0 && pos < room ? table[pos >> a.shift] : -1;
+      slot[i] = (int)pos & ((1 << a.shift) - 1);
+      if ((unsigned)page[i] >= (unsigned)a.n_pages) page[i] = -1;
+    }
+    return true;
   }
+  __device__ __forceinline__ int64_t at(const int64_t (&st)[3], int i) const { return page[i] * st[0] + head[i] * st[1] + slot[i] * st[2]; }
+};
+
+// 9207 rows of 8 heads, d = 128, bf16 (50 MB read and written): 15.5 us, the quantising's instructions more than the memory (20 with
+// all of them in 64 bits).
+template <typename T, int D> __global__ __launch_bounds__(kPagedThreads) void q4_fill_kernel(PagedFillArgs a) {
+  constexpr int N = RowShape<D>::N;
+  const int tid = threadIdx.x, c = tid % RowShape<D>::C;
+  Slots<D> s;
+  if (!s.find(a, blockIdx.x, tid)) return;
+  float k[N][8], v[N][8];
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    if (s.page[i] >= 0) {
+      load8<true>(k[i], rows_of<T>(a.k, a.ks, s.row[i], s.head[i]) + 8 * c);
+      load8<true>(v[i], rows_of<T>(a.v, a.vs, s.row[i], s.head[i]) + 8 * c);
+    }
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    if (s.page[i] >= 0) {
+      put_codes<D>(reinterpret_cast<uint32_t*>(reinterpret_cast<char*>(a.kpages) + s.at(a.kps, i)), c, quantised<T>(k[i]));
+      put_codes<D>(reinterpret_cast<uint32_t*>(reinterpret_cast<char*>(a.vpages) + s.at(a.vps, i)), c, quantised<T>(v[i]));
+    }
 }
 
-template <int D> __device__ __forceinline__ void values8(float (&x)[8], const uint32_t* row, int c) {
-  const uint32_t n = row[c], pair = row[D / 8 + c / 4];
-  const float s = bf16_lo(pair), l = bf16_hi(pair);
+__device__ __forceinline__ void values8(float (&x)[8], Codes y) {
+  const float s = bf16_lo(y.pair), l = bf16_hi(y.pair);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = fmaf(s, (float)(n >> (4 * i) & 15u), l);
+  for (int i = 0; i < 8; ++i) x[i] = fmaf(s, (float)(y.n >> (4 * i) & 15u), l);
 }
+template <int D> __device__ __forceinline__ Codes codes_of(const void* pages, int64_t at, int c) {
+  const uint32_t* row = reinterpret_cast<const uint32_t*>(reinterpret_cast<const char*>(pages) + at);
+  return {row[c], row[D / 8 + c / 4]};
+}
+// 56866 rows of 8 heads, d = 128, bf16 (306 MB read and written): 60.4 us, 5.1 TB/s; 6066 of 16 heads, d = 64, fp32 (57 MB) 17.5 with two
+// rows a lane, 18.3 with one.  `once`: the rows are more than the last cache holds, so that nobody finds them there: 4 x 32767 tokens
+// with an attention of 32 queries each behind them 442 us (475 without), but 7 x 8192 with 64 queries 240 (234).
+constexpr int64_t kLastCache = (int64_t)256 << 20;   // bytes
 template <typename T, int D> __global__ __launch_bounds__(kPagedThreads) void q4_read_kernel(PagedReadArgs a) {
-  constexpr int C = D / 8;
-  const int tid = threadIdx.x, head = blockIdx.x % a.Hkv, c = tid % C;
-  const SeqTile at = find_tile<kRows>(a.cu, a.n_seqs, a.total, blockIdx.x / a.Hkv, tid & 63);
-  if (at.first < 0 || at.seq == a.n_seqs) return;
-  const int base = packed_row(a.cu, at.seq, a.total), n = packed_row(a.cu, at.seq + 1, a.total) - base;
-  const int64_t room = (int64_t)a.width << a.shift;
-  for (int r = tid / C; r < kRows; r += kPagedThreads / C) {
-    const int row = at.first + r;
-    if (row >= n) continue;
-    const int64_t pos = (int64_t)a.start[at.seq] + row;
-    const int page = pos < 0 || pos >= room ? -1 : a.table[(int64_t)at.seq * a.width + (pos >> a.shift)];
-    float k[8] = {}, v[8] = {};
-    if ((unsigned)page < (unsigned)a.n_pages) {
-      const int slot = (int)pos & ((1 << a.shift) - 1);
-      values8<D>(k, reinterpret_cast<const uint32_t*>(reinterpret_cast<const char*>(a.kpages) + page * a.kps[0] + head * a.kps[1] + slot * a.kps[2]), c);
-      values8<D>(v, reinterpret_cast<const uint32_t*>(reinterpret_cast<const char*>(a.vpages) + page * a.vps[0] + head * a.vps[1] + slot * a.vps[2]), c);
+  constexpr int N = RowShape<D>::N;
+  const int tid = threadIdx.x, c = tid % RowShape<D>::C;
+  const bool once = (int64_t)a.total * a.Hkv * (2 * D * (int)sizeof(T)) > kLastCache;
+  Slots<D> s;
+  if (!s.find(a, blockIdx.x, tid)) return;
+  Codes k[N], v[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    k[i] = v[i] = {0u, 0u};
+    if (s.page[i] >= 0) {
+      k[i] = codes_of<D>(a.kpages, s.at(a.kps, i), c);
+      v[i] = codes_of<D>(a.vpages, s.at(a.vps, i), c);
     }
-    store8(rows_of<T>(a.k, a.ks, base + row, head) + 8 * c, k);
-    store8(rows_of<T>(a.v, a.vs, base + row, head) + 8 * c, v);
   }
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    if (s.row[i] >= 0) {
+      float x[8];
+      values8(x, k[i]);
+      store8(rows_of<T>(a.k, a.ks, s.row[i], s.head[i]) + 8 * c, x, once);
+      values8(x, v[i]);
+      store8(rows_of<T>(a.v, a.vs, s.row[i], s.head[i]) + 8 * c, x, once);
+    }
 }
 
 // Whole pages: a workgroup copies one head of one page, keys and values, in five pieces a row.
@@ -243,7 +330,7 @@ template <typename T, int D> __global__ __launch_bounds__(kPagedThreads) void q4
     if (wave < 2 && lane < D / 8) {
       float x[8];
       load8(x, (wave == 0 ? rows_of<T>(a.k, a.ks, b, kvh) : rows_of<T>(a.v, a.vs, b, kvh)) + 8 * c);
-      const Codes y = quantised(x);
+      const Codes y = quantised<T>(x);
       put_codes<D>(sm_new[wave], c, y);
       const int page = table[own >> a.shift];
       if (tile == 0 && (unsigned)page < (unsigned)a.n_pages) {
@@ -473,7 +560,9 @@ template <typename T, int D> hipError_t decode(const PagedDecodeArgs& a, hipStre
   return e != hipSuccess || a.splits == 1 ? e : launch_paged_join(a, sizeof(T) == 2, s);
 }
 
-unsigned row_groups(int total, int n_seqs, int Hkv) { return (unsigned)(packed_tiles(total, n_seqs, kRows) * Hkv); }
+int64_t row_groups(int total, int n_seqs, int Hkv, int d) {
+  return packed_tiles(total, n_seqs, d == 128 ? RowShape<128>::ROWS : RowShape<64>::ROWS) * ((Hkv + kHeads - 1) / kHeads);
+}
 
 }  // namespace
 
@@ -489,7 +578,7 @@ bool paged_q4_decode_fits(int B, int H, int Hkv, int d, PagedSplit s) {
   return decode_units(B, H, Hkv, d) * s.splits <= most_workgroups(kPagedThreads) &&
          (s.splits == 1 || (int64_t)B * H <= most_workgroups(kPagedThreads));
 }
-bool paged_q4_rows_fit(int total, int n_seqs, int Hkv) { return packed_tiles(total, n_seqs, kRows) * Hkv <= most_workgroups(kPagedThreads); }
+bool paged_q4_rows_fit(int total, int n_seqs, int Hkv, int d) { return row_groups(total, n_seqs, Hkv, d) <= most_workgroups(kPagedThreads); }
 
 hipError_t launch_paged_q4_decode(const PagedDecodeArgs& a, bool bf16, hipStream_t s) {
   if (bf16) return a.d == 128 ? decode<uint16_t, 128>(a, s) : decode<uint16_t, 64>(a, s);
@@ -497,14 +586,14 @@ hipError_t launch_paged_q4_decode(const PagedDecodeArgs& a, bool bf16, hipStream
 }
 
 hipError_t launch_paged_q4_fill(const PagedFillArgs& a, bool bf16, hipStream_t s) {
-  const dim3 grid(row_groups(a.total, a.n_seqs, a.Hkv));
+  const dim3 grid((unsigned)row_groups(a.total, a.n_seqs, a.Hkv, a.d));
   if (bf16) a.d == 128 ? q4_fill_kernel<uint16_t, 128><<<grid, kPagedThreads, 0, s>>>(a) : q4_fill_kernel<uint16_t, 64><<<grid, kPagedThreads, 0, s>>>(a);
   else a.d == 128 ? q4_fill_kernel<float, 128><<<grid, kPagedThreads, 0, s>>>(a) : q4_fill_kernel<float, 64><<<grid, kPagedThreads, 0, s>>>(a);
   return hipGetLastError();
 }
 
 hipError_t launch_paged_q4_read(const PagedReadArgs& a, bool bf16, hipStream_t s) {
-  const dim3 grid(row_groups(a.total, a.n_seqs, a.Hkv));
+  const dim3 grid((unsigned)row_groups(a.total, a.n_seqs, a.Hkv, a.d));
   if (bf16) a.d == 128 ? q4_read_kernel<uint16_t, 128><<<grid, kPagedThreads, 0, s>>>(a) : q4_read_kernel<uint16_t, 64><<<grid, kPagedThreads, 0, s>>>(a);
   else a.d == 128 ? q4_read_kernel<float, 128><<<grid, kPagedThreads, 0, s>>>(a) : q4_read_kernel<float, 64><<<grid, kPagedThreads, 0, s>>>(a);
   return hipGetLastError();

@@ -25,7 +25,7 @@ struct PagedReadArgs {
 
 PagedSplit paged_q4_split(int B, int H, int Hkv, int d, int64_t max_len);
 bool paged_q4_decode_fits(int B, int H, int Hkv, int d, PagedSplit s);
-bool paged_q4_rows_fit(int total, int n_seqs, int Hkv);
+bool paged_q4_rows_fit(int total, int n_seqs, int Hkv, int d);
 hipError_t launch_paged_q4_decode(const PagedDecodeArgs& a, bool bf16, hipStream_t s);
 hipError_t launch_paged_q4_fill(const PagedFillArgs& a, bool bf16, hipStream_t s);
 hipError_t launch_paged_q4_read(const PagedReadArgs& a, bool bf16, hipStream_t s);
