@@ -30,6 +30,16 @@ template <int BIT> __device__ __forceinline__ uint32_t beside(uint32_t x) {
 }
 template <int BIT> __device__ __forceinline__ float beside(float x) { return __uint_as_float(beside<BIT>(__float_as_uint(x))); }
 
+// The value of lane `from` of this lane's GR neighbours.
+template <int GR> __device__ __forceinline__ float of_group(float x, int from) {
+  const int v = __float_as_int(x);
+  if (GR == 2) return __int_as_float(from == 0 ? __builtin_amdgcn_mov_dpp(v, 0xa0, 0xf, 0xf, true) : __builtin_amdgcn_mov_dpp(v, 0xf5, 0xf, 0xf, true));
+  return __int_as_float(from == 0   ? __builtin_amdgcn_mov_dpp(v, 0x00, 0xf, 0xf, true)
+                        : from == 1 ? __builtin_amdgcn_mov_dpp(v, 0x55, 0xf, 0xf, true)
+                        : from == 2 ? __builtin_amdgcn_mov_dpp(v, 0xaa, 0xf, 0xf, true)
+                                    : __builtin_amdgcn_mov_dpp(v, 0xff, 0xf, 0xf, true));
+}
+
 // ---- rows -------------------------------------------------------------------------------------------
 
 // Codes of 8 of 32 values that four neighbouring lanes hold, and the group's (scale, lowest value).
@@ -282,12 +292,18 @@ template <typename T> constexpr int kWeightParts = sizeof(T) == 2 ? 2 : 3;
 constexpr float kMiddle = 7.5f;
 constexpr uint32_t kMinusMiddle = 0xc0f0c0f0u;
 
-// x's first bf16 part, two at a time; what it leaves stays in a and b.
+// Two values' first bf16 parts, cut off; what they leave stays in a and b.
 __device__ __forceinline__ uint32_t take_part(float& a, float& b) {
-  const uint32_t w = pack_bf16(a, b);
-  a -= bf16_lo(w);
-  b -= bf16_hi(w);
+  const uint32_t w = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+  a -= __uint_as_float(__float_as_uint(a) & 0xffff0000u);
+  b -= __uint_as_float(__float_as_uint(b) & 0xffff0000u);
   return w;
+}
+// Their N parts, the last one rounded.
+template <int N> __device__ __forceinline__ void parts_of(uint32_t (&w)[N], float a, float b) {
+#pragma unroll
+  for (int p = 0; p < N - 1; ++p) w[p] = take_part(a, b);
+  w[N - 1] = pack_bf16(a, b);
 }
 
 __device__ __forceinline__ uint32_t codes_bf16(uint32_t bytes, bool upper) {
@@ -300,10 +316,12 @@ __device__ __forceinline__ int seen_tokens(const PagedDecodeArgs& a, int b) {
   return t < 0 || t > a.room - own ? 0 : t + own;
 }
 
-template <typename T, int D> __global__ __launch_bounds__(kPagedThreads) void q4_decode_kernel(PagedDecodeArgs a) {
+// ONE: a page holds whole tiles of 16 keys (pages of 8 tokens do not), so that their pages and addresses are the same for all lanes, which
+// then add nothing but a fixed offset to them: 572 vector instructions a tile of 32 keys, d = 128, with addresses of their own, 379 without.
+template <typename T, int D, bool ONE> __global__ __launch_bounds__(kPagedThreads, sizeof(T) == 2 ? 3 : 2) void q4_decode_kernel(PagedDecodeArgs a) {
   using S = Shape4<D>;
   typedef typename S::KeyCodes KeyCodes;
-  constexpr int GR = S::GR, HC = S::HC, ST = S::ST, E = S::E, PARTS = kQueryParts<T>, WPARTS = kWeightParts<T>, ROW = q4_row(D), U = 2, R = 16 * U;
+  constexpr int GR = S::GR, HC = S::HC, ST = S::ST, E = S::E, PARTS = kQueryParts<T>, WPARTS = kWeightParts<T>, ROW = q4_row(D), U = 2, R = 16 * U, NS = 4 / GR;
   __shared__ float sm_o[kWaves][HC][D + 4], sm_m[kWaves][HC], sm_l[kWaves][HC];
   __shared__ __align__(16) uint32_t sm_new[2][ROW / 4];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, L = lane >> 4;
@@ -352,16 +370,17 @@ template <typename T, int D> __global__ __launch_bounds__(kPagedThreads) void q4
     if (h < heads && g == mine) load8(x, rows_of<T>(a.q, a.qs, b, h0 + h) + D / 4 * L + 8 * t);
 #pragma unroll
     for (int e = 0; e < 8; ++e) qsum += x[e];
+    u32x4 w[PARTS];
 #pragma unroll
-    for (int p = 0; p < PARTS; ++p) {
-      u32x4 w;
+    for (int j = 0; j < 4; ++j) {
+      const int e = j < 2 ? 4 * j : 4 * j - 7;   // the order that codes_bf16 leaves them in: 0 2 4 6 1 3 5 7
+      uint32_t y[PARTS];
+      parts_of(y, x[e], x[e + 2]);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int e = j < 2 ? 4 * j : 4 * j - 7;   // the order that codes_bf16 leaves them in: 0 2 4 6 1 3 5 7
-        w[j] = take_part(x[e], x[e + 2]);
-      }
-      q[p][t] = as_bf16x8(w);
+      for (int p = 0; p < PARTS; ++p) w[p][j] = y[p];
     }
+#pragma unroll
+    for (int p = 0; p < PARTS; ++p) q[p][t] = as_bf16x8(w[p]);
   }
   qsum = sum_over_groups(qsum);
   const float sc = a.scale * kLog2e;
@@ -370,13 +389,15 @@ template <typename T, int D> __global__ __launch_bounds__(kPagedThreads) void q4
   for (int e = 0; e < E; ++e) o[e] = kZeroF4;
   float m = -INFINITY, l = 0.f, low = 0.f;
 
+  // pages of the tile at t0: of its 16-key parts, or of the key that this lane loads and of its four value rows
   struct Pages { int k[U], v[U]; };
+  auto page_of = [&](int token) { return token < to ? table[token >> a.shift] : -1; };
   auto pages = [&](int t0) {
     Pages p;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      p.k[u] = t0 + 16 * u + i < to ? table[(t0 + 16 * u + i) >> a.shift] : -1;
-      p.v[u] = t0 + 16 * u + 4 * L < to ? table[(t0 + 16 * u + 4 * L) >> a.shift] : -1;
+      p.k[u] = page_of(t0 + 16 * u + (ONE ? 0 : i));
+      p.v[u] = ONE ? 0 : page_of(t0 + 16 * u + 4 * L);
     }
     return p;
   };
@@ -386,18 +407,36 @@ template <typename T, int D> __global__ __launch_bounds__(kPagedThreads) void q4
     uint32_t v[U][4], kp[U][4], vp[U][4];   // value codes and the pairs of keys and values of tokens 4 L + r
   };
   // rows that are not there are read from page 0: in bounds, and masked
+  const uint32_t k_codes = (uint32_t)(i * a.kps[2]) + q4_piece(D) * L, k_pairs = (uint32_t)(4 * L * a.kps[2]) + D / 2 + 4 * g;
+  const uint32_t v_codes = (uint32_t)(4 * L * a.vps[2]) + (uint32_t)sizeof(typename S::ValueCodes) * i, v_pairs = (uint32_t)(4 * L * a.vps[2]) + D / 2 + 4 * g;
   auto load = [&](Tile& x, const Pages& p, int t0) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int key = t0 + 16 * u + i, four = t0 + 16 * u + 4 * L;
-      x.k[u] = *reinterpret_cast<const KeyCodes*>(kc + (there(p.k[u]) ? p.k[u] * a.kps[0] + (key & in_page) * a.kps[2] : 0) + q4_piece(D) * L);
-      const char* ks = kc + (there(p.v[u]) ? p.v[u] * a.kps[0] + (four & in_page) * a.kps[2] : 0);
-      const char* vs = vc + (there(p.v[u]) ? p.v[u] * a.vps[0] + (four & in_page) * a.vps[2] : 0);
+      if constexpr (ONE) {
+        // opaque here, or their extensions to 64 bits leave the loop and take a vector addition each
+        uint32_t kco = k_codes, kpo = k_pairs, vco = v_codes, vpo = v_pairs;
+        asm volatile("" : "+v"(kco), "+v"(kpo), "+v"(vco), "+v"(vpo));
+        const int token = t0 + 16 * u, page = there(p.k[u]) ? p.k[u] : -1;
+        const char* ks = kc + (page >= 0 ? page * a.kps[0] + (token & in_page) * a.kps[2] : 0);
+        const char* vs = vc + (page >= 0 ? page * a.vps[0] + (token & in_page) * a.vps[2] : 0);
+        x.k[u] = *reinterpret_cast<const KeyCodes*>(ks + kco);
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        x.kp[u][r] = reinterpret_cast<const uint32_t*>(ks + r * a.kps[2])[D / 8 + g];
-        x.vp[u][r] = reinterpret_cast<const uint32_t*>(vs + r * a.vps[2])[D / 8 + g];
-        x.v[u][r] = reinterpret_cast<const typename S::ValueCodes*>(vs + r * a.vps[2])[i];
+        for (int r = 0; r < 4; ++r) {
+          x.kp[u][r] = *reinterpret_cast<const uint32_t*>(ks + r * a.kps[2] + kpo);
+          x.vp[u][r] = *reinterpret_cast<const uint32_t*>(vs + r * a.vps[2] + vpo);
+          x.v[u][r] = *reinterpret_cast<const typename S::ValueCodes*>(vs + r * a.vps[2] + vco);
+        }
+      } else {
+        const int key = t0 + 16 * u + i, four = t0 + 16 * u + 4 * L;
+        x.k[u] = *reinterpret_cast<const KeyCodes*>(kc + (there(p.k[u]) ? p.k[u] * a.kps[0] + (key & in_page) * a.kps[2] : 0) + q4_piece(D) * L);
+        const char* ks = kc + (there(p.v[u]) ? p.v[u] * a.kps[0] + (four & in_page) * a.kps[2] : 0);
+        const char* vs = vc + (there(p.v[u]) ? p.v[u] * a.vps[0] + (four & in_page) * a.vps[2] : 0);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          x.kp[u][r] = reinterpret_cast<const uint32_t*>(ks + r * a.kps[2])[D / 8 + g];
+          x.vp[u][r] = reinterpret_cast<const uint32_t*>(vs + r * a.vps[2])[D / 8 + g];
+          x.v[u][r] = reinterpret_cast<const typename S::ValueCodes*>(vs + r * a.vps[2])[i];
+        }
       }
     }
   };
@@ -406,6 +445,10 @@ template <typename T, int D> __global__ __launch_bounds__(kPagedThreads) void q4
   int t0 = from + wave * R;
   Pages here = pages(t0);   // looked up a tile ahead
   for (; t0 < to; t0 += step) {
+    if (ONE) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) here.k[u] = __builtin_amdgcn_readfirstlane(here.k[u]);
+    }
     Tile x;
     load(x, here, t0);
     const Pages next = pages(t0 + step);
@@ -422,13 +465,19 @@ template <typename T, int D> __global__ __launch_bounds__(kPagedThreads) void q4
           }
       }
     }
-    float w[U][4];
+    // scores: this lane keeps those of tokens 4 L + g + GR n, n < NS
+    float w[U][NS];
     uint32_t in[U];
     bool whole = true;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int key = t0 + 16 * u + i;
-      in[u] = (uint32_t)__builtin_amdgcn_ballot_w64(key < to && (there(here.k[u]) || key == own)) & 0xffffu;
+      if (ONE) {
+        const int left = min(max(to - t0 - 16 * u, 0), 16), mine_at = own - t0 - 16 * u;
+        in[u] = (there(here.k[u]) ? (1u << left) - 1u : 0u) | ((unsigned)mine_at < 16u ? 1u << mine_at : 0u);
+      } else {
+        in[u] = (uint32_t)__builtin_amdgcn_ballot_w64(key < to && (there(here.k[u]) || key == own)) & 0xffffu;
+      }
       whole = whole && in[u] == 0xffffu;
       f32x4 s = kZeroF4;
 #pragma unroll
@@ -438,28 +487,37 @@ template <typename T, int D> __global__ __launch_bounds__(kPagedThreads) void q4
 #pragma unroll
         for (int p = PARTS - 1; p >= 0; --p) s = mfma16(codes, q[p][t], s);
       }
+      float y[4];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        float y = fmaf(bf16_lo(x.kp[u][r]), s[r], bf16_hi(x.kp[u][r]) * qsum);
-        y += beside<1>(y);
-        if (GR == 4) y += beside<2>(y);
-        w[u][r] = y * sc;
+      for (int r = 0; r < 4; ++r) y[r] = fmaf(bf16_lo(x.kp[u][r]), s[r], bf16_hi(x.kp[u][r]) * qsum);
+      // the groups' parts added up: of two tokens a lane keeps one and hands the other to the lane beside it
+      const float first = (g & 1 ? y[1] : y[0]) + beside<1>(g & 1 ? y[0] : y[1]), second = (g & 1 ? y[3] : y[2]) + beside<1>(g & 1 ? y[2] : y[3]);
+      if constexpr (GR == 4) {
+        w[u][0] = ((g & 2 ? second : first) + beside<2>(g & 2 ? first : second)) * sc;
+      } else {
+        w[u][0] = first * sc;
+        w[u][1] = second * sc;
       }
     }
     if (!whole) {
       // what is not there gets no weight, and its values, which may be anything, become zero
 #pragma unroll
-      for (int u = 0; u < U; ++u)
+      for (int u = 0; u < U; ++u) {
+#pragma unroll
+        for (int n = 0; n < NS; ++n)
+          if (!(in[u] >> (4 * L + g + GR * n) & 1u)) w[u][n] = -INFINITY;
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-          if (!(in[u] >> (4 * L + r) & 1u)) {
-            w[u][r] = -INFINITY;
-            x.vp[u][r] = 0u;
-          }
+          if (!(in[u] >> (4 * L + r) & 1u)) x.vp[u][r] = 0u;
+      }
     }
     float top = -INFINITY;
 #pragma unroll
-    for (int u = 0; u < U; ++u) top = fmaxf(top, fmaxf(fmaxf(w[u][0], w[u][1]), fmaxf(w[u][2], w[u][3])));
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int n = 0; n < NS; ++n) top = fmaxf(top, w[u][n]);
+    top = fmaxf(top, beside<1>(top));
+    if (GR == 4) top = fmaxf(top, beside<2>(top));
     top = max_over_groups(top);
     if (__builtin_amdgcn_ballot_w64(top > m + 8.f) != 0) {   // weights stay below 2^8 (packed_fwd.hip)
       const float up = fmaxf(m, top), by = __builtin_amdgcn_exp2f(m - (up == -INFINITY ? 0.f : up));
@@ -472,21 +530,28 @@ template <typename T, int D> __global__ __launch_bounds__(kPagedThreads) void q4
     const float ref = m == -INFINITY ? 0.f : m;
     u32x4 weights[WPARTS];
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+    for (int u = 0; u < U; ++u) {
+#pragma unroll
+      for (int n = 0; n < NS; ++n) {
+        w[u][n] = __builtin_amdgcn_exp2f(w[u][n] - ref);
+        l += w[u][n];
+      }
 #pragma unroll
       for (int r = 0; r < 4; r += 2) {
         float y[2];
 #pragma unroll
         for (int z = 0; z < 2; ++z) {
-          const float p = __builtin_amdgcn_exp2f(w[u][r + z] - ref);
-          l += p;
+          const float p = of_group<GR>(w[u][(r + z) / GR], (r + z) % GR);
           low = fmaf(p, bf16_hi(x.vp[u][r + z]), low);
           y[z] = p * bf16_lo(x.vp[u][r + z]);
         }
+        uint32_t z[WPARTS];
+        parts_of(z, y[0], y[1]);
 #pragma unroll
-        for (int p = 0; p < WPARTS; ++p) weights[p][2 * u + r / 2] = take_part(y[0], y[1]);
-        if (sizeof(T) == 4) low = fmaf(kMiddle, bf16_lo(weights[0][2 * u + r / 2]), fmaf(kMiddle, bf16_hi(weights[0][2 * u + r / 2]), low));
+        for (int p = 0; p < WPARTS; ++p) weights[p][2 * u + r / 2] = z[p];
+        if (sizeof(T) == 4) low = fmaf(kMiddle, bf16_lo(z[0]), fmaf(kMiddle, bf16_hi(z[0]), low));
       }
+    }
     // channels of the same byte's half and parity at a time: a byte of each of two tokens, then one of the next
 #pragma unroll
     for (int half = 0; half < E / 4; ++half) {
@@ -507,6 +572,8 @@ template <typename T, int D> __global__ __launch_bounds__(kPagedThreads) void q4
     }
     here = next;
   }
+  l += beside<1>(l);
+  if (GR == 4) l += beside<2>(l);
   l = sum_over_groups(l);
   low = sum_over_groups(low);
 
@@ -555,7 +622,8 @@ int64_t decode_units(int B, int H, int Hkv, int d) {
 
 template <typename T, int D> hipError_t decode(const PagedDecodeArgs& a, hipStream_t s) {
   const unsigned workgroups = (unsigned)(decode_units(a.B, a.H, a.Hkv, D) * a.splits);
-  q4_decode_kernel<T, D><<<dim3(workgroups), dim3(kPagedThreads), 0, s>>>(a);
+  if (a.shift >= 4) q4_decode_kernel<T, D, true><<<dim3(workgroups), dim3(kPagedThreads), 0, s>>>(a);
+  else q4_decode_kernel<T, D, false><<<dim3(workgroups), dim3(kPagedThreads), 0, s>>>(a);
   const hipError_t e = hipGetLastError();
   return e != hipSuccess || a.splits == 1 ? e : launch_paged_join(a, sizeof(T) == 2, s);
 }
