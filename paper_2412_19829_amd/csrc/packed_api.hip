@@ -112,13 +112,21 @@ gf_status check_table(int width, int shift, int max_len, int* room) {
   return GF_OK;
 }
 
-PagedSplit split_of(bool q4, int B, int H, int Hkv, int d, int room) {
-  return q4 ? paged_q4_split(B, H, Hkv, d, room) : paged_split(B, H, Hkv, room);
+// Rows of [H, d] sums that the call keeps (1: none), keys per workgroup and workgroups along a sequence, or (q4) along all of them.
+struct DecodePlan {
+  int64_t rows;
+  PagedSplit split;
+};
+DecodePlan plan_of(bool q4, int B, int H, int Hkv, int d, int room) {
+  if (q4) {
+    const int parts = paged_q4_parts(B, H, Hkv, d, room);
+    return {parts == 1 ? 1 : (int64_t)parts + B, {0, parts}};
+  }
+  const PagedSplit s = paged_split(B, H, Hkv, room);
+  return {s.splits == 1 ? 1 : (int64_t)B * s.splits, s};
 }
-size_t decode_bytes(bool q4, int B, int H, int Hkv, int d, int room) {
-  const PagedSplit s = split_of(q4, B, H, Hkv, d, room);
-  if (s.splits == 1) return 0;
-  return ((size_t)B * H * s.splits * (d + 2) * sizeof(float) + 255) / 256 * 256;
+size_t decode_bytes(const DecodePlan& plan, int H, int d) {
+  return plan.rows == 1 ? 0 : ((size_t)plan.rows * H * (d + 2) * sizeof(float) + 255) / 256 * 256;
 }
 
 gf_status status(hipError_t e) { return e == hipSuccess ? GF_OK : GF_ERR_DEVICE; }
@@ -131,7 +139,7 @@ size_t decode_workspace(bool q4, int B, int H, int Hkv, int d, int table_width, 
   if (!p || B < 1 || check_heads(p->dtype, H, Hkv, d) != GF_OK || check_paged(Hkv, d, 1, p, &shift, kps, vps, q4) != GF_OK ||
       check_table(table_width, shift, max_len, &room) != GF_OK)
     return 0;
-  return decode_bytes(q4, B, H, Hkv, d, room);
+  return decode_bytes(plan_of(q4, B, H, Hkv, d, room), H, d);
 }
 
 gf_status decode_step(bool q4, const void* q, const void* k, const void* v, void* out, void* kpages, void* vpages,
@@ -150,13 +158,13 @@ gf_status decode_step(bool q4, const void* q, const void* k, const void* v, void
       (st = strides2(p->v_stride, a.vs, Hkv, d)) != GF_OK || (st = strides2(p->o_stride, a.os, H, d)) != GF_OK)
     return st;
   if (B == 0) return GF_OK;
-  const PagedSplit s = split_of(q4, B, H, Hkv, d, a.room);
-  if (!(q4 ? paged_q4_decode_fits(B, H, Hkv, d, s) : paged_decode_fits(B, H, Hkv, s))) return GF_ERR_UNSUPPORTED;
+  const DecodePlan plan = plan_of(q4, B, H, Hkv, d, a.room);
+  if (!(q4 ? paged_q4_decode_fits(B, H, Hkv, d, a.room) : paged_decode_fits(B, H, Hkv, plan.split))) return GF_ERR_UNSUPPORTED;
   if (n_pages < 1) return GF_ERR_INVALID_ARG;
   if (!q || !out || !kpages || !vpages || (!table && table_width > 0) || !lens || !k != !v) return GF_ERR_INVALID_ARG;
   if (misaligned(bits(q, k, v, out, kpages, vpages), 16) || misaligned(bits(table, lens), 4)) return GF_ERR_INVALID_ARG;
   if (out == q || out == k || out == v || out == kpages || out == vpages || kpages == vpages) return GF_ERR_INVALID_ARG;
-  const size_t need = decode_bytes(q4, B, H, Hkv, d, a.room);
+  const size_t need = decode_bytes(plan, H, d);
   if (need > 0 && (!workspace || workspace_bytes < need)) return GF_ERR_WORKSPACE;
   if (need > 0 && misaligned(bits(workspace), 256)) return GF_ERR_INVALID_ARG;
   if ((st = check_device(hip_stream)) != GF_OK) return st;
@@ -174,11 +182,11 @@ gf_status decode_step(bool q4, const void* q, const void* k, const void* v, void
   a.d = d;
   a.n_pages = n_pages;
   a.width = table_width;
-  a.chunk = s.chunk;
-  a.splits = s.splits;
+  a.chunk = plan.split.chunk;
+  a.splits = plan.split.splits;
   a.scale = p->softmax_scale;
   a.sums = static_cast<float*>(workspace);
-  if (s.splits > 1) a.stats = a.sums + (size_t)B * H * s.splits * d;
+  if (need > 0) a.stats = a.sums + (size_t)plan.rows * H * d;
   const bool bf16 = p->dtype == GF_BF16;
   const hipStream_t on = reinterpret_cast<hipStream_t>(hip_stream);
   return status(q4 ? launch_paged_q4_decode(a, bf16, on) : launch_paged_decode(a, bf16, on));

@@ -371,8 +371,10 @@ int64_t decode_units(int B, int H, int Hkv) { return (int64_t)B * Hkv * (((int64
 template <typename T, int D> hipError_t decode(const PagedDecodeArgs& a, hipStream_t s) {
   const unsigned workgroups = (unsigned)(decode_units(a.B, a.H, a.Hkv) * a.splits);
   paged_decode_kernel<T, D><<<dim3(workgroups), dim3(kPagedThreads), 0, s>>>(a);
-  const hipError_t e = hipGetLastError();
-  return e != hipSuccess || a.splits == 1 ? e : launch_paged_join(a, sizeof(T) == 2, s);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.splits == 1) return e;
+  paged_join_kernel<T, D><<<dim3((unsigned)((int64_t)a.B * a.H)), dim3(kPagedThreads), 0, s>>>(a);
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -398,13 +400,6 @@ bool paged_fill_fits(int total, int n_seqs, int Hkv) { return packed_tiles(total
 hipError_t launch_paged_decode(const PagedDecodeArgs& a, bool bf16, hipStream_t s) {
   if (bf16) return a.d == 128 ? decode<uint16_t, 128>(a, s) : decode<uint16_t, 64>(a, s);
   return a.d == 128 ? decode<float, 128>(a, s) : decode<float, 64>(a, s);
-}
-
-hipError_t launch_paged_join(const PagedDecodeArgs& a, bool bf16, hipStream_t s) {
-  const dim3 grid((unsigned)((int64_t)a.B * a.H));
-  if (bf16) a.d == 128 ? paged_join_kernel<uint16_t, 128><<<grid, kPagedThreads, 0, s>>>(a) : paged_join_kernel<uint16_t, 64><<<grid, kPagedThreads, 0, s>>>(a);
-  else a.d == 128 ? paged_join_kernel<float, 128><<<grid, kPagedThreads, 0, s>>>(a) : paged_join_kernel<float, 64><<<grid, kPagedThreads, 0, s>>>(a);
-  return hipGetLastError();
 }
 
 hipError_t launch_paged_fill(const PagedFillArgs& a, bool bf16, hipStream_t s) {

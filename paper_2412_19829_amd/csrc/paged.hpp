@@ -43,8 +43,6 @@ PagedSplit paged_split(int B, int H, int Hkv, int64_t max_len);
 bool paged_decode_fits(int B, int H, int Hkv, PagedSplit s);
 bool paged_fill_fits(int total, int n_seqs, int Hkv);
 hipError_t launch_paged_decode(const PagedDecodeArgs& a, bool bf16, hipStream_t s);
-// The chunks' sums and statistics of a step over either kind of cache into its outputs.
-hipError_t launch_paged_join(const PagedDecodeArgs& a, bool bf16, hipStream_t s);
 hipError_t launch_paged_fill(const PagedFillArgs& a, bool bf16, hipStream_t s);
 hipError_t launch_pages_copy(const PagesCopyArgs& a, bool bf16, hipStream_t s);
 

@@ -40,6 +40,27 @@ template <int GR> __device__ __forceinline__ float of_group(float x, int from) {
                                     : __builtin_amdgcn_mov_dpp(v, 0xff, 0xf, 0xf, true));
 }
 
+// The largest, or the sum, of all lanes' values.
+template <bool MAX> __device__ __forceinline__ float over_lanes(float x) {
+  auto with = [](float a, float b) { return MAX ? fmaxf(a, b) : a + b; };
+  x = with(x, beside<1>(x));
+  x = with(x, beside<2>(x));
+  x = with(x, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x141, 0xf, 0xf, true)));   // halves of a row of 16, mirrored
+  x = with(x, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x140, 0xf, 0xf, true)));   // rows, mirrored
+  return MAX ? max_over_groups(x) : sum_over_groups(x);
+}
+
+// The sum of the lanes up to this one.
+__device__ __forceinline__ int sum_up_to(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);   // from 1, 2, 4 and 8 lanes before in the row of 16
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);   // the last of the row before, to rows 1 and 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);   // the last of row 1, to rows 2 and 3
+  return x;
+}
+
 // ---- rows -------------------------------------------------------------------------------------------
 
 // Codes of 8 of 32 values that four neighbouring lanes hold, and the group's (scale, lowest value).
@@ -126,27 +147,37 @@ template <typename T> __device__ __forceinline__ Codes quantised(const float (&x
 }
 
 // 8 values of a row; what a kernel reads or writes for the last time may pass the caches by.
-template <bool ONCE = false, typename V> __device__ __forceinline__ V get(const V* p) { return ONCE ? __builtin_nontemporal_load(p) : *p; }
+template <bool ONCE = false, typename V> __device__ __forceinline__ V take(const V* p) { return ONCE ? __builtin_nontemporal_load(p) : *p; }
 template <typename V> __device__ __forceinline__ void put(V* p, V x, bool once) {
   if (once) __builtin_nontemporal_store(x, p);
   else *p = x;
 }
-template <bool ONCE = false> __device__ __forceinline__ void load8(float (&x)[8], const uint16_t* p) {
-  const u32x4 w = get<ONCE>(reinterpret_cast<const u32x4*>(p));
+template <typename T> struct Eight;
+template <> struct Eight<uint16_t> {
+  u32x4 w;
+  template <bool ONCE = false> __device__ __forceinline__ void get(const uint16_t* p) { w = take<ONCE>(reinterpret_cast<const u32x4*>(p)); }
+  __device__ __forceinline__ void values(float (&x)[8]) const {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[2 * i] = bf16_lo(w[i]);
-    x[2 * i + 1] = bf16_hi(w[i]);
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = bf16_lo(w[i]);
+      x[2 * i + 1] = bf16_hi(w[i]);
+    }
   }
-}
-template <bool ONCE = false> __device__ __forceinline__ void load8(float (&x)[8], const float* p) {
-  const f32x4 a = get<ONCE>(reinterpret_cast<const f32x4*>(p)), b = get<ONCE>(reinterpret_cast<const f32x4*>(p + 4));
+};
+template <> struct Eight<float> {
+  f32x4 a, b;
+  template <bool ONCE = false> __device__ __forceinline__ void get(const float* p) {
+    a = take<ONCE>(reinterpret_cast<const f32x4*>(p));
+    b = take<ONCE>(reinterpret_cast<const f32x4*>(p + 4));
+  }
+  __device__ __forceinline__ void values(float (&x)[8]) const {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[i] = a[i];
-    x[4 + i] = b[i];
+    for (int i = 0; i < 4; ++i) {
+      x[i] = a[i];
+      x[4 + i] = b[i];
+    }
   }
-}
+};
 __device__ __forceinline__ void store8(uint16_t* p, const float (&x)[8], bool once) {
   put(reinterpret_cast<u32x4*>(p), u32x4{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])}, once);
 }
@@ -172,14 +203,31 @@ template <int D> struct Slots {
   template <typename A> __device__ __forceinline__ bool find(const A& a, int block, int tid) {
     using S = RowShape<D>;
     const int sets = (a.Hkv + kHeads - 1) / kHeads;
-    const SeqTile at = find_tile<S::ROWS>(a.cu, a.n_seqs, a.total, block / sets, tid & 63);
-    if (at.first < 0 || at.seq == a.n_seqs) return false;
-    const int base = packed_row(a.cu, at.seq, a.total), n = packed_row(a.cu, at.seq + 1, a.total) - base;
-    const int64_t room = (int64_t)a.width << a.shift, from = a.start[at.seq];
-    const int32_t* table = a.table + (int64_t)at.seq * a.width;
+    const int tile = block / sets, lane = tid & 63;
+    int seq, base, n;
+    int64_t from;
+    if (a.n_seqs < 64) {   // find_tile's search, with the starts on their way beside the offsets
+      const int cu = packed_row(a.cu, min(lane, a.n_seqs), a.total), start = a.start[min(lane, a.n_seqs - 1)];
+      seq = __popcll(__builtin_amdgcn_ballot_w64(lane <= a.n_seqs && cu / S::ROWS + lane <= tile)) - 1;
+      if (seq < 0 || seq >= a.n_seqs) return false;
+      base = __builtin_amdgcn_readlane(cu, seq);
+      n = __builtin_amdgcn_readlane(cu, seq + 1) - base;
+      from = __builtin_amdgcn_readlane(start, seq);
+    } else {
+      const SeqTile at = find_tile<S::ROWS>(a.cu, a.n_seqs, a.total, tile, lane);
+      if (at.first < 0 || at.seq == a.n_seqs) return false;
+      seq = at.seq;
+      base = packed_row(a.cu, seq, a.total);
+      n = packed_row(a.cu, seq + 1, a.total) - base;
+      from = a.start[seq];
+    }
+    const int first = (tile - seq - base / S::ROWS) * S::ROWS;
+    if (first < 0) return false;
+    const int64_t room = (int64_t)a.width << a.shift;
+    const int32_t* table = a.table + (int64_t)seq * a.width;
 #pragma unroll
     for (int i = 0; i < S::N; ++i) {
-      const int u = tid / S::C + i * S::STEP, r = at.first + u / kHeads;
+      const int u = tid / S::C + i * S::STEP, r = first + u / kHeads;
       const int64_t pos = from + r;
       head[i] = block % sets * kHeads + u % kHeads;
       const bool real = r < n && head[i] < a.Hkv;
@@ -200,18 +248,21 @@ template <typename T, int D> __global__ __launch_bounds__(kPagedThreads) void q4
   const int tid = threadIdx.x, c = tid % RowShape<D>::C;
   Slots<D> s;
   if (!s.find(a, blockIdx.x, tid)) return;
-  float k[N][8], v[N][8];
+  Eight<T> k[N], v[N];
 #pragma unroll
   for (int i = 0; i < N; ++i)
     if (s.page[i] >= 0) {
-      load8<true>(k[i], rows_of<T>(a.k, a.ks, s.row[i], s.head[i]) + 8 * c);
-      load8<true>(v[i], rows_of<T>(a.v, a.vs, s.row[i], s.head[i]) + 8 * c);
+      k[i].template get<true>(rows_of<T>(a.k, a.ks, s.row[i], s.head[i]) + 8 * c);
+      v[i].template get<true>(rows_of<T>(a.v, a.vs, s.row[i], s.head[i]) + 8 * c);
     }
 #pragma unroll
   for (int i = 0; i < N; ++i)
     if (s.page[i] >= 0) {
-      put_codes<D>(reinterpret_cast<uint32_t*>(reinterpret_cast<char*>(a.kpages) + s.at(a.kps, i)), c, quantised<T>(k[i]));
-      put_codes<D>(reinterpret_cast<uint32_t*>(reinterpret_cast<char*>(a.vpages) + s.at(a.vps, i)), c, quantised<T>(v[i]));
+      float x[8];
+      k[i].values(x);
+      put_codes<D>(reinterpret_cast<uint32_t*>(reinterpret_cast<char*>(a.kpages) + s.at(a.kps, i)), c, quantised<T>(x));
+      v[i].values(x);
+      put_codes<D>(reinterpret_cast<uint32_t*>(reinterpret_cast<char*>(a.vpages) + s.at(a.vps, i)), c, quantised<T>(x));
     }
 }
 
@@ -316,58 +367,194 @@ __device__ __forceinline__ int seen_tokens(const PagedDecodeArgs& a, int b) {
   return t < 0 || t > a.room - own ? 0 : t + own;
 }
 
+// The sequences' tokens lie one behind another in blocks of kBlock, at least one for each, and `parts` workgroups take equal shares of the
+// blocks, whatever the lengths are, which are known on the device alone.  A share may hold several sequences, or a part of one; what
+// part p finds of sequence b has row p + b of the workspace to itself, since from one such piece to the next p or b grows.
+constexpr int kBlock = 32 * kWaves;   // a tile for each wave
+constexpr int kSetUp = 2;             // what beginning a sequence costs, in blocks: counted in front of its own
+__host__ __device__ constexpr int64_t blocks_of(int64_t tokens) { return tokens < 1 ? 1 : (tokens + kBlock - 1) / kBlock; }
+__device__ __forceinline__ int units_of(int tokens) { return kSetUp + (int)blocks_of(tokens); }
+__device__ __forceinline__ int first_unit(int part, int parts, int total) { return (int)((int64_t)part * total / parts); }
+// The part that holds a unit.
+__device__ __forceinline__ int part_of(int unit, int parts, int total) { return (int)((((int64_t)unit + 1) * parts + total - 1) / total) - 1; }
+
+struct Cut {
+  int total, parts;     // units, and workgroups that have any
+  int b, base;          // the sequence that holds the part's first unit, and that sequence's first unit
+  int from, known, tokens;   // what this lane's sequence, from + lane, sees, for the first `known` lanes
+  __device__ __forceinline__ int seen(const PagedDecodeArgs& a, int seq) const {
+    return __builtin_amdgcn_readfirstlane(seq - from < known ? __builtin_amdgcn_readlane(tokens, seq - from) : seen_tokens(a, seq));
+  }
+};
+__device__ __forceinline__ Cut cut_at(const PagedDecodeArgs& a, int part, int lane) {
+  Cut x = {-1, 0, 0, 0, 0, 0, 0};
+  int count = a.B, target = 0;
+  for (;;) {   // a 64th of the sequences a lane
+    const int per = (count + 63) / 64;
+    int sum = 0;
+    for (int j = 0; j < per; ++j)
+      if (lane * per + j < count) sum += units_of(x.tokens = seen_tokens(a, x.b + lane * per + j));
+    if (per == 1) {
+      x.from = x.b;
+      x.known = count;
+    }
+    sum = sum_up_to(sum);
+    if (x.total < 0) {
+      x.total = __builtin_amdgcn_readlane(sum, 63);
+      x.parts = min(a.splits, x.total);
+      if (part >= x.parts) return x;
+      target = first_unit(part, x.parts, x.total);
+    }
+    const int before = __popcll(__builtin_amdgcn_ballot_w64(x.base + sum <= target));   // lanes whose sequences lie in front
+    if (before > 0) x.base += __builtin_amdgcn_readlane(sum, before - 1);
+    x.b += before * per;
+    if (per == 1) return x;
+    count = min(per, count - before * per);
+  }
+}
+
 // ONE: a page holds whole tiles of 16 keys (pages of 8 tokens do not), so that their pages and addresses are the same for all lanes, which
 // then add nothing but a fixed offset to them: 572 vector instructions a tile of 32 keys, d = 128, with addresses of their own, 379 without.
 template <typename T, int D, bool ONE> __global__ __launch_bounds__(kPagedThreads, sizeof(T) == 2 ? 3 : 2) void q4_decode_kernel(PagedDecodeArgs a) {
   using S = Shape4<D>;
   typedef typename S::KeyCodes KeyCodes;
+  typedef typename S::ValueCodes ValueCodes;
   constexpr int GR = S::GR, HC = S::HC, ST = S::ST, E = S::E, PARTS = kQueryParts<T>, WPARTS = kWeightParts<T>, ROW = q4_row(D), U = 2, R = 16 * U, NS = 4 / GR;
   __shared__ float sm_o[kWaves][HC][D + 4], sm_m[kWaves][HC], sm_l[kWaves][HC];
   __shared__ __align__(16) uint32_t sm_new[2][ROW / 4];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, L = lane >> 4;
   const int G = a.H / a.Hkv, tiles = (G + HC - 1) / HC;
-  int id = blockIdx.x;   // chunks slowest, as in the other cache's step
-  const int tile = id % tiles;
-  id /= tiles;
-  const int kvh = id % a.Hkv;
-  id /= a.Hkv;
-  const int b = id % a.B, split = id / a.B;
+  const int tile = blockIdx.x % tiles, kvh = blockIdx.x / tiles % a.Hkv, part = blockIdx.x / (tiles * a.Hkv);
   const int h0 = kvh * G + tile * HC, heads = min(G - tile * HC, HC);
-  const int n = seen_tokens(a, b), from = split * a.chunk, to = min(n, from + a.chunk);
-  if (split > 0 && from >= n) return;   // the joining kernel knows as much
-
-  const int own = a.k && n > 0 ? n - 1 : -1;   // the new token's position
+  Cut cut = cut_at(a, part, lane);
+  if (part >= cut.parts) return;
+  int unit = first_unit(part, cut.parts, cut.total);
+  const int last_unit = first_unit(part + 1, cut.parts, cut.total);
   const char* kc = reinterpret_cast<const char*>(a.kpages) + kvh * a.kps[1];
   const char* vc = reinterpret_cast<const char*>(a.vpages) + kvh * a.vps[1];
-  const int32_t* table = a.table + (int64_t)b * a.width;
   const int in_page = (1 << a.shift) - 1;
 
-  // the new token's row, for its slot and for the tile that sees it: nobody reads the slot in this call
-  if (own >= from && own < to) {
-    const int c = lane % (D / 8);
-    if (wave < 2 && lane < D / 8) {
-      float x[8];
-      load8(x, (wave == 0 ? rows_of<T>(a.k, a.ks, b, kvh) : rows_of<T>(a.v, a.vs, b, kvh)) + 8 * c);
-      const Codes y = quantised<T>(x);
-      put_codes<D>(sm_new[wave], c, y);
-      const int page = table[own >> a.shift];
-      if (tile == 0 && (unsigned)page < (unsigned)a.n_pages) {
-        char* row = wave == 0 ? reinterpret_cast<char*>(a.kpages) + page * a.kps[0] + kvh * a.kps[1] + (own & in_page) * a.kps[2]
-                              : reinterpret_cast<char*>(a.vpages) + page * a.vps[0] + kvh * a.vps[1] + (own & in_page) * a.vps[2];
-        put_codes<D>(reinterpret_cast<uint32_t*>(row), c, y);
-      }
-    }
-    __syncthreads();
-  }
+  // a part that ends while it sets a sequence up leaves it to the next one
+  while (cut.base + kSetUp < last_unit) {
+  const int b = cut.b, n = cut.seen(a, b), first = cut.base + kSetUp;
+  const int from = max(unit - first, 0) * kBlock, to = (int)min((int64_t)n, (int64_t)(last_unit - first) * kBlock);
+  const bool whole_sequence = unit <= first && last_unit - cut.base >= units_of(n);
+  unit = cut.base += units_of(n);
+  ++cut.b;
+  const int own = a.k && n > 0 ? n - 1 : -1;   // the new token's position
+  const int32_t* table = a.table + (int64_t)b * a.width;
 
+  // pages of the tile at t0: of its 16-key parts, or of the key that this lane loads and of its four value rows
+  struct Pages { int k[U], v[U]; };
+  auto page_of = [&](int token) { return token < to ? table[token >> a.shift] : -1; };
+  auto pages = [&](int t0) {
+    Pages p;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      p.k[u] = page_of(t0 + 16 * u + (ONE ? 0 : i));
+      p.v[u] = ONE ? 0 : page_of(t0 + 16 * u + 4 * L);
+    }
+    return p;
+  };
+  auto there = [&](int page) { return (unsigned)page < (unsigned)a.n_pages; };
+  // Everything that the first tile waits for sets out at once.  Pages are looked up two tiles ahead.
+  const int step = kWaves * R;
+  int t0 = from + wave * R;
+  Pages here = pages(t0), next = pages(t0 + step);
   // column i: query head i / GR, group i % GR
   const int h = i / GR, g = i % GR, mine = L * GR / 4;   // mine: the group of this lane's channels
+  Eight<T> raw[ST];
+#pragma unroll
+  for (int t = 0; t < ST; ++t) {
+    raw[t] = {};
+    if (h < heads && g == mine) raw[t].get(rows_of<T>(a.q, a.qs, b, h0 + h) + D / 4 * L + 8 * t);
+  }
+  const bool brings_own = own >= from && own < to, my_own = brings_own && wave < 2 && lane < D / 8;
+  Eight<T> fresh = {};
+  int own_page = -1;
+  if (my_own) {
+    fresh.get((wave == 0 ? rows_of<T>(a.k, a.ks, b, kvh) : rows_of<T>(a.v, a.vs, b, kvh)) + 8 * lane);
+    own_page = table[own >> a.shift];
+  }
+
+  // rows that are not there are read from page 0: in bounds, and masked
+  const uint32_t k_codes = (uint32_t)(i * a.kps[2]) + q4_piece(D) * L, k_pairs = (uint32_t)(4 * L * a.kps[2]) + D / 2 + 4 * g;
+  const uint32_t v_codes = (uint32_t)(4 * L * a.vps[2]) + (uint32_t)sizeof(ValueCodes) * i, v_pairs = (uint32_t)(4 * L * a.vps[2]) + D / 2 + 4 * g;
+  auto row_at = [&](const char* pages, const int64_t (&st)[3], int page, int token) {
+    return pages + (there(page) ? page * st[0] + (token & in_page) * st[2] : 0);
+  };
+  struct Keys {
+    KeyCodes codes[U];
+    uint32_t pair[U][4];     // of tokens 4 L + r
+  };
+  auto load_keys = [&](Keys& x, const Pages& p, int t0) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if constexpr (ONE) {
+        // opaque here, or their extensions to 64 bits leave the loop and take a vector addition each
+        uint32_t codes = k_codes, pairs = k_pairs;
+        asm volatile("" : "+v"(codes), "+v"(pairs));
+        const char* at = row_at(kc, a.kps, p.k[u], t0 + 16 * u);
+        x.codes[u] = *reinterpret_cast<const KeyCodes*>(at + codes);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x.pair[u][r] = *reinterpret_cast<const uint32_t*>(at + r * a.kps[2] + pairs);
+      } else {
+        x.codes[u] = *reinterpret_cast<const KeyCodes*>(row_at(kc, a.kps, p.k[u], t0 + 16 * u + i) + q4_piece(D) * L);
+        const char* at = row_at(kc, a.kps, p.v[u], t0 + 16 * u + 4 * L);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x.pair[u][r] = reinterpret_cast<const uint32_t*>(at + r * a.kps[2])[D / 8 + g];
+      }
+    }
+  };
+  struct Values {
+    uint32_t codes[U][4], pair[U][4];
+  };
+  auto load_values = [&](Values& x, const Pages& p, int t0) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      uint32_t codes = v_codes, pairs = v_pairs;
+      if (ONE) asm volatile("" : "+v"(codes), "+v"(pairs));
+      const char* at = ONE ? row_at(vc, a.vps, p.k[u], t0 + 16 * u) : row_at(vc, a.vps, p.v[u], t0 + 16 * u + 4 * L) - 4 * L * a.vps[2];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        x.pair[u][r] = *reinterpret_cast<const uint32_t*>(at + r * a.vps[2] + pairs);
+        x.codes[u][r] = *reinterpret_cast<const ValueCodes*>(at + r * a.vps[2] + codes);
+      }
+    }
+  };
+
+  auto settle = [&](Pages& p) {
+    if (ONE) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) p.k[u] = __builtin_amdgcn_readfirstlane(p.k[u]);
+    }
+  };
+  settle(here);
+  Keys keys;
+  load_keys(keys, here, t0);
+
+  // the new token's row, for its slot and for the tile that sees it: nobody reads the slot in this call
+  if (brings_own) {
+    if (my_own) {
+      float x[8];
+      fresh.values(x);
+      const Codes y = quantised<T>(x);
+      put_codes<D>(sm_new[wave], lane, y);
+      if (tile == 0 && there(own_page)) {
+        char* row = wave == 0 ? reinterpret_cast<char*>(a.kpages) + own_page * a.kps[0] + kvh * a.kps[1] + (own & in_page) * a.kps[2]
+                              : reinterpret_cast<char*>(a.vpages) + own_page * a.vps[0] + kvh * a.vps[1] + (own & in_page) * a.vps[2];
+        put_codes<D>(reinterpret_cast<uint32_t*>(row), lane, y);
+      }
+    }
+    lds_barrier();
+  }
+
   bf16x8 q[PARTS][ST];
   float qsum = 0.f;
 #pragma unroll
   for (int t = 0; t < ST; ++t) {
-    float x[8] = {};
-    if (h < heads && g == mine) load8(x, rows_of<T>(a.q, a.qs, b, h0 + h) + D / 4 * L + 8 * t);
+    float x[8];
+    raw[t].values(x);
 #pragma unroll
     for (int e = 0; e < 8; ++e) qsum += x[e];
     u32x4 w[PARTS];
@@ -389,80 +576,20 @@ template <typename T, int D, bool ONE> __global__ __launch_bounds__(kPagedThread
   for (int e = 0; e < E; ++e) o[e] = kZeroF4;
   float m = -INFINITY, l = 0.f, low = 0.f;
 
-  // pages of the tile at t0: of its 16-key parts, or of the key that this lane loads and of its four value rows
-  struct Pages { int k[U], v[U]; };
-  auto page_of = [&](int token) { return token < to ? table[token >> a.shift] : -1; };
-  auto pages = [&](int t0) {
-    Pages p;
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      p.k[u] = page_of(t0 + 16 * u + (ONE ? 0 : i));
-      p.v[u] = ONE ? 0 : page_of(t0 + 16 * u + 4 * L);
-    }
-    return p;
-  };
-  auto there = [&](int page) { return (unsigned)page < (unsigned)a.n_pages; };
-  struct Tile {
-    KeyCodes k[U];
-    uint32_t v[U][4], kp[U][4], vp[U][4];   // value codes and the pairs of keys and values of tokens 4 L + r
-  };
-  // rows that are not there are read from page 0: in bounds, and masked
-  const uint32_t k_codes = (uint32_t)(i * a.kps[2]) + q4_piece(D) * L, k_pairs = (uint32_t)(4 * L * a.kps[2]) + D / 2 + 4 * g;
-  const uint32_t v_codes = (uint32_t)(4 * L * a.vps[2]) + (uint32_t)sizeof(typename S::ValueCodes) * i, v_pairs = (uint32_t)(4 * L * a.vps[2]) + D / 2 + 4 * g;
-  auto load = [&](Tile& x, const Pages& p, int t0) {
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if constexpr (ONE) {
-        // opaque here, or their extensions to 64 bits leave the loop and take a vector addition each
-        uint32_t kco = k_codes, kpo = k_pairs, vco = v_codes, vpo = v_pairs;
-        asm volatile("" : "+v"(kco), "+v"(kpo), "+v"(vco), "+v"(vpo));
-        const int token = t0 + 16 * u, page = there(p.k[u]) ? p.k[u] : -1;
-        const char* ks = kc + (page >= 0 ? page * a.kps[0] + (token & in_page) * a.kps[2] : 0);
-        const char* vs = vc + (page >= 0 ? page * a.vps[0] + (token & in_page) * a.vps[2] : 0);
-        x.k[u] = *reinterpret_cast<const KeyCodes*>(ks + kco);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          x.kp[u][r] = *reinterpret_cast<const uint32_t*>(ks + r * a.kps[2] + kpo);
-          x.vp[u][r] = *reinterpret_cast<const uint32_t*>(vs + r * a.vps[2] + vpo);
-          x.v[u][r] = *reinterpret_cast<const typename S::ValueCodes*>(vs + r * a.vps[2] + vco);
-        }
-      } else {
-        const int key = t0 + 16 * u + i, four = t0 + 16 * u + 4 * L;
-        x.k[u] = *reinterpret_cast<const KeyCodes*>(kc + (there(p.k[u]) ? p.k[u] * a.kps[0] + (key & in_page) * a.kps[2] : 0) + q4_piece(D) * L);
-        const char* ks = kc + (there(p.v[u]) ? p.v[u] * a.kps[0] + (four & in_page) * a.kps[2] : 0);
-        const char* vs = vc + (there(p.v[u]) ? p.v[u] * a.vps[0] + (four & in_page) * a.vps[2] : 0);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          x.kp[u][r] = reinterpret_cast<const uint32_t*>(ks + r * a.kps[2])[D / 8 + g];
-          x.vp[u][r] = reinterpret_cast<const uint32_t*>(vs + r * a.vps[2])[D / 8 + g];
-          x.v[u][r] = reinterpret_cast<const typename S::ValueCodes*>(vs + r * a.vps[2])[i];
-        }
-      }
-    }
-  };
-
-  const int step = kWaves * R;
-  int t0 = from + wave * R;
-  Pages here = pages(t0);   // looked up a tile ahead
+  // A tile's values are on their way while its scores are taken, the next tile's keys, in the registers of this one's, from then on.
   for (; t0 < to; t0 += step) {
-    if (ONE) {
-#pragma unroll
-      for (int u = 0; u < U; ++u) here.k[u] = __builtin_amdgcn_readfirstlane(here.k[u]);
-    }
-    Tile x;
-    load(x, here, t0);
-    const Pages next = pages(t0 + step);
-    if ((unsigned)(own - t0) < (unsigned)R) {   // this tile holds the new token
+    Values x;
+    load_values(x, here, t0);
+    settle(next);
+    const Pages later = pages(t0 + 2 * step);
+    const bool has_own = (unsigned)(own - t0) < (unsigned)R;   // this tile holds the new token
+    if (has_own) {
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        if (t0 + 16 * u + i == own) x.k[u] = *reinterpret_cast<const KeyCodes*>(reinterpret_cast<const char*>(sm_new[0]) + q4_piece(D) * L);
+        if (t0 + 16 * u + i == own) keys.codes[u] = *reinterpret_cast<const KeyCodes*>(reinterpret_cast<const char*>(sm_new[0]) + q4_piece(D) * L);
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-          if (t0 + 16 * u + 4 * L + r == own) {
-            x.kp[u][r] = sm_new[0][D / 8 + g];
-            x.vp[u][r] = sm_new[1][D / 8 + g];
-            x.v[u][r] = reinterpret_cast<const typename S::ValueCodes*>(sm_new[1])[i];
-          }
+          if (t0 + 16 * u + 4 * L + r == own) keys.pair[u][r] = sm_new[0][D / 8 + g];
       }
     }
     // scores: this lane keeps those of tokens 4 L + g + GR n, n < NS
@@ -482,14 +609,14 @@ template <typename T, int D, bool ONE> __global__ __launch_bounds__(kPagedThread
       f32x4 s = kZeroF4;
 #pragma unroll
       for (int t = 0; t < ST; ++t) {
-        const uint32_t even = x.k[u][t] & kNibbles, odd = x.k[u][t] >> 4 & kNibbles;
+        const uint32_t even = keys.codes[u][t] & kNibbles, odd = keys.codes[u][t] >> 4 & kNibbles;
         const bf16x8 codes = as_bf16x8(u32x4{codes_bf16(even, false), codes_bf16(even, true), codes_bf16(odd, false), codes_bf16(odd, true)});
 #pragma unroll
         for (int p = PARTS - 1; p >= 0; --p) s = mfma16(codes, q[p][t], s);
       }
       float y[4];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) y[r] = fmaf(bf16_lo(x.kp[u][r]), s[r], bf16_hi(x.kp[u][r]) * qsum);
+      for (int r = 0; r < 4; ++r) y[r] = fmaf(bf16_lo(keys.pair[u][r]), s[r], bf16_hi(keys.pair[u][r]) * qsum);
       // the groups' parts added up: of two tokens a lane keeps one and hands the other to the lane beside it
       const float first = (g & 1 ? y[1] : y[0]) + beside<1>(g & 1 ? y[0] : y[1]), second = (g & 1 ? y[3] : y[2]) + beside<1>(g & 1 ? y[2] : y[3]);
       if constexpr (GR == 4) {
@@ -498,6 +625,17 @@ template <typename T, int D, bool ONE> __global__ __launch_bounds__(kPagedThread
         w[u][0] = first * sc;
         w[u][1] = second * sc;
       }
+    }
+    if (t0 + step < to) load_keys(keys, next, t0 + step);
+    if (has_own) {
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (t0 + 16 * u + 4 * L + r == own) {
+            x.pair[u][r] = sm_new[1][D / 8 + g];
+            x.codes[u][r] = reinterpret_cast<const ValueCodes*>(sm_new[1])[i];
+          }
     }
     if (!whole) {
       // what is not there gets no weight, and its values, which may be anything, become zero
@@ -508,7 +646,7 @@ template <typename T, int D, bool ONE> __global__ __launch_bounds__(kPagedThread
           if (!(in[u] >> (4 * L + g + GR * n) & 1u)) w[u][n] = -INFINITY;
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-          if (!(in[u] >> (4 * L + r) & 1u)) x.vp[u][r] = 0u;
+          if (!(in[u] >> (4 * L + r) & 1u)) x.pair[u][r] = 0u;
       }
     }
     float top = -INFINITY;
@@ -542,8 +680,8 @@ template <typename T, int D, bool ONE> __global__ __launch_bounds__(kPagedThread
 #pragma unroll
         for (int z = 0; z < 2; ++z) {
           const float p = of_group<GR>(w[u][(r + z) / GR], (r + z) % GR);
-          low = fmaf(p, bf16_hi(x.vp[u][r + z]), low);
-          y[z] = p * bf16_lo(x.vp[u][r + z]);
+          low = fmaf(p, bf16_hi(x.pair[u][r + z]), low);
+          y[z] = p * bf16_lo(x.pair[u][r + z]);
         }
         uint32_t z[WPARTS];
         parts_of(z, y[0], y[1]);
@@ -558,7 +696,7 @@ template <typename T, int D, bool ONE> __global__ __launch_bounds__(kPagedThread
       uint32_t two[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        two[j] = __builtin_amdgcn_perm(x.v[j / 2][2 * (j % 2) + 1], x.v[j / 2][2 * (j % 2)], half ? 0x07030602u : 0x05010400u);
+        two[j] = __builtin_amdgcn_perm(x.codes[j / 2][2 * (j % 2) + 1], x.codes[j / 2][2 * (j % 2)], half ? 0x07030602u : 0x05010400u);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         u32x4 codes;
@@ -571,6 +709,7 @@ template <typename T, int D, bool ONE> __global__ __launch_bounds__(kPagedThread
       }
     }
     here = next;
+    next = later;
   }
   l += beside<1>(l);
   if (GR == 4) l += beside<2>(l);
@@ -588,7 +727,7 @@ template <typename T, int D, bool ONE> __global__ __launch_bounds__(kPagedThread
 #pragma unroll
       for (int r = 0; r < 4; ++r) sm_o[wave][h][E * (4 * L + r) + e] = o[e][r] + low;
   }
-  __syncthreads();
+  lds_barrier();
   const int c = tid % D;
   for (int x = tid / D; x < heads; x += kPagedThreads / D) {
     float top = -INFINITY, sum = 0.f, acc = 0.f;
@@ -601,10 +740,10 @@ template <typename T, int D, bool ONE> __global__ __launch_bounds__(kPagedThread
       sum = fmaf(sm_l[y][x], by, sum);
       acc = fmaf(sm_o[y][x][c], by, acc);
     }
-    if (a.splits == 1) {
+    if (whole_sequence) {
       Storage<T>::store(rows_of<T>(a.out, a.os, b, h0 + x), c, sum == 0.f ? 0.f : acc / sum);
     } else {
-      const int64_t at = ((int64_t)b * a.H + h0 + x) * a.splits + split;
+      const int64_t at = (int64_t)(part + b) * a.H + h0 + x;
       a.sums[at * D + c] = acc;
       if (c == 0) {
         a.stats[2 * at] = top;
@@ -612,20 +751,68 @@ template <typename T, int D, bool ONE> __global__ __launch_bounds__(kPagedThread
       }
     }
   }
+  lds_barrier();   // the next sequence's sums go to the same places
+  }
 }
 
-// Workgroups of an uncut call.
-int64_t decode_units(int B, int H, int Hkv, int d) {
-  const int hc = q4_heads(d);
-  return (int64_t)B * Hkv * (((int64_t)H / Hkv + hc - 1) / hc);
+// Joins the pieces of a sequence that is cut in front of part blockIdx.x / ceil(H / kWaves) + 1, if that is its first cut: a wave for each
+// head, which takes the statistics of 64 pieces at once and their sums one after another.
+template <typename T, int D> __global__ __launch_bounds__(kPagedThreads) void q4_join_kernel(PagedDecodeArgs a) {
+  constexpr int N = D / 64;   // columns of a lane
+  typedef float Columns __attribute__((ext_vector_type(N)));
+  const int lane = threadIdx.x & 63, sets = (a.H + kWaves - 1) / kWaves;
+  const int h = blockIdx.x % sets * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), part = blockIdx.x / sets + 1;
+  const Cut cut = cut_at(a, part, lane);
+  const int first = cut.base + kSetUp;   // its first block
+  if (h >= a.H || part >= cut.parts || first >= first_unit(part, cut.parts, cut.total) || first < first_unit(part - 1, cut.parts, cut.total))
+    return;
+  const int n = cut.seen(a, cut.b);
+  const int pieces = part_of(cut.base + units_of(n) - 1, cut.parts, cut.total) - (part - 1) + 1;
+  const int64_t at = (int64_t)(part - 1 + cut.b) * a.H + h;   // the first one; the next are H rows on each
+  float top = -INFINITY, sum = 0.f;
+  Columns acc = {};
+  for (int s0 = 0; s0 < pieces; s0 += 64) {
+    const int here = min(64, pieces - s0);
+    float m = -INFINITY, l = 0.f;
+    if (lane < here) {
+      m = a.stats[2 * (at + (int64_t)(s0 + lane) * a.H)];
+      l = a.stats[2 * (at + (int64_t)(s0 + lane) * a.H) + 1];
+    }
+    Columns x[8];
+    auto load = [&](int s) {   // set out beside the statistics
+#pragma unroll
+      for (int y = 0; y < 8; ++y)
+        x[y] = s + y < here ? *reinterpret_cast<const Columns*>(a.sums + (at + (int64_t)(s0 + s + y) * a.H) * D + N * lane) : Columns{};
+    };
+    load(0);
+    const float up = fmaxf(top, over_lanes<true>(m));
+    const float ref = up == -INFINITY ? 0.f : up, keep = __builtin_amdgcn_exp2f(top - ref), by = __builtin_amdgcn_exp2f(m - ref);
+    top = up;
+    acc *= keep;
+    sum = fmaf(sum, keep, over_lanes<false>(l * by));
+    for (int s = 0;;) {
+#pragma unroll
+      for (int y = 0; y < 8; ++y) acc += x[y] * __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(by), min(s + y, 63)));
+      s += 8;
+      if (s >= here) break;
+      load(s);
+    }
+  }
+#pragma unroll
+  for (int x = 0; x < N; ++x) Storage<T>::store(rows_of<T>(a.out, a.os, cut.b, h), N * lane + x, sum == 0.f ? 0.f : acc[x] / sum);
 }
+
+// Workgroups of a part: one for the query heads that fit its columns.
+int64_t decode_units(int H, int Hkv, int d) { return (int64_t)Hkv * ((H / Hkv + q4_heads(d) - 1) / q4_heads(d)); }
 
 template <typename T, int D> hipError_t decode(const PagedDecodeArgs& a, hipStream_t s) {
-  const unsigned workgroups = (unsigned)(decode_units(a.B, a.H, a.Hkv, D) * a.splits);
-  if (a.shift >= 4) q4_decode_kernel<T, D, true><<<dim3(workgroups), dim3(kPagedThreads), 0, s>>>(a);
-  else q4_decode_kernel<T, D, false><<<dim3(workgroups), dim3(kPagedThreads), 0, s>>>(a);
+  const dim3 grid((unsigned)(decode_units(a.H, a.Hkv, D) * a.splits));
+  if (a.shift >= 4) q4_decode_kernel<T, D, true><<<grid, dim3(kPagedThreads), 0, s>>>(a);
+  else q4_decode_kernel<T, D, false><<<grid, dim3(kPagedThreads), 0, s>>>(a);
   const hipError_t e = hipGetLastError();
-  return e != hipSuccess || a.splits == 1 ? e : launch_paged_join(a, sizeof(T) == 2, s);
+  if (e != hipSuccess || a.splits == 1) return e;
+  q4_join_kernel<T, D><<<dim3((unsigned)(a.splits - 1) * ((a.H + kWaves - 1) / kWaves)), dim3(kPagedThreads), 0, s>>>(a);
+  return hipGetLastError();
 }
 
 int64_t row_groups(int total, int n_seqs, int Hkv, int d) {
@@ -634,17 +821,14 @@ int64_t row_groups(int total, int n_seqs, int Hkv, int d) {
 
 }  // namespace
 
-PagedSplit paged_q4_split(int B, int H, int Hkv, int d, int64_t max_len) {
-  constexpr int64_t kWorkgroups = 1536;
-  const int64_t units = decode_units(B, H, Hkv, d);
-  const int64_t share = units < kWorkgroups ? (max_len * units + kWorkgroups - 1) / kWorkgroups : max_len;
-  const int64_t chunk = std::max<int64_t>(128, (share + 63) / 64 * 64);
-  return {(int)chunk, (int)std::max<int64_t>(1, (max_len + chunk - 1) / chunk)};
+// Four workgroups for every compute unit, as many as run there at once, and no part without a block if all sequences are the longest.
+int paged_q4_parts(int B, int H, int Hkv, int d, int64_t max_len) {
+  constexpr int64_t kWorkgroups = 768;
+  return (int)std::max<int64_t>(1, std::min(kWorkgroups / decode_units(H, Hkv, d), B * (kSetUp + blocks_of(max_len))));
 }
-
-bool paged_q4_decode_fits(int B, int H, int Hkv, int d, PagedSplit s) {
-  return decode_units(B, H, Hkv, d) * s.splits <= most_workgroups(kPagedThreads) &&
-         (s.splits == 1 || (int64_t)B * H <= most_workgroups(kPagedThreads));
+bool paged_q4_decode_fits(int B, int H, int Hkv, int d, int64_t max_len) {
+  return decode_units(H, Hkv, d) * paged_q4_parts(B, H, Hkv, d, max_len) <= most_workgroups(kPagedThreads) &&
+         B * (kSetUp + blocks_of(max_len)) < (1ll << 31);   // units are counted in 32 bits
 }
 bool paged_q4_rows_fit(int total, int n_seqs, int Hkv, int d) { return row_groups(total, n_seqs, Hkv, d) <= most_workgroups(kPagedThreads); }
 

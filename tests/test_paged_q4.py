@@ -329,6 +329,16 @@ def test_decode_cut_along_its_length(dtype, H, Hkv, d, page, lens):
 
 
 @gpu
+@pytest.mark.parametrize("B,H,Hkv,d,most", [(64, 4, 4, 64, 40), (65, 2, 1, 128, 300), (150, 8, 8, 64, 20), (333, 1, 1, 64, 700), (700, 2, 2, 128, 12)])
+def test_decode_of_many_sequences(B, H, Hkv, d, most):
+    """Shares of the work that hold several sequences, and sequences that lie in several shares, idle ones among them."""
+    gen = torch.Generator().manual_seed(B)
+    lens = torch.randint(-2, most, (B,), generator=gen).tolist()
+    lens[B // 2] = 8 * most
+    check_step("bf16", 16, *step(gen, "bf16", H, Hkv, d, 16, lens))
+
+
+@gpu
 def test_decode_keeps_large_offsets_of_values_and_keys():
     # groups whose values lie far from zero, close together
     gen = torch.Generator().manual_seed(8)
@@ -368,6 +378,22 @@ def test_what_is_no_number_stays_where_it_is_seen(dtype):
     want[:] = False
     want[2, :4, :32] = True
     assert torch.equal(torch.isnan(out).cpu(), want) and bool((out[:2] == 0).all())
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_read_of_more_than_the_last_cache_holds(dtype):
+    gen = torch.Generator().manual_seed(5)
+    T, Hkv, d, page = ref.TYPES[dtype], 16, 128, 64
+    n = (300 << 20) // (2 * Hkv * d * (2 if dtype == "bf16" else 4)) + 5
+    kp, vp = sound_pages(gen, 3, Hkv, page, d), sound_pages(gen, 3, Hkv, page, d)
+    table = torch.randint(0, 3, (1, -(-n // page)), generator=gen).to(torch.int32)
+    ko, vo = (torch.zeros(n, Hkv, d, dtype=T, device="cuda") for _ in range(2))
+    gb.gformer_paged_read_q4(kp, vp, ko, vo, table.cuda(), ints(0), ints(0, n))
+    for got, pages in ((ko, kp), (vo, vp)):
+        held = ref.values(pages).float().to(T).cuda().transpose(1, 2)         # [pages, tokens, heads, d]
+        want = held[table[0].long().cuda()].flatten(0, 1)[:n]
+        assert torch.equal(got, want)
 
 
 @gpu
