@@ -117,10 +117,10 @@ struct DecodePlan {
   int64_t rows;
   PagedSplit split;
 };
-DecodePlan plan_of(bool q4, int B, int H, int Hkv, int d, int room) {
+DecodePlan plan_of(bool q4, int dtype, int B, int H, int Hkv, int d, int room) {
   if (q4) {
-    const int parts = paged_q4_parts(B, H, Hkv, d, room);
-    return {parts == 1 ? 1 : (int64_t)parts + B, {0, parts}};
+    const int parts = paged_q4_parts(dtype == GF_BF16, B, H, Hkv, d, room);
+    return {parts == 1 || !paged_q4_cuts(room) ? 1 : (int64_t)parts + B, {0, parts}};
   }
   const PagedSplit s = paged_split(B, H, Hkv, room);
   return {s.splits == 1 ? 1 : (int64_t)B * s.splits, s};
@@ -139,7 +139,7 @@ size_t decode_workspace(bool q4, int B, int H, int Hkv, int d, int table_width, 
   if (!p || B < 1 || check_heads(p->dtype, H, Hkv, d) != GF_OK || check_paged(Hkv, d, 1, p, &shift, kps, vps, q4) != GF_OK ||
       check_table(table_width, shift, max_len, &room) != GF_OK)
     return 0;
-  return decode_bytes(plan_of(q4, B, H, Hkv, d, room), H, d);
+  return decode_bytes(plan_of(q4, p->dtype, B, H, Hkv, d, room), H, d);
 }
 
 gf_status decode_step(bool q4, const void* q, const void* k, const void* v, void* out, void* kpages, void* vpages,
@@ -158,8 +158,8 @@ gf_status decode_step(bool q4, const void* q, const void* k, const void* v, void
       (st = strides2(p->v_stride, a.vs, Hkv, d)) != GF_OK || (st = strides2(p->o_stride, a.os, H, d)) != GF_OK)
     return st;
   if (B == 0) return GF_OK;
-  const DecodePlan plan = plan_of(q4, B, H, Hkv, d, a.room);
-  if (!(q4 ? paged_q4_decode_fits(B, H, Hkv, d, a.room) : paged_decode_fits(B, H, Hkv, plan.split))) return GF_ERR_UNSUPPORTED;
+  const DecodePlan plan = plan_of(q4, p->dtype, B, H, Hkv, d, a.room);
+  if (!(q4 ? paged_q4_decode_fits(p->dtype == GF_BF16, B, H, Hkv, d, a.room) : paged_decode_fits(B, H, Hkv, plan.split))) return GF_ERR_UNSUPPORTED;
   if (n_pages < 1) return GF_ERR_INVALID_ARG;
   if (!q || !out || !kpages || !vpages || (!table && table_width > 0) || !lens || !k != !v) return GF_ERR_INVALID_ARG;
   if (misaligned(bits(q, k, v, out, kpages, vpages), 16) || misaligned(bits(table, lens), 4)) return GF_ERR_INVALID_ARG;

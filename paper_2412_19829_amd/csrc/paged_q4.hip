@@ -8,6 +8,9 @@
 // which leaves them in every one of them, and there a weight takes its own group's scale for the second product, whose rows (channels) count
 // in their own group's columns alone.  16 columns are 4 heads of 128 channels, or 8 of 64.
 // A code becomes an operand by way of fp8: the byte n is n 2^-9 for n < 16, two of which one instruction converts.
+// Memory bounds it up to 4 query heads of 128 channels a key head (8 of 64), beyond that the vector instructions, which every further 4 (8) take
+// again.  us, kernel alone: 220,039 keys of 8 sequences, 32 / 8 heads, d = 128, bf16 (282 MB) 55.3, 5.1 TB/s; 88,074 in 32 ragged ones
+// (114 MB) 27.7; six fp32 sequences of 10,167 in all, 16 heads, d = 64 11.4; one of 2047, 12 heads, d = 64 6.4, and 4.8 to join.
 #include "paged_q4.hpp"
 
 #include "f32_mfma.hpp"
@@ -332,6 +335,11 @@ template <int D> struct Shape4 {
   typedef typename std::conditional<D == 128, u32x4, u32x2>::type KeyCodes;
   typedef typename std::conditional<D == 128, uint32_t, uint16_t>::type ValueCodes;
 };
+// Whether the next tile's keys are loaded ahead, and the workgroups that a compute unit runs at once, by the registers that the sums and queries
+// take.  us: 8 x 16000 tokens, 32 / 8 heads, d = 128, bf16 40.8 ahead with three, 50.9 without and with four (spilled); 8 x 16000, 16 heads,
+// d = 64 52.8 ahead and 49.8 without, with four; 57.7 with five (spilled).  fp32, d = 128 47.9 with two, 57.5 with three.
+template <int D> constexpr bool kAhead = D == 128;
+template <typename T, int D> constexpr int kAtOnce = sizeof(T) == 2 ? (D == 128 ? 3 : 4) : (D == 128 ? 2 : 3);
 constexpr int q4_heads(int d) { return d == 128 ? Shape4<128>::HC : Shape4<64>::HC; }
 
 // Parts in bf16 that a factor of the products is taken in.  Queries: bf16 is one, fp32 the three that hold its 24 bits.  Weights times scales: two
@@ -414,375 +422,393 @@ __device__ __forceinline__ Cut cut_at(const PagedDecodeArgs& a, int part, int la
 }
 
 // ONE: a page holds whole tiles of 16 keys (pages of 8 tokens do not), so that their pages and addresses are the same for all lanes, which
-// then add nothing but a fixed offset to them: 572 vector instructions a tile of 32 keys, d = 128, with addresses of their own, 379 without.
-template <typename T, int D, bool ONE> __global__ __launch_bounds__(kPagedThreads, sizeof(T) == 2 ? 3 : 2) void q4_decode_kernel(PagedDecodeArgs a) {
+// then add nothing but a fixed offset to them: with addresses of their own they took 193 of 572 vector instructions a tile of 32 keys, d = 128
+// (355 are left).
+template <typename T, int D, bool ONE> __global__ __launch_bounds__(kPagedThreads, (kAtOnce<T, D>)) void q4_decode_kernel(PagedDecodeArgs a) {
   using S = Shape4<D>;
   typedef typename S::KeyCodes KeyCodes;
   typedef typename S::ValueCodes ValueCodes;
   constexpr int GR = S::GR, HC = S::HC, ST = S::ST, E = S::E, PARTS = kQueryParts<T>, WPARTS = kWeightParts<T>, ROW = q4_row(D), U = 2, R = 16 * U, NS = 4 / GR;
+  constexpr bool AHEAD = kAhead<D>;
   __shared__ float sm_o[kWaves][HC][D + 4], sm_m[kWaves][HC], sm_l[kWaves][HC];
   __shared__ __align__(16) uint32_t sm_new[2][ROW / 4];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, L = lane >> 4;
   const int G = a.H / a.Hkv, tiles = (G + HC - 1) / HC;
-  const int tile = blockIdx.x % tiles, kvh = blockIdx.x / tiles % a.Hkv, part = blockIdx.x / (tiles * a.Hkv);
+  // workgroups that read the same rows for other query heads are eight apart: on one XCD
+  const int work = a.Hkv * a.splits, even = work / 8 * 8 * tiles, id = blockIdx.x;
+  const int tile = id < even ? id / 8 % tiles : (id - even) % tiles, w = id < even ? id / (8 * tiles) * 8 + id % 8 : work / 8 * 8 + (id - even) / tiles;
+  const int kvh = w % a.Hkv, part = w / a.Hkv;
   const int h0 = kvh * G + tile * HC, heads = min(G - tile * HC, HC);
-  Cut cut = cut_at(a, part, lane);
-  if (part >= cut.parts) return;
-  int unit = first_unit(part, cut.parts, cut.total);
-  const int last_unit = first_unit(part + 1, cut.parts, cut.total);
+  Cut cut;
+  int unit, last_unit;
+  if (!a.stats && a.splits == a.B) {   // a sequence each
+    cut = {0, 0, part, 0, 0, 0, 0};
+    unit = 0;
+    last_unit = kSetUp + 1;
+  } else {
+    cut = cut_at(a, part, lane);
+    if (part >= cut.parts) return;
+    unit = first_unit(part, cut.parts, cut.total);
+    last_unit = first_unit(part + 1, cut.parts, cut.total);
+  }
   const char* kc = reinterpret_cast<const char*>(a.kpages) + kvh * a.kps[1];
   const char* vc = reinterpret_cast<const char*>(a.vpages) + kvh * a.vps[1];
   const int in_page = (1 << a.shift) - 1;
 
   // a part that ends while it sets a sequence up leaves it to the next one
   while (cut.base + kSetUp < last_unit) {
-  const int b = cut.b, n = cut.seen(a, b), first = cut.base + kSetUp;
-  const int from = max(unit - first, 0) * kBlock, to = (int)min((int64_t)n, (int64_t)(last_unit - first) * kBlock);
-  const bool whole_sequence = unit <= first && last_unit - cut.base >= units_of(n);
-  unit = cut.base += units_of(n);
-  ++cut.b;
-  const int own = a.k && n > 0 ? n - 1 : -1;   // the new token's position
-  const int32_t* table = a.table + (int64_t)b * a.width;
+    const int b = cut.b, n = cut.seen(a, b), first = cut.base + kSetUp;
+    const int from = max(unit - first, 0) * kBlock, to = (int)min((int64_t)n, (int64_t)(last_unit - first) * kBlock);   // at most 2^30
+    const bool whole_sequence = unit <= first && last_unit - cut.base >= units_of(n);
+    unit = cut.base += units_of(n);
+    ++cut.b;
+    const int own = a.k && n > 0 ? n - 1 : -1;   // the new token's position
+    const int32_t* table = a.table + (int64_t)b * a.width;
 
-  // pages of the tile at t0: of its 16-key parts, or of the key that this lane loads and of its four value rows
-  struct Pages { int k[U], v[U]; };
-  auto page_of = [&](int token) { return token < to ? table[token >> a.shift] : -1; };
-  auto pages = [&](int t0) {
-    Pages p;
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      p.k[u] = page_of(t0 + 16 * u + (ONE ? 0 : i));
-      p.v[u] = ONE ? 0 : page_of(t0 + 16 * u + 4 * L);
-    }
-    return p;
-  };
-  auto there = [&](int page) { return (unsigned)page < (unsigned)a.n_pages; };
-  // Everything that the first tile waits for sets out at once.  Pages are looked up two tiles ahead.
-  const int step = kWaves * R;
-  int t0 = from + wave * R;
-  Pages here = pages(t0), next = pages(t0 + step);
-  // column i: query head i / GR, group i % GR
-  const int h = i / GR, g = i % GR, mine = L * GR / 4;   // mine: the group of this lane's channels
-  Eight<T> raw[ST];
-#pragma unroll
-  for (int t = 0; t < ST; ++t) {
-    raw[t] = {};
-    if (h < heads && g == mine) raw[t].get(rows_of<T>(a.q, a.qs, b, h0 + h) + D / 4 * L + 8 * t);
-  }
-  const bool brings_own = own >= from && own < to, my_own = brings_own && wave < 2 && lane < D / 8;
-  Eight<T> fresh = {};
-  int own_page = -1;
-  if (my_own) {
-    fresh.get((wave == 0 ? rows_of<T>(a.k, a.ks, b, kvh) : rows_of<T>(a.v, a.vs, b, kvh)) + 8 * lane);
-    own_page = table[own >> a.shift];
-  }
-
-  // rows that are not there are read from page 0: in bounds, and masked
-  const uint32_t k_codes = (uint32_t)(i * a.kps[2]) + q4_piece(D) * L, k_pairs = (uint32_t)(4 * L * a.kps[2]) + D / 2 + 4 * g;
-  const uint32_t v_codes = (uint32_t)(4 * L * a.vps[2]) + (uint32_t)sizeof(ValueCodes) * i, v_pairs = (uint32_t)(4 * L * a.vps[2]) + D / 2 + 4 * g;
-  auto row_at = [&](const char* pages, const int64_t (&st)[3], int page, int token) {
-    return pages + (there(page) ? page * st[0] + (token & in_page) * st[2] : 0);
-  };
-  struct Keys {
-    KeyCodes codes[U];
-    uint32_t pair[U][4];     // of tokens 4 L + r
-  };
-  auto load_keys = [&](Keys& x, const Pages& p, int t0) {
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if constexpr (ONE) {
-        // opaque here, or their extensions to 64 bits leave the loop and take a vector addition each
-        uint32_t codes = k_codes, pairs = k_pairs;
-        asm volatile("" : "+v"(codes), "+v"(pairs));
-        const char* at = row_at(kc, a.kps, p.k[u], t0 + 16 * u);
-        x.codes[u] = *reinterpret_cast<const KeyCodes*>(at + codes);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) x.pair[u][r] = *reinterpret_cast<const uint32_t*>(at + r * a.kps[2] + pairs);
-      } else {
-        x.codes[u] = *reinterpret_cast<const KeyCodes*>(row_at(kc, a.kps, p.k[u], t0 + 16 * u + i) + q4_piece(D) * L);
-        const char* at = row_at(kc, a.kps, p.v[u], t0 + 16 * u + 4 * L);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) x.pair[u][r] = reinterpret_cast<const uint32_t*>(at + r * a.kps[2])[D / 8 + g];
-      }
-    }
-  };
-  struct Values {
-    uint32_t codes[U][4], pair[U][4];
-  };
-  auto load_values = [&](Values& x, const Pages& p, int t0) {
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      uint32_t codes = v_codes, pairs = v_pairs;
-      if (ONE) asm volatile("" : "+v"(codes), "+v"(pairs));
-      const char* at = ONE ? row_at(vc, a.vps, p.k[u], t0 + 16 * u) : row_at(vc, a.vps, p.v[u], t0 + 16 * u + 4 * L) - 4 * L * a.vps[2];
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        x.pair[u][r] = *reinterpret_cast<const uint32_t*>(at + r * a.vps[2] + pairs);
-        x.codes[u][r] = *reinterpret_cast<const ValueCodes*>(at + r * a.vps[2] + codes);
-      }
-    }
-  };
-
-  auto settle = [&](Pages& p) {
-    if (ONE) {
-#pragma unroll
-      for (int u = 0; u < U; ++u) p.k[u] = __builtin_amdgcn_readfirstlane(p.k[u]);
-    }
-  };
-  settle(here);
-  Keys keys;
-  load_keys(keys, here, t0);
-
-  // the new token's row, for its slot and for the tile that sees it: nobody reads the slot in this call
-  if (brings_own) {
-    if (my_own) {
-      float x[8];
-      fresh.values(x);
-      const Codes y = quantised<T>(x);
-      put_codes<D>(sm_new[wave], lane, y);
-      if (tile == 0 && there(own_page)) {
-        char* row = wave == 0 ? reinterpret_cast<char*>(a.kpages) + own_page * a.kps[0] + kvh * a.kps[1] + (own & in_page) * a.kps[2]
-                              : reinterpret_cast<char*>(a.vpages) + own_page * a.vps[0] + kvh * a.vps[1] + (own & in_page) * a.vps[2];
-        put_codes<D>(reinterpret_cast<uint32_t*>(row), lane, y);
-      }
-    }
-    lds_barrier();
-  }
-
-  bf16x8 q[PARTS][ST];
-  float qsum = 0.f;
-#pragma unroll
-  for (int t = 0; t < ST; ++t) {
-    float x[8];
-    raw[t].values(x);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) qsum += x[e];
-    u32x4 w[PARTS];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int e = j < 2 ? 4 * j : 4 * j - 7;   // the order that codes_bf16 leaves them in: 0 2 4 6 1 3 5 7
-      uint32_t y[PARTS];
-      parts_of(y, x[e], x[e + 2]);
-#pragma unroll
-      for (int p = 0; p < PARTS; ++p) w[p][j] = y[p];
-    }
-#pragma unroll
-    for (int p = 0; p < PARTS; ++p) q[p][t] = as_bf16x8(w[p]);
-  }
-  qsum = sum_over_groups(qsum);
-  const float sc = a.scale * kLog2e;
-  f32x4 o[E];
-#pragma unroll
-  for (int e = 0; e < E; ++e) o[e] = kZeroF4;
-  float m = -INFINITY, l = 0.f, low = 0.f;
-
-  // A tile's values are on their way while its scores are taken, the next tile's keys, in the registers of this one's, from then on.
-  for (; t0 < to; t0 += step) {
-    Values x;
-    load_values(x, here, t0);
-    settle(next);
-    const Pages later = pages(t0 + 2 * step);
-    const bool has_own = (unsigned)(own - t0) < (unsigned)R;   // this tile holds the new token
-    if (has_own) {
+    // pages of the tile at t0: of its 16-key parts, or of the key that this lane loads and of its four value rows
+    struct Pages { int k[U], v[U]; };
+    auto page_of = [&](int token) { return token < to ? table[token >> a.shift] : -1; };
+    auto pages = [&](int t0) {
+      Pages p;
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        if (t0 + 16 * u + i == own) keys.codes[u] = *reinterpret_cast<const KeyCodes*>(reinterpret_cast<const char*>(sm_new[0]) + q4_piece(D) * L);
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if (t0 + 16 * u + 4 * L + r == own) keys.pair[u][r] = sm_new[0][D / 8 + g];
+        p.k[u] = page_of(t0 + 16 * u + (ONE ? 0 : i));
+        p.v[u] = ONE ? 0 : page_of(t0 + 16 * u + 4 * L);
       }
-    }
-    // scores: this lane keeps those of tokens 4 L + g + GR n, n < NS
-    float w[U][NS];
-    uint32_t in[U];
-    bool whole = true;
+      return p;
+    };
+    auto there = [&](int page) { return (unsigned)page < (unsigned)a.n_pages; };
+    // Everything that the first tile waits for sets out at once.  Pages are looked up two tiles ahead.
+    const int step = kWaves * R;
+    int t0 = from + wave * R;
+    Pages here = pages(t0), next = pages(t0 + step);
+    // column i: query head i / GR, group i % GR
+    const int h = i / GR, g = i % GR, mine = L * GR / 4;   // mine: the group of this lane's channels
+    Eight<T> raw[ST];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int key = t0 + 16 * u + i;
+    for (int t = 0; t < ST; ++t) {
+      raw[t] = {};
+      if (h < heads && g == mine) raw[t].get(rows_of<T>(a.q, a.qs, b, h0 + h) + D / 4 * L + 8 * t);
+    }
+    const bool brings_own = own >= from && own < to, my_own = brings_own && wave < 2 && lane < D / 8;
+    Eight<T> fresh = {};
+    int own_page = -1;
+    if (my_own) {
+      fresh.get((wave == 0 ? rows_of<T>(a.k, a.ks, b, kvh) : rows_of<T>(a.v, a.vs, b, kvh)) + 8 * lane);
+      own_page = table[own >> a.shift];
+    }
+
+    // rows that are not there are read from page 0: in bounds, and masked
+    const uint32_t k_codes = (uint32_t)(i * a.kps[2]) + q4_piece(D) * L, k_pairs = (uint32_t)(4 * L * a.kps[2]) + D / 2 + 4 * g;
+    const uint32_t v_codes = (uint32_t)(4 * L * a.vps[2]) + (uint32_t)sizeof(ValueCodes) * i, v_pairs = (uint32_t)(4 * L * a.vps[2]) + D / 2 + 4 * g;
+    auto row_at = [&](const char* pages, const int64_t (&st)[3], int page, int token) {
+      return pages + (there(page) ? page * st[0] + (token & in_page) * st[2] : 0);
+    };
+    struct Keys {
+      KeyCodes codes[U];
+      uint32_t pair[U][4];     // of tokens 4 L + r
+    };
+    auto load_keys = [&](Keys& x, const Pages& p, int t0) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if constexpr (ONE) {
+          // opaque here, or their extensions to 64 bits leave the loop and take a vector addition each
+          uint32_t codes = k_codes, pairs = k_pairs;
+          asm volatile("" : "+v"(codes), "+v"(pairs));
+          const char* at = row_at(kc, a.kps, p.k[u], t0 + 16 * u);
+          x.codes[u] = *reinterpret_cast<const KeyCodes*>(at + codes);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) x.pair[u][r] = *reinterpret_cast<const uint32_t*>(at + r * a.kps[2] + pairs);
+        } else {
+          x.codes[u] = *reinterpret_cast<const KeyCodes*>(row_at(kc, a.kps, p.k[u], t0 + 16 * u + i) + q4_piece(D) * L);
+          const char* at = row_at(kc, a.kps, p.v[u], t0 + 16 * u + 4 * L);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) x.pair[u][r] = reinterpret_cast<const uint32_t*>(at + r * a.kps[2])[D / 8 + g];
+        }
+      }
+    };
+    struct Values {
+      uint32_t codes[U][4], pair[U][4];
+    };
+    auto load_values = [&](Values& x, const Pages& p, int t0) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        uint32_t codes = v_codes, pairs = v_pairs;
+        if (ONE) asm volatile("" : "+v"(codes), "+v"(pairs));
+        const char* at = ONE ? row_at(vc, a.vps, p.k[u], t0 + 16 * u) : row_at(vc, a.vps, p.v[u], t0 + 16 * u + 4 * L) - 4 * L * a.vps[2];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          x.pair[u][r] = *reinterpret_cast<const uint32_t*>(at + r * a.vps[2] + pairs);
+          x.codes[u][r] = *reinterpret_cast<const ValueCodes*>(at + r * a.vps[2] + codes);
+        }
+      }
+    };
+
+    auto settle = [&](Pages& p) {
       if (ONE) {
-        const int left = min(max(to - t0 - 16 * u, 0), 16), mine_at = own - t0 - 16 * u;
-        in[u] = (there(here.k[u]) ? (1u << left) - 1u : 0u) | ((unsigned)mine_at < 16u ? 1u << mine_at : 0u);
-      } else {
-        in[u] = (uint32_t)__builtin_amdgcn_ballot_w64(key < to && (there(here.k[u]) || key == own)) & 0xffffu;
-      }
-      whole = whole && in[u] == 0xffffu;
-      f32x4 s = kZeroF4;
 #pragma unroll
-      for (int t = 0; t < ST; ++t) {
-        const uint32_t even = keys.codes[u][t] & kNibbles, odd = keys.codes[u][t] >> 4 & kNibbles;
-        const bf16x8 codes = as_bf16x8(u32x4{codes_bf16(even, false), codes_bf16(even, true), codes_bf16(odd, false), codes_bf16(odd, true)});
-#pragma unroll
-        for (int p = PARTS - 1; p >= 0; --p) s = mfma16(codes, q[p][t], s);
+        for (int u = 0; u < U; ++u) p.k[u] = __builtin_amdgcn_readfirstlane(p.k[u]);
       }
-      float y[4];
-#pragma unroll
-      for (int r = 0; r < 4; ++r) y[r] = fmaf(bf16_lo(keys.pair[u][r]), s[r], bf16_hi(keys.pair[u][r]) * qsum);
-      // the groups' parts added up: of two tokens a lane keeps one and hands the other to the lane beside it
-      const float first = (g & 1 ? y[1] : y[0]) + beside<1>(g & 1 ? y[0] : y[1]), second = (g & 1 ? y[3] : y[2]) + beside<1>(g & 1 ? y[2] : y[3]);
-      if constexpr (GR == 4) {
-        w[u][0] = ((g & 2 ? second : first) + beside<2>(g & 2 ? first : second)) * sc;
-      } else {
-        w[u][0] = first * sc;
-        w[u][1] = second * sc;
+    };
+    settle(here);
+    Keys keys;
+    if (AHEAD) load_keys(keys, here, t0);
+
+    // the new token's row, for its slot and for the tile that sees it: nobody reads the slot in this call
+    if (brings_own) {
+      if (my_own) {
+        float x[8];
+        fresh.values(x);
+        const Codes y = quantised<T>(x);
+        put_codes<D>(sm_new[wave], lane, y);
+        if (tile == 0 && there(own_page)) {
+          char* row = wave == 0 ? reinterpret_cast<char*>(a.kpages) + own_page * a.kps[0] + kvh * a.kps[1] + (own & in_page) * a.kps[2]
+                                : reinterpret_cast<char*>(a.vpages) + own_page * a.vps[0] + kvh * a.vps[1] + (own & in_page) * a.vps[2];
+          put_codes<D>(reinterpret_cast<uint32_t*>(row), lane, y);
+        }
       }
+      lds_barrier();
     }
-    if (t0 + step < to) load_keys(keys, next, t0 + step);
-    if (has_own) {
+
+    bf16x8 q[PARTS][ST];
+    float qsum = 0.f;
+#pragma unroll
+    for (int t = 0; t < ST; ++t) {
+      float x[8];
+      raw[t].values(x);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) qsum += x[e];
+      u32x4 w[PARTS];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int e = j < 2 ? 4 * j : 4 * j - 7;   // the order that codes_bf16 leaves them in: 0 2 4 6 1 3 5 7
+        uint32_t y[PARTS];
+        parts_of(y, x[e], x[e + 2]);
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) w[p][j] = y[p];
+      }
+#pragma unroll
+      for (int p = 0; p < PARTS; ++p) q[p][t] = as_bf16x8(w[p]);
+    }
+    qsum = sum_over_groups(qsum);
+    const float sc = a.scale * kLog2e;
+    f32x4 o[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = kZeroF4;
+    float m = -INFINITY, l = 0.f, low = 0.f;
+
+    // A tile's values are on their way while its scores are taken, the next tile's keys, in the registers of this one's, from then on.
+    for (; t0 < to; t0 += step) {
+      Values x;
+      if (!AHEAD) load_keys(keys, here, t0);
+      load_values(x, here, t0);
+      settle(next);
+      const Pages later = pages(t0 + 2 * step);
+      const bool has_own = (unsigned)(own - t0) < (unsigned)R;   // this tile holds the new token
+      if (has_own) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          if (t0 + 16 * u + i == own) keys.codes[u] = *reinterpret_cast<const KeyCodes*>(reinterpret_cast<const char*>(sm_new[0]) + q4_piece(D) * L);
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (t0 + 16 * u + 4 * L + r == own) keys.pair[u][r] = sm_new[0][D / 8 + g];
+        }
+      }
+      // scores: this lane keeps those of tokens 4 L + g + GR n, n < NS
+      float w[U][NS];
+      uint32_t in[U];
+      bool whole = true;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int key = t0 + 16 * u + i;
+        if (ONE) {
+          const int left = min(max(to - t0 - 16 * u, 0), 16), mine_at = own - t0 - 16 * u;
+          in[u] = (there(here.k[u]) ? (1u << left) - 1u : 0u) | ((unsigned)mine_at < 16u ? 1u << mine_at : 0u);
+        } else {
+          in[u] = (uint32_t)__builtin_amdgcn_ballot_w64(key < to && (there(here.k[u]) || key == own)) & 0xffffu;
+        }
+        whole = whole && in[u] == 0xffffu;
+        f32x4 s = kZeroF4;
+#pragma unroll
+        for (int t = 0; t < ST; ++t) {
+          const uint32_t even = keys.codes[u][t] & kNibbles, odd = keys.codes[u][t] >> 4 & kNibbles;
+          const bf16x8 codes = as_bf16x8(u32x4{codes_bf16(even, false), codes_bf16(even, true), codes_bf16(odd, false), codes_bf16(odd, true)});
+#pragma unroll
+          for (int p = PARTS - 1; p >= 0; --p) s = mfma16(codes, q[p][t], s);
+        }
+        float y[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) y[r] = fmaf(bf16_lo(keys.pair[u][r]), s[r], bf16_hi(keys.pair[u][r]) * qsum);
+        // the groups' parts added up: of two tokens a lane keeps one and hands the other to the lane beside it
+        const float first = (g & 1 ? y[1] : y[0]) + beside<1>(g & 1 ? y[0] : y[1]), second = (g & 1 ? y[3] : y[2]) + beside<1>(g & 1 ? y[2] : y[3]);
+        if constexpr (GR == 4) {
+          w[u][0] = ((g & 2 ? second : first) + beside<2>(g & 2 ? first : second)) * sc;
+        } else {
+          w[u][0] = first * sc;
+          w[u][1] = second * sc;
+        }
+      }
+      if (AHEAD && t0 + step < to) load_keys(keys, next, t0 + step);
+      if (has_own) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (t0 + 16 * u + 4 * L + r == own) {
+              x.pair[u][r] = sm_new[1][D / 8 + g];
+              x.codes[u][r] = reinterpret_cast<const ValueCodes*>(sm_new[1])[i];
+            }
+      }
+      if (!whole) {
+        // what is not there gets no weight, and its values, which may be anything, become zero
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+#pragma unroll
+          for (int n = 0; n < NS; ++n)
+            if (!(in[u] >> (4 * L + g + GR * n) & 1u)) w[u][n] = -INFINITY;
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (!(in[u] >> (4 * L + r) & 1u)) x.pair[u][r] = 0u;
+        }
+      }
+      float top = -INFINITY;
 #pragma unroll
       for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if (t0 + 16 * u + 4 * L + r == own) {
-            x.pair[u][r] = sm_new[1][D / 8 + g];
-            x.codes[u][r] = reinterpret_cast<const ValueCodes*>(sm_new[1])[i];
-          }
-    }
-    if (!whole) {
-      // what is not there gets no weight, and its values, which may be anything, become zero
+        for (int n = 0; n < NS; ++n) top = fmaxf(top, w[u][n]);
+      top = fmaxf(top, beside<1>(top));
+      if (GR == 4) top = fmaxf(top, beside<2>(top));
+      top = max_over_groups(top);
+      if (__builtin_amdgcn_ballot_w64(top > m + 8.f) != 0) {   // weights stay below 2^8 (packed_fwd.hip)
+        const float up = fmaxf(m, top), by = __builtin_amdgcn_exp2f(m - (up == -INFINITY ? 0.f : up));
+        m = up;
+        l *= by;
+        low *= by;
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] *= by;
+      }
+      const float ref = m == -INFINITY ? 0.f : m;
+      u32x4 weights[WPARTS];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
 #pragma unroll
-        for (int n = 0; n < NS; ++n)
-          if (!(in[u] >> (4 * L + g + GR * n) & 1u)) w[u][n] = -INFINITY;
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if (!(in[u] >> (4 * L + r) & 1u)) x.pair[u][r] = 0u;
-      }
-    }
-    float top = -INFINITY;
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int n = 0; n < NS; ++n) top = fmaxf(top, w[u][n]);
-    top = fmaxf(top, beside<1>(top));
-    if (GR == 4) top = fmaxf(top, beside<2>(top));
-    top = max_over_groups(top);
-    if (__builtin_amdgcn_ballot_w64(top > m + 8.f) != 0) {   // weights stay below 2^8 (packed_fwd.hip)
-      const float up = fmaxf(m, top), by = __builtin_amdgcn_exp2f(m - (up == -INFINITY ? 0.f : up));
-      m = up;
-      l *= by;
-      low *= by;
-#pragma unroll
-      for (int e = 0; e < E; ++e) o[e] *= by;
-    }
-    const float ref = m == -INFINITY ? 0.f : m;
-    u32x4 weights[WPARTS];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-#pragma unroll
-      for (int n = 0; n < NS; ++n) {
-        w[u][n] = __builtin_amdgcn_exp2f(w[u][n] - ref);
-        l += w[u][n];
-      }
-#pragma unroll
-      for (int r = 0; r < 4; r += 2) {
-        float y[2];
-#pragma unroll
-        for (int z = 0; z < 2; ++z) {
-          const float p = of_group<GR>(w[u][(r + z) / GR], (r + z) % GR);
-          low = fmaf(p, bf16_hi(x.pair[u][r + z]), low);
-          y[z] = p * bf16_lo(x.pair[u][r + z]);
+        for (int n = 0; n < NS; ++n) {
+          w[u][n] = __builtin_amdgcn_exp2f(w[u][n] - ref);
+          l += w[u][n];
         }
-        uint32_t z[WPARTS];
-        parts_of(z, y[0], y[1]);
 #pragma unroll
-        for (int p = 0; p < WPARTS; ++p) weights[p][2 * u + r / 2] = z[p];
-        if (sizeof(T) == 4) low = fmaf(kMiddle, bf16_lo(z[0]), fmaf(kMiddle, bf16_hi(z[0]), low));
+        for (int r = 0; r < 4; r += 2) {
+          float y[2];
+#pragma unroll
+          for (int z = 0; z < 2; ++z) {
+            const float p = of_group<GR>(w[u][(r + z) / GR], (r + z) % GR);
+            low = fmaf(p, bf16_hi(x.pair[u][r + z]), low);
+            y[z] = p * bf16_lo(x.pair[u][r + z]);
+          }
+          uint32_t z[WPARTS];
+          parts_of(z, y[0], y[1]);
+#pragma unroll
+          for (int p = 0; p < WPARTS; ++p) weights[p][2 * u + r / 2] = z[p];
+          if (sizeof(T) == 4) low = fmaf(kMiddle, bf16_lo(z[0]), fmaf(kMiddle, bf16_hi(z[0]), low));
+        }
       }
-    }
-    // channels of the same byte's half and parity at a time: a byte of each of two tokens, then one of the next
+      // channels of the same byte's half and parity at a time: a byte of each of two tokens, then one of the next
 #pragma unroll
-    for (int half = 0; half < E / 4; ++half) {
-      uint32_t two[4];
+      for (int half = 0; half < E / 4; ++half) {
+        uint32_t two[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        two[j] = __builtin_amdgcn_perm(x.codes[j / 2][2 * (j % 2) + 1], x.codes[j / 2][2 * (j % 2)], half ? 0x07030602u : 0x05010400u);
+        for (int j = 0; j < 4; ++j)
+          two[j] = __builtin_amdgcn_perm(x.codes[j / 2][2 * (j % 2) + 1], x.codes[j / 2][2 * (j % 2)], half ? 0x07030602u : 0x05010400u);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        u32x4 codes;
+        for (int e = 0; e < 4; ++e) {
+          u32x4 codes;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) codes[j] = codes_bf16(two[j] >> (4 * (e % 2)) & kNibbles, e >= 2);
-        if (sizeof(T) == 4)
-          o[4 * half + e] = mfma16(as_bf16x8(u32x4{kMinusMiddle, kMinusMiddle, kMinusMiddle, kMinusMiddle}), as_bf16x8(weights[0]), o[4 * half + e]);
+          for (int j = 0; j < 4; ++j) codes[j] = codes_bf16(two[j] >> (4 * (e % 2)) & kNibbles, e >= 2);
+          if (sizeof(T) == 4)
+            o[4 * half + e] = mfma16(as_bf16x8(u32x4{kMinusMiddle, kMinusMiddle, kMinusMiddle, kMinusMiddle}), as_bf16x8(weights[0]), o[4 * half + e]);
 #pragma unroll
-        for (int p = WPARTS - 1; p >= 0; --p) o[4 * half + e] = mfma16(as_bf16x8(codes), as_bf16x8(weights[p]), o[4 * half + e]);
+          for (int p = WPARTS - 1; p >= 0; --p) o[4 * half + e] = mfma16(as_bf16x8(codes), as_bf16x8(weights[p]), o[4 * half + e]);
+        }
       }
+      here = next;
+      next = later;
     }
-    here = next;
-    next = later;
-  }
-  l += beside<1>(l);
-  if (GR == 4) l += beside<2>(l);
-  l = sum_over_groups(l);
-  low = sum_over_groups(low);
+    l += beside<1>(l);
+    if (GR == 4) l += beside<2>(l);
+    l = sum_over_groups(l);
+    low = sum_over_groups(low);
 
-  // join the waves: a channel counts in its own group's column
-  if (L == 0 && g == 0) {
-    sm_m[wave][h] = m;
-    sm_l[wave][h] = l;
-  }
-  if (g == mine) {
-#pragma unroll
-    for (int e = 0; e < E; ++e)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) sm_o[wave][h][E * (4 * L + r) + e] = o[e][r] + low;
-  }
-  lds_barrier();
-  const int c = tid % D;
-  for (int x = tid / D; x < heads; x += kPagedThreads / D) {
-    float top = -INFINITY, sum = 0.f, acc = 0.f;
-#pragma unroll
-    for (int y = 0; y < kWaves; ++y) top = fmaxf(top, sm_m[y][x]);
-    const float ref = top == -INFINITY ? 0.f : top;
-#pragma unroll
-    for (int y = 0; y < kWaves; ++y) {
-      const float by = __builtin_amdgcn_exp2f(sm_m[y][x] - ref);
-      sum = fmaf(sm_l[y][x], by, sum);
-      acc = fmaf(sm_o[y][x][c], by, acc);
+    // join the waves: a channel counts in its own group's column
+    if (L == 0 && g == 0) {
+      sm_m[wave][h] = m;
+      sm_l[wave][h] = l;
     }
-    if (whole_sequence) {
-      Storage<T>::store(rows_of<T>(a.out, a.os, b, h0 + x), c, sum == 0.f ? 0.f : acc / sum);
-    } else {
-      const int64_t at = (int64_t)(part + b) * a.H + h0 + x;
-      a.sums[at * D + c] = acc;
-      if (c == 0) {
-        a.stats[2 * at] = top;
-        a.stats[2 * at + 1] = sum;
+    if (g == mine) {
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) sm_o[wave][h][E * (4 * L + r) + e] = o[e][r] + low;
+    }
+    lds_barrier();
+    const int c = tid % D;
+    for (int x = tid / D; x < heads; x += kPagedThreads / D) {
+      float top = -INFINITY, sum = 0.f, acc = 0.f;
+#pragma unroll
+      for (int y = 0; y < kWaves; ++y) top = fmaxf(top, sm_m[y][x]);
+      const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+      for (int y = 0; y < kWaves; ++y) {
+        const float by = __builtin_amdgcn_exp2f(sm_m[y][x] - ref);
+        sum = fmaf(sm_l[y][x], by, sum);
+        acc = fmaf(sm_o[y][x][c], by, acc);
+      }
+      if (whole_sequence) {
+        Storage<T>::store(rows_of<T>(a.out, a.os, b, h0 + x), c, sum == 0.f ? 0.f : acc / sum);
+      } else {
+        const int64_t at = (int64_t)(part + b) * a.H + h0 + x;
+        a.sums[at * D + c] = acc;
+        if (c == 0) {
+          a.stats[2 * at] = top;
+          a.stats[2 * at + 1] = sum;
+        }
       }
     }
-  }
-  lds_barrier();   // the next sequence's sums go to the same places
+    lds_barrier();   // the next sequence's sums go to the same places
   }
 }
 
-// Joins the pieces of a sequence that is cut in front of part blockIdx.x / ceil(H / kWaves) + 1, if that is its first cut: a wave for each
-// head, which takes the statistics of 64 pieces at once and their sums one after another.
-template <typename T, int D> __global__ __launch_bounds__(kPagedThreads) void q4_join_kernel(PagedDecodeArgs a) {
+// Joins the pieces of a sequence that is cut in front of a part, if that is its first cut: W waves for each head, which take every W-th
+// piece, the statistics of 64 at once and their sums eight by eight.
+template <typename T, int D, int W> __global__ __launch_bounds__(kPagedThreads) void q4_join_kernel(PagedDecodeArgs a) {
   constexpr int N = D / 64;   // columns of a lane
   typedef float Columns __attribute__((ext_vector_type(N)));
-  const int lane = threadIdx.x & 63, sets = (a.H + kWaves - 1) / kWaves;
-  const int h = blockIdx.x % sets * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), part = blockIdx.x / sets + 1;
+  __shared__ float sm_top[kWaves], sm_sum[kWaves];
+  __shared__ __align__(8) float sm_acc[kWaves][D];
+  constexpr int HEADS = kWaves / W;   // of a workgroup
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), sets = (a.H + HEADS - 1) / HEADS;
+  const int h = blockIdx.x % sets * HEADS + wave / W, part = blockIdx.x / sets + 1;
   const Cut cut = cut_at(a, part, lane);
   const int first = cut.base + kSetUp;   // its first block
-  if (h >= a.H || part >= cut.parts || first >= first_unit(part, cut.parts, cut.total) || first < first_unit(part - 1, cut.parts, cut.total))
-    return;
+  if (part >= cut.parts || first >= first_unit(part, cut.parts, cut.total) || first < first_unit(part - 1, cut.parts, cut.total)) return;
+  if (W < kWaves && h >= a.H) return;   // no barrier follows
   const int n = cut.seen(a, cut.b);
   const int pieces = part_of(cut.base + units_of(n) - 1, cut.parts, cut.total) - (part - 1) + 1;
-  const int64_t at = (int64_t)(part - 1 + cut.b) * a.H + h;   // the first one; the next are H rows on each
+  const int mine = (pieces - wave % W + W - 1) / W;
+  const int64_t at = (int64_t)(part - 1 + cut.b + wave % W) * a.H + h, next = (int64_t)W * a.H;   // this wave's first one, and how far the next is
   float top = -INFINITY, sum = 0.f;
   Columns acc = {};
-  for (int s0 = 0; s0 < pieces; s0 += 64) {
-    const int here = min(64, pieces - s0);
+  for (int s0 = 0; s0 < mine; s0 += 64) {
+    const int here = min(64, mine - s0);
     float m = -INFINITY, l = 0.f;
     if (lane < here) {
-      m = a.stats[2 * (at + (int64_t)(s0 + lane) * a.H)];
-      l = a.stats[2 * (at + (int64_t)(s0 + lane) * a.H) + 1];
+      m = a.stats[2 * (at + (s0 + lane) * next)];
+      l = a.stats[2 * (at + (s0 + lane) * next) + 1];
     }
     Columns x[8];
     auto load = [&](int s) {   // set out beside the statistics
 #pragma unroll
       for (int y = 0; y < 8; ++y)
-        x[y] = s + y < here ? *reinterpret_cast<const Columns*>(a.sums + (at + (int64_t)(s0 + s + y) * a.H) * D + N * lane) : Columns{};
+        x[y] = s + y < here ? *reinterpret_cast<const Columns*>(a.sums + (at + (s0 + s + y) * next) * D + N * lane) : Columns{};
     };
     load(0);
     const float up = fmaxf(top, over_lanes<true>(m));
@@ -798,9 +824,29 @@ template <typename T, int D> __global__ __launch_bounds__(kPagedThreads) void q4
       load(s);
     }
   }
+  if constexpr (W > 1) {
+    *reinterpret_cast<Columns*>(&sm_acc[wave][N * lane]) = acc;
+    if (lane == 0) {
+      sm_top[wave] = top;
+      sm_sum[wave] = sum;
+    }
+    __syncthreads();
+    if (wave % W != 0) return;
+    for (int y = 1; y < W; ++y) top = fmaxf(top, sm_top[wave + y]);
+    const float ref = top == -INFINITY ? 0.f : top;
+    acc = {};
+    sum = 0.f;
+    for (int y = 0; y < W; ++y) {
+      const float by = __builtin_amdgcn_exp2f(sm_top[wave + y] - ref);
+      acc += *reinterpret_cast<const Columns*>(&sm_acc[wave + y][N * lane]) * by;
+      sum = fmaf(sm_sum[wave + y], by, sum);
+    }
+  }
 #pragma unroll
   for (int x = 0; x < N; ++x) Storage<T>::store(rows_of<T>(a.out, a.os, cut.b, h), N * lane + x, sum == 0.f ? 0.f : acc[x] / sum);
 }
+
+constexpr int kManyPieces = 24;
 
 // Workgroups of a part: one for the query heads that fit its columns.
 int64_t decode_units(int H, int Hkv, int d) { return (int64_t)Hkv * ((H / Hkv + q4_heads(d) - 1) / q4_heads(d)); }
@@ -810,8 +856,10 @@ template <typename T, int D> hipError_t decode(const PagedDecodeArgs& a, hipStre
   if (a.shift >= 4) q4_decode_kernel<T, D, true><<<grid, dim3(kPagedThreads), 0, s>>>(a);
   else q4_decode_kernel<T, D, false><<<grid, dim3(kPagedThreads), 0, s>>>(a);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.splits == 1) return e;
-  q4_join_kernel<T, D><<<dim3((unsigned)(a.splits - 1) * ((a.H + kWaves - 1) / kWaves)), dim3(kPagedThreads), 0, s>>>(a);
+  if (e != hipSuccess || !a.stats) return e;
+  // many pieces a sequence take a workgroup a head
+  if (a.splits >= kManyPieces * a.B) q4_join_kernel<T, D, kWaves><<<dim3((unsigned)(a.splits - 1) * a.H), dim3(kPagedThreads), 0, s>>>(a);
+  else q4_join_kernel<T, D, 1><<<dim3((unsigned)(a.splits - 1) * ((a.H + kWaves - 1) / kWaves)), dim3(kPagedThreads), 0, s>>>(a);
   return hipGetLastError();
 }
 
@@ -821,13 +869,16 @@ int64_t row_groups(int total, int n_seqs, int Hkv, int d) {
 
 }  // namespace
 
-// Four workgroups for every compute unit, as many as run there at once, and no part without a block if all sequences are the longest.
-int paged_q4_parts(int B, int H, int Hkv, int d, int64_t max_len) {
-  constexpr int64_t kWorkgroups = 768;
-  return (int)std::max<int64_t>(1, std::min(kWorkgroups / decode_units(H, Hkv, d), B * (kSetUp + blocks_of(max_len))));
+// As many workgroups as run at once on 256 compute units, and no part without a unit if all sequences are the longest.  Sequences of one
+// block, which are not cut, take one each.
+int paged_q4_parts(bool bf16, int B, int H, int Hkv, int d, int64_t max_len) {
+  if (!paged_q4_cuts(max_len)) return B;
+  const int at_once = bf16 ? (d == 128 ? kAtOnce<uint16_t, 128> : kAtOnce<uint16_t, 64>) : (d == 128 ? kAtOnce<float, 128> : kAtOnce<float, 64>);
+  return (int)std::max<int64_t>(1, std::min(256 * at_once / decode_units(H, Hkv, d), B * (kSetUp + blocks_of(max_len))));
 }
-bool paged_q4_decode_fits(int B, int H, int Hkv, int d, int64_t max_len) {
-  return decode_units(H, Hkv, d) * paged_q4_parts(B, H, Hkv, d, max_len) <= most_workgroups(kPagedThreads) &&
+bool paged_q4_cuts(int64_t max_len) { return max_len > kBlock; }
+bool paged_q4_decode_fits(bool bf16, int B, int H, int Hkv, int d, int64_t max_len) {
+  return decode_units(H, Hkv, d) * paged_q4_parts(bf16, B, H, Hkv, d, max_len) <= most_workgroups(kPagedThreads) &&
          B * (kSetUp + blocks_of(max_len)) < (1ll << 31);   // units are counted in 32 bits
 }
 bool paged_q4_rows_fit(int total, int n_seqs, int Hkv, int d) { return row_groups(total, n_seqs, Hkv, d) <= most_workgroups(kPagedThreads); }

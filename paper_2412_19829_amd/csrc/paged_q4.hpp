@@ -23,10 +23,11 @@ struct PagedReadArgs {
   int64_t ks[2], vs[2], kps[3], vps[3];
 };
 
-// Workgroups that share the sequences' tokens, for each set of heads: PagedDecodeArgs::splits (chunk is not used).  More than one: sums and
-// stats hold parts + B rows, [parts + B, H, d] and [parts + B, H, 2].
-int paged_q4_parts(int B, int H, int Hkv, int d, int64_t max_len);
-bool paged_q4_decode_fits(int B, int H, int Hkv, int d, int64_t max_len);
+// Workgroups that share the sequences' tokens, for each set of heads: PagedDecodeArgs::splits (chunk is not used).  Where they are more than one
+// and may cut a sequence, sums and stats hold parts + B rows, [parts + B, H, d] and [parts + B, H, 2]; else both are null.
+int paged_q4_parts(bool bf16, int B, int H, int Hkv, int d, int64_t max_len);
+bool paged_q4_cuts(int64_t max_len);
+bool paged_q4_decode_fits(bool bf16, int B, int H, int Hkv, int d, int64_t max_len);
 bool paged_q4_rows_fit(int total, int n_seqs, int Hkv, int d);
 hipError_t launch_paged_q4_decode(const PagedDecodeArgs& a, bool bf16, hipStream_t s);
 hipError_t launch_paged_q4_fill(const PagedFillArgs& a, bool bf16, hipStream_t s);
