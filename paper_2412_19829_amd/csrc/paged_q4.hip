@@ -441,7 +441,7 @@ template <typename T, int D, bool ONE> __global__ __launch_bounds__(kPagedThread
   const int h0 = kvh * G + tile * HC, heads = min(G - tile * HC, HC);
   Cut cut;
   int unit, last_unit;
-  if (!a.stats && a.splits == a.B) {   // a sequence each
+  if (a.room <= kBlock) {   // a sequence each
     cut = {0, 0, part, 0, 0, 0, 0};
     unit = 0;
     last_unit = kSetUp + 1;
@@ -858,7 +858,7 @@ template <typename T, int D> hipError_t decode(const PagedDecodeArgs& a, hipStre
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !a.stats) return e;
   // many pieces a sequence take a workgroup a head
-  if (a.splits >= kManyPieces * a.B) q4_join_kernel<T, D, kWaves><<<dim3((unsigned)(a.splits - 1) * a.H), dim3(kPagedThreads), 0, s>>>(a);
+  if (a.splits >= (int64_t)kManyPieces * a.B) q4_join_kernel<T, D, kWaves><<<dim3((unsigned)(a.splits - 1) * a.H), dim3(kPagedThreads), 0, s>>>(a);
   else q4_join_kernel<T, D, 1><<<dim3((unsigned)(a.splits - 1) * ((a.H + kWaves - 1) / kWaves)), dim3(kPagedThreads), 0, s>>>(a);
   return hipGetLastError();
 }

@@ -329,6 +329,14 @@ def test_decode_cut_along_its_length(dtype, H, Hkv, d, page, lens):
 
 
 @gpu
+@pytest.mark.parametrize("H,d,lens", [(520, 64, [300]), (400, 128, [129, 140])])
+def test_decode_of_so_many_heads_that_nothing_is_cut(H, d, lens):
+    gen = torch.Generator().manual_seed(H)
+    assert gb.gformer_paged_decode_q4_workspace_bytes(len(lens), H, H, d, max(lens) + 1) == 0
+    check_step("bf16", 16, *step(gen, "bf16", H, H, d, 16, lens))
+
+
+@gpu
 @pytest.mark.parametrize("B,H,Hkv,d,most", [(64, 4, 4, 64, 40), (65, 2, 1, 128, 300), (150, 8, 8, 64, 20), (333, 1, 1, 64, 700), (700, 2, 2, 128, 12)])
 def test_decode_of_many_sequences(B, H, Hkv, d, most):
     """Shares of the work that hold several sequences, and sequences that lie in several shares, idle ones among them."""
