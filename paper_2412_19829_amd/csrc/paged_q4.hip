@@ -195,17 +195,18 @@ template <int D> __device__ __forceinline__ void put_codes(uint32_t* row, int c,
   if (c % 4 == 0) row[D / 8 + c / 4] = x.pair;
 }
 
-// Packed rows into their slots, or out of them: a workgroup takes ROWS rows of kHeads heads, a lane 8 channels of two of them.
-constexpr int kHeads = 4;
-template <int D> struct RowShape {
-  static constexpr int C = D / 8, STEP = kPagedThreads / C, N = 2, ROWS = N * STEP / kHeads;   // lanes a row; rows of all lanes, of one
+// Packed rows into their slots, or out of them: a workgroup takes ROWS rows of HB heads, a lane 8 channels of N of them.  Four heads where they
+// come in fours, which leaves fewer lanes idle where sequences have few rows each; at thousands of rows it makes no difference.
+constexpr int kReadRows = 2, kFillRows = 2;
+template <int D, int N_, int HB> struct RowShape {
+  static constexpr int C = D / 8, STEP = kPagedThreads / C, N = N_, ROWS = N * STEP / HB;   // lanes a row; rows of all lanes, of one
 };
 // Where a lane's rows are: rows of the packed tensors (negative: none), and their slots (page negative: none).
-template <int D> struct Slots {
-  int row[RowShape<D>::N], head[RowShape<D>::N], page[RowShape<D>::N], slot[RowShape<D>::N];
+template <int D, int N, int HB> struct Slots {
+  int row[N], head[N], page[N], slot[N];
   template <typename A> __device__ __forceinline__ bool find(const A& a, int block, int tid) {
-    using S = RowShape<D>;
-    const int sets = (a.Hkv + kHeads - 1) / kHeads;
+    using S = RowShape<D, N, HB>;
+    const int sets = (a.Hkv + HB - 1) / HB;
     const int tile = block / sets, lane = tid & 63;
     int seq, base, n;
     int64_t from;
@@ -230,9 +231,9 @@ template <int D> struct Slots {
     const int32_t* table = a.table + (int64_t)seq * a.width;
 #pragma unroll
     for (int i = 0; i < S::N; ++i) {
-      const int u = tid / S::C + i * S::STEP, r = first + u / kHeads;
+      const int u = tid / S::C + i * S::STEP, r = first + u / HB;
       const int64_t pos = from + r;
-      head[i] = block % sets * kHeads + u % kHeads;
+      head[i] = block % sets * HB + u % HB;
       const bool real = r < n && head[i] < a.Hkv;
       row[i] = real ? base + r : -1;
       page[i] = real && pos >= 0 && pos < room ? table[pos >> a.shift] : -1;
@@ -244,28 +245,29 @@ template <int D> struct Slots {
   __device__ __forceinline__ int64_t at(const int64_t (&st)[3], int i) const { return page[i] * st[0] + head[i] * st[1] + slot[i] * st[2]; }
 };
 
-// 9207 rows of 8 heads, d = 128, bf16 (50 MB read and written): 15.5 us, the quantising's instructions more than the memory (20 with
-// all of them in 64 bits).
-template <typename T, int D> __global__ __launch_bounds__(kPagedThreads) void q4_fill_kernel(PagedFillArgs a) {
-  constexpr int N = RowShape<D>::N;
-  const int tid = threadIdx.x, c = tid % RowShape<D>::C;
-  Slots<D> s;
-  if (!s.find(a, blockIdx.x, tid)) return;
-  Eight<T> k[N], v[N];
+// Keys and values in workgroups of their own, which halves what a lane quantises in turn: 128 tokens of 12 heads, d = 64 5.2 us (6.6 in
+// the same ones).  9207 rows of 8 heads, d = 128, bf16 (50 MB read and written): 14.0 us, the quantising's instructions more than the memory (20
+// with all of them in 64 bits; 15.9 with one row a lane, 14.2 with four).
+template <typename T, int D, int HB> __global__ __launch_bounds__(kPagedThreads) void q4_fill_kernel(PagedFillArgs a) {
+  constexpr int N = kFillRows;
+  const int tid = threadIdx.x, c = tid % (D / 8);
+  const bool values = blockIdx.x & 1;
+  Slots<D, N, HB> s;
+  if (!s.find(a, blockIdx.x >> 1, tid)) return;
+  const T* rows = reinterpret_cast<const T*>(values ? a.v : a.k) + 8 * c;
+  char* pages = reinterpret_cast<char*>(values ? a.vpages : a.kpages);
+  const int64_t* from = values ? a.vs : a.ks;
+  const int64_t* to = values ? a.vps : a.kps;
+  Eight<T> x[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    if (s.page[i] >= 0) x[i].template get<true>(rows + s.row[i] * from[0] + s.head[i] * from[1]);
 #pragma unroll
   for (int i = 0; i < N; ++i)
     if (s.page[i] >= 0) {
-      k[i].template get<true>(rows_of<T>(a.k, a.ks, s.row[i], s.head[i]) + 8 * c);
-      v[i].template get<true>(rows_of<T>(a.v, a.vs, s.row[i], s.head[i]) + 8 * c);
-    }
-#pragma unroll
-  for (int i = 0; i < N; ++i)
-    if (s.page[i] >= 0) {
-      float x[8];
-      k[i].values(x);
-      put_codes<D>(reinterpret_cast<uint32_t*>(reinterpret_cast<char*>(a.kpages) + s.at(a.kps, i)), c, quantised<T>(x));
-      v[i].values(x);
-      put_codes<D>(reinterpret_cast<uint32_t*>(reinterpret_cast<char*>(a.vpages) + s.at(a.vps, i)), c, quantised<T>(x));
+      float y[8];
+      x[i].values(y);
+      put_codes<D>(reinterpret_cast<uint32_t*>(pages + s.page[i] * to[0] + s.head[i] * to[1] + s.slot[i] * to[2]), c, quantised<T>(y));
     }
 }
 
@@ -282,11 +284,11 @@ template <int D> __device__ __forceinline__ Codes codes_of(const void* pages, in
 // rows a lane, 18.3 with one.  `once`: the rows are more than the last cache holds, so that nobody finds them there: 4 x 32767 tokens
 // with an attention of 32 queries each behind them 442 us (475 without), but 7 x 8192 with 64 queries 240 (234).
 constexpr int64_t kLastCache = (int64_t)256 << 20;   // bytes
-template <typename T, int D> __global__ __launch_bounds__(kPagedThreads) void q4_read_kernel(PagedReadArgs a) {
-  constexpr int N = RowShape<D>::N;
-  const int tid = threadIdx.x, c = tid % RowShape<D>::C;
+template <typename T, int D, int HB> __global__ __launch_bounds__(kPagedThreads) void q4_read_kernel(PagedReadArgs a) {
+  constexpr int N = kReadRows;
+  const int tid = threadIdx.x, c = tid % (D / 8);
   const bool once = (int64_t)a.total * a.Hkv * (2 * D * (int)sizeof(T)) > kLastCache;
-  Slots<D> s;
+  Slots<D, N, HB> s;
   if (!s.find(a, blockIdx.x, tid)) return;
   Codes k[N], v[N];
 #pragma unroll
@@ -863,8 +865,22 @@ template <typename T, int D> hipError_t decode(const PagedDecodeArgs& a, hipStre
   return hipGetLastError();
 }
 
-int64_t row_groups(int total, int n_seqs, int Hkv, int d) {
-  return packed_tiles(total, n_seqs, d == 128 ? RowShape<128>::ROWS : RowShape<64>::ROWS) * ((Hkv + kHeads - 1) / kHeads);
+int heads_together(int Hkv) { return Hkv % 4 == 0 ? 4 : 1; }
+int64_t row_groups(int total, int n_seqs, int Hkv, int d, int n) {
+  const int hb = heads_together(Hkv), rows = n * (d == 128 ? RowShape<128, 1, 1>::ROWS : RowShape<64, 1, 1>::ROWS) / hb;
+  return packed_tiles(total, n_seqs, rows) * (Hkv / hb);
+}
+template <typename T, int D> hipError_t fill(const PagedFillArgs& a, hipStream_t s) {
+  const dim3 grid((unsigned)(2 * row_groups(a.total, a.n_seqs, a.Hkv, D, kFillRows)));
+  if (heads_together(a.Hkv) == 4) q4_fill_kernel<T, D, 4><<<grid, kPagedThreads, 0, s>>>(a);
+  else q4_fill_kernel<T, D, 1><<<grid, kPagedThreads, 0, s>>>(a);
+  return hipGetLastError();
+}
+template <typename T, int D> hipError_t read(const PagedReadArgs& a, hipStream_t s) {
+  const dim3 grid((unsigned)row_groups(a.total, a.n_seqs, a.Hkv, D, kReadRows));
+  if (heads_together(a.Hkv) == 4) q4_read_kernel<T, D, 4><<<grid, kPagedThreads, 0, s>>>(a);
+  else q4_read_kernel<T, D, 1><<<grid, kPagedThreads, 0, s>>>(a);
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -881,7 +897,7 @@ bool paged_q4_decode_fits(bool bf16, int B, int H, int Hkv, int d, int64_t max_l
   return decode_units(H, Hkv, d) * paged_q4_parts(bf16, B, H, Hkv, d, max_len) <= most_workgroups(kPagedThreads) &&
          B * (kSetUp + blocks_of(max_len)) < (1ll << 31);   // units are counted in 32 bits
 }
-bool paged_q4_rows_fit(int total, int n_seqs, int Hkv, int d) { return row_groups(total, n_seqs, Hkv, d) <= most_workgroups(kPagedThreads); }
+bool paged_q4_rows_fit(int total, int n_seqs, int Hkv, int d) { return 2 * row_groups(total, n_seqs, Hkv, d, std::min(kFillRows, kReadRows)) <= most_workgroups(kPagedThreads); }
 
 hipError_t launch_paged_q4_decode(const PagedDecodeArgs& a, bool bf16, hipStream_t s) {
   if (bf16) return a.d == 128 ? decode<uint16_t, 128>(a, s) : decode<uint16_t, 64>(a, s);
@@ -889,17 +905,13 @@ hipError_t launch_paged_q4_decode(const PagedDecodeArgs& a, bool bf16, hipStream
 }
 
 hipError_t launch_paged_q4_fill(const PagedFillArgs& a, bool bf16, hipStream_t s) {
-  const dim3 grid((unsigned)row_groups(a.total, a.n_seqs, a.Hkv, a.d));
-  if (bf16) a.d == 128 ? q4_fill_kernel<uint16_t, 128><<<grid, kPagedThreads, 0, s>>>(a) : q4_fill_kernel<uint16_t, 64><<<grid, kPagedThreads, 0, s>>>(a);
-  else a.d == 128 ? q4_fill_kernel<float, 128><<<grid, kPagedThreads, 0, s>>>(a) : q4_fill_kernel<float, 64><<<grid, kPagedThreads, 0, s>>>(a);
-  return hipGetLastError();
+  if (bf16) return a.d == 128 ? fill<uint16_t, 128>(a, s) : fill<uint16_t, 64>(a, s);
+  return a.d == 128 ? fill<float, 128>(a, s) : fill<float, 64>(a, s);
 }
 
 hipError_t launch_paged_q4_read(const PagedReadArgs& a, bool bf16, hipStream_t s) {
-  const dim3 grid((unsigned)row_groups(a.total, a.n_seqs, a.Hkv, a.d));
-  if (bf16) a.d == 128 ? q4_read_kernel<uint16_t, 128><<<grid, kPagedThreads, 0, s>>>(a) : q4_read_kernel<uint16_t, 64><<<grid, kPagedThreads, 0, s>>>(a);
-  else a.d == 128 ? q4_read_kernel<float, 128><<<grid, kPagedThreads, 0, s>>>(a) : q4_read_kernel<float, 64><<<grid, kPagedThreads, 0, s>>>(a);
-  return hipGetLastError();
+  if (bf16) return a.d == 128 ? read<uint16_t, 128>(a, s) : read<uint16_t, 64>(a, s);
+  return a.d == 128 ? read<float, 128>(a, s) : read<float, 64>(a, s);
 }
 
 hipError_t launch_pages_q4_copy(const PagesCopyArgs& a, hipStream_t s) {

@@ -167,11 +167,11 @@ def spread(t, wide):
 
 @gpu
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("d,page,wide", [(64, 8, False), (128, 16, True), (64, 64, True), (128, 8, False)])
-def test_fill_and_read(dtype, d, page, wide):
+@pytest.mark.parametrize("d,page,wide,Hkv", [(64, 8, False, 3), (128, 16, True, 4), (64, 64, True, 8), (128, 8, False, 1)])
+def test_fill_and_read(dtype, d, page, wide, Hkv):
     gen = torch.Generator().manual_seed(d + page)
     T = ref.TYPES[dtype]
-    lens, start, width, pages, Hkv = [37, 0, 1, 50, 20], [3, 5, 7, -4, 0], 7, 40, 3
+    lens, start, width, pages = [37, 0, 1, 50, 20], [3, 5, 7, -4, 0], 7, 40
     total = sum(lens) + 6
     k, v = special(gen, total, Hkv, d, T), special(gen, total, Hkv, d, T).flip(0).contiguous()
     table = torch.randperm(pages, generator=gen)[:5 * width].view(5, width).to(torch.int32)
@@ -202,6 +202,29 @@ def test_fill_and_read(dtype, d, page, wide):
                 exp[at + i] = held[int(table[s, pos // page]), :, pos % page] if ok else 0.0
             at += n
         assert torch.equal(torch.nan_to_num(got.cpu().float(), 1e9), torch.nan_to_num(exp.float().to(T).float(), 1e9))
+
+
+@gpu
+@pytest.mark.parametrize("n_seqs", [1, 62, 63, 64, 65, 200])
+def test_rows_of_many_sequences(n_seqs):
+    """One to three rows of each, some of none, a batch padded behind them."""
+    gen = torch.Generator().manual_seed(n_seqs)
+    lens = torch.randint(0, 4, (n_seqs,), generator=gen).tolist()
+    lens[0] = 3
+    start = torch.randint(0, 30, (n_seqs,), generator=gen).tolist()
+    total, Hkv, d, page = sum(lens) + 5, 2, 64, 8
+    table = torch.randperm(5 * n_seqs, generator=gen).view(n_seqs, 5).to(torch.int32)
+    k, v = torch.randn(total, Hkv, d, generator=gen), torch.randn(total, Hkv, d, generator=gen)
+    kp, vp = noise(gen, 5 * n_seqs, Hkv, page, 40), noise(gen, 5 * n_seqs, Hkv, page, 40)
+    want = [expected_fill(p, x, table, start, lens, page) for p, x in ((kp, k), (vp, v))]
+    cu = ints(*pref.offsets(lens))
+    gb.gformer_paged_fill_q4(k.cuda(), v.cuda(), kp, vp, table.cuda(), ints(*start), cu)
+    same_bytes(kp, want[0], "keys")
+    same_bytes(vp, want[1], "values")
+    ko, vo = torch.full((total, Hkv, d), 7.0, device="cuda"), torch.full((total, Hkv, d), 7.0, device="cuda")
+    gb.gformer_paged_read_q4(kp, vp, ko, vo, table.cuda(), ints(*start), cu)
+    for got, x in ((ko, k), (vo, v)):
+        assert torch.equal(got[:sum(lens)].cpu(), ref.values(ref.rows(x[:sum(lens)])).float()) and bool((got[sum(lens):] == 7.0).all())
 
 
 @gpu
