@@ -246,8 +246,8 @@ template <int D, int N, int HB> struct Slots {
 };
 
 // Keys and values in workgroups of their own, which halves what a lane quantises in turn: 128 tokens of 12 heads, d = 64 5.2 us (6.6 in
-// the same ones).  9207 rows of 8 heads, d = 128, bf16 (50 MB read and written): 14.0 us, the quantising's instructions more than the memory (20
-// with all of them in 64 bits; 15.9 with one row a lane, 14.2 with four).
+// the same ones).  9207 rows of 8 heads, d = 128, bf16 (50 MB read and written): 14.0 us, of which vector instructions take 8.6 and the
+// memory would take 10 (20 with all of them in 64 bits; 15.9 with one row a lane, 14.2 with four).
 template <typename T, int D, int HB> __global__ __launch_bounds__(kPagedThreads) void q4_fill_kernel(PagedFillArgs a) {
   constexpr int N = kFillRows;
   const int tid = threadIdx.x, c = tid % (D / 8);

@@ -1,7 +1,7 @@
-// Rotary positions (rotary.hpp).  The angles, which take 64 bits, are taken once for all heads of a row.  Memory bounds it: 9223 rows of
-// 32 / 8 heads, d = 128, bf16 (148 MB read and written) 31.4 us, 4.7 TB/s; 4 rows of 12 / 12 heads, d = 64: 4.7.  What is read need
-// not stay in the caches, what is written is what attention reads next: with such loads alone 31.4 (34.5 without) and, with packed attention
-// over 281-token sequences behind it, 138 us (142); with such stores too 28.3 and 143.
+// Rotary positions (rotary.hpp).  The angles, which take 64 bits, are taken once for all heads of a row.  Memory bounds it: 9407 rows, 9207
+// of which turn, of 32 / 8 heads, d = 128, bf16 (148 MB read and written) 28.7 us, 5.1 TB/s; 4 rows of 12 / 12 heads, d = 64: 2.7, launch and trips to
+// memory.  What is read need not stay in the caches, what is written is what attention reads next: over more tensors in turn 31.4 us with
+// such loads and 34.5 without, with packed attention over sequences of 281 behind it 138 and 142; with such stores too 28.3, but 143 then.
 #include "rotary.hpp"
 
 #include "mfma.hpp"
@@ -185,7 +185,7 @@ template <typename T, int D, int ROWS, bool INTERLEAVED> __global__ __launch_bou
   }
 }
 
-constexpr int kManyRows = 1024;   // from here on a workgroup takes kRows rows, below it one
+constexpr int kManyRows = 1024;   // from here on, four rows for every compute unit, a workgroup takes kRows rows, below it one
 
 template <typename T, int D, int ROWS> void launch(const RotaryArgs& a, hipStream_t s) {
   const dim3 grid((unsigned)(((int64_t)a.total + ROWS - 1) / ROWS));
