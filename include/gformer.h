@@ -418,7 +418,8 @@ gf_status gformer_paged_read_q4(const void* kpages, const void* vpages, void* k,
                                 const gformer_paged_params* p, void* hip_stream);
 
 /* gformer_paged_decode over this cache.  The new token is seen as its slot holds it, quantised.  Scores and sums take the values
- * that codes stand for unrounded; bf16 calls round the weights, times the values' scales, to bf16. */
+ * that codes stand for unrounded; weights times the values' scales are taken to 16 bits (bf16 calls) or 24.  Equal calls give equal bits; a
+ * sequence's sums are cut where the lengths of all the call's sequences say.  Sums of values above 2^110 may overflow. */
 size_t gformer_paged_decode_q4_workspace_bytes(int B, int H, int Hkv, int d, int table_width, int max_len,
                                                const gformer_paged_params* p);
 gf_status gformer_paged_decode_q4(const void* q, const void* k, const void* v, void* out, void* kpages,

@@ -129,6 +129,7 @@ def test_positions_by_row(dtype, interleaved, H, Hkv, d, rot, wide):
 @gpu
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("lens,start", [([5], [0]), ([1], [100]), ([0, 3, 0, 0, 70, 1, 0], [9, 4000, 3, 1, 0, 1 << 30, 2]), ([33] * 40, None),
+                                        ([2, 0, 1] * 70, list(range(210))), ([1] * 5000, None),
                                         ([300, 31, 32, 33], [0, 1, 2, 3]), ([], [])])
 @pytest.mark.parametrize("tail", [0, 9])
 def test_packed(dtype, lens, start, tail):
