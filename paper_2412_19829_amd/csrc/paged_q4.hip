@@ -415,7 +415,8 @@ __device__ __forceinline__ Cut cut_at(const PagedDecodeArgs& a, int part, int la
       if (part >= x.parts) return x;
       target = first_unit(part, x.parts, x.total);
     }
-    const int before = __popcll(__builtin_amdgcn_ballot_w64(x.base + sum <= target));   // lanes whose sequences lie in front
+    // lanes whose sequences lie in front; never all, also where somebody changes the lengths meanwhile
+    const int before = min(__popcll(__builtin_amdgcn_ballot_w64(x.base + sum <= target)), (count - 1) / per);
     if (before > 0) x.base += __builtin_amdgcn_readlane(sum, before - 1);
     x.b += before * per;
     if (per == 1) return x;
@@ -458,7 +459,7 @@ template <typename T, int D, bool ONE> __global__ __launch_bounds__(kPagedThread
   const int in_page = (1 << a.shift) - 1;
 
   // a part that ends while it sets a sequence up leaves it to the next one
-  while (cut.base + kSetUp < last_unit) {
+  while (cut.base + kSetUp < last_unit && cut.b < a.B) {
     const int b = cut.b, n = cut.seen(a, b), first = cut.base + kSetUp;
     const int from = max(unit - first, 0) * kBlock, to = (int)min((int64_t)n, (int64_t)(last_unit - first) * kBlock);   // at most 2^30
     const bool whole_sequence = unit <= first && last_unit - cut.base >= units_of(n);
@@ -794,7 +795,7 @@ template <typename T, int D, int W> __global__ __launch_bounds__(kPagedThreads) 
   if (part >= cut.parts || first >= first_unit(part, cut.parts, cut.total) || first < first_unit(part - 1, cut.parts, cut.total)) return;
   if (W < kWaves && h >= a.H) return;   // no barrier follows
   const int n = cut.seen(a, cut.b);
-  const int pieces = part_of(cut.base + units_of(n) - 1, cut.parts, cut.total) - (part - 1) + 1;
+  const int pieces = min(part_of(cut.base + units_of(n) - 1, cut.parts, cut.total), cut.parts - 1) - (part - 1) + 1;
   const int mine = (pieces - wave % W + W - 1) / W;
   const int64_t at = (int64_t)(part - 1 + cut.b + wave % W) * a.H + h, next = (int64_t)W * a.H;   // this wave's first one, and how far the next is
   float top = -INFINITY, sum = 0.f;
