@@ -8,7 +8,7 @@
 // which leaves them in every one of them, and there a weight takes its own group's scale for the second product, whose rows (channels) count
 // in their own group's columns alone.  16 columns are 4 heads of 128 channels, or 8 of 64.
 // A code becomes an operand by way of fp8: the byte n is n 2^-9 for n < 16, two of which one instruction converts.
-// Memory bounds it up to 4 query heads of 128 channels a key head (8 of 64), beyond that the vector instructions, which every further 4 (8) take
+// Memory bounds it up to 4 query heads of 128 channels a key head (8 of 64), beyond that the vector instructions, which every further 8 take
 // again.  us, kernel alone: 220,039 keys of 8 sequences, 32 / 8 heads, d = 128, bf16 (282 MB) 55.3, 5.1 TB/s; 88,074 in 32 ragged ones
 // (114 MB) 27.7; six fp32 sequences of 10,167 in all, 16 heads, d = 64 11.4; one of 2047, 12 heads, d = 64 6.4, and 4.8 to join.
 #include "paged_q4.hpp"
@@ -341,9 +341,7 @@ template <int D> struct Shape4 {
 // take.  us: 8 x 16000 tokens, 32 / 8 heads, d = 128, bf16 40.8 ahead with three, 50.9 without and with four (spilled); 8 x 16000, 16 heads,
 // d = 64 52.8 ahead and 49.8 without, with four; 57.7 with five (spilled).  fp32, d = 128 47.9 with two, 57.5 with three.
 template <int D> constexpr bool kAhead = D == 128;
-template <typename T, int D> constexpr int kAtOnce = sizeof(T) == 2 ? (D == 128 ? 3 : 4) : (D == 128 ? 2 : 3);
-constexpr int q4_heads(int d) { return d == 128 ? Shape4<128>::HC : Shape4<64>::HC; }
-
+template <typename T, int D, int C> constexpr int kAtOnce = sizeof(T) == 2 ? (D == 128 ? 4 - C : 4) : (D == 128 ? 2 : 3);
 // Parts in bf16 that a factor of the products is taken in.  Queries: bf16 is one, fp32 the three that hold its 24 bits.  Weights times scales: two
 // for bf16 calls and three for fp32.  In one part their rounding meets codes from 0 to 15, whose sum the lowest values' cancels nearly:
 // the output of 2048 to 32768 random tokens is then off by 1.8 to 2.4 times one rounding of it, in two by one.
@@ -427,21 +425,21 @@ __device__ __forceinline__ Cut cut_at(const PagedDecodeArgs& a, int part, int la
 // ONE: a page holds whole tiles of 16 keys (pages of 8 tokens do not), so that their pages and addresses are the same for all lanes, which
 // then add nothing but a fixed offset to them: with addresses of their own they took 193 of 572 vector instructions a tile of 32 keys, d = 128
 // (355 are left).
-template <typename T, int D, bool ONE> __global__ __launch_bounds__(kPagedThreads, (kAtOnce<T, D>)) void q4_decode_kernel(PagedDecodeArgs a) {
+template <typename T, int D, bool ONE, int C> __global__ __launch_bounds__(kPagedThreads, (kAtOnce<T, D, C>)) void q4_decode_kernel(PagedDecodeArgs a) {
   using S = Shape4<D>;
   typedef typename S::KeyCodes KeyCodes;
   typedef typename S::ValueCodes ValueCodes;
-  constexpr int GR = S::GR, HC = S::HC, ST = S::ST, E = S::E, PARTS = kQueryParts<T>, WPARTS = kWeightParts<T>, ROW = q4_row(D), U = 2, R = 16 * U, NS = 4 / GR;
+  constexpr int GR = S::GR, HC = S::HC, HW = C * HC, ST = S::ST, E = S::E, PARTS = kQueryParts<T>, WPARTS = kWeightParts<T>, ROW = q4_row(D), U = 2, R = 16 * U, NS = 4 / GR;
   constexpr bool AHEAD = kAhead<D>;
-  __shared__ float sm_o[kWaves][HC][D + 4], sm_m[kWaves][HC], sm_l[kWaves][HC];
+  __shared__ float sm_o[kWaves][HW][D + 4], sm_m[kWaves][HW], sm_l[kWaves][HW];
   __shared__ __align__(16) uint32_t sm_new[2][ROW / 4];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, L = lane >> 4;
-  const int G = a.H / a.Hkv, tiles = (G + HC - 1) / HC;
+  const int G = a.H / a.Hkv, tiles = (G + HW - 1) / HW;
   // workgroups that read the same rows for other query heads are eight apart: on one XCD
   const int work = a.Hkv * a.splits, even = work / 8 * 8 * tiles, id = blockIdx.x;
   const int tile = id < even ? id / 8 % tiles : (id - even) % tiles, w = id < even ? id / (8 * tiles) * 8 + id % 8 : work / 8 * 8 + (id - even) / tiles;
   const int kvh = w % a.Hkv, part = w / a.Hkv;
-  const int h0 = kvh * G + tile * HC, heads = min(G - tile * HC, HC);
+  const int h0 = kvh * G + tile * HW, heads = min(G - tile * HW, HW);
   Cut cut;
   int unit, last_unit;
   if (a.room <= kBlock) {   // a sequence each
@@ -485,14 +483,16 @@ template <typename T, int D, bool ONE> __global__ __launch_bounds__(kPagedThread
     const int step = kWaves * R;
     int t0 = from + wave * R;
     Pages here = pages(t0), next = pages(t0 + step);
-    // column i: query head i / GR, group i % GR
+    // column i of set c: query head HC c + i / GR, group i % GR
     const int h = i / GR, g = i % GR, mine = L * GR / 4;   // mine: the group of this lane's channels
-    Eight<T> raw[ST];
+    Eight<T> raw[C][ST];
 #pragma unroll
-    for (int t = 0; t < ST; ++t) {
-      raw[t] = {};
-      if (h < heads && g == mine) raw[t].get(rows_of<T>(a.q, a.qs, b, h0 + h) + D / 4 * L + 8 * t);
-    }
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int t = 0; t < ST; ++t) {
+        raw[c][t] = {};
+        if (HC * c + h < heads && g == mine) raw[c][t].get(rows_of<T>(a.q, a.qs, b, h0 + HC * c + h) + D / 4 * L + 8 * t);
+      }
     const bool brings_own = own >= from && own < to, my_own = brings_own && wave < 2 && lane < D / 8;
     Eight<T> fresh = {};
     int own_page = -1;
@@ -573,32 +573,36 @@ template <typename T, int D, bool ONE> __global__ __launch_bounds__(kPagedThread
       lds_barrier();
     }
 
-    bf16x8 q[PARTS][ST];
-    float qsum = 0.f;
+    bf16x8 q[C][PARTS][ST];
+    float qsum[C], m[C], l[C], low[C];
+    f32x4 o[C][E];
 #pragma unroll
-    for (int t = 0; t < ST; ++t) {
-      float x[8];
-      raw[t].values(x);
+    for (int c = 0; c < C; ++c) {
+      qsum[c] = l[c] = low[c] = 0.f;
+      m[c] = -INFINITY;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) qsum += x[e];
-      u32x4 w[PARTS];
+      for (int t = 0; t < ST; ++t) {
+        float x[8];
+        raw[c][t].values(x);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int e = j < 2 ? 4 * j : 4 * j - 7;   // the order that codes_bf16 leaves them in: 0 2 4 6 1 3 5 7
-        uint32_t y[PARTS];
-        parts_of(y, x[e], x[e + 2]);
+        for (int e = 0; e < 8; ++e) qsum[c] += x[e];
+        u32x4 w[PARTS];
 #pragma unroll
-        for (int p = 0; p < PARTS; ++p) w[p][j] = y[p];
+        for (int j = 0; j < 4; ++j) {
+          const int e = j < 2 ? 4 * j : 4 * j - 7;   // the order that codes_bf16 leaves them in: 0 2 4 6 1 3 5 7
+          uint32_t y[PARTS];
+          parts_of(y, x[e], x[e + 2]);
+#pragma unroll
+          for (int p = 0; p < PARTS; ++p) w[p][j] = y[p];
+        }
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) q[c][p][t] = as_bf16x8(w[p]);
       }
+      qsum[c] = sum_over_groups(qsum[c]);
 #pragma unroll
-      for (int p = 0; p < PARTS; ++p) q[p][t] = as_bf16x8(w[p]);
+      for (int e = 0; e < E; ++e) o[c][e] = kZeroF4;
     }
-    qsum = sum_over_groups(qsum);
     const float sc = a.scale * kLog2e;
-    f32x4 o[E];
-#pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = kZeroF4;
-    float m = -INFINITY, l = 0.f, low = 0.f;
 
     // A tile's values are on their way while its scores are taken, the next tile's keys, in the registers of this one's, from then on.
     for (; t0 < to; t0 += step) {
@@ -618,7 +622,7 @@ template <typename T, int D, bool ONE> __global__ __launch_bounds__(kPagedThread
         }
       }
       // scores: this lane keeps those of tokens 4 L + g + GR n, n < NS
-      float w[U][NS];
+      float w[C][U][NS];
       uint32_t in[U];
       bool whole = true;
 #pragma unroll
@@ -631,24 +635,31 @@ template <typename T, int D, bool ONE> __global__ __launch_bounds__(kPagedThread
           in[u] = (uint32_t)__builtin_amdgcn_ballot_w64(key < to && (there(here.k[u]) || key == own)) & 0xffffu;
         }
         whole = whole && in[u] == 0xffffu;
-        f32x4 s = kZeroF4;
+        f32x4 s[C];
+#pragma unroll
+        for (int c = 0; c < C; ++c) s[c] = kZeroF4;
 #pragma unroll
         for (int t = 0; t < ST; ++t) {
           const uint32_t even = keys.codes[u][t] & kNibbles, odd = keys.codes[u][t] >> 4 & kNibbles;
           const bf16x8 codes = as_bf16x8(u32x4{codes_bf16(even, false), codes_bf16(even, true), codes_bf16(odd, false), codes_bf16(odd, true)});
 #pragma unroll
-          for (int p = PARTS - 1; p >= 0; --p) s = mfma16(codes, q[p][t], s);
-        }
-        float y[4];
+          for (int c = 0; c < C; ++c)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) y[r] = fmaf(bf16_lo(keys.pair[u][r]), s[r], bf16_hi(keys.pair[u][r]) * qsum);
-        // the groups' parts added up: of two tokens a lane keeps one and hands the other to the lane beside it
-        const float first = (g & 1 ? y[1] : y[0]) + beside<1>(g & 1 ? y[0] : y[1]), second = (g & 1 ? y[3] : y[2]) + beside<1>(g & 1 ? y[2] : y[3]);
-        if constexpr (GR == 4) {
-          w[u][0] = ((g & 2 ? second : first) + beside<2>(g & 2 ? first : second)) * sc;
-        } else {
-          w[u][0] = first * sc;
-          w[u][1] = second * sc;
+            for (int p = PARTS - 1; p >= 0; --p) s[c] = mfma16(codes, q[c][p][t], s[c]);
+        }
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          float y[4];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) y[r] = fmaf(bf16_lo(keys.pair[u][r]), s[c][r], bf16_hi(keys.pair[u][r]) * qsum[c]);
+          // the groups' parts added up: of two tokens a lane keeps one and hands the other to the lane beside it
+          const float first = (g & 1 ? y[1] : y[0]) + beside<1>(g & 1 ? y[0] : y[1]), second = (g & 1 ? y[3] : y[2]) + beside<1>(g & 1 ? y[2] : y[3]);
+          if constexpr (GR == 4) {
+            w[c][u][0] = ((g & 2 ? second : first) + beside<2>(g & 2 ? first : second)) * sc;
+          } else {
+            w[c][u][0] = first * sc;
+            w[c][u][1] = second * sc;
+          }
         }
       }
       if (AHEAD && t0 + step < to) load_keys(keys, next, t0 + step);
@@ -668,51 +679,57 @@ template <typename T, int D, bool ONE> __global__ __launch_bounds__(kPagedThread
         for (int u = 0; u < U; ++u) {
 #pragma unroll
           for (int n = 0; n < NS; ++n)
-            if (!(in[u] >> (4 * L + g + GR * n) & 1u)) w[u][n] = -INFINITY;
+            if (!(in[u] >> (4 * L + g + GR * n) & 1u)) {
+#pragma unroll
+              for (int c = 0; c < C; ++c) w[c][u][n] = -INFINITY;
+            }
 #pragma unroll
           for (int r = 0; r < 4; ++r)
             if (!(in[u] >> (4 * L + r) & 1u)) x.pair[u][r] = 0u;
         }
       }
-      float top = -INFINITY;
+      u32x4 weights[C][WPARTS];
 #pragma unroll
-      for (int u = 0; u < U; ++u)
+      for (int c = 0; c < C; ++c) {
+        float top = -INFINITY;
 #pragma unroll
-        for (int n = 0; n < NS; ++n) top = fmaxf(top, w[u][n]);
-      top = fmaxf(top, beside<1>(top));
-      if (GR == 4) top = fmaxf(top, beside<2>(top));
-      top = max_over_groups(top);
-      if (__builtin_amdgcn_ballot_w64(top > m + 8.f) != 0) {   // weights stay below 2^8 (packed_fwd.hip)
-        const float up = fmaxf(m, top), by = __builtin_amdgcn_exp2f(m - (up == -INFINITY ? 0.f : up));
-        m = up;
-        l *= by;
-        low *= by;
+        for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int e = 0; e < E; ++e) o[e] *= by;
-      }
-      const float ref = m == -INFINITY ? 0.f : m;
-      u32x4 weights[WPARTS];
+          for (int n = 0; n < NS; ++n) top = fmaxf(top, w[c][u][n]);
+        top = fmaxf(top, beside<1>(top));
+        if (GR == 4) top = fmaxf(top, beside<2>(top));
+        top = max_over_groups(top);
+        if (__builtin_amdgcn_ballot_w64(top > m[c] + 8.f) != 0) {   // weights stay below 2^8 (packed_fwd.hip)
+          const float up = fmaxf(m[c], top), by = __builtin_amdgcn_exp2f(m[c] - (up == -INFINITY ? 0.f : up));
+          m[c] = up;
+          l[c] *= by;
+          low[c] *= by;
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-#pragma unroll
-        for (int n = 0; n < NS; ++n) {
-          w[u][n] = __builtin_amdgcn_exp2f(w[u][n] - ref);
-          l += w[u][n];
+          for (int e = 0; e < E; ++e) o[c][e] *= by;
         }
+        const float ref = m[c] == -INFINITY ? 0.f : m[c];
 #pragma unroll
-        for (int r = 0; r < 4; r += 2) {
-          float y[2];
+        for (int u = 0; u < U; ++u) {
 #pragma unroll
-          for (int z = 0; z < 2; ++z) {
-            const float p = of_group<GR>(w[u][(r + z) / GR], (r + z) % GR);
-            low = fmaf(p, bf16_hi(x.pair[u][r + z]), low);
-            y[z] = p * bf16_lo(x.pair[u][r + z]);
+          for (int n = 0; n < NS; ++n) {
+            w[c][u][n] = __builtin_amdgcn_exp2f(w[c][u][n] - ref);
+            l[c] += w[c][u][n];
           }
-          uint32_t z[WPARTS];
-          parts_of(z, y[0], y[1]);
 #pragma unroll
-          for (int p = 0; p < WPARTS; ++p) weights[p][2 * u + r / 2] = z[p];
-          if (sizeof(T) == 4) low = fmaf(kMiddle, bf16_lo(z[0]), fmaf(kMiddle, bf16_hi(z[0]), low));
+          for (int r = 0; r < 4; r += 2) {
+            float y[2];
+#pragma unroll
+            for (int z = 0; z < 2; ++z) {
+              const float p = of_group<GR>(w[c][u][(r + z) / GR], (r + z) % GR);
+              low[c] = fmaf(p, bf16_hi(x.pair[u][r + z]), low[c]);
+              y[z] = p * bf16_lo(x.pair[u][r + z]);
+            }
+            uint32_t z[WPARTS];
+            parts_of(z, y[0], y[1]);
+#pragma unroll
+            for (int p = 0; p < WPARTS; ++p) weights[c][p][2 * u + r / 2] = z[p];
+            if (sizeof(T) == 4) low[c] = fmaf(kMiddle, bf16_lo(z[0]), fmaf(kMiddle, bf16_hi(z[0]), low[c]));
+          }
         }
       }
       // channels of the same byte's half and parity at a time: a byte of each of two tokens, then one of the next
@@ -727,30 +744,36 @@ template <typename T, int D, bool ONE> __global__ __launch_bounds__(kPagedThread
           u32x4 codes;
 #pragma unroll
           for (int j = 0; j < 4; ++j) codes[j] = codes_bf16(two[j] >> (4 * (e % 2)) & kNibbles, e >= 2);
-          if (sizeof(T) == 4)
-            o[4 * half + e] = mfma16(as_bf16x8(u32x4{kMinusMiddle, kMinusMiddle, kMinusMiddle, kMinusMiddle}), as_bf16x8(weights[0]), o[4 * half + e]);
 #pragma unroll
-          for (int p = WPARTS - 1; p >= 0; --p) o[4 * half + e] = mfma16(as_bf16x8(codes), as_bf16x8(weights[p]), o[4 * half + e]);
+          for (int c = 0; c < C; ++c) {
+            f32x4& sum = o[c][4 * half + e];
+            if (sizeof(T) == 4)
+              sum = mfma16(as_bf16x8(u32x4{kMinusMiddle, kMinusMiddle, kMinusMiddle, kMinusMiddle}), as_bf16x8(weights[c][0]), sum);
+#pragma unroll
+            for (int p = WPARTS - 1; p >= 0; --p) sum = mfma16(as_bf16x8(codes), as_bf16x8(weights[c][p]), sum);
+          }
         }
       }
       here = next;
       next = later;
     }
-    l += beside<1>(l);
-    if (GR == 4) l += beside<2>(l);
-    l = sum_over_groups(l);
-    low = sum_over_groups(low);
-
     // join the waves: a channel counts in its own group's column
-    if (L == 0 && g == 0) {
-      sm_m[wave][h] = m;
-      sm_l[wave][h] = l;
-    }
-    if (g == mine) {
 #pragma unroll
-      for (int e = 0; e < E; ++e)
+    for (int c = 0; c < C; ++c) {
+      l[c] += beside<1>(l[c]);
+      if (GR == 4) l[c] += beside<2>(l[c]);
+      l[c] = sum_over_groups(l[c]);
+      low[c] = sum_over_groups(low[c]);
+      if (L == 0 && g == 0) {
+        sm_m[wave][HC * c + h] = m[c];
+        sm_l[wave][HC * c + h] = l[c];
+      }
+      if (g == mine) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) sm_o[wave][h][E * (4 * L + r) + e] = o[e][r] + low;
+        for (int e = 0; e < E; ++e)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) sm_o[wave][HC * c + h][E * (4 * L + r) + e] = o[c][e][r] + low[c];
+      }
     }
     lds_barrier();
     const int c = tid % D;
@@ -851,13 +874,29 @@ template <typename T, int D, int W> __global__ __launch_bounds__(kPagedThreads) 
 
 constexpr int kManyPieces = 24;
 
+// Sets of columns that a workgroup holds.  Two, which widen a code once for both, where a key head has more query heads than the four of one, in
+// calls that fill the compute units all the same.  us, one set and two: 16 x 16000 tokens, 32 / 4 heads, d = 128 65.4 and 55.3; 48 x 16000, 32 / 1 152 and
+// 121; one of 16000, 8 / 1 12.3 and 14.1.  At d = 64, where a set is eight heads, 32 x 16000, 16 / 1 35.1 and 40.2.  fp32 has no registers for a second one.
+int column_sets(bool bf16, int B, int H, int Hkv, int d, int64_t max_len) {
+  constexpr int HC = Shape4<128>::HC;
+  const int64_t workgroups = (int64_t)Hkv * ((H / Hkv + 2 * HC - 1) / (2 * HC));
+  return bf16 && d == 128 && H / Hkv > HC && workgroups * B * blocks_of(max_len) >= 256 * kAtOnce<uint16_t, 128, 2> ? 2 : 1;
+}
 // Workgroups of a part: one for the query heads that fit its columns.
-int64_t decode_units(int H, int Hkv, int d) { return (int64_t)Hkv * ((H / Hkv + q4_heads(d) - 1) / q4_heads(d)); }
+int64_t decode_units(bool bf16, int B, int H, int Hkv, int d, int64_t max_len) {
+  const int heads = column_sets(bf16, B, H, Hkv, d, max_len) * (d == 128 ? Shape4<128>::HC : Shape4<64>::HC);
+  return (int64_t)Hkv * ((H / Hkv + heads - 1) / heads);
+}
 
+template <typename T, int D, int C> void decode_pages(const PagedDecodeArgs& a, dim3 grid, hipStream_t s) {
+  if (a.shift >= 4) q4_decode_kernel<T, D, true, C><<<grid, dim3(kPagedThreads), 0, s>>>(a);
+  else q4_decode_kernel<T, D, false, C><<<grid, dim3(kPagedThreads), 0, s>>>(a);
+}
 template <typename T, int D> hipError_t decode(const PagedDecodeArgs& a, hipStream_t s) {
-  const dim3 grid((unsigned)(decode_units(a.H, a.Hkv, D) * a.splits));
-  if (a.shift >= 4) q4_decode_kernel<T, D, true><<<grid, dim3(kPagedThreads), 0, s>>>(a);
-  else q4_decode_kernel<T, D, false><<<grid, dim3(kPagedThreads), 0, s>>>(a);
+  constexpr bool BF16 = sizeof(T) == 2;
+  const dim3 grid((unsigned)(decode_units(BF16, a.B, a.H, a.Hkv, D, a.room) * a.splits));
+  if (column_sets(BF16, a.B, a.H, a.Hkv, D, a.room) == 2) decode_pages<T, D, BF16 && D == 128 ? 2 : 1>(a, grid, s);
+  else decode_pages<T, D, 1>(a, grid, s);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !a.stats) return e;
   // many pieces a sequence take a workgroup a head
@@ -890,12 +929,14 @@ template <typename T, int D> hipError_t read(const PagedReadArgs& a, hipStream_t
 // block, which are not cut, take one each.
 int paged_q4_parts(bool bf16, int B, int H, int Hkv, int d, int64_t max_len) {
   if (!paged_q4_cuts(max_len)) return B;
-  const int at_once = bf16 ? (d == 128 ? kAtOnce<uint16_t, 128> : kAtOnce<uint16_t, 64>) : (d == 128 ? kAtOnce<float, 128> : kAtOnce<float, 64>);
-  return (int)std::max<int64_t>(1, std::min(256 * at_once / decode_units(H, Hkv, d), B * (kSetUp + blocks_of(max_len))));
+  const int at_once = !bf16      ? (d == 128 ? kAtOnce<float, 128, 1> : kAtOnce<float, 64, 1>)
+                      : d == 64 ? kAtOnce<uint16_t, 64, 1>
+                      : column_sets(bf16, B, H, Hkv, d, max_len) == 2 ? kAtOnce<uint16_t, 128, 2> : kAtOnce<uint16_t, 128, 1>;
+  return (int)std::max<int64_t>(1, std::min(256 * at_once / decode_units(bf16, B, H, Hkv, d, max_len), B * (kSetUp + blocks_of(max_len))));
 }
 bool paged_q4_cuts(int64_t max_len) { return max_len > kBlock; }
 bool paged_q4_decode_fits(bool bf16, int B, int H, int Hkv, int d, int64_t max_len) {
-  return decode_units(H, Hkv, d) * paged_q4_parts(bf16, B, H, Hkv, d, max_len) <= most_workgroups(kPagedThreads) &&
+  return decode_units(bf16, B, H, Hkv, d, max_len) * paged_q4_parts(bf16, B, H, Hkv, d, max_len) <= most_workgroups(kPagedThreads) &&
          B * (kSetUp + blocks_of(max_len)) < (1ll << 31);   // units are counted in 32 bits
 }
 bool paged_q4_rows_fit(int total, int n_seqs, int Hkv, int d) { return 2 * row_groups(total, n_seqs, Hkv, d, std::min(kFillRows, kReadRows)) <= most_workgroups(kPagedThreads); }

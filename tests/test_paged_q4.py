@@ -352,6 +352,19 @@ def test_decode_cut_along_its_length(dtype, H, Hkv, d, page, lens):
 
 
 @gpu
+@pytest.mark.parametrize("H,Hkv,page,lens,many", [(16, 2, 16, [700, 3, 129], 200), (12, 1, 8, [300, -1, 500], 300), (40, 4, 64, [200, 90], 100), (5, 1, 16, [260], 700)])
+def test_decode_of_two_sets_of_query_heads(H, Hkv, page, lens, many):
+    """Calls large enough that a workgroup takes eight query heads: long ones among single tokens."""
+    gen = torch.Generator().manual_seed(H)
+    lens = lens + torch.randint(0, 2, (many,), generator=gen).tolist()
+    args = step(gen, "bf16", H, Hkv, 128, page, lens)
+    check_step("bf16", page, *args)
+    first = args[2].clone()
+    args[0]()
+    assert torch.equal(first, args[2])
+
+
+@gpu
 @pytest.mark.parametrize("H,d,lens", [(520, 64, [300]), (400, 128, [129, 140])])
 def test_decode_of_so_many_heads_that_nothing_is_cut(H, d, lens):
     gen = torch.Generator().manual_seed(H)
