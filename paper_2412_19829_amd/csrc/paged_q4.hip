@@ -4,9 +4,9 @@
 // decode: with codes n, scales s and lowest values l of the keys' groups g of 32 channels c, and Q_g the sum of a query's channels there,
 //   q.k_j = sum_g ( s_jg sum_c q_c n_jc + l_jg Q_g ),   sum_j p_j v_jc = sum_j (p_j s_jg) n_jc + sum_j p_j l_jg
 // so that codes are the matrix operands, which bf16 holds exactly, and scales meet 16 x 16 tiles.  The tiles' columns are pairs
-// (query head, group): a column's query is zero outside its group, its scores' parts are added over the columns of a head,
-// which leaves them in every one of them, and there a weight takes its own group's scale for the second product, whose rows (channels) count
-// in their own group's columns alone.  16 columns are 4 heads of 128 channels, or 8 of 64.
+// (query head, group): a column's query is zero outside its group; its scores' parts are added over the columns of a head, which leaves every
+// token's score in one of them; and a weight, handed back to all of them, takes their groups' scales for the second product, whose rows
+// (channels) count in their own group's columns alone.  16 columns are 4 heads of 128 channels, or 8 of 64.
 // A code becomes an operand by way of fp8: the byte n is n 2^-9 for n < 16, two of which one instruction converts.
 // Memory bounds it up to 4 query heads of 128 channels a key head (8 of 64), beyond that the vector instructions, which every further 8 take
 // again.  us, kernel alone: 220,039 keys of 8 sequences, 32 / 8 heads, d = 128, bf16 (282 MB) 55.3, 5.1 TB/s; 88,074 in 32 ragged ones
