@@ -464,6 +464,44 @@ def test_far_pages():
 
 
 @gpu
+@pytest.mark.parametrize("quick", [True, False])
+def test_a_named_stream_and_the_binding_without_its_module(quick, monkeypatch):
+    """Every call on a stream that is named, through the extension module and through the binding's own code."""
+    gen = torch.Generator().manual_seed(16)
+    H, Hkv, d, page, lens = 8, 2, 64, 16, [700, 30]
+    if not quick:
+        monkeypatch.setattr(gb, "_quick", lambda *a: False)
+    kp, vp = sound_pages(gen, 100, Hkv, page, d), sound_pages(gen, 100, Hkv, page, d)
+    kw, vw = kp.cpu().clone(), vp.cpu().clone()
+    table = torch.randperm(98, generator=gen)[:92].view(2, 46).to(torch.int32)
+    k, v = torch.randn(5, Hkv, d, generator=gen).cuda(), torch.randn(5, Hkv, d, generator=gen).cuda()
+    q, out = torch.randn(2, H, d, generator=gen).cuda(), torch.zeros(2, H, d, device="cuda")
+    ko, vo = torch.zeros_like(k), torch.zeros_like(v)
+    tab, ln, start, cu = table.cuda(), ints(*lens), ints(698, 28), ints(0, 3, 5)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    on = side.cuda_stream
+    gb.gformer_paged_fill_q4(k, v, kp, vp, tab, start, cu, stream=on)
+    gb.gformer_paged_decode_q4(q, k[:2], v[:2], out, kp, vp, tab, ln, softmax_scale=0.125, stream=on)
+    gb.gformer_paged_read_q4(kp, vp, ko, vo, tab, start, cu, stream=on)
+    gb.gformer_pages_copy_q4(kp, vp, ints(3), ints(99), stream=on)
+    torch.cuda.synchronize()
+    kw, vw = (expected_fill(p, x.cpu(), table, [698, 28], [3, 2], page) for p, x in ((kw, k), (vw, v)))
+    for b, n in enumerate(lens):     # the step's own tokens, in front of the rows that the fill had put there
+        for p, x in ((kw, k), (vw, v)):
+            p[table[b, n // page], :, n % page] = ref.rows(x[b])
+    want, bound = ref.decode(q, kw, vw, table, [n + 1 for n in lens], page, 0.125, "f32", 46 * page)
+    pref.check(out, want, bound, "out")
+    for got, p in ((ko, kw), (vo, vw)):
+        held = ref.values(p).float()
+        rows = [held[table[0, t // page], :, t % page] for t in (698, 699, 700)] + [held[table[1, t // page], :, t % page] for t in (28, 29)]
+        assert torch.equal(got.cpu(), torch.stack(rows))
+    kw[99], vw[99] = kw[3], vw[3]
+    same_bytes(kp, kw, "keys")
+    same_bytes(vp, vw, "values")
+
+
+@gpu
 def test_streams_and_graphs():
     """Calls on another stream, and a captured run of fill, step and read that is replayed with new inputs."""
     gen = torch.Generator().manual_seed(6)

@@ -151,6 +151,27 @@ def test_packed(dtype, lens, start, tail):
 
 
 @gpu
+def test_a_named_stream_and_the_binding_without_its_module(monkeypatch):
+    gen = torch.Generator().manual_seed(3)
+    q, k = inputs(gen, "bf16", 50, 4, 2, 64, True)
+    freqs, pos, cu = rotary_frequencies(64), ints(list(range(50))), ints([0, 20, 50])
+    got = []
+    for quick in (True, False):
+        if not quick:
+            monkeypatch.setattr(gb, "_quick", lambda *a: False)
+        for where in (dict(positions=pos), dict(cu=cu), dict(cu=cu, start=ints([0, 20]))):
+            side = torch.cuda.Stream()
+            side.wait_stream(torch.cuda.current_stream())
+            qo, ko = torch.zeros_like(q), torch.zeros_like(k)
+            torch.cuda.synchronize()
+            gb.gformer_rotary(q, k, qo, ko, freqs, stream=side.cuda_stream, **where)
+            torch.cuda.synchronize()
+            got.append((qo, ko))
+    assert all(torch.equal(a, b) for x, y in zip(got[:3], got[3:]) for a, b in zip(x, y))
+    assert all(torch.equal(a, b) for a, b in zip(got[0], got[2])) and not torch.equal(got[0][0], got[1][0])
+
+
+@gpu
 def test_what_is_no_number_stays_in_its_pair():
     x = torch.ones(2, 1, 64, device="cuda")
     x[0, 0, 5], x[1, 0, 40] = math.nan, math.inf
