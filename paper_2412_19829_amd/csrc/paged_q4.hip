@@ -424,7 +424,7 @@ __device__ __forceinline__ Cut cut_at(const PagedDecodeArgs& a, int part, int la
 
 // ONE: a page holds whole tiles of 16 keys (pages of 8 tokens do not), so that their pages and addresses are the same for all lanes, which
 // then add nothing but a fixed offset to them: with addresses of their own they took 193 of 572 vector instructions a tile of 32 keys, d = 128
-// (355 are left).
+// (339 are left).
 template <typename T, int D, bool ONE, int C> __global__ __launch_bounds__(kPagedThreads, (kAtOnce<T, D, C>)) void q4_decode_kernel(PagedDecodeArgs a) {
   using S = Shape4<D>;
   typedef typename S::KeyCodes KeyCodes;
@@ -623,18 +623,17 @@ template <typename T, int D, bool ONE, int C> __global__ __launch_bounds__(kPage
       }
       // scores: this lane keeps those of tokens 4 L + g + GR n, n < NS
       float w[C][U][NS];
-      uint32_t in[U];
-      bool whole = true;
+      // tokens of part u that are there, as bits
+      auto there_of = [&](int u) {
+        const int key = t0 + 16 * u + i;
+        if (!ONE) return (uint32_t)__builtin_amdgcn_ballot_w64(key < to && (there(here.k[u]) || key == own)) & 0xffffu;
+        const int left = min(max(to - t0 - 16 * u, 0), 16), mine_at = own - t0 - 16 * u;
+        return (there(here.k[u]) ? (1u << left) - 1u : 0u) | ((unsigned)mine_at < 16u ? 1u << mine_at : 0u);
+      };
+      bool whole = t0 + R <= to;
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int key = t0 + 16 * u + i;
-        if (ONE) {
-          const int left = min(max(to - t0 - 16 * u, 0), 16), mine_at = own - t0 - 16 * u;
-          in[u] = (there(here.k[u]) ? (1u << left) - 1u : 0u) | ((unsigned)mine_at < 16u ? 1u << mine_at : 0u);
-        } else {
-          in[u] = (uint32_t)__builtin_amdgcn_ballot_w64(key < to && (there(here.k[u]) || key == own)) & 0xffffu;
-        }
-        whole = whole && in[u] == 0xffffu;
+        whole = whole && (ONE ? there(here.k[u]) : there_of(u) == 0xffffu);
         f32x4 s[C];
 #pragma unroll
         for (int c = 0; c < C; ++c) s[c] = kZeroF4;
@@ -677,15 +676,16 @@ template <typename T, int D, bool ONE, int C> __global__ __launch_bounds__(kPage
         // what is not there gets no weight, and its values, which may be anything, become zero
 #pragma unroll
         for (int u = 0; u < U; ++u) {
+          const uint32_t in = there_of(u);
 #pragma unroll
           for (int n = 0; n < NS; ++n)
-            if (!(in[u] >> (4 * L + g + GR * n) & 1u)) {
+            if (!(in >> (4 * L + g + GR * n) & 1u)) {
 #pragma unroll
               for (int c = 0; c < C; ++c) w[c][u][n] = -INFINITY;
             }
 #pragma unroll
           for (int r = 0; r < 4; ++r)
-            if (!(in[u] >> (4 * L + r) & 1u)) x.pair[u][r] = 0u;
+            if (!(in >> (4 * L + r) & 1u)) x.pair[u][r] = 0u;
         }
       }
       u32x4 weights[C][WPARTS];
