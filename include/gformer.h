@@ -401,7 +401,8 @@ gf_status gformer_pages_copy(void* kpages, void* vpages, const int32_t* src, con
  * (of two as near the even one; n = 0 where s = 0), so that no value is off by more than s / 2.  A group with a value that is not finite, or
  * of magnitude 2^127 or more, stands for values that are no number.  These calls take gformer_paged_params too:
  * dtype is that of q, k, v and out; kpage_stride and vpage_stride are in BYTES, multiples of d / 8, all zero for dense
- * [n_pages, Hkv, page_size, d / 2 + d / 8]. */
+ * [n_pages, Hkv, page_size, d / 2 + d / 8].  Strides by which two rows that a call writes (out; k and v of
+ * gformer_paged_read_q4) would share memory are GF_ERR_INVALID_ARG. */
 
 /* gformer_paged_fill, quantising the rows. */
 gf_status gformer_paged_fill_q4(const void* k, const void* v, void* kpages, void* vpages,
@@ -438,7 +439,8 @@ gf_status gformer_pages_copy_q4(void* kpages, void* vpages, const int32_t* src, 
  * the channels behind them are taken over.  Angles are taken in 64 bits (of magnitude 2^50 at most), products in 32, results are
  * rounded once.  Conventions of the packed calls.
  *   q, q_out : device [total, H, d], read / written; q_out may be q itself, with the same strides (in place)
- *   k, k_out : device [total, Hkv, d], likewise; k NULL: queries alone (Hkv = 0)
+ *   k, k_out : device [total, Hkv, d], likewise; k NULL: queries alone (Hkv = 0).  No two rows of q_out, or of k_out,
+ *              may share memory (GF_ERR_INVALID_ARG)
  *   freqs    : device fp32 [rot / 2], dense: any base and any stretching of the context is in them
  *   positions: device int32 [total], the row's position, any number; or NULL for packed sequences:
  *   cu, start: row i of sequence s, cu[s] .. cu[s+1]-1, is at start[s] + i (start NULL: i).  Rows behind the last

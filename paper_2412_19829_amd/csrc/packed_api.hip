@@ -36,6 +36,15 @@ gf_status strides2(const int64_t* in, int64_t* out, int heads, int d) {
   return in[0] > kMaxTokenStride ? GF_ERR_UNSUPPORTED : GF_OK;
 }
 
+// Whether no two rows of [rows, heads, d] share memory, through strides that strides2() has taken.
+bool apart(const int64_t* s, int rows, int heads, int d) {
+  if (rows < 2 || heads < 2 || s[1] <= (s[0] - d) / (heads - 1)) return true;   // a row's heads in front of the next row
+  const int64_t last = (rows - 1) * s[0];                                       // below 2^50
+  for (int64_t h = 1, at = s[1]; h < heads && at < last + d; ++h, at += s[1])   // head h of row 0 beside head 0 of any row
+    if (at % s[0] < d || (at / s[0] < rows - 1 && s[0] - at % s[0] < d)) return false;
+  return true;
+}
+
 // (page, head, token) strides of [pages, heads, page, d], multiples of `unit`
 gf_status strides3(const int64_t* in, int64_t* out, int heads, int page, int d, int unit) {
   if (in[0] == 0 && in[1] == 0 && in[2] == 0) {
@@ -164,6 +173,7 @@ gf_status decode_step(bool q4, const void* q, const void* k, const void* v, void
   if (!q || !out || !kpages || !vpages || (!table && table_width > 0) || !lens || !k != !v) return GF_ERR_INVALID_ARG;
   if (misaligned(bits(q, k, v, out, kpages, vpages), 16) || misaligned(bits(table, lens), 4)) return GF_ERR_INVALID_ARG;
   if (out == q || out == k || out == v || out == kpages || out == vpages || kpages == vpages) return GF_ERR_INVALID_ARG;
+  if (q4 && !apart(a.os, B, H, d)) return GF_ERR_INVALID_ARG;
   const size_t need = decode_bytes(plan, H, d);
   if (need > 0 && (!workspace || workspace_bytes < need)) return GF_ERR_WORKSPACE;
   if (need > 0 && misaligned(bits(workspace), 256)) return GF_ERR_INVALID_ARG;
@@ -406,6 +416,7 @@ gf_status gformer_paged_read_q4(const void* kpages, const void* vpages, void* k,
   if (!k || !v || (!table && table_width > 0) || !start || !cu || (n_pages > 0 && (!kpages || !vpages))) return GF_ERR_INVALID_ARG;
   if (misaligned(bits(k, v, kpages, vpages), 16) || misaligned(bits(table, start, cu), 4)) return GF_ERR_INVALID_ARG;
   if (k == v || k == kpages || k == vpages || v == kpages || v == vpages) return GF_ERR_INVALID_ARG;
+  if (!apart(a.ks, total, Hkv, d) || !apart(a.vs, total, Hkv, d)) return GF_ERR_INVALID_ARG;
   if ((st = check_device(hip_stream)) != GF_OK) return st;
   a.kpages = kpages;
   a.vpages = vpages;
@@ -464,7 +475,8 @@ gf_status gformer_rotary(const void* q, const void* k, void* q_out, void* k_out,
   if (positions ? cu || start || n_seqs != 0 : !cu) return GF_ERR_INVALID_ARG;
   if (misaligned(bits(q, k, q_out, k_out), 16) || misaligned(bits(freqs, positions, cu, start), 4)) return GF_ERR_INVALID_ARG;
   if (q_out == k || q_out == k_out || (k && k_out == q)) return GF_ERR_INVALID_ARG;
-  // in place, or apart
+  if (!apart(a.qos, total, H, d) || (k && !apart(a.kos, total, Hkv, d))) return GF_ERR_INVALID_ARG;
+  // in place, or elsewhere
   if ((q_out == q && memcmp(a.qs, a.qos, sizeof(a.qs))) || (k && k_out == k && memcmp(a.ks, a.kos, sizeof(a.ks)))) return GF_ERR_INVALID_ARG;
   if ((st = check_device(hip_stream)) != GF_OK) return st;
   a.q = q;
