@@ -20,8 +20,17 @@ def _gpu_available() -> bool:
         return False
 
 
+# Tests of refusals with a call in them that is not refused: without a GPU it ends where the device is asked for, with one it would
+# read made-up addresses.
+NO_GPU_ONLY = ("test_paged_q4.py::test_row_calls_and_copy_refusals",)
+
+
 def pytest_collection_modifyitems(config, items):
     if _gpu_available():
+        skip = pytest.mark.skip(reason="hands made-up addresses to a call that is not refused")
+        for item in items:
+            if item.nodeid.endswith(NO_GPU_ONLY):
+                item.add_marker(skip)
         return
     skip = pytest.mark.skip(reason="no GPU in this process")
     for item in items:
