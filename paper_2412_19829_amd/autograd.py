@@ -118,7 +118,9 @@ class _GformerRotary(torch.autograd.Function):
 def gformer_rotary_positions(q, k, freqs, *, positions=None, cu=None, start=None, interleaved: int = 0, factor: float = 1.0):
     """Queries [total, H, d] and keys [total, Hkv, d] (None: queries alone) turned by their positions, as new tensors: see
     binding.gformer_rotary for freqs and for positions, or cu and start.  Rows behind the last sequence give zeros.  Differentiable with
-    respect to q and k, any number of times: the gradients turn back.  Both ways can be captured in a graph, under the condition of
-    gformer_packed_attention."""
+    respect to q and k, any number of times: the gradients turn back; frequencies that want a gradient are refused.  Both ways can be
+    captured in a graph, under the condition of gformer_packed_attention."""
+    if freqs.requires_grad and torch.is_grad_enabled():
+        raise ValueError("freqs has no gradient: hand over freqs.detach()")
     out = gb.rotary_node(q, k, freqs, positions, cu, start, int(interleaved), float(factor))
     return _GformerRotary.apply(q, k, freqs, positions, cu, start, int(interleaved), 0, float(factor)) if out is None else out
