@@ -8,9 +8,12 @@
 // token's score in one of them; and a weight, handed back to all of them, takes their groups' scales for the second product, whose rows
 // (channels) count in their own group's columns alone.  16 columns are 4 heads of 128 channels, or 8 of 64.
 // A code becomes an operand by way of fp8: the byte n is n 2^-9 for n < 16, two of which one instruction converts.
-// Memory bounds it up to 4 query heads of 128 channels a key head (8 of 64), beyond that the vector instructions, which every further 8 take
-// again.  us, kernel alone: 220,039 keys of 8 sequences, 32 / 8 heads, d = 128, bf16 (282 MB) 55.3, 5.1 TB/s; 88,074 in 32 ragged ones
-// (114 MB) 27.7; six fp32 sequences of 10,167 in all, 16 heads, d = 64 11.4; one of 2047, 12 heads, d = 64 6.4, and 4.8 to join.
+// Memory bounds it up to 4 query heads of 128 channels a key head, beyond that the instructions that these columns take: codes are widened
+// anew for every eight heads.  us, kernel alone: 220,039 keys of 8 sequences, 32 / 8 heads, d = 128, bf16 (282 MB) 56.6, 5.0 TB/s; 88,074 in 32
+// ragged ones (114 MB) 28.7; 48 of 16000, 32 / 1 heads (123 MB) 121: 468 vector instructions (73 us) and 48 products (30) a tile of 32 keys and eight
+// heads; over a cache of bf16 118.  d = 64, 8 of 16000, 16 heads (164 MB) 45.6: 270 vector and 144 scalar instructions a tile, which at d = 128 are
+// 339 and 146 for twice the bytes; in fp32 56.8, and 44.0 for 32 / 8 heads, d = 128.  Six fp32 sequences of 10,167 keys in all, 16 heads, d = 64 11.8;
+// one of 2047, 12 heads, d = 64 6.9, and 4.5 to join.
 #include "paged_q4.hpp"
 
 #include "f32_mfma.hpp"
@@ -246,8 +249,9 @@ template <int D, int N, int HB> struct Slots {
 };
 
 // Keys and values in workgroups of their own, which halves what a lane quantises in turn: 128 tokens of 12 heads, d = 64 5.2 us (6.6 in
-// the same ones).  9207 rows of 8 heads, d = 128, bf16 (50 MB read and written): 14.0 us, of which vector instructions take 8.6 and the
-// memory would take 10 (20 with all of them in 64 bits; 15.9 with one row a lane, 14.2 with four).
+// the same ones).  7206 rows of 8 heads, d = 128, bf16 (39 MB read and written): 13.5 us, of which vector instructions take 8.6 and the
+// memory would take 7.9 (20 with all of them in 64 bits; 15.9 with one row a lane, 14.2 with four); fp32, whose scales are always taken in
+// 64 bits (68 MB) 17.4, the memory 13.9.
 template <typename T, int D, int HB> __global__ __launch_bounds__(kPagedThreads) void q4_fill_kernel(PagedFillArgs a) {
   constexpr int N = kFillRows;
   const int tid = threadIdx.x, c = tid % (D / 8);
@@ -288,7 +292,7 @@ template <int D> __device__ __forceinline__ Codes codes_of(const void* pages, in
   const uint32_t* row = reinterpret_cast<const uint32_t*>(reinterpret_cast<const char*>(pages) + at);
   return {row[c], row[D / 8 + c / 4]};
 }
-// 56866 rows of 8 heads, d = 128, bf16 (306 MB read and written): 60.4 us, 5.1 TB/s; 6066 of 16 heads, d = 64, fp32 (57 MB) 17.5 with two
+// 56866 rows of 8 heads, d = 128, bf16 (306 MB read and written): 60.9 us, 5.0 TB/s; 6066 of 16 heads, d = 64, fp32 (57 MB) 17.5 with two
 // rows a lane, 18.3 with one.  `once`: the rows are more than the last cache holds, so that nobody finds them there: 4 x 32767 tokens
 // with an attention of 32 queries each behind them 442 us (475 without), but 7 x 8192 with 64 queries 240 (234).
 constexpr int64_t kLastCache = (int64_t)256 << 20;   // bytes
@@ -327,7 +331,8 @@ template <typename T, int D, int HB> __global__ __launch_bounds__(kPagedThreads)
   }
 }
 
-// Whole pages: a workgroup copies one head of one page, keys and values, in five pieces a row.
+// Whole pages: a workgroup copies one head of one page, keys and values, in five pieces a row.  2000 pages of 64 tokens, 8 heads, d = 128 (328 MB
+// read and written): 68.5 us, 4.8 TB/s; 4000 of 16 tokens, 12 heads, d = 64 (123 MB) 37.0: a workgroup there is 80 pieces; one page 2.5.
 template <int D> __global__ __launch_bounds__(kPagedThreads) void q4_copy_kernel(PagesCopyArgs a) {
   typedef typename std::conditional<D == 128, u32x4, u32x2>::type Piece;
   const int copy = blockIdx.x / a.Hkv, head = blockIdx.x % a.Hkv;
@@ -396,7 +401,11 @@ __device__ __forceinline__ int seen_tokens(const PagedDecodeArgs& a, int b) {
 // blocks, whatever the lengths are, which are known on the device alone.  A share may hold several sequences, or a part of one; what
 // part p finds of sequence b has row p + b of the workspace to itself, since from one such piece to the next p or b grows.
 constexpr int kBlock = 32 * kWaves;   // a tile for each wave
-constexpr int kSetUp = 2;             // what beginning a sequence costs, in blocks: counted in front of its own
+// What beginning a sequence costs, in blocks: counted in front of its own.  us with none, one, two and four: 32 ragged sequences of up to 8191,
+// 32 / 8 heads, d = 128 36.1, 32.3, 32.3, 33.1; 16 of 8000 and 200 of 50 78.0, 60.7, 54.2, 58.1; 255 of 100 and one of 1000 27.6, 27.8, 26.4, 29.3; 64 of
+// 0 to 1000 21.8, 20.7, 22.8, 23.2.  A row that sees nothing counts as one of a block, and is worked through like it: 8 of 16000 take 40.9, among 248
+// idle rows 54.1.
+constexpr int kSetUp = 2;
 __host__ __device__ constexpr int64_t blocks_of(int64_t tokens) { return tokens < 1 ? 1 : (tokens + kBlock - 1) / kBlock; }
 __device__ __forceinline__ int units_of(int tokens) { return kSetUp + (int)blocks_of(tokens); }
 __device__ __forceinline__ int first_unit(int part, int parts, int total) { return (int)((int64_t)part * total / parts); }
@@ -889,6 +898,9 @@ template <typename T, int D, int W> __global__ __launch_bounds__(kPagedThreads) 
   for (int x = 0; x < N; ++x) Storage<T>::store(rows_of<T>(a.out, a.os, cut.b, h), N * lane + x, sum == 0.f ? 0.f : acc[x] / sum);
 }
 
+// From so many possible pieces a sequence on, a head's are joined by a workgroup, below by a wave.  us of the step, by a wave and by a workgroup, d = 128:
+// 12 pieces (8 x 32767 tokens, 32 / 8 heads) 73.3 and 73.8, 24 (4) 41.8 and 42.0, 48 (2) 27.7 and 26.6, 96 (1) 23.7 and 19.1; 16 (32 x 16000, 8 / 1) 31.6 and
+// 34.8, 32 (16) 25.0 and 26.0, 64 (8) 25.1 and 21.0.
 constexpr int kManyPieces = 24;
 
 // Sets of columns that a workgroup holds.  Two, which widen a code once for both, where a key head has more query heads than the four of one, in

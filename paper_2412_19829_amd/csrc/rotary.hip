@@ -1,4 +1,4 @@
-// Rotary positions (rotary.hpp).  The angles, which take 64 bits, are taken once for all heads of a row.  Memory bounds it: 9407 rows, 9207
+// Rotary positions (rotary.hpp).  The angles, which take 64 bits, are taken once for all heads of a row.  Memory bounds it: 7406 rows, 7206
 // of which turn, of 32 / 8 heads, d = 128, bf16 (148 MB read and written) 28.7 us, 5.1 TB/s; 4 rows of 12 / 12 heads, d = 64: 2.7, launch and trips to
 // memory.  What is read need not stay in the caches, what is written is what attention reads next: over more tensors in turn 31.4 us with
 // such loads and 34.5 without, with packed attention over sequences of 281 behind it 138 and 142; with such stores too 28.3, but 143 then.
@@ -185,7 +185,10 @@ template <typename T, int D, int ROWS, bool INTERLEAVED> __global__ __launch_bou
   }
 }
 
-constexpr int kManyRows = 1024;   // from here on, four rows for every compute unit, a workgroup takes kRows rows, below it one
+// From here on, four rows for every compute unit, a workgroup takes kRows rows, below it one.  us with one and with four: 32 / 8 heads, d = 128, bf16 512
+// rows 4.6 and 5.9, 1024 6.0 and 7.0, 2048 10.7 and 11.2, 4096 18.5 and 17.1; 12 / 12 heads, d = 64 1024 6.4 and 6.3, 2048 6.0 and 5.1, 4096 9.7 and 7.3.  Rows of
+// many bytes would want it at about 2500.
+constexpr int kManyRows = 1024;
 
 template <typename T, int D, int ROWS> void launch(const RotaryArgs& a, hipStream_t s) {
   const dim3 grid((unsigned)(((int64_t)a.total + ROWS - 1) / ROWS));
