@@ -45,11 +45,8 @@ def read(pages, n, dtype):
     return out[0].cpu()[:, 0]
 
 
-@gpu
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("d", [64, 128])
-def test_a_lowest_value_far_below_the_step(dtype, d):
-    """All 128 steps of 8 bits with every code, the lowest value from 2^-6 to 2^-60 steps on either side of zero."""
+def hard_rows(d):
+    """Rows of one head: all 128 steps of 8 bits with every code, the lowest value from 2^-6 to 2^-60 steps on either side of zero."""
     page, gen = 4096, torch.Generator().manual_seed(d)
     r = torch.arange(page)
     scale = (1 + (r % 128) / 128) * 2.0 ** (r // 128 % 9 * 13.0 - 50)
@@ -60,9 +57,33 @@ def test_a_lowest_value_far_below_the_step(dtype, d):
     low = scale[:, None] * 2.0 ** -far.double() * (torch.randint(0, 3, far.shape, generator=gen) - 1.0)
     pair = torch.stack([scale[:, None].expand_as(low), low], -1).to(torch.bfloat16)
     rows[:, d // 2:] = pair.contiguous().view(torch.uint8).view(page, -1)
+    return rows
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_a_lowest_value_far_below_the_step(dtype, d):
+    """All 128 steps of 8 bits with every code, the lowest value from 2^-6 to 2^-60 steps on either side of zero."""
+    rows = hard_rows(d)
     want = rounded(*ref.parts(rows), dtype)
     assert dtype == "f32" or int((want != ref.values(rows).float().to(torch.bfloat16)).sum()) > 1000      # where two roundings differ from one
-    assert torch.equal(read(rows.view(1, 1, page, -1).cuda(), page, dtype), want)
+    assert torch.equal(read(rows.view(1, 1, *rows.shape).cuda(), len(rows), dtype), want)
+
+
+@gpu
+def test_such_rows_past_the_caches():
+    """More rows than the last cache holds, which go past it: those are written twice there, too."""
+    rows, d = hard_rows(128), 128
+    n = (256 << 20) // (2 * d * 2) + 777
+    pages = rows.view(4, 1, len(rows) // 4, -1).cuda()
+    gen = torch.Generator().manual_seed(3)
+    table = torch.randint(0, 4, (1, -(-n // pages.shape[2])), generator=gen).to(torch.int32)
+    k, v = (torch.zeros(n, 1, d, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    ints = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    gb.gformer_paged_read_q4(pages, pages.clone(), k, v, table.cuda(), ints(0), ints(0, n))
+    want = rounded(*ref.parts(rows), "bf16").cuda().view(4, -1, d)[table[0].long().cuda()].flatten(0, 1)[:n]
+    assert torch.equal(k[:, 0], want) and torch.equal(v[:, 0], want)
 
 
 @gpu
